@@ -18,6 +18,12 @@
  *   cure_commit     the winning path committed: its cache rows moved after the
  *                   context in every layer, the emitted tokens, the new context
  *                   length and the draft-cache replay start   (Sec. 3.5, Alg. 1)
+ *   cure_rope_append  new rows' queries and keys normalised per head and rotated
+ *                   by their positions, keys and values written to the cache
+ *   cure_prompt_attn  causal attention of whole prompts, chunks of them or single
+ *                   tokens, packed without padding: what fills the context
+ *   cure_prefix_attn  cure_tree_attn for sequences that share a prefix, whose
+ *                   keys and values are read once for all of them
  *   cure_margins_noalloc  cure_margins for callers that cannot allocate: its
  *                   scratch is a fixed array inside the library
  *   cure_read_ceiling  not a step of the method: a plain streaming read, the
@@ -358,6 +364,158 @@ cure_status cure_commit(void* k, void* v, int32_t dtype, int32_t n_layers, int64
                         int32_t chain_len, int32_t n_max, int32_t* new_ctx_len, int32_t* emit,
                         int32_t* emit_cnt, int32_t* replay_start, int32_t* commit_status,
                         void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Rotary positions and the cache rows of new tokens -- what an attention layer
+ * does before cure_tree_attn or cure_prompt_attn can read its keys and values.
+ *
+ * For the n_rows[b] new rows of each sequence b (a prompt's tokens, or the nodes
+ * of a candidate tree), row n of it:
+ *   queries, keys  every head x of d columns is normalised where a weight is given,
+ *                    x^ = x * rsqrt(mean(x^2) + eps) * weight,
+ *                  and its first rot columns rotated in pairs (a, b) by the angle
+ *                  t = pos * inv_freq[i]:
+ *                    y_a = mscale * (x^_a cos t - x^_b sin t)
+ *                    y_b = mscale * (x^_a sin t + x^_b cos t)
+ *                  where pair i is columns (i, i + rot/2), or (2i, 2i + 1) with
+ *                  CURE_ROPE_INTERLEAVED; columns from rot on are not rotated.
+ *   pos            pos_off[b] + ctx_len[b] + n, or with a tree
+ *                  pos_off[b] + ctx_len[b] + depth(n) (a root has depth 0), the
+ *                  position that the node has once cure_commit has moved its path
+ *   q_out          [row][hq][d] takes the queries, at the row that they came from
+ *   k_cache, v_cache  row kv_off[b] + ctx_len[b] + n takes the keys and the values
+ * Arithmetic in float32 (the angle's reduction in float64), one rounding at the end.
+ *
+ * Layout:
+ *   q, k, v    rows of [hq][d], [hkv][d], [hkv][d] dtype elements, q_ld, k_ld and
+ *              v_ld elements apart (so they may lie in one fused projection's
+ *              output). Sequence b's first row is row_off[b], or b * n_max where
+ *              row_off is NULL (rows padded to n_max per sequence). hq = 0: no
+ *              queries, q and q_out are ignored; hkv = 0: no keys and values.
+ *   n_rows     [batch] int32, at most n_max
+ *   parent     [batch][n_max] int32 as for cure_tree_attn, or NULL: a sequence
+ *   row_off, kv_off  [batch] int64;  ctx_len, pos_off  [batch] int32 (pos_off may be
+ *              NULL: 0)
+ *   q_weight, k_weight  [d] dtype, each may be NULL: not normalised
+ *   inv_freq   [rot/2] float32 (cure_rope_frequencies computes the usual ones)
+ *   rows       rows that q, k, v and q_out hold;  cache_rows  rows of the caches
+ *   row_status [batch] int32 output: CURE_OK, or CURE_ERR_BAD_TREE when the
+ *              sequence's parent array is malformed, its sizes are negative,
+ *              n_rows exceeds n_max, or its rows or cache rows reach past rows or
+ *              cache_rows. Nothing of such a sequence is written.
+ * q_out may be q itself where q_ld = hq * d. Cache rows of different sequences
+ * must not overlap. Rows that belong to no sequence are not written.
+ * Supports d a multiple of 16 up to 256, rot a multiple of 16 up to d, n_max <= 256
+ * with a tree, batch <= 65535. All row pointers, weights and row distances must be
+ * multiples of 16 bytes (else CURE_ERR_INVALID_ARG). No workspace.
+ */
+#define CURE_ROPE_INTERLEAVED 1u
+
+cure_status cure_rope_append(const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                             const void* v, int64_t v_ld, int32_t dtype, int64_t rows,
+                             int32_t batch, int32_t n_max, const int64_t* row_off,
+                             const int32_t* n_rows, const int32_t* parent,
+                             const int64_t* kv_off, const int32_t* ctx_len,
+                             const int32_t* pos_off, int32_t hq, int32_t hkv, int32_t d,
+                             const void* q_weight, const void* k_weight, float eps,
+                             const float* inv_freq, int32_t rot, uint32_t flags, float mscale,
+                             void* q_out, void* k_cache, void* v_cache, int64_t cache_rows,
+                             int32_t* row_status, void* stream);
+
+/* Frequencies of a rotation over rot columns, computed on the host in float64:
+ * f_i = base^(-2i/rot), i < rot/2, changed for contexts longer than the trained one
+ * (factor >= 1 times as long; orig_len tokens where it is used) by scaling:
+ *   CURE_ROPE_PLAIN   not at all
+ *   CURE_ROPE_LINEAR  f_i / factor
+ *   CURE_ROPE_BASE    base * factor^(rot/(rot-2)) in place of base
+ *   CURE_ROPE_BANDS   by the turns u = orig_len * f_i / 2 pi that a pair makes: kept
+ *                     from u >= p1 on, f_i / factor up to u <= p0, blended linearly in
+ *                     u between (0 < p0 < p1, usually 1 and 4)
+ *   CURE_ROPE_RAMP    by the pair's index: kept before the pair that makes p0 turns,
+ *                     f_i / factor from the one that makes p1 (p0 > p1 > 0, usually 32
+ *                     and 1), a linear ramp between; mscale = 0.1 ln(factor) + 1
+ * Writes host_inv_freq [rot/2] and host_mscale (1 except for CURE_ROPE_RAMP), both
+ * host memory. rot even and >= 0, base > 1.
+ */
+enum { CURE_ROPE_PLAIN = 0, CURE_ROPE_LINEAR = 1, CURE_ROPE_BASE = 2, CURE_ROPE_BANDS = 3,
+       CURE_ROPE_RAMP = 4 };
+
+cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor,
+                                  double orig_len, double p0, double p1, float* host_inv_freq,
+                                  float* host_mscale);
+
+/* ------------------------------------------------------------------------- */
+/* Attention over prompts: causal, grouped heads, packed sequences.
+ *
+ * New token i < n_rows[b] of sequence b attends, in every query head h (key/value
+ * head h / (hq/hkv)), to the cache rows kv_off[b] .. kv_off[b] + ctx_len[b] + i: the
+ * context before it and the new tokens up to itself, whose keys and values are in the
+ * cache already (cure_rope_append). Whole prompts have ctx_len 0, chunks of long
+ * ones and single tokens what came before.
+ *   o[r][h]   = sum_j softmax_j * v_j,  r = row_off[b] + i
+ *   lse[r][h] = log sum_j exp(scale * <q, k_j>)
+ *
+ * Layout:
+ *   q, o       [rows][hq][d] dtype / out_dtype; sequence b's rows are row_off[b] ..
+ *              row_off[b] + n_rows[b] - 1; other rows of o and lse are not written
+ *   k, v       cache rows of [hkv][d] dtype
+ *   lse        [rows][hq] float32 (may be NULL)
+ *   row_off, kv_off  [batch] int64;  n_rows, ctx_len  [batch] int32 (device)
+ *   host_n_rows, host_ctx_len  host copies that the launch is planned from. The
+ *              device's n_rows may be smaller (a captured call replayed on shorter
+ *              prompts), not larger: tokens past the host's longest n_rows may get no
+ *              output. ctx_len may differ either way.
+ * The values that a row sees must be finite; keys and values after it (later
+ * tokens, and whatever the cache holds behind the sequence) may be anything.
+ * Supports d in {64, 128}, hq % hkv == 0, 0 < scale < inf, batch <= 65535.
+ * kv_split: 0 = automatic, else the number of splits of the longest context.
+ * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
+ * 16-byte aligned. q, k, v: 16-byte aligned; o: 8 (bf16) or 16 bytes (float32).
+ * bf16: probabilities are rounded to bf16 for their product and lse sums the rounded
+ * ones (within 2^-8 of the exact sum). float32: float32 throughout.
+ */
+size_t cure_prompt_attn_workspace_size(int32_t batch, int64_t rows, int32_t hq, int32_t hkv,
+                                       int32_t d, const int32_t* host_n_rows,
+                                       const int32_t* host_ctx_len, int32_t kv_split);
+
+cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* o, float* lse,
+                             int32_t dtype, int32_t out_dtype, int32_t batch, int64_t rows,
+                             int32_t hq, int32_t hkv, int32_t d, float scale,
+                             const int64_t* row_off, const int32_t* n_rows,
+                             const int64_t* kv_off, const int32_t* ctx_len,
+                             const int32_t* host_n_rows, const int32_t* host_ctx_len,
+                             int32_t kv_split, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Tree attention over a shared prefix: cure_tree_attn for a batch whose sequences all
+ * begin with the same prefix_len tokens, stored once in cache rows prefix_off ..
+ * prefix_off + prefix_len - 1. Node n of sequence b attends to those, to its
+ * sequence's own ctx_len[b] rows from kv_off[b] on and to the tree rows on its root
+ * path behind them. The prefix is read once for all nodes of all sequences; the own
+ * rows take cure_tree_attn, and log-sum-exps join the two.
+ * Arguments, layout and outputs as for cure_tree_attn (ctx_len counts a sequence's
+ * own rows only; the position of a node is prefix_len + ctx_len + depth, which
+ * cure_rope_append's pos_off = prefix_len gives). prefix_len = 0 is cure_tree_attn.
+ * kv_split: splits of the prefix, 0 = automatic.
+ * A malformed tree is reported in tree_status, and that sequence's o and lse are then
+ * unspecified. Prefix values must be finite.
+ * Supports 0 < scale < inf, batch <= 1024 (where prefix_len > 0), and what
+ * cure_tree_attn supports. Alignment as for cure_prompt_attn. workspace:
+ * cure_prefix_attn_workspace_size(...) bytes for the same arguments.
+ */
+size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int32_t hkv, int32_t d,
+                                       int32_t n_max, int32_t prefix_len,
+                                       const int32_t* host_ctx_len,
+                                       const int32_t* host_n_nodes, int32_t kv_split);
+
+cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* o, float* lse,
+                             int32_t dtype, int32_t out_dtype, int32_t batch, int32_t hq,
+                             int32_t hkv, int32_t d, float scale, int64_t prefix_off,
+                             int32_t prefix_len, const int64_t* kv_off, const int32_t* ctx_len,
+                             const int32_t* n_nodes, const int32_t* parent, int32_t n_max,
+                             const int32_t* host_ctx_len, const int32_t* host_n_nodes,
+                             int32_t kv_split, int32_t* tree_status, void* workspace,
+                             size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Read ceiling -- a measurement aid, not a step of the method.

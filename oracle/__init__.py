@@ -31,6 +31,10 @@ unless the paper (or the decision being reproduced) fixes another precision:
                        ranked alternatives by a full stable sort, the branch
                        budget per UFP, and the budget-capped assembly of the
                        parent/token arrays.
+* ``rope_append``, ``tree_positions``, ``prompt_attention``, ``prefix_attention``
+                    -- around the verify step: rotary positions of new rows,
+                       causal attention over prompts, and tree attention over
+                       a prefix that sequences share.
 
 Inputs are the same bytes the GPU path receives: bf16 arrives as raw uint16
 bit patterns and is widened here exactly to float32 by this package's own
@@ -42,9 +46,11 @@ from .tree import ancestors, tree_attention
 from .accept import accept
 from .repair import topk, branch_budget, repair_tree
 from .commit import commit_kv, commit_tokens
+from .prompt import rope_append, tree_positions, attend, prompt_attention, prefix_attention
 
 __all__ = [
     "widen_bf16", "as_float32", "margins", "ufp_select",
     "ancestors", "tree_attention", "accept",
     "topk", "branch_budget", "repair_tree", "commit_kv", "commit_tokens",
+    "rope_append", "tree_positions", "attend", "prompt_attention", "prefix_attention",
 ]

@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(LIB_DIR, "libcure.so")
 NATIVE_PATH = os.path.join(LIB_DIR, "_native.so")
 INCLUDE = os.path.join(ROOT, "include")
 
-SOURCES = ["api.cpp", "margins.hip", "accept.hip", "tree_attn.hip", "repair.hip", "commit.hip", "ceiling.hip"]
+SOURCES = ["api.cpp", "margins.hip", "accept.hip", "tree_attn.hip", "repair.hip", "commit.hip", "rope.hip",
+           "prompt_attn.hip", "ceiling.hip"]
 
 # Packed fp32 arithmetic is disabled for all device code.
 HIPCC_FLAGS = [

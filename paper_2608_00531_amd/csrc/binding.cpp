@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -517,6 +518,320 @@ PyObject* py_commit(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// Makes a tensor's device the current one for a call's launches.
+class OnDevice {
+ public:
+  explicit OnDevice(const at::Tensor& t) {
+    c10::DeviceIndex now = 0;
+    if (c10::hip::GetDevice(&now) != hipSuccess || now == t.device().index()) return;
+    was_ = c10::hip::ExchangeDevice(t.device().index());
+  }
+  ~OnDevice() {
+    if (was_ >= 0) (void)c10::hip::SetDevice(was_);
+  }
+  OnDevice(const OnDevice&) = delete;
+
+ private:
+  c10::DeviceIndex was_ = -1;
+};
+
+// Scratch memory of one call, from the tensor library's allocator: handed on to a later call on
+// the same stream only, and a captured call's lies in its graph's own pool, so that graphs replayed
+// on different streams do not share it.
+struct Scratch {
+  at::Tensor buffer;
+  void* ptr = nullptr;
+  size_t bytes = 0;
+  Scratch(const at::Tensor& like, size_t need) {
+    if (need == 0) return;
+    buffer = empty({(int64_t)need}, at::kByte, like);
+    ptr = buffer.data_ptr();
+    bytes = need;
+  }
+};
+
+// An optional tensor argument: undefined for None.
+at::Tensor optional(PyObject* o) { return o == Py_None ? at::Tensor() : gpu_tensor(o); }
+
+void want_ints(const at::Tensor& t, at::ScalarType type, c10::IntArrayRef shape, const char* name) {
+  if (!t.defined()) return;
+  if (t.scalar_type() != type) fail(std::string(name) + (type == at::kLong ? " must be int64" : " must be int32"));
+  if (t.sizes() != shape)
+    fail(std::string(name) + ": expected shape " + shape_text(shape) + ", got " + shape_text(t.sizes()));
+}
+
+void same_device(const at::Tensor& t, const at::Tensor& like) {
+  if (t.defined() && t.device() != like.device()) fail("tensor arguments must live on one device");
+}
+
+template <typename T>
+T* data(const at::Tensor& t) {
+  return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr;
+}
+
+// The output: the caller's tensor, checked, or a new one.
+at::Tensor output(PyObject* o, c10::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
+  if (o == Py_None) return empty(shape, type, like);
+  at::Tensor t = gpu_tensor(o);
+  same_device(t, like);
+  if (t.sizes() != shape || t.scalar_type() != type || !t.is_contiguous())
+    fail("out must be contiguous, of the result's type and of shape " + shape_text(shape));
+  return t;
+}
+
+at::ScalarType out_dtype(PyObject* o, const at::Tensor& like) {
+  if (o == Py_None) return like.scalar_type();
+  if (!THPDtype_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, "out_dtype must be a torch.dtype");
+    throw PyError{};
+  }
+  return reinterpret_cast<THPDtype*>(o)->scalar_type;
+}
+
+// A layer's caches: [rows, hkv, d], contiguous.
+void want_caches(const at::Tensor& k, const at::Tensor& v, const at::Tensor& like, int64_t d) {
+  if (k.dim() != 3 || k.sizes() != v.sizes() || k.size(2) != d) fail("the caches must both be [rows, hkv, d]");
+  if (k.scalar_type() != like.scalar_type() || v.scalar_type() != like.scalar_type())
+    fail("the caches must have the rows' dtype");
+  if (!k.is_contiguous() || !v.is_contiguous()) fail("the caches must be contiguous");
+  same_device(k, like);
+  same_device(v, like);
+}
+
+// Rows of [heads][d] one distance apart: x [rows, heads, d] or [batch, n_max, heads, d].
+// Copied where the heads of a row are not together or the rows not evenly apart.
+at::Tensor even_rows(at::Tensor x, int64_t* ld) {
+  const int64_t n = x.dim(), heads = x.size(n - 2), d = x.size(n - 1);
+  const auto even = [&]() {
+    if (x.stride(n - 1) != 1 || (heads > 1 && x.stride(n - 2) != d)) return false;
+    if (n == 3) *ld = x.size(0) > 1 ? x.stride(0) : heads * d;
+    else if (x.size(1) > 1) *ld = x.stride(1);
+    else *ld = x.size(0) > 1 ? x.stride(0) : heads * d;
+    if (*ld < heads * d) return false;
+    return n == 3 || x.size(0) <= 1 || x.stride(0) == x.size(1) * *ld;
+  };
+  if (d == 0 || !even()) {
+    x = x.contiguous();
+    *ld = heads * d;
+  }
+  return x;
+}
+
+// rope_append(q, k, v, k_cache, v_cache, kv_off, ctx_len, n_rows, inv_freq, parent, row_off, pos_off,
+//             q_weight, k_weight, eps, interleaved, mscale, n_max, out)
+PyObject* py_rope_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 19);
+    at::Tensor q = optional(args[0]), k = gpu_tensor(args[1]), v = gpu_tensor(args[2]);
+    const at::Tensor kc = gpu_tensor(args[3]), vc = gpu_tensor(args[4]);
+    at::Tensor kv_off = gpu_tensor(args[5]), ctx = gpu_tensor(args[6]), rows_of = gpu_tensor(args[7]);
+    at::Tensor freq = optional(args[8]), parent = optional(args[9]), row_off = optional(args[10]),
+               pos_off = optional(args[11]), qw = optional(args[12]), kw = optional(args[13]);
+    const float eps = as_f32(args[14]), mscale = as_f32(args[16]);
+    const bool interleaved = truth(args[15]);
+    const bool packed = row_off.defined();
+    const int64_t dims = packed ? 3 : 4;
+    if (k.dim() != dims || v.dim() != dims || (q.defined() && q.dim() != dims))
+      fail(packed ? "with row_off, q, k and v must be [rows, heads, d]"
+                  : "q, k and v must be [batch, n_max, heads, d] (or [rows, heads, d] with row_off)");
+    const int64_t d = k.size(-1), hkv = k.size(-2), hq = q.defined() ? q.size(-2) : 0;
+    const auto lead = k.sizes().slice(0, dims - 2);
+    if (k.sizes() != v.sizes() || (q.defined() && (q.sizes().slice(0, dims - 2) != lead || q.size(-1) != d)))
+      fail("q, k and v must have the same rows and head dim");
+    const int32_t dtype = dtype_code(k);
+    if (v.scalar_type() != k.scalar_type() || (q.defined() && q.scalar_type() != k.scalar_type()))
+      fail("q, k and v must have one dtype");
+    want_caches(kc, vc, k, d);
+    if (kc.size(1) != hkv) fail("the caches must have the heads of k");
+    if (rows_of.dim() != 1) fail("n_rows must be [batch]");
+    const int64_t batch = rows_of.size(0);
+    int64_t rows = k.size(0), n_max = rows;
+    if (!packed) {
+      if (k.size(0) != batch) fail("n_rows must have an entry for each sequence of k");
+      n_max = k.size(1);
+      rows = batch * n_max;
+    }
+    if (args[17] != Py_None) {
+      const int64_t want = as_i32(args[17]);
+      if (packed) n_max = want;
+      else if (want != n_max) fail("n_max does not match the padded rows");
+    }
+    if (rows > INT32_MAX || n_max > INT32_MAX) fail("too many rows");
+    want_ints(rows_of, at::kInt, {batch}, "n_rows");
+    want_ints(ctx, at::kInt, {batch}, "ctx_len");
+    want_ints(kv_off, at::kLong, {batch}, "kv_off");
+    want_ints(row_off, at::kLong, {batch}, "row_off");
+    want_ints(pos_off, at::kInt, {batch}, "pos_off");
+    want_ints(parent, at::kInt, {batch, n_max}, "parent");
+    int32_t rot = 0;
+    if (freq.defined()) {
+      if (freq.scalar_type() != at::kFloat || freq.dim() != 1) fail("inv_freq must be float32 [rot / 2]");
+      if (freq.size(0) > d) fail("inv_freq has more entries than a head has pairs");
+      rot = 2 * (int32_t)freq.size(0);
+      freq = freq.contiguous();
+    }
+    for (at::Tensor* w : {&qw, &kw}) {
+      if (!w->defined()) continue;
+      if (w->scalar_type() != k.scalar_type() || w->dim() != 1 || w->size(0) != d)
+        fail("the norm weights must be [d] of the rows' dtype");
+      *w = w->contiguous();
+    }
+    for (const at::Tensor* x : {&q, &v, &kv_off, &ctx, &rows_of, &freq, &parent, &row_off, &pos_off, &qw, &kw})
+      same_device(*x, k);
+    for (at::Tensor* x : {&kv_off, &ctx, &rows_of, &parent, &row_off, &pos_off})
+      if (x->defined()) *x = x->contiguous();
+    int64_t q_ld = 0, k_ld = 0, v_ld = 0;
+    if (q.defined()) q = even_rows(q, &q_ld);
+    k = even_rows(k, &k_ld);
+    v = even_rows(v, &v_ld);
+    at::Tensor out;
+    if (q.defined()) out = output(args[18], q.sizes(), q.scalar_type(), k);
+    else if (args[18] != Py_None) fail("out needs q");
+    at::Tensor status = empty({batch}, at::kInt, k);
+    const OnDevice on(k);
+    void* s = stream_of(k);
+    const void *qp = data<void>(q), *kp = data<void>(k), *vp = data<void>(v), *qwp = data<void>(qw), *kwp = data<void>(kw);
+    void *op = data<void>(out), *kcp = data<void>(kc), *vcp = data<void>(vc);
+    const int64_t *rop = data<int64_t>(row_off), *kop = data<int64_t>(kv_off);
+    const int32_t *np = data<int32_t>(rows_of), *pp = data<int32_t>(parent), *cp = data<int32_t>(ctx),
+                  *pop = data<int32_t>(pos_off);
+    const float* fp = data<float>(freq);
+    int32_t* stp = data<int32_t>(status);
+    const int64_t cache_rows = kc.size(0);
+    check(unlocked([&] {
+            return cure_rope_append(qp, q_ld, kp, k_ld, vp, v_ld, dtype, rows, (int32_t)batch, (int32_t)n_max, rop, np,
+                                    pp, kop, cp, pop, (int32_t)hq, (int32_t)hkv, (int32_t)d, qwp, kwp, eps, fp, rot,
+                                    interleaved ? CURE_ROPE_INTERLEAVED : 0u, mscale, op, kcp, vcp, cache_rows, stp, s);
+          }), "cure_rope_append");
+    PyObject* r = PyTuple_New(2);
+    if (!r) throw PyError{};
+    if (q.defined()) {
+      PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(out));
+    } else {
+      Py_INCREF(Py_None);
+      PyTuple_SET_ITEM(r, 0, Py_None);
+    }
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(status));
+    return r;
+  });
+}
+
+// (o, lse or None[, status])
+PyObject* attn_result(const at::Tensor& o, const at::Tensor& lse, const at::Tensor& status) {
+  PyObject* r = PyTuple_New(status.defined() ? 3 : 2);
+  if (!r) throw PyError{};
+  PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(o));
+  if (lse.defined()) {
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(lse));
+  } else {
+    Py_INCREF(Py_None);
+    PyTuple_SET_ITEM(r, 1, Py_None);
+  }
+  if (status.defined()) PyTuple_SET_ITEM(r, 2, THPVariable_Wrap(status));
+  return r;
+}
+
+// prompt_attn(q, k, v, row_off, n_rows, kv_off, ctx_len, host_n_rows, host_ctx_len, scale, out_dtype,
+//             kv_split, with_lse, out)
+PyObject* py_prompt_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 14);
+    at::Tensor t[7];                     // q, k, v, row_off, n_rows, kv_off, ctx_len
+    for (int i = 0; i < 7; ++i) t[i] = gpu_tensor(args[i]);
+    const at::Tensor &q = t[0], &k = t[1], &v = t[2];
+    if (q.dim() != 3 || !q.is_contiguous()) fail("q must be [rows, hq, d], contiguous");
+    const int64_t rows = q.size(0), hq = q.size(1), d = q.size(2);
+    want_caches(k, v, q, d);
+    if (t[4].dim() != 1) fail("n_rows must be [batch]");
+    const int64_t batch = t[4].size(0), hkv = k.size(1);
+    want_ints(t[3], at::kLong, {batch}, "row_off");
+    want_ints(t[4], at::kInt, {batch}, "n_rows");
+    want_ints(t[5], at::kLong, {batch}, "kv_off");
+    want_ints(t[6], at::kInt, {batch}, "ctx_len");
+    for (int i = 3; i < 7; ++i) {
+      same_device(t[i], q);
+      t[i] = t[i].contiguous();
+    }
+    const std::vector<int32_t> hn = host_sizes(args[7], batch), hc = host_sizes(args[8], batch);
+    const float scale = as_f32(args[9]);
+    const int32_t split = as_i32(args[11]);
+    const bool with_lse = truth(args[12]);
+    at::Tensor o = output(args[13], q.sizes(), out_dtype(args[10], q), q);
+    at::Tensor lse = with_lse ? empty({rows, hq}, at::kFloat, q) : at::Tensor();
+    const int32_t dt = dtype_code(q), odt = dtype_code(o);
+    const OnDevice on(q);
+    void* s = stream_of(q);
+    const Scratch ws(q, cure_prompt_attn_workspace_size((int32_t)batch, rows, (int32_t)hq, (int32_t)hkv, (int32_t)d,
+                                                        hn.data(), hc.data(), split));
+    const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
+    void* op = o.data_ptr();
+    float* lp = data<float>(lse);
+    const int64_t *rop = data<int64_t>(t[3]), *kop = data<int64_t>(t[5]);
+    const int32_t *np = data<int32_t>(t[4]), *cp = data<int32_t>(t[6]);
+    check(unlocked([&] {
+            return cure_prompt_attn(qp, kp, vp, op, lp, dt, odt, (int32_t)batch, rows, (int32_t)hq, (int32_t)hkv,
+                                    (int32_t)d, scale, rop, np, kop, cp, hn.data(), hc.data(), split, ws.ptr, ws.bytes,
+                                    s);
+          }), "cure_prompt_attn");
+    return attn_result(o, lse, at::Tensor());
+  });
+}
+
+// prefix_attn(q, k, v, prefix_off, prefix_len, kv_off, ctx_len, n_nodes, parent, host_ctx_len, host_n_nodes,
+//             scale, out_dtype, kv_split, with_lse, out)
+PyObject* py_prefix_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 16);
+    const at::Tensor q = gpu_tensor(args[0]), k = gpu_tensor(args[1]), v = gpu_tensor(args[2]);
+    at::Tensor t[4];                     // kv_off, ctx_len, n_nodes, parent
+    for (int i = 0; i < 4; ++i) t[i] = gpu_tensor(args[5 + i]);
+    if (q.dim() != 4 || !q.is_contiguous()) fail("q must be [batch, n_max, hq, d], contiguous");
+    const int64_t batch = q.size(0), n_max = q.size(1), hq = q.size(2), d = q.size(3);
+    want_caches(k, v, q, d);
+    const int64_t hkv = k.size(1);
+    want_ints(t[0], at::kLong, {batch}, "kv_off");
+    want_ints(t[1], at::kInt, {batch}, "ctx_len");
+    want_ints(t[2], at::kInt, {batch}, "n_nodes");
+    want_ints(t[3], at::kInt, {batch, n_max}, "parent");
+    for (at::Tensor& x : t) {
+      same_device(x, q);
+      x = x.contiguous();
+    }
+    const int64_t prefix_off = PyLong_AsLongLong(args[3]);
+    if (prefix_off == -1 && PyErr_Occurred()) throw PyError{};
+    const int64_t prefix_len = PyLong_AsLongLong(args[4]);
+    if (prefix_len == -1 && PyErr_Occurred()) throw PyError{};
+    if (prefix_off < 0 || prefix_len < 0 || prefix_off > k.size(0) - prefix_len)
+      fail("the prefix must lie inside the cache");
+    if (prefix_len > INT32_MAX) fail("the prefix is too long");
+    const std::vector<int32_t> hc = host_sizes(args[9], batch), hn = host_sizes(args[10], batch);
+    const float scale = as_f32(args[11]);
+    const int32_t split = as_i32(args[13]);
+    const bool with_lse = truth(args[14]);
+    at::Tensor o = output(args[15], q.sizes(), out_dtype(args[12], q), q);
+    at::Tensor lse = with_lse ? empty({batch, n_max, hq}, at::kFloat, q) : at::Tensor();
+    at::Tensor status = empty({batch}, at::kInt, q);
+    const int32_t dt = dtype_code(q), odt = dtype_code(o);
+    const OnDevice on(q);
+    void* s = stream_of(q);
+    const Scratch ws(q, cure_prefix_attn_workspace_size((int32_t)batch, (int32_t)hq, (int32_t)hkv, (int32_t)d,
+                                                        (int32_t)n_max, (int32_t)prefix_len, hc.data(), hn.data(),
+                                                        split));
+    const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
+    void* op = o.data_ptr();
+    float* lp = data<float>(lse);
+    const int64_t* kop = data<int64_t>(t[0]);
+    const int32_t *cp = data<int32_t>(t[1]), *np = data<int32_t>(t[2]), *pp = data<int32_t>(t[3]);
+    int32_t* stp = data<int32_t>(status);
+    check(unlocked([&] {
+            return cure_prefix_attn(qp, kp, vp, op, lp, dt, odt, (int32_t)batch, (int32_t)hq, (int32_t)hkv, (int32_t)d,
+                                    scale, prefix_off, (int32_t)prefix_len, kop, cp, np, pp, (int32_t)n_max, hc.data(),
+                                    hn.data(), split, stp, ws.ptr, ws.bytes, s);
+          }), "cure_prefix_attn");
+    return attn_result(o, lse, status);
+  });
+}
+
 // setup(CureError, host_i32)
 PyObject* py_setup(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -530,8 +845,9 @@ PyObject* py_setup(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(setup),       FAST(margins), FAST(tree_attn), FAST(accept),
-                         FAST(repair_tree), FAST(commit),  {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(setup),       FAST(margins),     FAST(tree_attn),   FAST(accept),
+                         FAST(repair_tree), FAST(commit),      FAST(rope_append), FAST(prompt_attn),
+                         FAST(prefix_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,993 @@
+// cure_prompt_attn: causal attention of new tokens over their context and themselves
+// (whole prompts, chunks of them, single tokens), sequences packed without padding.
+// cure_prefix_attn: tree verification of sequences that share a prefix, whose keys and
+// values are read once for all of them; each node's own context and tree take
+// cure_tree_attn, and the two parts are joined by their log-sum-exps.
+//
+// Both are one kernel over (tile of query rows, kv-head, split of the keys): query row R of
+// a kv-head is query head R % group of token R / group, so the heads that share keys share
+// a tile. It sees the keys up to its own position (a prompt) or all of them (a prefix, where
+// the tokens are the nodes of all sequences, without those that a sequence does not have).
+//
+//   S^T = K Q^T,  P = 2^(c S - m),  l += sum P,  O^T += V^T P^T,  o = O / l
+// in one pass over the keys with the running reference m and sum l in fp32. P is rounded to
+// bf16 for its product, as the matrix instruction takes no wider operand beside bf16
+// values, and l sums the rounded values, so that o is a weighted mean of v exactly.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "common.hpp"
+#include "host_util.hpp"
+#include "mfma_tile.hpp"
+
+namespace cure {
+namespace {
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kStep = 32;            // tokens per step of the key loop
+constexpr int kWaves = 4;            // waves per workgroup, 32 query rows each
+constexpr int kRows = 32 * kWaves;   // query rows per tile
+constexpr int kMinTps = 256;         // tokens per split, at least
+constexpr int kMaxPrefixBatch = 1024;
+
+struct Args {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  int32_t out_bf16;
+  int32_t hq, hkv, group;
+  int32_t batch, n_max;
+  float scale_log2;
+  const int64_t* row_off;            // prompt: first row of q and o per sequence
+  const int32_t* n_rows;             // tokens, or nodes, per sequence
+  const int64_t* kv_off;
+  const int32_t* ctx_len;
+  int64_t prefix_off;
+  int32_t prefix_len;
+  int32_t tps, max_splits;
+  float* part_o;                     // [row][hq][max_splits][d]
+  float* part_lse;                   // [row][hq][max_splits]
+};
+
+CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int s) {
+  return (row * a.hq + head) * a.max_splits + s;
+}
+
+// Splits of `keys` keys; the last one runs to the end.
+CURE_DEV int split_count(const Args& a, int keys) {
+  return max(1, min((keys + a.tps - 1) / a.tps, a.max_splits));
+}
+
+// What a workgroup works on: packed query rows r0 .. of `rows` in all, against cache rows
+// key0 + [begin, end).
+struct Work {
+  int hk, r0, rows, s, splits;
+  int begin, end, keys;
+  int64_t key0;
+  int64_t row0;                      // prompt: the sequence's first row
+  int ctx;
+};
+
+struct Shared {
+  int first[kMaxPrefixBatch + 1];    // prefix: nodes before each sequence
+};
+
+// Prompt: grid (kv-heads x tiles, splits, sequences); a sequence's last tiles, which see the
+// most keys, come first.
+CURE_DEV bool locate_prompt(const Args& a, Work& w) {
+  const int b = blockIdx.z, x = blockIdx.x / a.hkv;
+  w.hk = blockIdx.x - x * a.hkv;
+  const int n_raw = a.n_rows[b];
+  w.ctx = a.ctx_len[b];
+  w.row0 = a.row_off[b];
+  w.key0 = a.kv_off[b];
+  asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.row0), "s"(w.key0));
+  const int n = min(n_raw, a.n_max);
+  w.rows = n * a.group;
+  const int tiles = (w.rows + kRows - 1) / kRows;
+  if (n <= 0 || x >= tiles) return false;
+  w.r0 = (tiles - 1 - x) * kRows;
+  w.keys = w.ctx + (min(w.r0 + kRows, w.rows) - 1) / a.group + 1;
+  return true;
+}
+
+// Prefix: grid (kv-heads x tiles, splits); the tiles hold the existing nodes of all
+// sequences in order, whose counts are summed here.
+CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
+  const int x = blockIdx.x / a.hkv;
+  w.hk = blockIdx.x - x * a.hkv;
+  if (threadIdx.x < kWave) {
+    const int lane = threadIdx.x;
+    int sum = 0;
+    if (lane == 0) sh.first[0] = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+      const int b = b0 + lane;
+      int v = b < a.batch ? min(max(a.n_rows[b], 0), a.n_max) : 0;
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) {
+        const int u = __shfl_up(v, d);
+        if (lane >= d) v += u;
+      }
+      if (b < a.batch) sh.first[b + 1] = sum + v;
+      sum += __shfl(v, kWave - 1);
+    }
+  }
+  __syncthreads();
+  w.rows = sh.first[a.batch] * a.group;
+  w.r0 = x * kRows;
+  w.key0 = a.prefix_off;
+  w.keys = a.prefix_len;
+  w.ctx = 0;
+  w.row0 = 0;
+  return w.r0 < w.rows;
+}
+
+template <bool kPrefix>
+CURE_DEV bool locate(const Args& a, Work& w, Shared& sh) {
+  if (!(kPrefix ? locate_prefix(a, w, sh) : locate_prompt(a, w))) return false;
+  w.s = blockIdx.y;
+  w.splits = split_count(a, w.keys);
+  if (w.s >= w.splits) return false;
+  w.begin = w.s * a.tps;
+  w.end = w.s == w.splits - 1 ? w.keys : w.begin + a.tps;
+  return true;
+}
+
+// Packed row R: its row of q and o, its query head and the last key that it sees.
+struct Row {
+  int64_t row;
+  int head, last;
+};
+template <bool kPrefix>
+CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
+  const int t = R / a.group;
+  Row r;
+  r.head = w.hk * a.group + (R - t * a.group);
+  if (kPrefix) {
+    int lo = 0, hi = a.batch - 1;                  // the last sequence with first[b] <= t
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (sh.first[mid] <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    r.row = (int64_t)lo * a.n_max + (t - sh.first[lo]);
+    r.last = w.keys - 1;
+  } else {
+    r.row = w.row0 + t;
+    r.last = w.ctx + t;
+  }
+  return r;
+}
+
+CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, float x3) {
+  if (a.out_bf16) {
+    uint2 pk;
+    pk.x = pack_bf16x2(x0, x1);
+    pk.y = pack_bf16x2(x2, x3);
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.o) + idx) = pk;
+  } else {
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.o) + idx) = make_float4(x0, x1, x2, x3);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// bf16 kernel: 32 query rows per wave, 32x32x16 matrix instructions.
+//
+// Lane l = 32 half + col owns query row col of its wave, half of its scores:
+//   S^T: A = K row col of the step's 32, columns 16 kk + 8 half .. +7; B = Q row col, same
+//        columns; D register r = score of token 8 (r / 4) + 4 half + r % 4
+//   O^T: k index 8 half + j of k-step ks stands for token 16 ks + 8 (j / 4) + 4 half + j % 4,
+//        the probability that the lane holds; A = V^T by transposed LDS reads;
+//        D register r of block i = column 32 i + 8 (r / 4) + 4 half + r % 4 of row col.
+// Rings of kRing steps of K and of V in LDS are filled by DMA. Step h forms the scores of
+// step h + 1, the probabilities of step h and the products of step h - 1: three parts that
+// do not wait for each other, so the matrix instructions and the softmax's vector
+// instructions of one wave interleave.
+template <int D>
+struct Geo {
+  using T = TileGeo<D>;
+  static constexpr int kRing = 4;
+  static constexpr int kBytes = kStep * T::kRowBytes;        // one step of K or V
+  static constexpr int kDma = kBytes / 1024 / kWaves;        // 1 KB blocks per wave and tensor
+  static_assert(kDma >= 1, "every wave moves part of each step");
+};
+
+// A row's probabilities of one step, as the products take them.
+struct Probs {
+  bf16x8 v[2];
+};
+
+template <int D, bool kPrefix>
+__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
+  using T = TileGeo<D>;
+  using G = Geo<D>;
+  constexpr int kRing = G::kRing;
+  constexpr int kKK = D / 16;                      // k-steps of the scores
+  constexpr int kBlk = D / 32;                     // 32-column blocks of the output
+  // Beyond what a step needs, the DMA of the two steps before it may be in flight.
+  constexpr int kVmWait = waitcnt_vm((kRing - 2) * 2 * G::kDma);
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[kRing * G::kBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_v[kRing * G::kBytes];
+  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
+  Shared& sh = reinterpret_cast<Shared&>(s_map);
+
+  Work w;
+  if (!locate<kPrefix>(a, w, sh)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+
+  // The tile stream: per wave and step, kDma blocks of K and of V. The buffer resource
+  // covers the step's own rows of the keys, so that the rest of a step reads as zeros and a
+  // step past the split's end reads nothing; its base moves on in 64 bits.
+  const uint32_t tok_bytes = (uint32_t)(a.hkv * T::kRowBytes);
+  uint32_t src[G::kDma];
+#pragma unroll
+  for (int j = 0; j < G::kDma; ++j) {
+    const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
+    const int row = byte / T::kRowBytes;
+    src[j] = (uint32_t)row * tok_bytes +
+             (uint32_t)(w.hk * T::kRowBytes + ((((byte % T::kRowBytes) >> 4) ^ T::swz(row)) << 4));
+  }
+  const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const uint32_t k_lds = lds_addr(s_k), v_lds = lds_addr(s_v);
+  const uint32_t dma0 = __builtin_amdgcn_readfirstlane(wave * G::kDma * 1024);
+  const int steps = (w.end - w.begin + kStep - 1) / kStep;
+  auto dma = [&](const char* p, uint32_t lds, int h) {
+    const int left = min(w.end - w.begin - h * kStep, kStep);
+    const i32x4 rsrc = raw_rsrc(p + (int64_t)h * kStep * tok_bytes, left > 0 ? (uint32_t)left * tok_bytes : 0u);
+#pragma unroll
+    for (int j = 0; j < G::kDma; ++j) dma16(lds + dma0 + j * 1024, src[j], rsrc);
+  };
+#pragma unroll
+  for (int h = 0; h < kRing; ++h) {
+    dma(kp, k_lds + h * G::kBytes, h);
+    if (h < 2) dma(vp, v_lds + h * G::kBytes, h);
+  }
+
+  // This lane's query row.
+  const int R = w.r0 + wave * 32 + col;
+  const bool row_ok = R < w.rows;
+  const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
+  bf16x8 q[kKK];
+  {
+    const uint16_t* qrow = reinterpret_cast<const uint16_t*>(a.q) + (me.row * a.hq + me.head) * D;
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) {
+      Pack8 p;
+      p.u = *reinterpret_cast<const uint4*>(qrow + kk * 16 + half * 8);
+      q[kk] = p.v;
+    }
+  }
+  // Keys that the wave's first and last row see, relative to the split; the steps it takes.
+  const bool wave_ok = w.r0 + wave * 32 < w.rows;
+  const int last = me.last - w.begin;
+  const int first_last = __builtin_amdgcn_readfirstlane(last);
+  const int last_last = __builtin_amdgcn_readlane(last, 31);
+  const int my_steps = wave_ok ? min(steps, max(0, (last_last + kStep) / kStep)) : 0;
+  const int full = min(my_steps, max(0, (first_last + 1) / kStep));   // steps that every row sees whole
+
+  // LDS addresses of this lane's operands in slot 0.
+  uint32_t k_at[kKK];
+#pragma unroll
+  for (int kk = 0; kk < kKK; ++kk) k_at[kk] = k_lds + T::offset(col, 2 * kk + half);
+  uint32_t v_at[kBlk];
+  {
+    const int j = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < kBlk; ++i)
+      v_at[i] = v_lds + T::offset(4 * half + (j >> 2), 4 * i + 2 * g + ((j & 3) >> 1)) + (j & 1) * 8;
+  }
+
+  f32x16 o[kBlk];
+#pragma unroll
+  for (int i = 0; i < kBlk; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  float m = 0.f, l = 0.f;
+  const float c = a.scale_log2;
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  // Lambdas take ring slots as byte offsets: constants in the main loop.
+  auto scores = [&](f32x16& x, uint32_t slot) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk)
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(k_at[kk] + slot), q[kk], x, 0, 0, 0);
+  };
+  auto values = [&](uint32_t slot, int ks, int i) {
+    Pack8 f;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) f.h[r] = lds_read_tr8(v_at[i] + slot + (16 * ks + 8 * r) * T::kRowBytes);
+    return f;
+  };
+  auto products = [&](const Probs& p, uint32_t slot) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i)
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(slot, ks, i).v, p.v[ks], o[i], 0, 0, 0);
+  };
+  // Probabilities against the reference m, and this lane's share of their sum.
+  auto exps = [&](const f32x16& x, Probs& p) {
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (__bf16)fast_exp2(fmaf(x[8 * ks + e], c, -m));
+      p.v[ks] = v;
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        l0 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[e], v[e + 1]}, ones, l0, false);
+        l1 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[e + 2], v[e + 3]}, ones, l1, false);
+      }
+    }
+    return l0 + l1;
+  };
+  auto row_max = [&](const f32x16& x) {
+    float mx = max3_raw(x[0], x[1], x[2]);
+#pragma unroll
+    for (int r = 3; r < 15; r += 2) mx = max3_raw(mx, x[r], x[r + 1]);
+    return max_halves(max3_raw(mx, x[15], x[15])) * c;
+  };
+  // Moves the reference where a row's maximum has risen by more than 2^8, which no row's has
+  // while every lane's probabilities sum to 2^8 at most.
+  auto settle = [&](const f32x16& x, Probs& p, float ls) {
+    if (__builtin_expect(__ballot(!(ls <= 256.f)) != 0, 0)) {
+      const float mx = row_max(x);
+      const bool grow = mx > m + kRescaleLog2;
+      const float alpha = grow ? fast_exp2(m - mx) : 1.f;
+      m = grow ? mx : m;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i) o[i] *= alpha;
+      ls = exps(x, p);
+    }
+    l += ls;
+  };
+  // The products of a step that some rows see in part: a token that a row does not see must
+  // not reach it, but 0 times an infinity or a NaN would. Where the step's values hold one, the
+  // products take zeros in its place and the rows that do see it take it as it is.
+  auto hidden_products = [&](const Probs& p, uint32_t slot, int h) {
+    float probe = 0.f;                             // a NaN from the first value that is not finite
+#pragma unroll
+    for (int n = 0; n < 2 * kBlk; ++n) {
+      const bf16x8 f = values(slot, n / kBlk, n % kBlk).v;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        probe = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f[e], f[e + 1]}, bf16x2{(__bf16)0.f, (__bf16)0.f}, probe, false);
+    }
+    if (__builtin_expect(__ballot(probe != 0.f) == 0, 1)) {
+      products(p, slot);
+      return;
+    }
+    const auto clean = [](uint32_t u) {
+      const uint32_t lo = (u & 0x7f80u) == 0x7f80u ? 0u : 0xffffu;
+      const uint32_t hi = (u & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
+      return u & (lo | hi);
+    };
+#pragma unroll
+    for (int n = 0; n < 2 * kBlk; ++n) {
+      Pack8 f = values(slot, n / kBlk, n % kBlk);
+      f.u = make_uint4(clean(f.u.x), clean(f.u.y), clean(f.u.z), clean(f.u.w));
+      o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p.v[n / kBlk], o[n % kBlk], 0, 0, 0);
+    }
+    for (int t = 0; t < kStep; ++t) {
+      const bool seen = h * kStep + t <= last;
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {              // columns 32 i + 8 g + 4 half .. +3
+          const uint32_t at = v_lds + slot + T::offset(t, 4 * i + g) + 8 * half;
+          const u32x2 u = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)at;
+          const float x[4] = {bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][4 * g + e] += seen && !(fabsf(x[e]) < INFINITY) ? x[e] : 0.f;
+        }
+    }
+  };
+  auto mask = [&](f32x16& x, int h) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      x[r] = h * kStep + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? x[r] : -INFINITY;
+  };
+  // Step h begins: its slots (h + 1 of K, h - 1 of V) have landed for every wave, and those that
+  // step h - 1 read (h of K, h - 2 of V) are refilled.
+  auto begin = [&](int h, uint32_t k_slot, uint32_t v_slot) {
+    __builtin_amdgcn_s_waitcnt(kVmWait);
+    __syncthreads();
+    dma(kp, k_lds + k_slot, h + kRing);
+    dma(vp, v_lds + v_slot, h + 2);
+  };
+
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (!row_ok) {
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) q[kk] = bf16x8{};
+  }
+  // Scores and probabilities of the present step, of the next and of the one before.
+  f32x16 x;
+  Probs p;
+  if (my_steps > 0) {
+    scores(x, 0);
+    if (full == 0) mask(x, 0);
+    // The first reference: the row's maximum. A row that sees nothing here has no finite
+    // one, and probabilities of zero against any.
+    const float mx = row_max(x);
+    m = mx == -INFINITY ? 0.f : mx;
+  }
+  begin(0, 0, 2 * G::kBytes);
+  int h = 1;
+  if (my_steps > 0) {
+    l = exps(x, p);
+    scores(x, G::kBytes);
+    // Steps that every row sees whole, a ring's turn at a time.
+    for (; h + kRing <= full; h += kRing) {
+#pragma unroll
+      for (int j = 1; j <= kRing; ++j) {           // step h + j - 1, j modulo the ring
+        f32x16 y;
+        Probs n;
+        begin(h + j - 1, j % kRing * G::kBytes, (j + 2) % kRing * G::kBytes);
+        scores(y, (j + 1) % kRing * G::kBytes);
+        const float ls = exps(x, n);
+        products(p, (j + 3) % kRing * G::kBytes);
+        settle(x, n, ls);
+        x = y;
+        p = n;
+      }
+    }
+    for (; h <= my_steps; ++h) {
+      const uint32_t slot = (uint32_t)(h % kRing) * G::kBytes;
+      begin(h, slot, (uint32_t)((h + 2) % kRing) * G::kBytes);
+      f32x16 y;
+      scores(y, (uint32_t)((h + 1) % kRing) * G::kBytes);
+      hidden_products(p, (uint32_t)((h + 3) % kRing) * G::kBytes, h - 1);
+      if (h < my_steps) {
+        if (h >= full) mask(x, h);
+        settle(x, p, exps(x, p));
+        x = y;
+      }
+    }
+  }
+  for (; h <= steps; ++h) begin(h, (uint32_t)(h % kRing) * G::kBytes, (uint32_t)((h + 2) % kRing) * G::kBytes);
+
+  __builtin_amdgcn_s_waitcnt(0);                   // the rings' trailing DMA lands before exit
+  if (!row_ok) return;
+  const float lt = sum_halves(l);
+  const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);   // a NaN stays one
+  const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
+  const bool whole = w.splits == 1 && !kPrefix;
+  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.s);
+  const int64_t orow = me.row * a.hq + me.head;
+#pragma unroll
+  for (int i = 0; i < kBlk; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d0 = 32 * i + 8 * g + 4 * half;
+      const float x0 = o[i][4 * g] * inv, x1 = o[i][4 * g + 1] * inv;
+      const float x2 = o[i][4 * g + 2] * inv, x3 = o[i][4 * g + 3] * inv;
+      if (whole) store4(a, orow * D + d0, x0, x1, x2, x3);
+      else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x0, x1, x2, x3);
+    }
+  if (half == 0) {
+    if (!whole) a.part_lse[pi] = lse;
+    else if (a.lse) a.lse[orow] = lse;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// fp32 kernel: 32 query rows per wave, 32x32x2 fp32 matrix instructions, products and
+// sums in fp32 throughout.
+//
+// Lane l = 32 half + col owns query row col of its wave:
+//   S^T: MFMA i of column group j takes k index half for column 8 j + 4 half + i, so one
+//        16-byte read of K (row col, columns 8 j + 4 half .. +3) feeds four; D register r =
+//        score of token 8 (r / 4) + 4 half + r % 4
+//   O^T: MFMA r takes k index half for that token, the probability the lane holds; output
+//        row c' of block i stands for column (D / 32) c' + i, so one read of V (the token's
+//        row, columns (D / 32) col ..) feeds all D / 32 blocks.
+template <int D>
+struct GeoF32 {
+  static constexpr int kRowBytes = 4 * D;
+  static constexpr int kBytes = kStep * kRowBytes;
+  static constexpr int kDma = kBytes / 1024 / kWaves;
+  static CURE_DEV int offset(int row, int chunk) { return row * kRowBytes + ((chunk ^ (row & 15)) << 4); }
+};
+
+template <int D, bool kPrefix>
+__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
+  using G = GeoF32<D>;
+  constexpr int kJ = D / 8;                        // column groups of the scores
+  constexpr int kBlk = D / 32;                     // output blocks
+  typedef float vfrag __attribute__((ext_vector_type(D / 32)));
+  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2][2][G::kBytes];   // [buffer][K, V]
+  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
+  Shared& sh = reinterpret_cast<Shared&>(s_map);
+
+  Work w;
+  if (!locate<kPrefix>(a, w, sh)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+
+  const uint32_t tok_bytes = (uint32_t)(a.hkv * G::kRowBytes);
+  uint32_t src[G::kDma];
+#pragma unroll
+  for (int j = 0; j < G::kDma; ++j) {
+    const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
+    const int row = byte / G::kRowBytes;
+    src[j] = (uint32_t)row * tok_bytes +
+             (uint32_t)(w.hk * G::kRowBytes + ((((byte % G::kRowBytes) >> 4) ^ (row & 15)) << 4));
+  }
+  const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const int steps = (w.end - w.begin + kStep - 1) / kStep;
+  auto dma = [&](int buf, int h) {
+    const int left = min(w.end - w.begin - h * kStep, kStep);
+    const uint32_t bytes = left > 0 ? (uint32_t)left * tok_bytes : 0u;
+    const int64_t at = (int64_t)h * kStep * tok_bytes;
+    const i32x4 rk = raw_rsrc(kp + at, bytes), rv = raw_rsrc(vp + at, bytes);
+#pragma unroll
+    for (int j = 0; j < G::kDma; ++j) {
+      const int blk = (wave * G::kDma + j) * 1024;
+      dma16(lds_addr(&s_kv[buf][0][blk]), src[j], rk);
+      dma16(lds_addr(&s_kv[buf][1][blk]), src[j], rv);
+    }
+  };
+  dma(0, 0);
+
+  const int R = w.r0 + wave * 32 + col;
+  const bool row_ok = R < w.rows;
+  const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
+  f32x4 q[kJ];
+  {
+    const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) q[j] = *reinterpret_cast<const f32x4*>(qrow + 8 * j + 4 * half);
+  }
+  const bool wave_ok = w.r0 + wave * 32 < w.rows;
+  const int last = me.last - w.begin;
+  const int first_last = __builtin_amdgcn_readfirstlane(last);
+  const int last_last = __builtin_amdgcn_readlane(last, 31);
+  const int my_steps = wave_ok ? min(steps, max(0, (last_last + kStep) / kStep)) : 0;
+
+  int k_off[kJ];
+#pragma unroll
+  for (int j = 0; j < kJ; ++j) k_off[j] = G::offset(col, 2 * j + half);
+  // V: row 8 (r / 4) + 4 half + r % 4. The swizzle takes a row's low four bits, so registers r
+  // and r + 8 are 16 rows apart.
+  int v_off[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const int byte = col * (D / 32) * 4;
+    v_off[r] = G::offset(8 * (r >> 2) + 4 * half + (r & 3), byte >> 4) + (byte & 15);
+  }
+
+  f32x16 o[kBlk];
+#pragma unroll
+  for (int i = 0; i < kBlk; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const float c = a.scale_log2;
+
+  __builtin_amdgcn_s_waitcnt(0);
+  if (!row_ok) {
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) q[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int h = 0, buf = 0; h < steps; ++h, buf ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0);                 // this wave's DMA into `buf` has landed
+    __syncthreads();                               // everyone's has; the other buffer is free
+    dma(buf ^ 1, h + 1);
+    if (h >= my_steps) continue;
+    const unsigned char* kt = s_kv[buf][0];
+    const unsigned char* vt = s_kv[buf][1];
+    const auto values = [&](int r) {
+      return *reinterpret_cast<const vfrag*>(vt + (r >> 3) * 16 * G::kRowBytes + v_off[r & 7]);
+    };
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + k_off[j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], q[j][i], x, 0, 0, 0);
+    }
+    const bool tail = h * kStep + kStep - 1 > first_last;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] *= c;
+      if (tail) x[r] = h * kStep + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? x[r] : -INFINITY;
+    }
+    float mt = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mt = fmaxf(mt, x[r]);
+    const float m_new = fmaxf(m, max_halves(mt));
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    if (__ballot(m_new > m)) {                     // a maximum rose: rescale (factor 1 for the others)
+      const float alpha = fast_exp2(m - m_use);
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i) o[i] *= alpha;
+    }
+    m = m_new;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = fast_exp2(x[r] - m_use);
+      l += x[r];
+    }
+    float probe = 0.f;                             // a NaN from a value of a masked step that is not finite
+    if (tail) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const vfrag f = values(r);
+#pragma unroll
+        for (int i = 0; i < kBlk; ++i) probe = fmaf(f[i], 0.f, probe);
+      }
+    }
+    if (__builtin_expect(__ballot(probe != 0.f) == 0, 1)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const vfrag f = values(r);
+#pragma unroll
+        for (int i = 0; i < kBlk; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], x[r], o[i], 0, 0, 0);
+      }
+      continue;
+    }
+    // As in the bf16 kernel: zeros for the values that are not finite, which the rows that see
+    // them take as they are.
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const vfrag f = values(r);
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i)
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(f[i]) < INFINITY ? f[i] : 0.f, x[r], o[i], 0, 0, 0);
+    }
+    for (int t = 0; t < kStep; ++t) {
+      const bool seen = h * kStep + t <= last;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int byte = (8 * (r >> 2) + 4 * half + (r & 3)) * (D / 32) * 4;
+        const vfrag f = *reinterpret_cast<const vfrag*>(vt + G::offset(t, byte >> 4) + (byte & 15));
+#pragma unroll
+        for (int i = 0; i < kBlk; ++i)
+          if (seen && !(fabsf(f[i]) < INFINITY)) o[i][r] += f[i];
+      }
+    }
+  }
+
+  __builtin_amdgcn_s_waitcnt(0);                   // the trailing DMA lands before exit
+  if (!row_ok) return;
+  const float lt = sum_halves(l);
+  const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
+  const float lse = lt == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(lt)) * kLn2;
+  const bool whole = w.splits == 1 && !kPrefix;
+  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.s);
+  const int64_t orow = me.row * a.hq + me.head;
+  // Lane's columns: (D / 32) c' + i for rows c' of the blocks, four consecutive ones at a time.
+#pragma unroll
+  for (int r = 0; r < 16; r += 4 / kBlk) {
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = o[e % kBlk][r + e / kBlk] * inv;
+    const int d0 = kBlk * (8 * (r >> 2) + 4 * half + (r & 3));
+    if (whole) store4(a, orow * D + d0, x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+  if (half == 0) {
+    if (!whole) a.part_lse[pi] = lse;
+    else if (a.lse) a.lse[orow] = lse;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the splits of a row, and for a prefix the tree part, by their log-sum-exps:
+// D / 4 lanes per (row, head), four columns each.
+struct MergeArgs : Args {
+  const float* tree_o;               // prefix: [batch][n_max][hq][d]
+  const float* tree_lse;             // [batch][n_max][hq]
+};
+
+template <int D, bool kPrefix>
+__global__ __launch_bounds__(256) void seq_merge(MergeArgs a) {
+  constexpr int kLanes = D / 4;
+  const int head = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const int col = (threadIdx.x % kLanes) * 4;
+  const int i = blockIdx.y, b = blockIdx.z;
+  if (head >= a.hq) return;
+  const int n = min(a.n_rows[b], a.n_max);
+  if (i >= n) return;
+  int splits;
+  int64_t row;
+  if (kPrefix) {
+    splits = split_count(a, a.prefix_len);
+    row = (int64_t)b * a.n_max + i;
+  } else {
+    // The tile of this row's head decides how many keys its splits covered.
+    const int rows = n * a.group, R = i * a.group + head % a.group;
+    const int end = min((R / kRows + 1) * kRows, rows);
+    splits = split_count(a, a.ctx_len[b] + (end - 1) / a.group + 1);
+    if (splits == 1) return;                       // written whole
+    row = a.row_off[b] + i;
+  }
+  const int64_t p0 = part_index(a, row, head, 0), orow = row * a.hq + head;
+  float m = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float lse, float4 v) {
+    if (lse == -INFINITY) return;                  // saw nothing
+    const float mn = fmaxf(m, lse);
+    const float w0 = fast_exp2((m - mn) * kLog2e), w1 = fast_exp2((lse - mn) * kLog2e);
+    m = mn;
+    sum = sum * w0 + w1;
+    acc.x = acc.x * w0 + v.x * w1;
+    acc.y = acc.y * w0 + v.y * w1;
+    acc.z = acc.z * w0 + v.z * w1;
+    acc.w = acc.w * w0 + v.w * w1;
+  };
+  for (int s = 0; s < splits; ++s)
+    add(a.part_lse[p0 + s], *reinterpret_cast<const float4*>(a.part_o + (p0 + s) * D + col));
+  if (kPrefix) add(a.tree_lse[orow], *reinterpret_cast<const float4*>(a.tree_o + orow * D + col));
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  store4(a, orow * D + col, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+  if (col == 0 && a.lse) a.lse[orow] = sum == 0.f ? -INFINITY : m + logf(sum);
+}
+
+// ---------------------------------------------------------------------------
+// Host: tiles, splits and workspace.
+struct Plan {
+  int tiles;                         // most tiles of a sequence (a prefix: of all nodes)
+  int tps, max_splits;
+};
+
+// Keys are split when the tiles alone leave workgroup slots (two per CU) empty.
+Plan make_plan(int64_t tiles_all, int64_t tiles_max, int hkv, int64_t keys_max, int32_t kv_split) {
+  Plan p{};
+  p.tiles = (int)std::min<int64_t>(tiles_max, INT32_MAX);
+  const auto round_step = [](int64_t t) { return std::max<int64_t>(64, (t + 63) / 64 * 64); };
+  int64_t splits = kv_split;
+  if (splits <= 0) {
+    const int64_t slots = 2 * (int64_t)device_cu_count();
+    splits = std::max<int64_t>(1, slots / std::max<int64_t>(1, tiles_all * hkv));
+    splits = std::min<int64_t>(splits, std::max<int64_t>(1, keys_max / kMinTps));
+  }
+  splits = std::min<int64_t>(splits, 65535);
+  p.tps = (int)std::min<int64_t>(round_step((keys_max + splits - 1) / splits), INT32_MAX / 2);
+  p.max_splits = (int)std::max<int64_t>(1, (keys_max + p.tps - 1) / p.tps);
+  return p;
+}
+
+size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int splits) {
+  const size_t parts = (size_t)rows * hq * splits;
+  return align_up(parts * d * sizeof(float), 256) + align_up(parts * sizeof(float), 256);
+}
+
+void set_parts(Args& a, void* ws, int64_t rows, int32_t d, int splits) {
+  const size_t parts = (size_t)rows * a.hq * splits;
+  a.part_o = static_cast<float*>(ws);
+  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(parts * d * sizeof(float), 256));
+}
+
+Plan prompt_plan(int32_t batch, int32_t hq, int32_t hkv, const int32_t* host_n_rows, const int32_t* host_ctx_len,
+                 int32_t kv_split) {
+  int64_t all = 0, most = 0, keys = 0, longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_rows[b];
+    if (n <= 0) continue;
+    const int64_t tiles = (n * (hq / hkv) + kRows - 1) / kRows;
+    all += tiles;
+    most = std::max(most, tiles);
+    keys = std::max(keys, n + host_ctx_len[b]);
+    longest = std::max(longest, n);
+  }
+  // The merge's grid holds the tokens of a sequence in 16 bits.
+  return make_plan(all, most, hkv, keys, longest > 65535 ? 1 : kv_split);
+}
+
+Plan prefix_plan(int32_t batch, int32_t hq, int32_t hkv, int32_t n_max, int32_t prefix_len,
+                 const int32_t* host_n_nodes, int32_t kv_split) {
+  int64_t nodes = 0;
+  for (int b = 0; b < batch; ++b) nodes += std::min(std::max(host_n_nodes[b], 0), n_max);
+  const int64_t tiles = (nodes * (hq / hkv) + kRows - 1) / kRows;
+  // The device may hold other counts than the host's copies: tiles for every node there may
+  // be, of which those past the last one end at once.
+  const int64_t most = ((int64_t)batch * n_max * (hq / hkv) + kRows - 1) / kRows;
+  return make_plan(tiles, most, hkv, prefix_len, kv_split);
+}
+
+template <bool kPrefix>
+void launch_attn(const Args& a, int32_t dtype, int32_t d, dim3 grid, hipStream_t st) {
+  const dim3 block(64 * kWaves);
+  if (dtype == CURE_BF16) {
+    if (d == 128) hipLaunchKernelGGL((seq_attn<128, kPrefix>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((seq_attn<64, kPrefix>), grid, block, 0, st, a);
+  } else {
+    if (d == 128) hipLaunchKernelGGL((seq_attn_f32<128, kPrefix>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((seq_attn_f32<64, kPrefix>), grid, block, 0, st, a);
+  }
+}
+
+template <bool kPrefix>
+void launch_merge(const MergeArgs& a, int32_t d, hipStream_t st) {
+  const int heads = 1024 / d;
+  const dim3 grid((unsigned)((a.hq + heads - 1) / heads), (unsigned)a.n_max, (unsigned)a.batch);
+  if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((seq_merge<64, kPrefix>), grid, dim3(256), 0, st, a);
+}
+
+// The checks that both calls make of their operands.
+cure_status check(const void* q, const void* k, const void* v, const void* o, int32_t dtype, int32_t out_dtype,
+                  int32_t hq, int32_t hkv, int32_t d, float scale) {
+  if (dtype != CURE_F32 && dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
+  if (out_dtype != CURE_F32 && out_dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
+  if (hq <= 0 || hkv <= 0 || hq % hkv != 0) return CURE_ERR_INVALID_ARG;
+  if (d != 64 && d != 128) return CURE_ERR_UNSUPPORTED;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return CURE_ERR_INVALID_ARG;
+  if ((int64_t)hkv * d * 4 * kStep > INT32_MAX) return CURE_ERR_UNSUPPORTED;
+  const uintptr_t in = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) |
+                       reinterpret_cast<uintptr_t>(v);
+  if (in % 16 != 0 || reinterpret_cast<uintptr_t>(o) % (out_dtype == CURE_BF16 ? 8 : 16) != 0)
+    return CURE_ERR_INVALID_ARG;
+  return CURE_OK;
+}
+
+}  // namespace
+}  // namespace cure
+
+using namespace cure;
+
+extern "C" size_t cure_prompt_attn_workspace_size(int32_t batch, int64_t rows, int32_t hq, int32_t hkv, int32_t d,
+                                                  const int32_t* host_n_rows, const int32_t* host_ctx_len,
+                                                  int32_t kv_split) {
+  if (batch <= 0 || rows <= 0 || hq <= 0 || hkv <= 0 || hq % hkv || d <= 0 || !host_n_rows || !host_ctx_len) return 0;
+  const Plan p = prompt_plan(batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+  return p.max_splits > 1 ? part_bytes(rows, hq, d, p.max_splits) : 0;
+}
+
+extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* o, float* lse,
+                                        int32_t dtype, int32_t out_dtype, int32_t batch, int64_t rows, int32_t hq,
+                                        int32_t hkv, int32_t d, float scale, const int64_t* row_off,
+                                        const int32_t* n_rows, const int64_t* kv_off, const int32_t* ctx_len,
+                                        const int32_t* host_n_rows, const int32_t* host_ctx_len, int32_t kv_split,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (batch < 0 || rows < 0 || kv_split < 0) return CURE_ERR_INVALID_ARG;
+  const cure_status bad = check(q, k, v, o, dtype, out_dtype, hq, hkv, d, scale);
+  if (bad != CURE_OK) return bad;
+  if (batch == 0 || rows == 0) return CURE_OK;
+  if (!q || !k || !v || !o || !row_off || !n_rows || !kv_off || !ctx_len || !host_n_rows || !host_ctx_len)
+    return CURE_ERR_INVALID_ARG;
+  if (batch > 65535) return CURE_ERR_UNSUPPORTED;
+  int64_t longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_rows[b], c = host_ctx_len[b];
+    if (n < 0 || c < 0 || n > rows) return CURE_ERR_INVALID_ARG;
+    if (n + c > INT32_MAX - 4096 || n * (hq / hkv) > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
+    longest = std::max(longest, n);
+  }
+  if (longest == 0) return CURE_OK;
+  const Plan p = prompt_plan(batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+  const size_t need = p.max_splits > 1 ? part_bytes(rows, hq, d, p.max_splits) : 0;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
+  if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
+  if ((int64_t)p.tiles * hkv * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
+  MergeArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.lse = lse;
+  a.out_bf16 = out_dtype == CURE_BF16;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.group = hq / hkv;
+  a.batch = batch;
+  a.n_max = (int32_t)longest;
+  a.scale_log2 = scale * kLog2e;
+  a.row_off = row_off;
+  a.n_rows = n_rows;
+  a.kv_off = kv_off;
+  a.ctx_len = ctx_len;
+  a.tps = p.tps;
+  a.max_splits = p.max_splits;
+  if (need > 0) set_parts(a, workspace, rows, d, p.max_splits);
+  hipStream_t st = as_stream(stream);
+  launch_attn<false>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.max_splits, (unsigned)batch), st);
+  if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
+  if (p.max_splits > 1) launch_merge<false>(a, d, st);
+  return launch_status();
+}
+
+namespace {
+// The workspace of cure_prefix_attn: the prefix's partials, the tree part's output and
+// log-sum-exps, and cure_tree_attn's own.
+struct PrefixSpace {
+  size_t parts, o, lse, tree;
+  size_t total() const { return parts + o + lse + tree; }
+};
+PrefixSpace prefix_space(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max, int splits,
+                         const int32_t* host_ctx_len, const int32_t* host_n_nodes) {
+  const size_t rows = (size_t)batch * n_max * hq;
+  return {part_bytes((int64_t)batch * n_max, hq, d, splits), align_up(rows * d * sizeof(float), 256),
+          align_up(rows * sizeof(float), 256),
+          cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0)};
+}
+}  // namespace
+
+extern "C" size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max,
+                                                  int32_t prefix_len, const int32_t* host_ctx_len,
+                                                  const int32_t* host_n_nodes, int32_t kv_split) {
+  if (batch <= 0 || hq <= 0 || hkv <= 0 || hq % hkv || d <= 0 || n_max <= 0 || prefix_len < 0 || !host_ctx_len ||
+      !host_n_nodes)
+    return 0;
+  if (prefix_len == 0) return cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0);
+  const Plan p = prefix_plan(batch, hq, hkv, n_max, prefix_len, host_n_nodes, kv_split);
+  return prefix_space(batch, hq, hkv, d, n_max, p.max_splits, host_ctx_len, host_n_nodes).total();
+}
+
+extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* o, float* lse,
+                                        int32_t dtype, int32_t out_dtype, int32_t batch, int32_t hq, int32_t hkv,
+                                        int32_t d, float scale, int64_t prefix_off, int32_t prefix_len,
+                                        const int64_t* kv_off, const int32_t* ctx_len, const int32_t* n_nodes,
+                                        const int32_t* parent, int32_t n_max, const int32_t* host_ctx_len,
+                                        const int32_t* host_n_nodes, int32_t kv_split, int32_t* tree_status,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (batch < 0 || n_max < 0 || kv_split < 0 || prefix_off < 0 || prefix_len < 0) return CURE_ERR_INVALID_ARG;
+  const cure_status bad = check(q, k, v, o, dtype, out_dtype, hq, hkv, d, scale);
+  if (bad != CURE_OK) return bad;
+  // Nothing shared, or no nodes: the tree attention is all there is.
+  if (batch == 0 || n_max == 0 || prefix_len == 0)
+    return cure_tree_attn(q, k, v, o, lse, dtype, out_dtype, batch, hq, hkv, d, scale, kv_off, ctx_len, n_nodes,
+                          parent, n_max, host_ctx_len, host_n_nodes, 0, 0, tree_status, workspace, workspace_bytes,
+                          stream);
+  if (n_max > CURE_MAX_TREE_NODES || batch > kMaxPrefixBatch || prefix_len > INT32_MAX - 4096)
+    return CURE_ERR_UNSUPPORTED;
+  if (!q || !k || !v || !o || !kv_off || !ctx_len || !n_nodes || !parent || !host_ctx_len || !host_n_nodes)
+    return CURE_ERR_INVALID_ARG;
+  for (int b = 0; b < batch; ++b)
+    if (host_ctx_len[b] < 0 || host_n_nodes[b] < 0 || host_n_nodes[b] > n_max) return CURE_ERR_INVALID_ARG;
+  const Plan p = prefix_plan(batch, hq, hkv, n_max, prefix_len, host_n_nodes, kv_split);
+  const PrefixSpace sp = prefix_space(batch, hq, hkv, d, n_max, p.max_splits, host_ctx_len, host_n_nodes);
+  if (!workspace || workspace_bytes < sp.total()) return CURE_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
+  if ((int64_t)p.tiles * hkv * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
+  MergeArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.lse = lse;
+  a.out_bf16 = out_dtype == CURE_BF16;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.group = hq / hkv;
+  a.batch = batch;
+  a.n_max = n_max;
+  a.scale_log2 = scale * kLog2e;
+  a.n_rows = n_nodes;
+  a.prefix_off = prefix_off;
+  a.prefix_len = prefix_len;
+  a.tps = p.tps;
+  a.max_splits = p.max_splits;
+  set_parts(a, workspace, (int64_t)batch * n_max, d, p.max_splits);
+  char* ws = static_cast<char*>(workspace) + sp.parts;
+  a.tree_o = reinterpret_cast<float*>(ws);
+  float* tree_lse = reinterpret_cast<float*>(ws + sp.o);
+  a.tree_lse = tree_lse;
+  hipStream_t st = as_stream(stream);
+  launch_attn<true>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.max_splits), st);
+  if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
+  const cure_status tree =
+      cure_tree_attn(q, k, v, ws, tree_lse, dtype, CURE_F32, batch, hq, hkv, d, scale, kv_off, ctx_len, n_nodes,
+                     parent, n_max, host_ctx_len, host_n_nodes, 0, 0, tree_status, ws + sp.o + sp.lse, sp.tree, stream);
+  if (tree != CURE_OK) return tree;
+  launch_merge<true>(a, d, st);
+  return launch_status();
+}

@@ -29,6 +29,8 @@ CURE_F32 = 0
 CURE_BF16 = 1
 CURE_ATTN_FORCE_VALU = 1
 CURE_MAX_TREE_NODES = 256
+CURE_ROPE_INTERLEAVED = 1
+_ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 _lock = threading.Lock()
 _lib = None
@@ -36,6 +38,7 @@ _ext = None
 
 _vp, _i32, _i64, _f32, _sz, _u32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                     ctypes.c_float, ctypes.c_size_t, ctypes.c_uint32)
+_f64 = ctypes.c_double
 
 _SIGNATURES = {
     "cure_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -68,6 +71,18 @@ _SIGNATURES = {
     "cure_commit": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i64, _i32, _i32, _i32,
                                    _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32,
                                    _vp, _vp, _vp, _vp, _vp, _vp]),
+    "cure_rope_append": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i32, _i32,
+                                        _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp,
+                                        _f32, _vp, _i32, _u32, _f32, _vp, _vp, _vp, _i64, _vp, _vp]),
+    "cure_rope_frequencies": (ctypes.c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]),
+    "cure_prompt_attn_workspace_size": (_sz, [_i32, _i64, _i32, _i32, _i32, _vp, _vp, _i32]),
+    "cure_prompt_attn": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i64, _i32, _i32,
+                                        _i32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz,
+                                        _vp]),
+    "cure_prefix_attn_workspace_size": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32]),
+    "cure_prefix_attn": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
+                                        _f32, _i64, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32,
+                                        _vp, _vp, _sz, _vp]),
 }
 
 
@@ -224,6 +239,73 @@ def cure_commit(k, v, kv_off, ctx_len, n_nodes, path, acc_len, token, bonus, cha
     """
     return _native().commit(k, v, kv_off, ctx_len, n_nodes, path, acc_len, token, bonus, chain_len,
                             layer_stride)
+
+
+def cure_rope_frequencies(rot, base=10000.0, scaling=None, factor=1.0, orig_len=0, low=None, high=None):
+    """Frequencies of a rotation over the first rot columns of a head.
+
+    scaling: None, "linear", "base", "bands" (low and high: turns over orig_len, 1 and 4
+    by default) or "ramp" (low and high: 1 and 32 turns by default), for contexts factor
+    times the trained one (orig_len tokens where it is used). Returns (float32 CPU
+    tensor [rot / 2], mscale).
+    """
+    if scaling not in _ROPE_SCALING:
+        raise CureError("unknown scaling %r (None, linear, base, bands or ramp)" % (scaling,))
+    low = 1.0 if low is None else low
+    high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
+    p0, p1 = (high, low) if scaling == "ramp" else (low, high)
+    if rot < 0:
+        raise CureError("rot must not be negative")
+    freq = torch.empty(rot // 2, dtype=torch.float32)
+    mscale = _f32()
+    _check(lib().cure_rope_frequencies(rot, base, _ROPE_SCALING[scaling], factor, orig_len, p0, p1,
+                                       _ptr(freq), ctypes.byref(mscale)), "cure_rope_frequencies")
+    return freq, mscale.value
+
+
+def cure_rope_append(q, k, v, k_cache, v_cache, kv_off, ctx_len, n_rows, inv_freq, parent=None,
+                     row_off=None, pos_off=None, q_weight=None, k_weight=None, eps=1e-6,
+                     interleaved=False, mscale=1.0, n_max=None, out=None):
+    """Normalise and rotate new rows' queries and keys; write keys and values to the cache.
+
+    q [batch, n_max, hq, d] (or None), k, v [batch, n_max, hkv, d]: each sequence's
+    rows padded to n_max; or, with row_off int64 [batch], packed [rows, heads, d] with
+    sequence b's rows from row_off[b] on and n_max a bound on n_rows (default: rows). Rows
+    may be slices of a fused projection's output. k_cache, v_cache [cache_rows, hkv, d].
+    kv_off int64, ctx_len, n_rows and pos_off int32 [batch]; parent int32 [batch, n_max]
+    where the rows are a tree's nodes; q_weight, k_weight [d] to normalise by; inv_freq
+    float32 [rot / 2] or None (all on the GPU). out: the queries' result, as q but
+    contiguous. Returns (queries, status [batch]); rows past a sequence's n_rows are
+    not written.
+    """
+    return _native().rope_append(q, k, v, k_cache, v_cache, kv_off, ctx_len, n_rows, inv_freq, parent,
+                                 row_off, pos_off, q_weight, k_weight, eps, interleaved, mscale, n_max, out)
+
+
+def cure_prompt_attn(q, k, v, row_off, n_rows, kv_off, ctx_len, host_n_rows, host_ctx_len, scale,
+                     out_dtype=None, kv_split=0, with_lse=True, out=None):
+    """Causal attention of packed new tokens over their contexts and themselves.
+
+    q [rows, hq, d], sequence b's n_rows[b] tokens from row_off[b] on; k, v: the caches
+    [cache_rows, hkv, d], in which a sequence's context and new tokens lie from kv_off[b]
+    on; row_off, kv_off int64, n_rows, ctx_len int32 [batch] (all on the GPU);
+    host_n_rows / host_ctx_len: host copies (numpy or lists). Returns (o [rows, hq, d],
+    lse [rows, hq] or None); rows of no sequence are not written.
+    """
+    return _native().prompt_attn(q, k, v, row_off, n_rows, kv_off, ctx_len, host_n_rows, host_ctx_len,
+                                 scale, out_dtype, kv_split, with_lse, out)
+
+
+def cure_prefix_attn(q, k, v, prefix_off, prefix_len, kv_off, ctx_len, n_nodes, parent, host_ctx_len,
+                     host_n_nodes, scale, out_dtype=None, kv_split=0, with_lse=True, out=None):
+    """Tree-masked verification attention of sequences that share a prefix.
+
+    As cure_tree_attn, with the prefix in cache rows prefix_off .. prefix_off + prefix_len
+    - 1 (host integers) before every sequence's own ctx_len rows.
+    Returns (o [batch, n_max, hq, d], lse [batch, n_max, hq] or None, tree_status [batch]).
+    """
+    return _native().prefix_attn(q, k, v, prefix_off, prefix_len, kv_off, ctx_len, n_nodes, parent,
+                                 host_ctx_len, host_n_nodes, scale, out_dtype, kv_split, with_lse, out)
 
 
 def cure_read_ceiling(buf):
