@@ -27,6 +27,7 @@ namespace cure {
 namespace {
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 32;            // tokens per step of the key loop
 constexpr int kWaves = 4;            // waves per workgroup, 32 query rows each
@@ -191,25 +192,41 @@ CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, f
 // instructions of one wave interleave.
 template <int D>
 struct Geo {
-  using T = TileGeo<D>;
   static constexpr int kRing = 4;
-  static constexpr int kBytes = kStep * T::kRowBytes;        // one step of K or V
+  static constexpr int kRowBytes = 2 * D;
+  static constexpr int kBytes = kStep * kRowBytes;           // one step of K or V
   static constexpr int kDma = kBytes / 1024 / kWaves;        // 1 KB blocks per wave and tensor
   static_assert(kDma >= 1, "every wave moves part of each step");
+  // Byte offset of a 16-byte chunk of a row, its index XORed by row so that a read's lanes
+  // spread over the 64 banks. A K read takes 16 bytes from each of 32 rows; the hardware serves
+  // it 16 lanes at a time, rows 0 - 3, 12 - 15, 20 - 27 and the others, which row bits 0, 1, 2 and
+  // 4 tell apart. A transposed V read takes 32 or 64 bytes from each of 4 rows.
+  static CURE_DEV int k_offset(int row, int chunk) {
+    const int low = row & 3, b2 = (row >> 2) & 1, b4 = (row >> 4) & 1;
+    const int f = D == 128 ? low << 2 | b4 << 1 | b2 : (low >> 1) << 2 | b4 << 1 | b2;
+    return row * kRowBytes + ((chunk ^ f) << 4);
+  }
+  static CURE_DEV int v_offset(int row, int chunk) {
+    const int low = row & 3, b2 = (row >> 2) & 1;
+    const int f = D == 128 ? low << 2 | b2 << 1 : (low >> 1) << 2 | b2 << 1;
+    return row * kRowBytes + ((chunk ^ f) << 4);
+  }
 };
 
 // A row's probabilities of one step, as the products take them.
 struct Probs {
-  bf16x8 v[2];
+  u32x4 u[2];
+  CURE_DEV void set(int pair, bf16x2 v) { u[pair >> 2][pair & 3] = __builtin_bit_cast(uint32_t, v); }
+  CURE_DEV bf16x8 operand(int ks) const { return __builtin_bit_cast(bf16x8, u[ks]); }
 };
 
 template <int D, bool kPrefix>
 __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
-  using T = TileGeo<D>;
   using G = Geo<D>;
   constexpr int kRing = G::kRing;
   constexpr int kKK = D / 16;                      // k-steps of the scores
   constexpr int kBlk = D / 32;                     // 32-column blocks of the output
+  constexpr int kAhead = 2;
   // Beyond what a step needs, the DMA of the two steps before it may be in flight.
   constexpr int kVmWait = waitcnt_vm((kRing - 2) * 2 * G::kDma);
   __shared__ __attribute__((aligned(1024))) unsigned char s_k[kRing * G::kBytes];
@@ -225,21 +242,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   // The tile stream: per wave and step, kDma blocks of K and of V. The buffer resource
   // covers the step's own rows of the keys, so that the rest of a step reads as zeros and a
   // step past the split's end reads nothing; its base moves on in 64 bits.
-  const uint32_t tok_bytes = (uint32_t)(a.hkv * T::kRowBytes);
-  uint32_t src[G::kDma];
+  const uint32_t tok_bytes = (uint32_t)(a.hkv * G::kRowBytes);
+  uint32_t k_src[G::kDma], v_src[G::kDma];
 #pragma unroll
   for (int j = 0; j < G::kDma; ++j) {
+    // The source of the chunk at this lane's place: XORed again, it is its own.
     const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
-    const int row = byte / T::kRowBytes;
-    src[j] = (uint32_t)row * tok_bytes +
-             (uint32_t)(w.hk * T::kRowBytes + ((((byte % T::kRowBytes) >> 4) ^ T::swz(row)) << 4));
+    const int row = byte / G::kRowBytes, chunk = (byte % G::kRowBytes) >> 4;
+    const uint32_t at = (uint32_t)row * tok_bytes + (uint32_t)(w.hk * G::kRowBytes);
+    k_src[j] = at + G::k_offset(row, chunk) % G::kRowBytes;
+    v_src[j] = at + G::v_offset(row, chunk) % G::kRowBytes;
   }
   const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const uint32_t k_lds = lds_addr(s_k), v_lds = lds_addr(s_v);
   const uint32_t dma0 = __builtin_amdgcn_readfirstlane(wave * G::kDma * 1024);
   const int steps = (w.end - w.begin + kStep - 1) / kStep;
-  auto dma = [&](const char* p, uint32_t lds, int h) {
+  auto dma = [&](const char* p, const uint32_t (&src)[G::kDma], uint32_t lds, int h) {
     const int left = min(w.end - w.begin - h * kStep, kStep);
     const i32x4 rsrc = raw_rsrc(p + (int64_t)h * kStep * tok_bytes, left > 0 ? (uint32_t)left * tok_bytes : 0u);
 #pragma unroll
@@ -247,8 +266,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   };
 #pragma unroll
   for (int h = 0; h < kRing; ++h) {
-    dma(kp, k_lds + h * G::kBytes, h);
-    if (h < 2) dma(vp, v_lds + h * G::kBytes, h);
+    dma(kp, k_src, k_lds + h * G::kBytes, h);
+    if (h < 2) dma(vp, v_src, v_lds + h * G::kBytes, h);
   }
 
   // This lane's query row.
@@ -276,13 +295,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   // LDS addresses of this lane's operands in slot 0.
   uint32_t k_at[kKK];
 #pragma unroll
-  for (int kk = 0; kk < kKK; ++kk) k_at[kk] = k_lds + T::offset(col, 2 * kk + half);
+  for (int kk = 0; kk < kKK; ++kk) k_at[kk] = k_lds + G::k_offset(col, 2 * kk + half);
   uint32_t v_at[kBlk];
   {
     const int j = lane & 15, g = (lane >> 4) & 1;
 #pragma unroll
     for (int i = 0; i < kBlk; ++i)
-      v_at[i] = v_lds + T::offset(4 * half + (j >> 2), 4 * i + 2 * g + ((j & 3) >> 1)) + (j & 1) * 8;
+      v_at[i] = v_lds + G::v_offset(4 * half + (j >> 2), 4 * i + 2 * g + ((j & 3) >> 1)) + (j & 1) * 8;
   }
 
   f32x16 o[kBlk];
@@ -304,7 +323,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   auto values = [&](uint32_t slot, int ks, int i) {
     Pack8 f;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) f.h[r] = lds_read_tr8(v_at[i] + slot + (16 * ks + 8 * r) * T::kRowBytes);
+    for (int r = 0; r < 2; ++r) f.h[r] = lds_read_tr8(v_at[i] + slot + (16 * ks + 8 * r) * G::kRowBytes);
     return f;
   };
   auto products = [&](const Probs& p, uint32_t slot) {
@@ -312,30 +331,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int i = 0; i < kBlk; ++i)
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(slot, ks, i).v, p.v[ks], o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(slot, ks, i).v, p.operand(ks), o[i], 0, 0, 0);
   };
   // Probabilities against the reference m, and this lane's share of their sum.
   auto exps = [&](const f32x16& x, Probs& p) {
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (__bf16)fast_exp2(fmaf(x[8 * ks + e], c, -m));
-      p.v[ks] = v;
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        l0 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[e], v[e + 1]}, ones, l0, false);
-        l1 = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[e + 2], v[e + 3]}, ones, l1, false);
-      }
+    for (int j = 0; j < 8; ++j) {
+      const bf16x2 v = {(__bf16)fast_exp2(fmaf(x[2 * j], c, -m)), (__bf16)fast_exp2(fmaf(x[2 * j + 1], c, -m))};
+      p.set(j, v);
+      if (j & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l1, false);
+      else l0 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l0, false);
     }
     return l0 + l1;
   };
   auto row_max = [&](const f32x16& x) {
-    float mx = max3_raw(x[0], x[1], x[2]);
+    float mx = x[0];
 #pragma unroll
-    for (int r = 3; r < 15; r += 2) mx = max3_raw(mx, x[r], x[r + 1]);
-    return max_halves(max3_raw(mx, x[15], x[15])) * c;
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+    return max_halves(mx) * c;
   };
   // Moves the reference where a row's maximum has risen by more than 2^8, which no row's has
   // while every lane's probabilities sum to 2^8 at most.
@@ -377,7 +391,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int n = 0; n < 2 * kBlk; ++n) {
       Pack8 f = values(slot, n / kBlk, n % kBlk);
       f.u = make_uint4(clean(f.u.x), clean(f.u.y), clean(f.u.z), clean(f.u.w));
-      o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p.v[n / kBlk], o[n % kBlk], 0, 0, 0);
+      o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p.operand(n / kBlk), o[n % kBlk], 0, 0, 0);
     }
     for (int t = 0; t < kStep; ++t) {
       const bool seen = h * kStep + t <= last;
@@ -385,7 +399,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
       for (int i = 0; i < kBlk; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {              // columns 32 i + 8 g + 4 half .. +3
-          const uint32_t at = v_lds + slot + T::offset(t, 4 * i + g) + 8 * half;
+          const uint32_t at = v_lds + slot + G::v_offset(t, 4 * i + g) + 8 * half;
           const u32x2 u = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)at;
           const float x[4] = {bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
 #pragma unroll
@@ -398,13 +412,57 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int r = 0; r < 16; ++r)
       x[r] = h * kStep + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? x[r] : -INFINITY;
   };
+  // A step in the middle of a row's keys: scores of the next step into y, probabilities of this
+  // one, whose scores are x, into n, products of the last one's, p; returns this lane's share of
+  // the sum. Every matrix instruction is followed by LDS reads for the one kAhead further on and by
+  // a share of the softmax, which the matrix unit's time hides.
+  auto middle = [&](const f32x16& x, f32x16& y, const Probs& p, Probs& n, uint32_t k_slot, uint32_t v_slot) {
+    constexpr int kPairs = 8 / kKK;                // pairs of probabilities per turn
+    bf16x8 kf[kKK];
+    Pack8 vf[kKK];
+    float e0[8], e1[8], l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      kf[i] = lds_read16(k_at[i] + k_slot);
+      vf[i] = values(v_slot, i / kBlk, i % kBlk);
+    }
+    const auto round = [&](int j) {                // pair j: scores 2 j and 2 j + 1
+      const bf16x2 v = {(__bf16)e0[j], (__bf16)e1[j]};
+      n.set(j, v);
+      if (j & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l1, false);
+      else l0 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l0, false);
+    };
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKK; ++i) {
+      y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], q[i], y, 0, 0, 0);
+      if (i + kAhead < kKK) kf[i + kAhead] = lds_read16(k_at[i + kAhead] + k_slot);
+#pragma unroll
+      for (int j = kPairs * i; j < kPairs * (i + 1); ++j) {
+        e0[j] = fast_exp2(fmaf(x[2 * j], c, -m));
+        e1[j] = fast_exp2(fmaf(x[2 * j + 1], c, -m));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      o[i % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i].v, p.operand(i / kBlk), o[i % kBlk], 0, 0, 0);
+      if (i + kAhead < kKK) vf[i + kAhead] = values(v_slot, (i + kAhead) / kBlk, (i + kAhead) % kBlk);
+      if (i > 0) {
+#pragma unroll
+        for (int j = kPairs * (i - 1); j < kPairs * i; ++j) round(j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int j = 8 - kPairs; j < 8; ++j) round(j);
+    return l0 + l1;
+  };
   // Step h begins: its slots (h + 1 of K, h - 1 of V) have landed for every wave, and those that
   // step h - 1 read (h of K, h - 2 of V) are refilled.
   auto begin = [&](int h, uint32_t k_slot, uint32_t v_slot) {
     __builtin_amdgcn_s_waitcnt(kVmWait);
     __syncthreads();
-    dma(kp, k_lds + k_slot, h + kRing);
-    dma(vp, v_lds + v_slot, h + 2);
+    dma(kp, k_src, k_lds + k_slot, h + kRing);
+    dma(vp, v_src, v_lds + v_slot, h + 2);
   };
 
   __builtin_amdgcn_s_waitcnt(0);
@@ -436,10 +494,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
         f32x16 y;
         Probs n;
         begin(h + j - 1, j % kRing * G::kBytes, (j + 2) % kRing * G::kBytes);
-        scores(y, (j + 1) % kRing * G::kBytes);
-        const float ls = exps(x, n);
-        products(p, (j + 3) % kRing * G::kBytes);
-        settle(x, n, ls);
+        settle(x, n, middle(x, y, p, n, (j + 1) % kRing * G::kBytes, (j + 3) % kRing * G::kBytes));
         x = y;
         p = n;
       }
