@@ -470,7 +470,7 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  * Supports d in {64, 128}, hq % hkv == 0, 0 < scale < inf, batch <= 65535.
  * kv_split: 0 = automatic, else the number of splits of the longest context.
  * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
- * 16-byte aligned. q, k, v: 16-byte aligned; o: 8 (bf16) or 16 bytes (float32).
+ * 16-byte aligned, as q, k, v and o are.
  * bf16: probabilities are rounded to bf16 for their product and lse sums the rounded
  * ones (within 2^-8 of the exact sum). float32: float32 throughout.
  */

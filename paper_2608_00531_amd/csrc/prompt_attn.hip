@@ -166,6 +166,17 @@ CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
   return r;
 }
 
+CURE_DEV void store8_f32(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+CURE_DEV void store8(const Args& a, int64_t idx, const float (&x)[8]) {
+  if (a.out_bf16)
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.o) + idx) =
+        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  else
+    store8_f32(reinterpret_cast<float*>(a.o) + idx, x);
+}
 CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, float x3) {
   if (a.out_bf16) {
     uint2 pk;
@@ -326,13 +337,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int r = 0; r < 2; ++r) f.h[r] = lds_read_tr8(v_at[i] + slot + (16 * ks + 8 * r) * G::kRowBytes);
     return f;
   };
-  auto products = [&](const Probs& p, uint32_t slot) {
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int i = 0; i < kBlk; ++i)
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(slot, ks, i).v, p.operand(ks), o[i], 0, 0, 0);
-  };
   // Probabilities against the reference m, and this lane's share of their sum.
   auto exps = [&](const f32x16& x, Probs& p) {
     float l0 = 0.f, l1 = 0.f;
@@ -370,29 +374,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   // not reach it, but 0 times an infinity or a NaN would. Where the step's values hold one, the
   // products take zeros in its place and the rows that do see it take it as it is.
   auto hidden_products = [&](const Probs& p, uint32_t slot, int h) {
-    float probe = 0.f;                             // a NaN from the first value that is not finite
+    Pack8 f[2 * kBlk];
+    float probe[2] = {0.f, 0.f};                   // a NaN from the first value that is not finite
 #pragma unroll
-    for (int n = 0; n < 2 * kBlk; ++n) {
-      const bf16x8 f = values(slot, n / kBlk, n % kBlk).v;
+    for (int n = 0; n < 2 * kBlk; ++n) f[n] = values(slot, n / kBlk, n % kBlk);
+#pragma unroll
+    for (int n = 0; n < 2 * kBlk; ++n)
 #pragma unroll
       for (int e = 0; e < 8; e += 2)
-        probe = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f[e], f[e + 1]}, bf16x2{(__bf16)0.f, (__bf16)0.f}, probe, false);
-    }
-    if (__builtin_expect(__ballot(probe != 0.f) == 0, 1)) {
-      products(p, slot);
-      return;
-    }
+        probe[n & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f[n].v[e], f[n].v[e + 1]},
+                                                       bf16x2{(__bf16)0.f, (__bf16)0.f}, probe[n & 1], false);
+    const bool finite = __ballot(probe[0] + probe[1] != 0.f) == 0;
     const auto clean = [](uint32_t u) {
       const uint32_t lo = (u & 0x7f80u) == 0x7f80u ? 0u : 0xffffu;
       const uint32_t hi = (u & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
       return u & (lo | hi);
     };
+    if (__builtin_expect(!finite, 0)) {
 #pragma unroll
-    for (int n = 0; n < 2 * kBlk; ++n) {
-      Pack8 f = values(slot, n / kBlk, n % kBlk);
-      f.u = make_uint4(clean(f.u.x), clean(f.u.y), clean(f.u.z), clean(f.u.w));
-      o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p.operand(n / kBlk), o[n % kBlk], 0, 0, 0);
+      for (int n = 0; n < 2 * kBlk; ++n)
+        f[n].u = make_uint4(clean(f[n].u.x), clean(f[n].u.y), clean(f[n].u.z), clean(f[n].u.w));
     }
+#pragma unroll
+    for (int n = 0; n < 2 * kBlk; ++n)
+      o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n].v, p.operand(n / kBlk), o[n % kBlk], 0, 0, 0);
+    if (__builtin_expect(finite, 1)) return;
     for (int t = 0; t < kStep; ++t) {
       const bool seen = h * kStep + t <= last;
 #pragma unroll
@@ -414,8 +420,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   };
   // A step in the middle of a row's keys: scores of the next step into y, probabilities of this
   // one, whose scores are x, into n, products of the last one's, p; returns this lane's share of
-  // the sum. Every matrix instruction is followed by LDS reads for the one kAhead further on and by
-  // a share of the softmax, which the matrix unit's time hides.
+  // the sum. Every matrix instruction is followed by LDS reads for the one kAhead turns on and by an
+  // equal share of the softmax, which the matrix unit's time hides.
   auto middle = [&](const f32x16& x, f32x16& y, const Probs& p, Probs& n, uint32_t k_slot, uint32_t v_slot) {
     constexpr int kPairs = 8 / kKK;                // pairs of probabilities per turn
     bf16x8 kf[kKK];
@@ -441,14 +447,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
 #pragma unroll
       for (int j = kPairs * i; j < kPairs * (i + 1); ++j) {
         e0[j] = fast_exp2(fmaf(x[2 * j], c, -m));
-        e1[j] = fast_exp2(fmaf(x[2 * j + 1], c, -m));
+        e1[j] = fmaf(x[2 * j + 1], c, -m);
       }
       __builtin_amdgcn_sched_barrier(0);
       o[i % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i].v, p.operand(i / kBlk), o[i % kBlk], 0, 0, 0);
       if (i + kAhead < kKK) vf[i + kAhead] = values(v_slot, (i + kAhead) / kBlk, (i + kAhead) % kBlk);
-      if (i > 0) {
 #pragma unroll
-        for (int j = kPairs * (i - 1); j < kPairs * i; ++j) round(j);
+      for (int j = kPairs * i; j < kPairs * (i + 1); ++j) {
+        e1[j] = fast_exp2(e1[j]);
+        if (j >= kPairs) round(j - kPairs);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -456,6 +463,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int j = 8 - kPairs; j < 8; ++j) round(j);
     return l0 + l1;
   };
+  auto slot_of = [](int step) { return (uint32_t)(step % kRing) * G::kBytes; };
   // Step h begins: its slots (h + 1 of K, h - 1 of V) have landed for every wave, and those that
   // step h - 1 read (h of K, h - 2 of V) are refilled.
   auto begin = [&](int h, uint32_t k_slot, uint32_t v_slot) {
@@ -499,20 +507,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
         p = n;
       }
     }
-    for (; h <= my_steps; ++h) {
-      const uint32_t slot = (uint32_t)(h % kRing) * G::kBytes;
-      begin(h, slot, (uint32_t)((h + 2) % kRing) * G::kBytes);
+    // The rest of those, and the first step that is seen in part: its products come a step later.
+    for (; h < my_steps && h <= full; ++h) {
       f32x16 y;
-      scores(y, (uint32_t)((h + 1) % kRing) * G::kBytes);
-      hidden_products(p, (uint32_t)((h + 3) % kRing) * G::kBytes, h - 1);
+      Probs n;
+      begin(h, slot_of(h), slot_of(h + 2));
+      if (h == full) mask(x, h);
+      settle(x, n, middle(x, y, p, n, slot_of(h + 1), slot_of(h + 3)));
+      x = y;
+      p = n;
+    }
+    // What is seen in part.
+    for (; h <= my_steps; ++h) {
+      begin(h, slot_of(h), slot_of(h + 2));
+      hidden_products(p, slot_of(h + 3), h - 1);
       if (h < my_steps) {
-        if (h >= full) mask(x, h);
+        mask(x, h);
         settle(x, p, exps(x, p));
-        x = y;
+        scores(x, slot_of(h + 1));
       }
     }
   }
-  for (; h <= steps; ++h) begin(h, (uint32_t)(h % kRing) * G::kBytes, (uint32_t)((h + 2) % kRing) * G::kBytes);
+  for (; h <= steps; ++h) begin(h, slot_of(h), slot_of(h + 2));
 
   __builtin_amdgcn_s_waitcnt(0);                   // the rings' trailing DMA lands before exit
   if (!row_ok) return;
@@ -522,15 +538,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const bool whole = w.splits == 1 && !kPrefix;
   const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.s);
   const int64_t orow = me.row * a.hq + me.head;
+  // Lanes l and l + 32 hold columns 0 - 3 and 4 - 7 of each eight of one row: they trade, so that each
+  // has eight together, of every other eight.
 #pragma unroll
   for (int i = 0; i < kBlk; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d0 = 32 * i + 8 * g + 4 * half;
-      const float x0 = o[i][4 * g] * inv, x1 = o[i][4 * g + 1] * inv;
-      const float x2 = o[i][4 * g + 2] * inv, x3 = o[i][4 * g + 3] * inv;
-      if (whole) store4(a, orow * D + d0, x0, x1, x2, x3);
-      else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x0, x1, x2, x3);
+    for (int g = 0; g < 4; g += 2) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[i][4 * g + e] * inv),
+                                                        __float_as_uint(o[i][4 * g + 4 + e] * inv), false, false);
+        y[e] = __uint_as_float(r[0]);
+        y[4 + e] = __uint_as_float(r[1]);
+      }
+      const int d0 = 32 * i + 8 * (g + half);
+      if (whole) store8(a, orow * D + d0, y);
+      else store8_f32(a.part_o + pi * D + d0, y);
     }
   if (half == 0) {
     if (!whole) a.part_lse[pi] = lse;
@@ -889,7 +913,7 @@ cure_status check(const void* q, const void* k, const void* v, const void* o, in
   if ((int64_t)hkv * d * 4 * kStep > INT32_MAX) return CURE_ERR_UNSUPPORTED;
   const uintptr_t in = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) |
                        reinterpret_cast<uintptr_t>(v);
-  if (in % 16 != 0 || reinterpret_cast<uintptr_t>(o) % (out_dtype == CURE_BF16 ? 8 : 16) != 0)
+  if (in % 16 != 0 || reinterpret_cast<uintptr_t>(o) % 16 != 0)
     return CURE_ERR_INVALID_ARG;
   return CURE_OK;
 }
