@@ -55,7 +55,7 @@ struct Args {
   const void* k_weight;
   float eps, inv_d, mscale;
   const float* inv_freq;
-  int32_t rot, interleaved;
+  int32_t rot;
   void* q_out;
   void* k_cache;
   void* v_cache;
@@ -110,19 +110,58 @@ CURE_DEV float group_sum(float x) {
 }
 
 // kLanes: lanes per head, the power of two (8 to 64) that holds its vectors.
-template <typename E, int kLanes>
+template <typename E, int kLanes, bool kInterleaved>
 __global__ __launch_bounds__(kThreads) void rope_append(Args a) {
   using V = Vec<E>;
   constexpr int kN = V::kN;
   constexpr int kGroups = kThreads / kLanes;       // heads in work at a time
   __shared__ int s_anc[CURE_MAX_TREE_NODES], s_depth[CURE_MAX_TREE_NODES];
-  __shared__ float s_cos[kMaxRows][kMaxPairs], s_sin[kMaxRows][kMaxPairs];
+  __shared__ __attribute__((aligned(16))) float s_cos[kMaxRows][kMaxPairs], s_sin[kMaxRows][kMaxPairs];
 
   const int b = blockIdx.y, tid = threadIdx.x;
-  // One round trip: the sequence's sizes and its tree.
+  const int n0 = blockIdx.x * a.rows_per_wg;
+  const int heads = a.hq + 2 * a.hkv;
+  const int lane = tid % kLanes;                   // within the head
+  const int col = lane * kN;
+  const bool in = col < a.d;
+
+  // Vectors in work: kBatch heads per thread, from head `head` of row n0 + r on, kGroups
+  // apart. The loads of the first need no more than the row's place.
+  u32x4 x[kBatch];
+  int r = 0, h = tid / kLanes;
+  const auto settle = [&](int& r, int& h) {
+    while (h >= heads) {
+      h -= heads;
+      ++r;
+    }
+  };
+  const auto fetch = [&](int64_t row0, int rows) {
+    int rr = r, hh = h;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u, hh += kGroups) {
+      settle(rr, hh);
+      x[u] = u32x4{0, 0, 0, 0};
+      if (!in || rr >= rows) continue;
+      const int64_t row = row0 + n0 + rr;
+      const int hk = hh - a.hq;
+      const E* src = hk < 0 ? static_cast<const E*>(a.q) + row * a.q_ld + (int64_t)hh * a.d
+                     : hk < a.hkv ? static_cast<const E*>(a.k) + row * a.k_ld + (int64_t)hk * a.d
+                                  : static_cast<const E*>(a.v) + row * a.v_ld + (int64_t)(hk - a.hkv) * a.d;
+      x[u] = *reinterpret_cast<const u32x4*>(src + col);
+    }
+  };
+
+  // One round trip: the sequence's sizes, its tree, the frequencies, the weights and,
+  // where rows are padded and so in place whatever the sizes are, the first vectors.
   const bool tree = a.parent != nullptr;
   int p = -1;
   if (tree && tid < a.n_max) p = a.parent[(int64_t)b * a.n_max + tid];
+  if (!a.row_off) fetch((int64_t)b * a.n_max, min(a.rows_per_wg, a.n_max - n0));
+  u32x4 wq16{0, 0, 0, 0}, wk16{0, 0, 0, 0};        // this lane's norm weights
+  if (in && a.q_weight) wq16 = *reinterpret_cast<const u32x4*>(static_cast<const E*>(a.q_weight) + col);
+  if (in && a.k_weight) wk16 = *reinterpret_cast<const u32x4*>(static_cast<const E*>(a.k_weight) + col);
+  const int pairs = a.rot / 2;
+  const float freq0 = pairs > 0 ? a.inv_freq[tid % pairs] : 0.f;
   const int64_t row0 = a.row_off ? a.row_off[b] : (int64_t)b * a.n_max;
   const int N = a.n_rows[b];
   const int L = a.ctx_len[b];
@@ -130,14 +169,27 @@ __global__ __launch_bounds__(kThreads) void rope_append(Args a) {
   const int64_t base = (int64_t)L + (a.pos_off ? a.pos_off[b] : 0);
   bool bad = N < 0 || N > a.n_max || L < 0 || off < 0 || off > a.cache_rows - L - N || row0 < 0 ||
              row0 > a.rows - N;
-  // Depths by pointer doubling: anc is the ancestor 2^round up (-1: past the root),
-  // depth the steps up to it. At most 8 rounds for 256 nodes.
-  if (tree) {
+  // Depths by pointer doubling: p becomes the ancestor 2^round up (-1: past the root), depth
+  // the steps up to it. Up to 64 nodes every wave does it by itself, with lane exchanges; more
+  // (at most 8 rounds for 256) go through LDS.
+  int depth = p >= 0;
+  if (tree && a.n_max <= kWave) {
+    const int l = tid % kWave;
+    p = l < a.n_max ? a.parent[(int64_t)b * a.n_max + l] : -1;
+    bad = bad || __ballot(l < N && (p < -1 || p >= l)) != 0;
+    p = l < N && !bad ? p : -1;
+    depth = p >= 0;
+    while (__ballot(p >= 0)) {
+      const int up = __shfl(p, max(p, 0)), more = __shfl(depth, max(p, 0));
+      depth += p >= 0 ? more : 0;
+      p = p >= 0 ? up : -1;
+    }
+  } else if (tree) {
     bad = __syncthreads_or(bad || (tid < N && (p < -1 || p >= tid)));
     if (!bad) {
       if (tid < N) {
         s_anc[tid] = p;
-        s_depth[tid] = p >= 0;
+        s_depth[tid] = depth;
       }
       while (__syncthreads_or(tid < N && p >= 0)) {
         int up = -1, more = 0;
@@ -155,129 +207,104 @@ __global__ __launch_bounds__(kThreads) void rope_append(Args a) {
     }
   }
   if (blockIdx.x == 0 && tid == 0) a.row_status[b] = bad ? CURE_ERR_BAD_TREE : CURE_OK;
-  const int n0 = blockIdx.x * a.rows_per_wg;
   if (bad || n0 >= N) return;
   const int nrows = min(a.rows_per_wg, N - n0);
+  if (a.row_off) fetch(row0, nrows);
 
-  const int pairs = a.rot / 2;
-  for (int i = tid; i < nrows * pairs; i += kThreads) {
-    const int r = i / pairs, f = i - r * pairs;
-    const int64_t pos = base + (tree ? s_depth[n0 + r] : n0 + r);
-    double turn = (double)pos * (double)a.inv_freq[f] * 0.15915494309189535;   // / 2 pi
-    turn -= rint(turn);
-    float sn, cs;
-    sincospif(2.f * (float)turn, &sn, &cs);
-    s_cos[r][f] = cs * a.mscale;
-    s_sin[r][f] = sn * a.mscale;
-  }
-
-  const int lane = tid % kLanes;                   // within the head
-  const int col = lane * kN;
-  const bool in = col < a.d;
-  // This lane's norm weights, and for the half layout its partner lane and the index
-  // of its first pair.
-  float wq[kN], wk[kN];
-#pragma unroll
-  for (int j = 0; j < kN; ++j) wq[j] = wk[j] = 1.f;
-  if (in && a.q_weight) V::widen(*reinterpret_cast<const u32x4*>(static_cast<const E*>(a.q_weight) + col), wq);
-  if (in && a.k_weight) V::widen(*reinterpret_cast<const u32x4*>(static_cast<const E*>(a.k_weight) + col), wk);
+  // The half layout's partner lane, and the index of this lane's first pair.
   const bool turned = col < a.rot;
   const bool low = col < pairs;
   const int hop = pairs / kN;                      // lanes between the halves
   const int other = threadIdx.x % kWave + (turned ? (low ? hop : -hop) : 0);
-  const int pair0 = a.interleaved ? col / 2 : (low ? col : col - pairs);
+  const int pair0 = !turned ? 0 : kInterleaved ? col / 2 : (low ? col : col - pairs);
+
+  for (int i = tid; i < (nrows * pairs + kWave - 1) / kWave * kWave; i += kThreads) {
+    const int row = min(i / max(pairs, 1), nrows - 1), f = i - row * pairs;
+    int up = n0 + row;
+    if (tree) up = a.n_max <= kWave ? __shfl(depth, up) : s_depth[up];
+    if (i >= nrows * pairs) continue;
+    const float freq = i == tid ? freq0 : a.inv_freq[f];
+    double turn = (double)(base + up) * (double)freq * 0.15915494309189535;   // / 2 pi
+    turn -= rint(turn);
+    float sn, cs;
+    sincospif(2.f * (float)turn, &sn, &cs);
+    s_cos[row][f] = cs * a.mscale;
+    s_sin[row][f] = sn * a.mscale;
+  }
   __syncthreads();
 
-  const int heads = a.hq + 2 * a.hkv;
-  const int items = nrows * heads;
-  int item = tid / kLanes;
-  int r = 0, h = item;
-  auto settle = [&]() {
-    while (h >= heads) {
-      h -= heads;
-      ++r;
-    }
-  };
+  float wq[kN], wk[kN];
+  V::widen(wq16, wq);
+  V::widen(wk16, wk);
   // Uniform over the workgroup, as the exchanges inside a wave need every lane.
+  const int items = nrows * heads;
   for (int i0 = 0; i0 < items; i0 += kBatch * kGroups) {
-    u32x4 x[kBatch];
-    E* dst[kBatch];
-    int kind[kBatch], row[kBatch];                 // 0 query, 1 key, 2 value, 3 none
+    if (i0 > 0) fetch(row0, nrows);
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      settle();
-      const bool live = item < items && in;
-      const int n = n0 + r;
-      const E* src = nullptr;
-      dst[u] = nullptr;
-      kind[u] = 3;
-      row[u] = min(r, kMaxRows - 1);
-      x[u] = u32x4{0, 0, 0, 0};
-      if (live) {
-        if (h < a.hq) {
-          src = static_cast<const E*>(a.q) + (row0 + n) * a.q_ld + (int64_t)h * a.d;
-          dst[u] = static_cast<E*>(a.q_out) + ((row0 + n) * a.hq + h) * a.d;
-          kind[u] = 0;
-        } else {
-          const bool val = h >= a.hq + a.hkv;
-          const int hk = h - a.hq - (val ? a.hkv : 0);
-          src = val ? static_cast<const E*>(a.v) + (row0 + n) * a.v_ld + (int64_t)hk * a.d
-                    : static_cast<const E*>(a.k) + (row0 + n) * a.k_ld + (int64_t)hk * a.d;
-          dst[u] = static_cast<E*>(val ? a.v_cache : a.k_cache) + ((off + L + n) * a.hkv + hk) * a.d;
-          kind[u] = val ? 2 : 1;
-        }
-        x[u] = *reinterpret_cast<const u32x4*>(src + col);
-      }
-      item += kGroups;
-      h += kGroups;
-    }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
+    for (int u = 0; u < kBatch; ++u, h += kGroups) {
+      settle(r, h);
+      const bool live = in && r < nrows;
+      const int row = min(r, kMaxRows - 1);
+      const bool query = h < a.hq, value = h >= a.hq + a.hkv;
       float y[kN];
       V::widen(x[u], y);
-      const bool key = kind[u] == 1;
       if (a.q_weight || a.k_weight) {
         float ss = 0.f;
 #pragma unroll
         for (int j = 0; j < kN; ++j) ss = fmaf(y[j], y[j], ss);
         ss = group_sum<kLanes>(ss);
         const float rs = rsqrtf(fmaf(ss, a.inv_d, a.eps));
-        const bool norm = kind[u] == 0 ? a.q_weight != nullptr : key && a.k_weight != nullptr;
+        const bool norm = query ? a.q_weight != nullptr : a.k_weight != nullptr;
 #pragma unroll
-        for (int j = 0; j < kN; ++j) y[j] = norm ? y[j] * rs * (key ? wk[j] : wq[j]) : y[j];
+        for (int j = 0; j < kN; ++j) y[j] = norm ? y[j] * rs * (query ? wq[j] : wk[j]) : y[j];
       }
-      float z[kN];
-      if (a.interleaved) {
+      // The pairs from pair0 on, a multiple of as many as are read: 16 bytes of LDS at a time (8
+      // for the two pairs of four interleaved columns).
+      constexpr int kReads = kInterleaved ? kN / 2 : kN, kWide = kReads < 4 ? kReads : 4;
+      typedef float wide __attribute__((ext_vector_type(kWide)));
+      float z[kN], c[kReads], s[kReads];
+#pragma unroll
+      for (int j = 0; j < kReads; j += kWide) {
+        const wide cv = *reinterpret_cast<const wide*>(&s_cos[row][pair0 + j]);
+        const wide sv = *reinterpret_cast<const wide*>(&s_sin[row][pair0 + j]);
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) {
+          c[j + i] = cv[i];
+          s[j + i] = sv[i];
+        }
+      }
+      if (kInterleaved) {
 #pragma unroll
         for (int j = 0; j < kN; j += 2) {
-          const int i = min(pair0 + j / 2, kMaxPairs - 1);
-          const float c = s_cos[row[u]][i], s = s_sin[row[u]][i];
-          z[j] = fmaf(y[j], c, -(y[j + 1] * s));
-          z[j + 1] = fmaf(y[j], s, y[j + 1] * c);
+          z[j] = fmaf(y[j], c[j / 2], -(y[j + 1] * s[j / 2]));
+          z[j + 1] = fmaf(y[j], s[j / 2], y[j + 1] * c[j / 2]);
         }
       } else {
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
-          const int i = min(pair0 + j, kMaxPairs - 1);
           const float o = __shfl(y[j], other);
-          const float c = s_cos[row[u]][i], s = s_sin[row[u]][i];
-          z[j] = fmaf(y[j], c, low ? -(o * s) : o * s);
+          z[j] = fmaf(y[j], c[j % kReads], low ? -(o * s[j % kReads]) : o * s[j % kReads]);
         }
       }
-      if (kind[u] == 2) *reinterpret_cast<u32x4*>(dst[u] + col) = x[u];
-      else if (kind[u] < 2) *reinterpret_cast<u32x4*>(dst[u] + col) = V::narrow(turned ? z : y);
+      if (!live) continue;
+      const int64_t n = n0 + r;
+      const int hk = h - a.hq;
+      E* dst = query ? static_cast<E*>(a.q_out) + ((row0 + n) * a.hq + h) * a.d
+                     : static_cast<E*>(value ? a.v_cache : a.k_cache) + ((off + L + n) * a.hkv + hk - (value ? a.hkv : 0)) * a.d;
+      *reinterpret_cast<u32x4*>(dst + col) = value ? x[u] : V::narrow(turned ? z : y);
     }
   }
 }
 
-template <typename E>
+template <typename E, bool kInterleaved>
 void launch(const Args& a, dim3 grid, hipStream_t st) {
   constexpr int kMost = 2 * kMaxPairs / Vec<E>::kN;      // lanes of the widest head
   const int lanes = a.d / Vec<E>::kN;
-  if (lanes <= 8) hipLaunchKernelGGL((rope_append<E, 8>), grid, dim3(kThreads), 0, st, a);
-  else if (lanes <= 16) hipLaunchKernelGGL((rope_append<E, 16>), grid, dim3(kThreads), 0, st, a);
-  else if (kMost == 32 || lanes <= 32) hipLaunchKernelGGL((rope_append<E, 32>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((rope_append<E, kMost>), grid, dim3(kThreads), 0, st, a);
+  const dim3 block(kThreads);
+  if (lanes <= 8) hipLaunchKernelGGL((rope_append<E, 8, kInterleaved>), grid, block, 0, st, a);
+  else if (lanes <= 16) hipLaunchKernelGGL((rope_append<E, 16, kInterleaved>), grid, block, 0, st, a);
+  else if (kMost == 32 || lanes <= 32) hipLaunchKernelGGL((rope_append<E, 32, kInterleaved>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((rope_append<E, kMost, kInterleaved>), grid, block, 0, st, a);
 }
 
 }  // namespace
@@ -328,12 +355,14 @@ extern "C" cure_status cure_rope_append(const void* q, int64_t q_ld, const void*
     return CURE_ERR_INVALID_ARG;
   Args a{q, k, v, q_ld, k_ld, v_ld, rows, cache_rows, n_max, 1, row_off, n_rows, parent, kv_off,
          ctx_len, pos_off, hq, hkv, d, q_weight, k_weight, eps, 1.f / (float)d, mscale, inv_freq,
-         rot, (flags & CURE_ROPE_INTERLEAVED) != 0, q_out, k_cache, v_cache, row_status};
+         rot, q_out, k_cache, v_cache, row_status};
   // Few rows are dealt out one to a workgroup; many share its start-up.
   if ((int64_t)batch * n_max >= 2048) a.rows_per_wg = kMaxRows;
   const dim3 grid((unsigned)std::max(1, (n_max + a.rows_per_wg - 1) / a.rows_per_wg), (unsigned)batch);
-  if (dtype == CURE_BF16) launch<uint16_t>(a, grid, as_stream(stream));
-  else launch<float>(a, grid, as_stream(stream));
+  const bool interleaved = flags & CURE_ROPE_INTERLEAVED;
+  hipStream_t st = as_stream(stream);
+  if (dtype == CURE_BF16) interleaved ? launch<uint16_t, true>(a, grid, st) : launch<uint16_t, false>(a, grid, st);
+  else interleaved ? launch<float, true>(a, grid, st) : launch<float, false>(a, grid, st);
   return launch_status();
 }
 
