@@ -776,6 +776,8 @@ struct MergeArgs : Args {
   const float* tree_lse;             // [batch][n_max][hq]
 };
 
+constexpr int kMerge = 8;
+
 template <int D, bool kPrefix>
 __global__ __launch_bounds__(256) void seq_merge(MergeArgs a) {
   constexpr int kLanes = D / 4;
@@ -799,22 +801,45 @@ __global__ __launch_bounds__(256) void seq_merge(MergeArgs a) {
     row = a.row_off[b] + i;
   }
   const int64_t p0 = part_index(a, row, head, 0), orow = row * a.hq + head;
+  // kMerge parts at a time, all of whose loads are under way together. Parts that saw
+  // nothing (a log-sum-exp of -inf) weigh nothing.
   float m = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float lse, float4 v) {
-    if (lse == -INFINITY) return;                  // saw nothing
-    const float mn = fmaxf(m, lse);
-    const float w0 = fast_exp2((m - mn) * kLog2e), w1 = fast_exp2((lse - mn) * kLog2e);
+  float4 v[kMerge];
+  float lse[kMerge];
+  if (kPrefix) {
+    m = a.tree_lse[orow];
+    acc = *reinterpret_cast<const float4*>(a.tree_o + orow * D + col);
+    sum = 1.f;
+  }
+  for (int s0 = 0; s0 < splits; s0 += kMerge) {
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < kMerge; ++u) {
+      const bool ok = s0 + u < splits;
+      v[u] = ok ? *reinterpret_cast<const float4*>(a.part_o + (p0 + s0 + u) * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+      lse[u] = ok ? a.part_lse[p0 + s0 + u] : -INFINITY;
+    }
+#pragma unroll
+    for (int u = 0; u < kMerge; ++u) mn = fmaxf(mn, lse[u]);
+    if (mn == -INFINITY) continue;
+    const float w0 = fast_exp2((m - mn) * kLog2e);
     m = mn;
-    sum = sum * w0 + w1;
-    acc.x = acc.x * w0 + v.x * w1;
-    acc.y = acc.y * w0 + v.y * w1;
-    acc.z = acc.z * w0 + v.z * w1;
-    acc.w = acc.w * w0 + v.w * w1;
-  };
-  for (int s = 0; s < splits; ++s)
-    add(a.part_lse[p0 + s], *reinterpret_cast<const float4*>(a.part_o + (p0 + s) * D + col));
-  if (kPrefix) add(a.tree_lse[orow], *reinterpret_cast<const float4*>(a.tree_o + orow * D + col));
+    sum *= w0;
+    acc.x *= w0;
+    acc.y *= w0;
+    acc.z *= w0;
+    acc.w *= w0;
+#pragma unroll
+    for (int u = 0; u < kMerge; ++u) {
+      const float w = fast_exp2((lse[u] - mn) * kLog2e);
+      sum += w;
+      acc.x = fmaf(w, v[u].x, acc.x);
+      acc.y = fmaf(w, v[u].y, acc.y);
+      acc.z = fmaf(w, v[u].z, acc.z);
+      acc.w = fmaf(w, v[u].w, acc.w);
+    }
+  }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   store4(a, orow * D + col, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (col == 0 && a.lse) a.lse[orow] = sum == 0.f ? -INFINITY : m + logf(sum);
