@@ -1,13 +1,14 @@
 // cure_prompt_attn: causal attention of new tokens over their context and themselves
 // (whole prompts, chunks of them, single tokens), sequences packed without padding.
 // cure_prefix_attn: tree verification of sequences that share a prefix, whose keys and
-// values are read once for all of them; each node's own context and tree take
-// cure_tree_attn, and the two parts are joined by their log-sum-exps.
+// values are read once for all of them; each sequence's own context and tree are more work
+// of the same launch, and a merge joins the parts by their log-sum-exps.
 //
 // Both are one kernel over (tile of query rows, kv-head, split of the keys): query row R of
 // a kv-head is query head R % group of token R / group, so the heads that share keys share
-// a tile. It sees the keys up to its own position (a prompt) or all of them (a prefix, where
-// the tokens are the nodes of all sequences, without those that a sequence does not have).
+// a tile. A row sees the keys up to its own position (a prompt), all of them (a prefix, where
+// the tokens are the nodes of all sequences, without those that a sequence does not have), or
+// its context and the nodes on its root path (a tree).
 //
 //   S^T = K Q^T,  P = 2^(c S - m),  l += sum P,  O^T += V^T P^T,  o = O / l
 // in one pass over the keys with the running reference m and sum l in fp32. P is rounded to
@@ -32,8 +33,14 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 32;            // tokens per step of the key loop
 constexpr int kWaves = 4;            // waves per workgroup, 32 query rows each
 constexpr int kRows = 32 * kWaves;   // query rows per tile
-constexpr int kMinTps = 256;         // tokens per split, at least
+constexpr int kNarrow = 32;          // query rows per tile of the fp32 kernel that shares them
 constexpr int kMaxPrefixBatch = 1024;
+constexpr int kAncWords = CURE_MAX_TREE_NODES / 64;
+
+// How keys are split: at most `most` splits of about tps tokens, at least one.
+struct Splits {
+  int32_t tps, most;
+};
 
 struct Args {
   const void* q;
@@ -49,38 +56,52 @@ struct Args {
   const int32_t* n_rows;             // tokens, or nodes, per sequence
   const int64_t* kv_off;
   const int32_t* ctx_len;
+  const int32_t* parent;             // prefix: the trees
+  int32_t* tree_status;
   int64_t prefix_off;
   int32_t prefix_len;
-  int32_t tps, max_splits;
-  float* part_o;                     // [row][hq][max_splits][d]
-  float* part_lse;                   // [row][hq][max_splits]
+  int32_t tile;                      // query rows of a tile
+  int32_t tiles, own_tiles;          // prefix: tiles of all nodes, and of a sequence's
+  Splits cut, own;                   // of a prompt's keys or the prefix, and of own rows
+  float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most
+  float* part_lse;                   // [row][hq][slots]
 };
 
-CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int s) {
-  return (row * a.hq + head) * a.max_splits + s;
+CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int slot) {
+  return (row * a.hq + head) * (a.cut.most + a.own.most) + slot;
 }
 
-// Splits of `keys` keys; the last one runs to the end.
-CURE_DEV int split_count(const Args& a, int keys) {
-  return max(1, min((keys + a.tps - 1) / a.tps, a.max_splits));
+// The splits of `keys` (at least one) keys: n of `per` tokens, whole steps, the last one shorter.
+struct Cut {
+  int n, per;
+};
+CURE_DEV Cut cut_of(const Splits& s, int keys) {
+  const int n = max(1, min((keys - 1) / s.tps + 1, s.most));
+  const int per = ((keys - 1) / n / kStep + 1) * kStep;
+  return Cut{(keys - 1) / per + 1, per};
 }
 
 // What a workgroup works on: packed query rows r0 .. of `rows` in all, against cache rows
 // key0 + [begin, end).
 struct Work {
-  int hk, r0, rows, s, splits;
-  int begin, end, keys;
+  int hk, r0, rows, slot, splits;
+  int begin, end;
   int64_t key0;
-  int64_t row0;                      // prompt: the sequence's first row
+  int64_t row0;                      // first row of the sequence (not for a prefix)
   int ctx;
+  int b;
+  bool tree;                         // a sequence's own rows, in cure_prefix_attn
 };
 
 struct Shared {
-  int first[kMaxPrefixBatch + 1];    // prefix: nodes before each sequence
+  int first[kMaxPrefixBatch + 1];    // nodes before each sequence
+  int parent[CURE_MAX_TREE_NODES];
+  unsigned long long anc[CURE_MAX_TREE_NODES][kAncWords];   // a tree's root paths, as bits
 };
 
 // Prompt: grid (kv-heads x tiles, splits, sequences); a sequence's last tiles, which see the
-// most keys, come first.
+// most keys, come first. A sequence's tiles stay together, as they share its keys in the L2: dealt
+// out in turn over the sequences, 16 prompts of 1 to 2048 tokens took 399 us instead of 253.
 CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   const int b = blockIdx.z, x = blockIdx.x / a.hkv;
   w.hk = blockIdx.x - x * a.hkv;
@@ -91,18 +112,52 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.row0), "s"(w.key0));
   const int n = min(n_raw, a.n_max);
   w.rows = n * a.group;
-  const int tiles = (w.rows + kRows - 1) / kRows;
+  const int tiles = (w.rows + a.tile - 1) / a.tile;
   if (n <= 0 || x >= tiles) return false;
-  w.r0 = (tiles - 1 - x) * kRows;
-  w.keys = w.ctx + (min(w.r0 + kRows, w.rows) - 1) / a.group + 1;
-  return true;
+  w.r0 = (tiles - 1 - x) * a.tile;
+  const int keys = w.ctx + (min(w.r0 + a.tile, w.rows) - 1) / a.group + 1;
+  const Cut c = cut_of(a.cut, keys);
+  w.tree = false;
+  w.slot = blockIdx.y;
+  w.splits = c.n;
+  w.begin = w.slot * c.per;
+  w.end = min(w.begin + c.per, keys);
+  return w.slot < c.n;
 }
 
-// Prefix: grid (kv-heads x tiles, splits); the tiles hold the existing nodes of all
-// sequences in order, whose counts are summed here.
+// Prefix: kv-heads x (tiles x splits of the prefix, then tiles x splits of each sequence's own
+// rows). The prefix's tiles hold the existing nodes of all sequences in order, whose counts are
+// summed here.
 CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
-  const int x = blockIdx.x / a.hkv;
+  int x = blockIdx.x / a.hkv;
   w.hk = blockIdx.x - x * a.hkv;
+  const int shared_units = a.tiles * a.cut.most;
+  w.tree = x >= shared_units;
+  if (w.tree) {
+    x -= shared_units;
+    const int tile = x % a.own_tiles;
+    x /= a.own_tiles;
+    const int b = w.b = x % a.batch, s = x / a.batch;
+    const int n_raw = a.n_rows[b];
+    w.ctx = a.ctx_len[b];
+    w.key0 = a.kv_off[b];
+    asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.key0));
+    const int n = min(n_raw, a.n_max);
+    w.rows = n * a.group;
+    w.r0 = tile * a.tile;
+    w.row0 = (int64_t)b * a.n_max;
+    if (n <= 0) {                                  // the empty tree is valid
+      if (tile == 0 && s == 0 && w.hk == 0 && threadIdx.x == 0 && a.tree_status) a.tree_status[b] = CURE_OK;
+      return false;
+    }
+    const int keys = w.ctx + n;
+    const Cut c = cut_of(a.own, keys);
+    w.slot = a.cut.most + s;
+    w.splits = c.n;
+    w.begin = s * c.per;
+    w.end = min(w.begin + c.per, keys);
+    return s < c.n && w.r0 < w.rows;
+  }
   if (threadIdx.x < kWave) {
     const int lane = threadIdx.x;
     int sum = 0;
@@ -120,50 +175,83 @@ CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
     }
   }
   __syncthreads();
+  const Cut c = cut_of(a.cut, a.prefix_len);
   w.rows = sh.first[a.batch] * a.group;
-  w.r0 = x * kRows;
+  w.r0 = x % a.tiles * a.tile;
+  w.slot = x / a.tiles;
+  w.splits = c.n;
+  w.begin = w.slot * c.per;
+  w.end = min(w.begin + c.per, a.prefix_len);
   w.key0 = a.prefix_off;
-  w.keys = a.prefix_len;
-  w.ctx = 0;
+  w.ctx = a.prefix_len;
   w.row0 = 0;
-  return w.r0 < w.rows;
+  return w.slot < c.n && w.r0 < w.rows;
 }
 
 template <bool kPrefix>
 CURE_DEV bool locate(const Args& a, Work& w, Shared& sh) {
-  if (!(kPrefix ? locate_prefix(a, w, sh) : locate_prompt(a, w))) return false;
-  w.s = blockIdx.y;
-  w.splits = split_count(a, w.keys);
-  if (w.s >= w.splits) return false;
-  w.begin = w.s * a.tps;
-  w.end = w.s == w.splits - 1 ? w.keys : w.begin + a.tps;
+  return kPrefix ? locate_prefix(a, w, sh) : locate_prompt(a, w);
+}
+
+// The ancestor bits of sequence b's nodes, for a workgroup of at least 256 threads whose work
+// reaches the tree's rows; reports the tree's status. False: malformed.
+CURE_DEV bool build_tree(const Args& a, const Work& w, Shared& sh) {
+  const int n = threadIdx.x, nodes = w.rows / a.group;
+  int p = -1;
+  if (n < nodes) p = a.parent[w.row0 + n];
+  const bool ok = !__syncthreads_or(n < nodes && (p < -1 || p >= n));
+  if (n == 0 && w.r0 == 0 && w.hk == 0 && a.tree_status) a.tree_status[w.b] = ok ? CURE_OK : CURE_ERR_BAD_TREE;
+  if (!ok) return false;
+  if (n < nodes) sh.parent[n] = p;
+  __syncthreads();
+  if (n < nodes) {
+    unsigned long long bits[kAncWords] = {};
+    for (int j = n; j >= 0; j = sh.parent[j]) {
+#pragma unroll
+      for (int i = 0; i < kAncWords; ++i) bits[i] |= j >> 6 == i ? 1ull << (j & 63) : 0ull;
+    }
+#pragma unroll
+    for (int i = 0; i < kAncWords; ++i) sh.anc[n][i] = bits[i];
+  }
+  __syncthreads();
   return true;
 }
 
-// Packed row R: its row of q and o, its query head and the last key that it sees.
+// Packed row R: its row of q and o, its query head, its token or node, and the last key that it
+// sees with all before it.
 struct Row {
   int64_t row;
-  int head, last;
+  int head, token, last;
 };
 template <bool kPrefix>
 CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
   const int t = R / a.group;
   Row r;
   r.head = w.hk * a.group + (R - t * a.group);
-  if (kPrefix) {
-    int lo = 0, hi = a.batch - 1;                  // the last sequence with first[b] <= t
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (sh.first[mid] <= t) lo = mid;
-      else hi = mid - 1;
-    }
-    r.row = (int64_t)lo * a.n_max + (t - sh.first[lo]);
-    r.last = w.keys - 1;
-  } else {
+  r.token = t;
+  if (!kPrefix || w.tree) {
     r.row = w.row0 + t;
-    r.last = w.ctx + t;
+    r.last = kPrefix ? w.ctx - 1 : w.ctx + t;
+    return r;
   }
+  int lo = 0, hi = a.batch - 1;                    // the last sequence with first[b] <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (sh.first[mid] <= t) lo = mid;
+    else hi = mid - 1;
+  }
+  r.row = (int64_t)lo * a.n_max + (t - sh.first[lo]);
+  r.last = w.ctx - 1;
   return r;
+}
+
+// Whether a row sees token t of its split: one up to `last`, or in a tree a node on its path.
+template <bool kPrefix>
+CURE_DEV bool sees(const Args& a, const Work& w, const Shared& sh, int t, int last, int node) {
+  if (!kPrefix || !w.tree) return t <= last;
+  const int j = t + w.begin - w.ctx, i = min(max(j, 0), CURE_MAX_TREE_NODES - 1);
+  const bool on_path = (sh.anc[node][i >> 6] >> (i & 63)) & 1;
+  return t <= last || (t + w.begin < w.end && on_path);
 }
 
 CURE_DEV void store8_f32(float* p, const float (&x)[8]) {
@@ -285,6 +373,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const int R = w.r0 + wave * 32 + col;
   const bool row_ok = R < w.rows;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
+  const int node = me.token;
   bf16x8 q[kKK];
   {
     const uint16_t* qrow = reinterpret_cast<const uint16_t*>(a.q) + (me.row * a.hq + me.head) * D;
@@ -300,8 +389,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const int last = me.last - w.begin;
   const int first_last = __builtin_amdgcn_readfirstlane(last);
   const int last_last = __builtin_amdgcn_readlane(last, 31);
-  const int my_steps = wave_ok ? min(steps, max(0, (last_last + kStep) / kStep)) : 0;
+  const int my_steps = !wave_ok ? 0 : kPrefix ? steps : min(steps, max(0, (last_last + kStep) / kStep));
   const int full = min(my_steps, max(0, (first_last + 1) / kStep));   // steps that every row sees whole
+  if (kPrefix && w.tree && w.end > w.ctx && !build_tree(a, w, sh)) {
+    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land after the workgroup ends
+    return;
+  }
 
   // LDS addresses of this lane's operands in slot 0.
   uint32_t k_at[kKK];
@@ -337,17 +430,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int r = 0; r < 2; ++r) f.h[r] = lds_read_tr8(v_at[i] + slot + (16 * ks + 8 * r) * G::kRowBytes);
     return f;
   };
-  // Probabilities against the reference m, and this lane's share of their sum.
-  auto exps = [&](const f32x16& x, Probs& p) {
-    float l0 = 0.f, l1 = 0.f;
+  // Probabilities against the reference m; returns `sum` with this lane's share of theirs.
+  auto exps = [&](const f32x16& x, Probs& p, float sum) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const bf16x2 v = {(__bf16)fast_exp2(fmaf(x[2 * j], c, -m)), (__bf16)fast_exp2(fmaf(x[2 * j + 1], c, -m))};
       p.set(j, v);
-      if (j & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l1, false);
-      else l0 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l0, false);
+      sum = __builtin_amdgcn_fdot2_f32_bf16(v, ones, sum, false);
     }
-    return l0 + l1;
+    return sum;
   };
   auto row_max = [&](const f32x16& x) {
     float mx = x[0];
@@ -355,20 +446,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
     return max_halves(mx) * c;
   };
-  // Moves the reference where a row's maximum has risen by more than 2^8, which no row's has
-  // while every lane's probabilities sum to 2^8 at most.
-  auto settle = [&](const f32x16& x, Probs& p, float ls) {
-    if (__builtin_expect(__ballot(!(ls <= 256.f)) != 0, 0)) {
+  // Takes over a step's sum. The reference moves where a row's maximum has risen by more than
+  // 2^8, which no row's has while no lane's sum has grown by more.
+  auto settle = [&](const f32x16& x, Probs& p, float sum) {
+    if (__builtin_expect(__ballot(!(sum - l <= 256.f)) != 0, 0)) {
       const float mx = row_max(x);
       const bool grow = mx > m + kRescaleLog2;
       const float alpha = grow ? fast_exp2(m - mx) : 1.f;
       m = grow ? mx : m;
-      l *= alpha;
 #pragma unroll
       for (int i = 0; i < kBlk; ++i) o[i] *= alpha;
-      ls = exps(x, p);
+      sum = exps(x, p, l * alpha);
     }
-    l += ls;
+    l = sum;
   };
   // The products of a step that some rows see in part: a token that a row does not see must
   // not reach it, but 0 times an infinity or a NaN would. Where the step's values hold one, the
@@ -400,7 +490,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
       o[n % kBlk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n].v, p.operand(n / kBlk), o[n % kBlk], 0, 0, 0);
     if (__builtin_expect(finite, 1)) return;
     for (int t = 0; t < kStep; ++t) {
-      const bool seen = h * kStep + t <= last;
+      const bool seen = sees<kPrefix>(a, w, sh, h * kStep + t, last, node);
 #pragma unroll
       for (int i = 0; i < kBlk; ++i)
 #pragma unroll
@@ -416,17 +506,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   auto mask = [&](f32x16& x, int h) {
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      x[r] = h * kStep + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? x[r] : -INFINITY;
+      x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
   };
   // A step in the middle of a row's keys: scores of the next step into y, probabilities of this
-  // one, whose scores are x, into n, products of the last one's, p; returns this lane's share of
-  // the sum. Every matrix instruction is followed by LDS reads for the one kAhead turns on and by an
+  // one, whose scores are x, into n, products of the last one's, p; returns the running sum. Every matrix instruction is followed by LDS reads for the one kAhead turns on and by an
   // equal share of the softmax, which the matrix unit's time hides.
   auto middle = [&](const f32x16& x, f32x16& y, const Probs& p, Probs& n, uint32_t k_slot, uint32_t v_slot) {
     constexpr int kPairs = 8 / kKK;                // pairs of probabilities per turn
     bf16x8 kf[kKK];
     Pack8 vf[kKK];
-    float e0[8], e1[8], l0 = 0.f, l1 = 0.f;
+    float e0[8], e1[8], sum = l;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       kf[i] = lds_read16(k_at[i] + k_slot);
@@ -435,8 +524,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     const auto round = [&](int j) {                // pair j: scores 2 j and 2 j + 1
       const bf16x2 v = {(__bf16)e0[j], (__bf16)e1[j]};
       n.set(j, v);
-      if (j & 1) l1 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l1, false);
-      else l0 = __builtin_amdgcn_fdot2_f32_bf16(v, ones, l0, false);
+      sum = __builtin_amdgcn_fdot2_f32_bf16(v, ones, sum, false);
     };
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[r] = 0.f;
@@ -461,7 +549,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     }
 #pragma unroll
     for (int j = 8 - kPairs; j < 8; ++j) round(j);
-    return l0 + l1;
+    return sum;
   };
   auto slot_of = [](int step) { return (uint32_t)(step % kRing) * G::kBytes; };
   // Step h begins: its slots (h + 1 of K, h - 1 of V) have landed for every wave, and those that
@@ -493,7 +581,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   begin(0, 0, 2 * G::kBytes);
   int h = 1;
   if (my_steps > 0) {
-    l = exps(x, p);
+    l = exps(x, p, 0.f);
     scores(x, G::kBytes);
     // Steps that every row sees whole, a ring's turn at a time.
     for (; h + kRing <= full; h += kRing) {
@@ -523,7 +611,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
       hidden_products(p, slot_of(h + 3), h - 1);
       if (h < my_steps) {
         mask(x, h);
-        settle(x, p, exps(x, p));
+        settle(x, p, exps(x, p, l));
         scores(x, slot_of(h + 1));
       }
     }
@@ -536,7 +624,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);   // a NaN stays one
   const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.s);
+  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
   const int64_t orow = me.row * a.hq + me.head;
   // Lanes l and l + 32 hold columns 0 - 3 and 4 - 7 of each eight of one row: they trade, so that each
   // has eight together, of every other eight.
@@ -625,6 +713,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   const int R = w.r0 + wave * 32 + col;
   const bool row_ok = R < w.rows;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
+  const int node = me.token;
   f32x4 q[kJ];
   {
     const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D;
@@ -635,7 +724,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   const int last = me.last - w.begin;
   const int first_last = __builtin_amdgcn_readfirstlane(last);
   const int last_last = __builtin_amdgcn_readlane(last, 31);
-  const int my_steps = wave_ok ? min(steps, max(0, (last_last + kStep) / kStep)) : 0;
+  const int my_steps = !wave_ok ? 0 : kPrefix ? steps : min(steps, max(0, (last_last + kStep) / kStep));
+  if (kPrefix && w.tree && w.end > w.ctx && !build_tree(a, w, sh)) {
+    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land after the workgroup ends
+    return;
+  }
 
   int k_off[kJ];
 #pragma unroll
@@ -685,7 +778,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       x[r] *= c;
-      if (tail) x[r] = h * kStep + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? x[r] : -INFINITY;
+      if (tail)
+        x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
     }
     float mt = x[0];
 #pragma unroll
@@ -732,7 +826,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
         o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(f[i]) < INFINITY ? f[i] : 0.f, x[r], o[i], 0, 0, 0);
     }
     for (int t = 0; t < kStep; ++t) {
-      const bool seen = h * kStep + t <= last;
+      const bool seen = sees<kPrefix>(a, w, sh, h * kStep + t, last, node);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int byte = (8 * (r >> 2) + 4 * half + (r & 3)) * (D / 32) * 4;
@@ -750,7 +844,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
   const float lse = lt == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.s);
+  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
   const int64_t orow = me.row * a.hq + me.head;
   // Lane's columns: (D / 32) c' + i for rows c' of the blocks, four consecutive ones at a time.
 #pragma unroll
@@ -769,60 +863,259 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// Joins the splits of a row, and for a prefix the tree part, by their log-sum-exps:
-// D / 4 lanes per (row, head), four columns each.
-struct MergeArgs : Args {
-  const float* tree_o;               // prefix: [batch][n_max][hq][d]
-  const float* tree_lse;             // [batch][n_max][hq]
-};
+// fp32 kernel for launches with few rows: a tile is 32 query rows, which all four waves
+// share. A step's scores take 64 matrix instructions at head dim 128 and as many its
+// products; each wave forms the scores of a quarter of the columns, which the waves add
+// through LDS, in one order, so that all hold the same, and the products of its own 32
+// columns (at head dim 64 of half the step's tokens as well; the halves are added at the end).
+//
+// As in the kernel above, with V read a column per lane: D register r of a wave's block i =
+// column 32 i + 8 (r / 4) + 4 half + r % 4.
+template <int D, bool kPrefix>
+__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
+  using G = GeoF32<D>;
+  constexpr int kJ = D / 8 / kWaves;               // column groups of a wave's scores
+  constexpr int kBlk = D / 32;
+  constexpr int kParts = kWaves / kBlk;            // waves that share a column block's tokens
+  constexpr int kRegs = 16 / kParts;               // score registers of a wave's tokens
+  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2][2][G::kBytes];   // [buffer][K, V]
+  __shared__ f32x4 s_x[kWaves][4][kWave];          // partial scores, at the end partial outputs
+  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
+  Shared& sh = reinterpret_cast<Shared&>(s_map);
 
+  Work w;
+  if (!locate<kPrefix>(a, w, sh)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int blk = wave % kBlk, r0 = wave / kBlk * kRegs;
+
+  const uint32_t tok_bytes = (uint32_t)(a.hkv * G::kRowBytes);
+  uint32_t src[G::kDma];
+#pragma unroll
+  for (int j = 0; j < G::kDma; ++j) {
+    const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
+    const int row = byte / G::kRowBytes;
+    src[j] = (uint32_t)row * tok_bytes +
+             (uint32_t)(w.hk * G::kRowBytes + ((((byte % G::kRowBytes) >> 4) ^ (row & 15)) << 4));
+  }
+  const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
+  const int steps = (w.end - w.begin + kStep - 1) / kStep;
+  auto dma = [&](int buf, int h) {
+    const int left = min(w.end - w.begin - h * kStep, kStep);
+    const uint32_t bytes = left > 0 ? (uint32_t)left * tok_bytes : 0u;
+    const int64_t at = (int64_t)h * kStep * tok_bytes;
+    const i32x4 rk = raw_rsrc(kp + at, bytes), rv = raw_rsrc(vp + at, bytes);
+#pragma unroll
+    for (int j = 0; j < G::kDma; ++j) {
+      const int b = (wave * G::kDma + j) * 1024;
+      dma16(lds_addr(&s_kv[buf][0][b]), src[j], rk);
+      dma16(lds_addr(&s_kv[buf][1][b]), src[j], rv);
+    }
+  };
+  dma(0, 0);
+
+  const int R = w.r0 + col;
+  const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
+  const int node = me.token;
+  f32x4 q[kJ];
+  {
+    const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D + wave * 8 * kJ;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) q[j] = *reinterpret_cast<const f32x4*>(qrow + 8 * j + 4 * half);
+  }
+  const int last = me.last - w.begin;
+  const int first_last = __builtin_amdgcn_readfirstlane(last);
+  if (kPrefix && w.tree && w.end > w.ctx && !build_tree(a, w, sh)) {
+    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land after the workgroup ends
+    return;
+  }
+
+  int k_off[kJ];
+#pragma unroll
+  for (int j = 0; j < kJ; ++j) k_off[j] = G::offset(col, 2 * (wave * kJ + j) + half);
+  // This wave's value of a step's token row, at column 32 blk + col.
+  const auto value = [&](const unsigned char* vt, int row) {
+    return *reinterpret_cast<const float*>(vt + G::offset(row, 8 * blk + (col >> 2)) + (col & 3) * 4);
+  };
+  const auto row_at = [&](int i) {                 // token row of this wave's score register r0 + i
+    const int r = r0 + i;
+    return 8 * (r >> 2) + 4 * half + (r & 3);
+  };
+
+  f32x16 o;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const float c = a.scale_log2;
+
+  __builtin_amdgcn_s_waitcnt(0);
+  for (int h = 0, buf = 0; h < steps; ++h, buf ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0);                 // this wave's DMA into `buf` has landed
+    __syncthreads();                               // everyone's has; the other buffer and s_x are free
+    dma(buf ^ 1, h + 1);
+    const unsigned char* kt = s_kv[buf][0];
+    const unsigned char* vt = s_kv[buf][1];
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) {
+      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + k_off[j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], q[j][i], x, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) s_x[wave][r / 4][lane] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
+    float f[kRegs];                                // values, on their way meanwhile
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) f[i] = value(vt, row_at(i));
+    __syncthreads();
+    const bool tail = h * kStep + kStep - 1 > first_last;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      f32x4 sum = s_x[0][b][lane];
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) sum += s_x[i][b][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * b + i] = sum[i] * c;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if (tail)
+        x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
+      mt = fmaxf(mt, x[r]);
+    }
+    const float m_new = fmaxf(m, max_halves(mt));
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    if (__ballot(m_new > m)) {                     // a maximum rose: rescale (factor 1 for the others)
+      const float alpha = fast_exp2(m - m_use);
+      l *= alpha;
+      o *= alpha;
+    }
+    m = m_new;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = fast_exp2(x[r] - m_use);
+      l += x[r];
+    }
+    float probe = 0.f;                             // a NaN from a value of a masked step that is not finite
+    if (tail) {
+#pragma unroll
+      for (int i = 0; i < kRegs; ++i) probe = fmaf(f[i], 0.f, probe);
+    }
+    const bool finite = __ballot(probe != 0.f) == 0;
+    if (__builtin_expect(!finite, 0)) {
+      // As in the bf16 kernel: zeros in the products, and the rows that see a value add it.
+      const int t0 = 2 * r0;                       // first token of this wave's registers
+      for (int t = t0; t < t0 + 2 * kRegs; ++t) {
+        const bool seen = sees<kPrefix>(a, w, sh, h * kStep + t, last, node);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int d = 8 * (r >> 2) + 4 * half + (r & 3);
+          const float v = *reinterpret_cast<const float*>(vt + G::offset(t, 8 * blk + (d >> 2)) + (d & 3) * 4);
+          o[r] += seen && !(fabsf(v) < INFINITY) ? v : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kRegs; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) {
+      float p = x[i];
+      if (kParts > 1) p = r0 ? x[(i + kRegs) % 16] : x[i];
+      o = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], p, o, 0, 0, 0);
+    }
+  }
+
+  __builtin_amdgcn_s_waitcnt(0);                   // the trailing DMA lands before exit
+  if (kParts > 1) {                                // the other tokens of this column block
+    static_assert(kParts <= 2, "at most two waves share a column block");
+    __syncthreads();
+    if (r0 > 0) {
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) s_x[blk][r / 4][lane] = f32x4{o[r], o[r + 1], o[r + 2], o[r + 3]};
+    }
+    __syncthreads();
+    if (r0 > 0) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] += s_x[blk][r / 4][lane][r % 4];
+  }
+  if (R >= w.rows) return;
+  const float lt = sum_halves(l);
+  const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
+  const float lse = lt == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(lt)) * kLn2;
+  const bool whole = w.splits == 1 && !kPrefix;
+  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
+  const int64_t orow = me.row * a.hq + me.head;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const int d0 = 32 * blk + 8 * b + 4 * half;
+    const float x0 = o[4 * b] * inv, x1 = o[4 * b + 1] * inv, x2 = o[4 * b + 2] * inv, x3 = o[4 * b + 3] * inv;
+    if (whole) store4(a, orow * D + d0, x0, x1, x2, x3);
+    else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x0, x1, x2, x3);
+  }
+  if (wave == 0 && half == 0) {
+    if (!whole) a.part_lse[pi] = lse;
+    else if (a.lse) a.lse[orow] = lse;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the parts of a row (a prompt's splits; a prefix's, then those of the own rows) by their
+// log-sum-exps: D / 4 lanes per (row, head), four columns each.
 constexpr int kMerge = 8;
 
 template <int D, bool kPrefix>
-__global__ __launch_bounds__(256) void seq_merge(MergeArgs a) {
+__global__ __launch_bounds__(256) void seq_merge(Args a) {
   constexpr int kLanes = D / 4;
   const int head = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
   const int col = (threadIdx.x % kLanes) * 4;
   const int i = blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
   const int n = min(a.n_rows[b], a.n_max);
+  const int ctx = a.ctx_len[b];
   if (i >= n) return;
-  int splits;
+  int shared, parts;                               // parts from slot 0 on, and in all
   int64_t row;
   if (kPrefix) {
-    splits = split_count(a, a.prefix_len);
+    shared = cut_of(a.cut, a.prefix_len).n;
+    parts = shared + cut_of(a.own, ctx + n).n;
     row = (int64_t)b * a.n_max + i;
   } else {
     // The tile of this row's head decides how many keys its splits covered.
     const int rows = n * a.group, R = i * a.group + head % a.group;
-    const int end = min((R / kRows + 1) * kRows, rows);
-    splits = split_count(a, a.ctx_len[b] + (end - 1) / a.group + 1);
-    if (splits == 1) return;                       // written whole
+    const int end = min((R / a.tile + 1) * a.tile, rows);
+    shared = parts = cut_of(a.cut, ctx + (end - 1) / a.group + 1).n;
+    if (parts == 1) return;                        // written whole
     row = a.row_off[b] + i;
   }
   const int64_t p0 = part_index(a, row, head, 0), orow = row * a.hq + head;
+  const int gap = a.cut.most - shared;             // slots that no split of the prefix has
   // kMerge parts at a time, all of whose loads are under way together. Parts that saw
   // nothing (a log-sum-exp of -inf) weigh nothing.
   float m = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float4 v[kMerge];
   float lse[kMerge];
-  if (kPrefix) {
-    m = a.tree_lse[orow];
-    acc = *reinterpret_cast<const float4*>(a.tree_o + orow * D + col);
-    sum = 1.f;
-  }
-  for (int s0 = 0; s0 < splits; s0 += kMerge) {
+  for (int s0 = 0; s0 < parts; s0 += kMerge) {
     float mn = m;
+    bool none = true;
 #pragma unroll
     for (int u = 0; u < kMerge; ++u) {
-      const bool ok = s0 + u < splits;
-      v[u] = ok ? *reinterpret_cast<const float4*>(a.part_o + (p0 + s0 + u) * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-      lse[u] = ok ? a.part_lse[p0 + s0 + u] : -INFINITY;
+      const bool ok = s0 + u < parts;
+      const int64_t at = p0 + s0 + u + (s0 + u < shared ? 0 : gap);
+      v[u] = ok ? *reinterpret_cast<const float4*>(a.part_o + at * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+      lse[u] = ok ? a.part_lse[at] : -INFINITY;
     }
 #pragma unroll
-    for (int u = 0; u < kMerge; ++u) mn = fmaxf(mn, lse[u]);
-    if (mn == -INFINITY) continue;
+    for (int u = 0; u < kMerge; ++u) {
+      mn = fmaxf(mn, lse[u]);
+      none = none && lse[u] == -INFINITY;
+    }
+    if (none) continue;
+    mn = mn == -INFINITY ? 0.f : mn;               // only NaNs, which come through
     const float w0 = fast_exp2((m - mn) * kLog2e);
     m = mn;
     sum *= w0;
@@ -848,63 +1141,90 @@ __global__ __launch_bounds__(256) void seq_merge(MergeArgs a) {
 // ---------------------------------------------------------------------------
 // Host: tiles, splits and workspace.
 struct Plan {
+  int tile;                          // query rows per tile
   int tiles;                         // most tiles of a sequence (a prefix: of all nodes)
-  int tps, max_splits;
+  int own_tiles;                     // prefix: most tiles of a sequence's own rows
+  Splits cut, own;
+  int slots() const { return cut.most + own.most; }
 };
 
-// Keys are split when the tiles alone leave workgroup slots (two per CU) empty.
-Plan make_plan(int64_t tiles_all, int64_t tiles_max, int hkv, int64_t keys_max, int32_t kv_split) {
-  Plan p{};
-  p.tiles = (int)std::min<int64_t>(tiles_max, INT32_MAX);
-  const auto round_step = [](int64_t t) { return std::max<int64_t>(64, (t + 63) / 64 * 64); };
-  int64_t splits = kv_split;
-  if (splits <= 0) {
-    const int64_t slots = 2 * (int64_t)device_cu_count();
-    splits = std::max<int64_t>(1, slots / std::max<int64_t>(1, tiles_all * hkv));
-    splits = std::min<int64_t>(splits, std::max<int64_t>(1, keys_max / kMinTps));
+// `most` splits of `keys`, or as many as there are whole steps.
+Splits splits_of(int64_t keys, int64_t most) {
+  most = std::max<int64_t>(1, std::min<int64_t>({most, (keys + kStep - 1) / kStep, 65535}));
+  const int64_t tps = ((keys + most - 1) / most + kStep - 1) / kStep * kStep;
+  return Splits{(int32_t)std::max<int64_t>(kStep, tps), (int32_t)most};
+}
+
+Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, const int32_t* host_n_rows,
+                 const int32_t* host_ctx_len, int32_t kv_split) {
+  const int64_t cus = device_cu_count(), group = hq / hkv;
+  int64_t tiles = 0, keys = 0, longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    tiles += (host_n_rows[b] * group + kRows - 1) / kRows;
+    longest = std::max<int64_t>(longest, host_n_rows[b]);
+    if (host_n_rows[b] > 0) keys = std::max<int64_t>(keys, (int64_t)host_n_rows[b] + host_ctx_len[b]);
   }
-  splits = std::min<int64_t>(splits, 65535);
-  p.tps = (int)std::min<int64_t>(round_step((keys_max + splits - 1) / splits), INT32_MAX / 2);
-  p.max_splits = (int)std::max<int64_t>(1, (keys_max + p.tps - 1) / p.tps);
+  Plan p{};
+  p.tile = dtype == CURE_F32 && tiles * hkv < cus ? kNarrow : kRows;
+  // A CU's share of the keys, tile by tile: tiles that see more are split.
+  int64_t work = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_rows[b], t = (n * group + p.tile - 1) / p.tile;
+    work += t * host_ctx_len[b] + t * (n + 1) / 2;
+    p.tiles = (int)std::max<int64_t>(p.tiles, t);
+  }
+  const int64_t few = longest * group <= 32 ? 3 : 1;
+  const int64_t tps = std::max<int64_t>(dtype == CURE_BF16 ? 256 : 128, work * hkv / cus / few);
+  // The merge's grid holds the tokens of a sequence in 16 bits.
+  const int64_t most = longest > 65535 ? 1 : kv_split > 0 ? kv_split : (keys + tps - 1) / tps;
+  p.cut = splits_of(keys, most);
   return p;
 }
 
-size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int splits) {
-  const size_t parts = (size_t)rows * hq * splits;
+Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t n_max, int32_t prefix_len,
+                 const int32_t* host_ctx_len, const int32_t* host_n_nodes, int32_t kv_split) {
+  const int64_t cus = device_cu_count(), group = hq / hkv;
+  const auto tiles_of = [&](int64_t nodes, int64_t tile) { return (nodes * group + tile - 1) / tile; };
+  int64_t nodes = 0, keys = 0, tiles = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_nodes[b];
+    nodes += n;
+    tiles += tiles_of(n, kRows);
+    if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
+  }
+  Plan p{};
+  p.tile = dtype == CURE_F32 && (tiles + tiles_of(nodes, kRows)) * hkv < cus ? kNarrow : kRows;
+  int64_t work = tiles_of(nodes, p.tile) * prefix_len;
+  for (int b = 0; b < batch; ++b)
+    work += tiles_of(host_n_nodes[b], p.tile) * ((int64_t)host_n_nodes[b] + host_ctx_len[b]);
+  const int64_t tps = std::max<int64_t>(dtype == CURE_BF16 ? 256 : 64, work * hkv / cus);
+  p.cut = splits_of(prefix_len, kv_split > 0 ? kv_split : prefix_len / tps);
+  p.own = splits_of(keys, (keys + tps - 1) / tps);
+  // The device may hold other counts than the host's copies: tiles for every node there may
+  // be, of which those past the last one end at once.
+  p.tiles = (int)std::min<int64_t>(tiles_of((int64_t)batch * n_max, p.tile), INT32_MAX);
+  p.own_tiles = (int)tiles_of(n_max, p.tile);
+  return p;
+}
+
+// Whether a call's parts go through the workspace: a prompt's where there are several.
+bool in_parts(const Plan& p) { return p.slots() > 1; }
+
+size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int slots) {
+  const size_t parts = (size_t)rows * hq * slots;
   return align_up(parts * d * sizeof(float), 256) + align_up(parts * sizeof(float), 256);
 }
 
-void set_parts(Args& a, void* ws, int64_t rows, int32_t d, int splits) {
-  const size_t parts = (size_t)rows * a.hq * splits;
+void set_plan(Args& a, const Plan& p, void* ws, int64_t rows, int32_t d) {
+  a.tile = p.tile;
+  a.tiles = p.tiles;
+  a.own_tiles = p.own_tiles;
+  a.cut = p.cut;
+  a.own = p.own;
+  if (!in_parts(p)) return;
+  const size_t parts = (size_t)rows * a.hq * p.slots();
   a.part_o = static_cast<float*>(ws);
   a.part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(parts * d * sizeof(float), 256));
-}
-
-Plan prompt_plan(int32_t batch, int32_t hq, int32_t hkv, const int32_t* host_n_rows, const int32_t* host_ctx_len,
-                 int32_t kv_split) {
-  int64_t all = 0, most = 0, keys = 0, longest = 0;
-  for (int b = 0; b < batch; ++b) {
-    const int64_t n = host_n_rows[b];
-    if (n <= 0) continue;
-    const int64_t tiles = (n * (hq / hkv) + kRows - 1) / kRows;
-    all += tiles;
-    most = std::max(most, tiles);
-    keys = std::max(keys, n + host_ctx_len[b]);
-    longest = std::max(longest, n);
-  }
-  // The merge's grid holds the tokens of a sequence in 16 bits.
-  return make_plan(all, most, hkv, keys, longest > 65535 ? 1 : kv_split);
-}
-
-Plan prefix_plan(int32_t batch, int32_t hq, int32_t hkv, int32_t n_max, int32_t prefix_len,
-                 const int32_t* host_n_nodes, int32_t kv_split) {
-  int64_t nodes = 0;
-  for (int b = 0; b < batch; ++b) nodes += std::min(std::max(host_n_nodes[b], 0), n_max);
-  const int64_t tiles = (nodes * (hq / hkv) + kRows - 1) / kRows;
-  // The device may hold other counts than the host's copies: tiles for every node there may
-  // be, of which those past the last one end at once.
-  const int64_t most = ((int64_t)batch * n_max * (hq / hkv) + kRows - 1) / kRows;
-  return make_plan(tiles, most, hkv, prefix_len, kv_split);
 }
 
 template <bool kPrefix>
@@ -913,6 +1233,9 @@ void launch_attn(const Args& a, int32_t dtype, int32_t d, dim3 grid, hipStream_t
   if (dtype == CURE_BF16) {
     if (d == 128) hipLaunchKernelGGL((seq_attn<128, kPrefix>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((seq_attn<64, kPrefix>), grid, block, 0, st, a);
+  } else if (a.tile == kNarrow) {
+    if (d == 128) hipLaunchKernelGGL((seq_attn_f32_shared<128, kPrefix>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((seq_attn_f32_shared<64, kPrefix>), grid, block, 0, st, a);
   } else {
     if (d == 128) hipLaunchKernelGGL((seq_attn_f32<128, kPrefix>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((seq_attn_f32<64, kPrefix>), grid, block, 0, st, a);
@@ -920,7 +1243,7 @@ void launch_attn(const Args& a, int32_t dtype, int32_t d, dim3 grid, hipStream_t
 }
 
 template <bool kPrefix>
-void launch_merge(const MergeArgs& a, int32_t d, hipStream_t st) {
+void launch_merge(const Args& a, int32_t d, hipStream_t st) {
   const int heads = 1024 / d;
   const dim3 grid((unsigned)((a.hq + heads - 1) / heads), (unsigned)a.n_max, (unsigned)a.batch);
   if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix>), grid, dim3(256), 0, st, a);
@@ -952,8 +1275,12 @@ extern "C" size_t cure_prompt_attn_workspace_size(int32_t batch, int64_t rows, i
                                                   const int32_t* host_n_rows, const int32_t* host_ctx_len,
                                                   int32_t kv_split) {
   if (batch <= 0 || rows <= 0 || hq <= 0 || hkv <= 0 || hq % hkv || d <= 0 || !host_n_rows || !host_ctx_len) return 0;
-  const Plan p = prompt_plan(batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
-  return p.max_splits > 1 ? part_bytes(rows, hq, d, p.max_splits) : 0;
+  size_t need = 0;                                 // of whichever type needs more
+  for (const int32_t dtype : {CURE_F32, CURE_BF16}) {
+    const Plan p = prompt_plan(dtype, batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+    if (in_parts(p)) need = std::max(need, part_bytes(rows, hq, d, p.slots()));
+  }
+  return need;
 }
 
 extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* o, float* lse,
@@ -977,12 +1304,12 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
     longest = std::max(longest, n);
   }
   if (longest == 0) return CURE_OK;
-  const Plan p = prompt_plan(batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
-  const size_t need = p.max_splits > 1 ? part_bytes(rows, hq, d, p.max_splits) : 0;
+  const Plan p = prompt_plan(dtype, batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+  const size_t need = in_parts(p) ? part_bytes(rows, hq, d, p.slots()) : 0;
   if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
   if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
   if ((int64_t)p.tiles * hkv * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
-  MergeArgs a{};
+  Args a{};
   a.q = q;
   a.k = k;
   a.v = v;
@@ -999,31 +1326,13 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   a.n_rows = n_rows;
   a.kv_off = kv_off;
   a.ctx_len = ctx_len;
-  a.tps = p.tps;
-  a.max_splits = p.max_splits;
-  if (need > 0) set_parts(a, workspace, rows, d, p.max_splits);
+  set_plan(a, p, workspace, rows, d);
   hipStream_t st = as_stream(stream);
-  launch_attn<false>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.max_splits, (unsigned)batch), st);
+  launch_attn<false>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.cut.most, (unsigned)batch), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
-  if (p.max_splits > 1) launch_merge<false>(a, d, st);
+  if (in_parts(p)) launch_merge<false>(a, d, st);
   return launch_status();
 }
-
-namespace {
-// The workspace of cure_prefix_attn: the prefix's partials, the tree part's output and
-// log-sum-exps, and cure_tree_attn's own.
-struct PrefixSpace {
-  size_t parts, o, lse, tree;
-  size_t total() const { return parts + o + lse + tree; }
-};
-PrefixSpace prefix_space(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max, int splits,
-                         const int32_t* host_ctx_len, const int32_t* host_n_nodes) {
-  const size_t rows = (size_t)batch * n_max * hq;
-  return {part_bytes((int64_t)batch * n_max, hq, d, splits), align_up(rows * d * sizeof(float), 256),
-          align_up(rows * sizeof(float), 256),
-          cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0)};
-}
-}  // namespace
 
 extern "C" size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max,
                                                   int32_t prefix_len, const int32_t* host_ctx_len,
@@ -1032,8 +1341,11 @@ extern "C" size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int
       !host_n_nodes)
     return 0;
   if (prefix_len == 0) return cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0);
-  const Plan p = prefix_plan(batch, hq, hkv, n_max, prefix_len, host_n_nodes, kv_split);
-  return prefix_space(batch, hq, hkv, d, n_max, p.max_splits, host_ctx_len, host_n_nodes).total();
+  int slots = 0;                                   // of whichever type takes more
+  for (const int32_t dtype : {CURE_F32, CURE_BF16})
+    slots = std::max(slots, prefix_plan(dtype, batch, hq, hkv, n_max, prefix_len, host_ctx_len, host_n_nodes,
+                                        kv_split).slots());
+  return part_bytes((int64_t)batch * n_max, hq, d, slots);
 }
 
 extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* o, float* lse,
@@ -1057,12 +1369,14 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
     return CURE_ERR_INVALID_ARG;
   for (int b = 0; b < batch; ++b)
     if (host_ctx_len[b] < 0 || host_n_nodes[b] < 0 || host_n_nodes[b] > n_max) return CURE_ERR_INVALID_ARG;
-  const Plan p = prefix_plan(batch, hq, hkv, n_max, prefix_len, host_n_nodes, kv_split);
-  const PrefixSpace sp = prefix_space(batch, hq, hkv, d, n_max, p.max_splits, host_ctx_len, host_n_nodes);
-  if (!workspace || workspace_bytes < sp.total()) return CURE_ERR_WORKSPACE;
+  for (int b = 0; b < batch; ++b)
+    if (host_ctx_len[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
+  const Plan p = prefix_plan(dtype, batch, hq, hkv, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
+  if (!workspace || workspace_bytes < part_bytes((int64_t)batch * n_max, hq, d, p.slots())) return CURE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
-  if ((int64_t)p.tiles * hkv * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
-  MergeArgs a{};
+  const int64_t units = ((int64_t)p.tiles * p.cut.most + (int64_t)p.own_tiles * batch * p.own.most) * hkv;
+  if (units * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
+  Args a{};
   a.q = q;
   a.k = k;
   a.v = v;
@@ -1076,22 +1390,16 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   a.n_max = n_max;
   a.scale_log2 = scale * kLog2e;
   a.n_rows = n_nodes;
+  a.kv_off = kv_off;
+  a.ctx_len = ctx_len;
+  a.parent = parent;
+  a.tree_status = tree_status;
   a.prefix_off = prefix_off;
   a.prefix_len = prefix_len;
-  a.tps = p.tps;
-  a.max_splits = p.max_splits;
-  set_parts(a, workspace, (int64_t)batch * n_max, d, p.max_splits);
-  char* ws = static_cast<char*>(workspace) + sp.parts;
-  a.tree_o = reinterpret_cast<float*>(ws);
-  float* tree_lse = reinterpret_cast<float*>(ws + sp.o);
-  a.tree_lse = tree_lse;
+  set_plan(a, p, workspace, (int64_t)batch * n_max, d);
   hipStream_t st = as_stream(stream);
-  launch_attn<true>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.max_splits), st);
+  launch_attn<true>(a, dtype, d, dim3((unsigned)units), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
-  const cure_status tree =
-      cure_tree_attn(q, k, v, ws, tree_lse, dtype, CURE_F32, batch, hq, hkv, d, scale, kv_off, ctx_len, n_nodes,
-                     parent, n_max, host_ctx_len, host_n_nodes, 0, 0, tree_status, ws + sp.o + sp.lse, sp.tree, stream);
-  if (tree != CURE_OK) return tree;
   launch_merge<true>(a, d, st);
   return launch_status();
 }

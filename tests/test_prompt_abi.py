@@ -176,8 +176,9 @@ def test_workspace_sizes(L):
     assert size(1) == 0 and size(4) >= 2 * 32 * 4 * 129 * 4 and size(8) > size(4)
     assert L.cure_prompt_attn_workspace_size(0, 2, 32, 8, 128, n[1], c[1], 0) == 0
     tree = L.cure_tree_attn_workspace_size(2, 32, 8, 128, 1, c[1], n[1], 0)
-    f = lambda length: L.cure_prefix_attn_workspace_size(2, 32, 8, 128, 1, length, c[1], n[1], 0)  # noqa: E731
-    assert f(0) == tree and f(100) >= tree + 2 * 32 * 2 * 129 * 4
+    f = lambda length, split=0: L.cure_prefix_attn_workspace_size(2, 32, 8, 128, 1, length, c[1], n[1], split)  # noqa: E731
+    parts = lambda slots: 2 * 32 * slots * 129 * 4  # noqa: E731
+    assert f(0) == tree and f(100) >= parts(2) and f(1000, 8) >= parts(9) and f(1000, 8) > f(1000, 1)
 
 
 @pytest.fixture
