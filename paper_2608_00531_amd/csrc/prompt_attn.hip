@@ -326,7 +326,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   constexpr int kKK = D / 16;                      // k-steps of the scores
   constexpr int kBlk = D / 32;                     // 32-column blocks of the output
   constexpr int kAhead = 2;
-  // Beyond what a step needs, the DMA of the two steps before it may be in flight.
+  // Beyond what a step needs, the DMA of the kRing - 2 steps before it may be in flight.
   constexpr int kVmWait = waitcnt_vm((kRing - 2) * 2 * G::kDma);
   __shared__ __attribute__((aligned(1024))) unsigned char s_k[kRing * G::kBytes];
   __shared__ __attribute__((aligned(1024))) unsigned char s_v[kRing * G::kBytes];
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
 #pragma unroll
   for (int h = 0; h < kRing; ++h) {
     dma(kp, k_src, k_lds + h * G::kBytes, h);
-    if (h < 2) dma(vp, v_src, v_lds + h * G::kBytes, h);
+    if (h < kRing - 2) dma(vp, v_src, v_lds + h * G::kBytes, h);
   }
 
   // This lane's query row.
@@ -558,7 +558,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     __builtin_amdgcn_s_waitcnt(kVmWait);
     __syncthreads();
     dma(kp, k_src, k_lds + k_slot, h + kRing);
-    dma(vp, v_src, v_lds + v_slot, h + 2);
+    dma(vp, v_src, v_lds + v_slot, h + kRing - 2);
   };
 
   __builtin_amdgcn_s_waitcnt(0);
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     const float mx = row_max(x);
     m = mx == -INFINITY ? 0.f : mx;
   }
-  begin(0, 0, 2 * G::kBytes);
+  begin(0, 0, slot_of(kRing - 2));
   int h = 1;
   if (my_steps > 0) {
     l = exps(x, p, 0.f);
@@ -589,8 +589,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
       for (int j = 1; j <= kRing; ++j) {           // step h + j - 1, j modulo the ring
         f32x16 y;
         Probs n;
-        begin(h + j - 1, j % kRing * G::kBytes, (j + 2) % kRing * G::kBytes);
-        settle(x, n, middle(x, y, p, n, (j + 1) % kRing * G::kBytes, (j + 3) % kRing * G::kBytes));
+        begin(h + j - 1, slot_of(j), slot_of(j + kRing - 2));
+        settle(x, n, middle(x, y, p, n, slot_of(j + 1), slot_of(j + kRing - 1)));
         x = y;
         p = n;
       }
@@ -599,16 +599,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     for (; h < my_steps && h <= full; ++h) {
       f32x16 y;
       Probs n;
-      begin(h, slot_of(h), slot_of(h + 2));
+      begin(h, slot_of(h), slot_of(h + kRing - 2));
       if (h == full) mask(x, h);
-      settle(x, n, middle(x, y, p, n, slot_of(h + 1), slot_of(h + 3)));
+      settle(x, n, middle(x, y, p, n, slot_of(h + 1), slot_of(h + kRing - 1)));
       x = y;
       p = n;
     }
     // What is seen in part.
     for (; h <= my_steps; ++h) {
-      begin(h, slot_of(h), slot_of(h + 2));
-      hidden_products(p, slot_of(h + 3), h - 1);
+      begin(h, slot_of(h), slot_of(h + kRing - 2));
+      hidden_products(p, slot_of(h + kRing - 1), h - 1);
       if (h < my_steps) {
         mask(x, h);
         settle(x, p, exps(x, p, l));
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
       }
     }
   }
-  for (; h <= steps; ++h) begin(h, slot_of(h), slot_of(h + 2));
+  for (; h <= steps; ++h) begin(h, slot_of(h), slot_of(h + kRing - 2));
 
   __builtin_amdgcn_s_waitcnt(0);                   // the rings' trailing DMA lands before exit
   if (!row_ok) return;
@@ -1155,51 +1155,120 @@ Splits splits_of(int64_t keys, int64_t most) {
   return Splits{(int32_t)std::max<int64_t>(kStep, tps), (int32_t)most};
 }
 
-Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, const int32_t* host_n_rows,
+// Splits that a plan considers of the longest keys.
+constexpr int kCandidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+
+// Estimated us, from measurements: a step of 32 keys with one workgroup on a CU (two on a CU take
+// turns: together they are no faster), and what a workgroup takes beside its steps, of which
+// the way of its part of `rows` rows to memory and back at a CU's share of the bandwidth.
+struct Cost {
+  double key, start, part;
+  Cost(int32_t dtype, int tile, int32_t d, double rows) {
+    const double step = dtype == CURE_BF16 ? (d == 128 ? 0.45 : 0.28) : (tile == kNarrow ? 2.2 : 3.6) * d / 128;
+    key = step / kStep;
+    start = 5;
+    part = std::min<double>(tile, rows) * d * 8 / 27e3;
+  }
+};
+
+Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t d, const int32_t* host_n_rows,
                  const int32_t* host_ctx_len, int32_t kv_split) {
   const int64_t cus = device_cu_count(), group = hq / hkv;
-  int64_t tiles = 0, keys = 0, longest = 0;
+  const auto tiles_of = [&](int64_t n, int64_t tile) { return (n * group + tile - 1) / tile; };
+  int64_t wide = 0, keys = 0, longest = 0, total = 0;
   for (int b = 0; b < batch; ++b) {
-    tiles += (host_n_rows[b] * group + kRows - 1) / kRows;
-    longest = std::max<int64_t>(longest, host_n_rows[b]);
-    if (host_n_rows[b] > 0) keys = std::max<int64_t>(keys, (int64_t)host_n_rows[b] + host_ctx_len[b]);
+    const int64_t n = host_n_rows[b];
+    wide += tiles_of(n, kRows);
+    total += n;
+    longest = std::max(longest, n);
+    if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   Plan p{};
-  p.tile = dtype == CURE_F32 && tiles * hkv < cus ? kNarrow : kRows;
-  // A CU's share of the keys, tile by tile: tiles that see more are split.
-  int64_t work = 0;
-  for (int b = 0; b < batch; ++b) {
-    const int64_t n = host_n_rows[b], t = (n * group + p.tile - 1) / p.tile;
-    work += t * host_ctx_len[b] + t * (n + 1) / 2;
-    p.tiles = (int)std::max<int64_t>(p.tiles, t);
-  }
-  const int64_t few = longest * group <= 32 ? 3 : 1;
-  const int64_t tps = std::max<int64_t>(dtype == CURE_BF16 ? 256 : 128, work * hkv / cus / few);
+  p.tile = dtype == CURE_F32 && wide * hkv < cus ? kNarrow : kRows;
+  p.tiles = (int)tiles_of(longest, p.tile);
   // The merge's grid holds the tokens of a sequence in 16 bits.
-  const int64_t most = longest > 65535 ? 1 : kv_split > 0 ? kv_split : (keys + tps - 1) / tps;
+  int64_t most = longest > 65535 ? 1 : kv_split;
+  if (most == 0) {
+    // The splits of the longest keys that are estimated to take least time: that of the CUs
+    // with the most workgroups, or of the longest workgroup. Measured us a call with 1, 2, 4 and 12
+    // splits: one prompt of 2k 52, 72 (two); 4 chunks of 256 - 512 tokens on 2k - 16k, head dim
+    // 64, 211, 185, 207, 222; 8 single tokens on 4k - 32k 385, 202, 120, 105.
+    const Cost cost(dtype, p.tile, d, (double)total * group / std::max<int64_t>(1, wide));
+    double best = 0;
+    for (const int s : kCandidates) {
+      const int64_t tps = std::max<int64_t>(kStep, (keys + s - 1) / s);
+      if (s > 1 && tps < (dtype == CURE_BF16 ? 256 : 96)) break;
+      int64_t units = 0;
+      double work = 0;
+      for (int b = 0; b < batch; ++b) {
+        const int64_t n = host_n_rows[b], t = tiles_of(n, p.tile);
+        const int64_t mean = host_ctx_len[b] + (n + 1) / 2 + std::min<int64_t>(n, p.tile / group) / 2;
+        units += t * std::max<int64_t>(1, (mean + tps - 1) / tps);
+        work += (double)t * mean;
+      }
+      units = std::max<int64_t>(1, units * hkv);
+      if (longest * group <= 32) {
+        // Single tokens and the like stream the cache once: as many workgroups as two per CU,
+        // whose tiles under way cover the memory's latency.
+        if (s == 1 || units <= 2 * cus) most = s;
+        continue;
+      }
+      const double each = cost.start + (s > 1 ? cost.part : 0);
+      const double all = (double)((units + cus - 1) / cus) * (work * hkv / units * cost.key + each);
+      const double time = std::max(all, tps * cost.key + each) + (s > 1 ? 5 : 0);
+      if (most == 0 || time < best) {
+        most = s;
+        best = time;
+      }
+    }
+  }
   p.cut = splits_of(keys, most);
   return p;
 }
 
-Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t n_max, int32_t prefix_len,
-                 const int32_t* host_ctx_len, const int32_t* host_n_nodes, int32_t kv_split) {
+Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max,
+                 int32_t prefix_len, const int32_t* host_ctx_len, const int32_t* host_n_nodes, int32_t kv_split) {
   const int64_t cus = device_cu_count(), group = hq / hkv;
   const auto tiles_of = [&](int64_t nodes, int64_t tile) { return (nodes * group + tile - 1) / tile; };
-  int64_t nodes = 0, keys = 0, tiles = 0;
+  int64_t nodes = 0, keys = 0, wide = 0;
   for (int b = 0; b < batch; ++b) {
     const int64_t n = host_n_nodes[b];
     nodes += n;
-    tiles += tiles_of(n, kRows);
+    wide += tiles_of(n, kRows);
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   Plan p{};
-  p.tile = dtype == CURE_F32 && (tiles + tiles_of(nodes, kRows)) * hkv < cus ? kNarrow : kRows;
-  int64_t work = tiles_of(nodes, p.tile) * prefix_len;
-  for (int b = 0; b < batch; ++b)
-    work += tiles_of(host_n_nodes[b], p.tile) * ((int64_t)host_n_nodes[b] + host_ctx_len[b]);
-  const int64_t tps = std::max<int64_t>(dtype == CURE_BF16 ? 256 : 64, work * hkv / cus);
-  p.cut = splits_of(prefix_len, kv_split > 0 ? kv_split : prefix_len / tps);
-  p.own = splits_of(keys, (keys + tps - 1) / tps);
+  p.tile = dtype == CURE_F32 && (wide + tiles_of(nodes, kRows)) * hkv < cus ? kNarrow : kRows;
+  const int64_t tiles = tiles_of(nodes, p.tile);
+  int64_t most = kv_split, own = 1;
+  // As for prompts; own rows are split as the prefix is, and fill the CUs around its
+  // workgroups. Measured us a call with 1, 2, 4 and 12 splits: 16 trees of 40 - 48 nodes on 8k 131,
+  // 122, 137, 171; 32 single tokens on 16k, head dim 64, 169, 92, 52, 27 (24 with 24, 26 with 32).
+  const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
+  double best = 0;
+  for (const int s : kCandidates) {
+    const int64_t tps = std::max<int64_t>(kStep, ((kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len) + s - 1) / s);
+    if (s > 1 && (kv_split > 0 || tps < (dtype == CURE_BF16 ? 256 : 64))) break;
+    const int64_t own_tps = std::max<int64_t>(tps, dtype == CURE_BF16 ? 256 : 64);
+    int64_t units = tiles * s * hkv;
+    double work = (double)tiles * prefix_len;
+    for (int b = 0; b < batch; ++b) {
+      const int64_t t = tiles_of(host_n_nodes[b], p.tile), k = (int64_t)host_n_nodes[b] + host_ctx_len[b];
+      units += t * std::max<int64_t>(1, (k + own_tps - 1) / own_tps) * hkv;
+      work += (double)t * k;
+    }
+    const double each = cost.start + cost.part, unit = tps * cost.key + each;
+    double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
+    // The fp32 kernel for few rows leaves room for one workgroup on a CU.
+    if (p.tile == kNarrow) time = std::max(time, (double)((tiles * s * hkv + cus - 1) / cus) * unit);
+    if (best == 0 || time < best) {
+      if (kv_split == 0) most = s;
+      own = (keys + own_tps - 1) / own_tps;
+      best = time;
+    }
+  }
+  p.cut = splits_of(prefix_len, most);
+  p.own = splits_of(keys, own);
   // The device may hold other counts than the host's copies: tiles for every node there may
   // be, of which those past the last one end at once.
   p.tiles = (int)std::min<int64_t>(tiles_of((int64_t)batch * n_max, p.tile), INT32_MAX);
@@ -1277,7 +1346,7 @@ extern "C" size_t cure_prompt_attn_workspace_size(int32_t batch, int64_t rows, i
   if (batch <= 0 || rows <= 0 || hq <= 0 || hkv <= 0 || hq % hkv || d <= 0 || !host_n_rows || !host_ctx_len) return 0;
   size_t need = 0;                                 // of whichever type needs more
   for (const int32_t dtype : {CURE_F32, CURE_BF16}) {
-    const Plan p = prompt_plan(dtype, batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+    const Plan p = prompt_plan(dtype, batch, hq, hkv, d, host_n_rows, host_ctx_len, kv_split);
     if (in_parts(p)) need = std::max(need, part_bytes(rows, hq, d, p.slots()));
   }
   return need;
@@ -1304,7 +1373,7 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
     longest = std::max(longest, n);
   }
   if (longest == 0) return CURE_OK;
-  const Plan p = prompt_plan(dtype, batch, hq, hkv, host_n_rows, host_ctx_len, kv_split);
+  const Plan p = prompt_plan(dtype, batch, hq, hkv, d, host_n_rows, host_ctx_len, kv_split);
   const size_t need = in_parts(p) ? part_bytes(rows, hq, d, p.slots()) : 0;
   if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
   if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
@@ -1343,7 +1412,7 @@ extern "C" size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int
   if (prefix_len == 0) return cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0);
   int slots = 0;                                   // of whichever type takes more
   for (const int32_t dtype : {CURE_F32, CURE_BF16})
-    slots = std::max(slots, prefix_plan(dtype, batch, hq, hkv, n_max, prefix_len, host_ctx_len, host_n_nodes,
+    slots = std::max(slots, prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes,
                                         kv_split).slots());
   return part_bytes((int64_t)batch * n_max, hq, d, slots);
 }
@@ -1371,7 +1440,7 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
     if (host_ctx_len[b] < 0 || host_n_nodes[b] < 0 || host_n_nodes[b] > n_max) return CURE_ERR_INVALID_ARG;
   for (int b = 0; b < batch; ++b)
     if (host_ctx_len[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
-  const Plan p = prefix_plan(dtype, batch, hq, hkv, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
+  const Plan p = prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
   if (!workspace || workspace_bytes < part_bytes((int64_t)batch * n_max, hq, d, p.slots())) return CURE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
   const int64_t units = ((int64_t)p.tiles * p.cut.most + (int64_t)p.own_tiles * batch * p.own.most) * hkv;
