@@ -37,6 +37,16 @@ constexpr int kNarrow = 32;          // query rows per tile of the fp32 kernel t
 constexpr int kMaxPrefixBatch = 1024;
 constexpr int kAncWords = CURE_MAX_TREE_NODES / 64;
 
+// Division by a launch's constant: x / d = the high half of x * (2^32 / d + 1) while x * d < 2^32.
+struct Div {
+  int32_t d;
+  uint32_t m;                        // 0: divide
+  static Div by(int32_t d, int64_t x_max) {
+    return Div{d, d > 1 && x_max * d < (int64_t(1) << 32) ? (uint32_t)((uint64_t(1) << 32) / (uint32_t)d + 1) : 0u};
+  }
+  CURE_DEV int operator()(int x) const { return m ? (int)__umulhi((uint32_t)x, m) : d == 1 ? x : x / d; }
+};
+
 // How keys are split: at most `most` splits of about tps tokens, at least one.
 struct Splits {
   int32_t tps, most;
@@ -50,6 +60,7 @@ struct Args {
   float* lse;
   int32_t out_bf16;
   int32_t hq, hkv, group;
+  Div by_group, by_hkv;
   int32_t batch, n_max;
   float scale_log2;
   const int64_t* row_off;            // prompt: first row of q and o per sequence
@@ -60,7 +71,7 @@ struct Args {
   int32_t* tree_status;
   int64_t prefix_off;
   int32_t prefix_len;
-  int32_t tile;                      // query rows of a tile
+  int32_t tile, tile_log2;           // query rows of a tile
   int32_t tiles, own_tiles;          // prefix: tiles of all nodes, and of a sequence's
   Splits cut, own;                   // of a prompt's keys or the prefix, and of own rows
   float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most
@@ -71,11 +82,13 @@ CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int slot) {
   return (row * a.hq + head) * (a.cut.most + a.own.most) + slot;
 }
 
-// The splits of `keys` (at least one) keys: n of `per` tokens, whole steps, the last one shorter.
+// The splits of `keys` (at least one) keys: n of `per` tokens, whole steps, the last one shorter
+// (a single one: all).
 struct Cut {
   int n, per;
 };
 CURE_DEV Cut cut_of(const Splits& s, int keys) {
+  if (s.most == 1) return Cut{1, keys};
   const int n = max(1, min((keys - 1) / s.tps + 1, s.most));
   const int per = ((keys - 1) / n / kStep + 1) * kStep;
   return Cut{(keys - 1) / per + 1, per};
@@ -103,7 +116,7 @@ struct Shared {
 // most keys, come first. A sequence's tiles stay together, as they share its keys in the L2: dealt
 // out in turn over the sequences, 16 prompts of 1 to 2048 tokens took 399 us instead of 253.
 CURE_DEV bool locate_prompt(const Args& a, Work& w) {
-  const int b = blockIdx.z, x = blockIdx.x / a.hkv;
+  const int b = blockIdx.z, x = a.by_hkv(blockIdx.x);
   w.hk = blockIdx.x - x * a.hkv;
   const int n_raw = a.n_rows[b];
   w.ctx = a.ctx_len[b];
@@ -112,10 +125,10 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.row0), "s"(w.key0));
   const int n = min(n_raw, a.n_max);
   w.rows = n * a.group;
-  const int tiles = (w.rows + a.tile - 1) / a.tile;
+  const int tiles = (w.rows + a.tile - 1) >> a.tile_log2;
   if (n <= 0 || x >= tiles) return false;
   w.r0 = (tiles - 1 - x) * a.tile;
-  const int keys = w.ctx + (min(w.r0 + a.tile, w.rows) - 1) / a.group + 1;
+  const int keys = w.ctx + a.by_group(min(w.r0 + a.tile, w.rows) - 1) + 1;
   const Cut c = cut_of(a.cut, keys);
   w.tree = false;
   w.slot = blockIdx.y;
@@ -129,7 +142,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
 // rows). The prefix's tiles hold the existing nodes of all sequences in order, whose counts are
 // summed here.
 CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
-  int x = blockIdx.x / a.hkv;
+  int x = a.by_hkv(blockIdx.x);
   w.hk = blockIdx.x - x * a.hkv;
   const int shared_units = a.tiles * a.cut.most;
   w.tree = x >= shared_units;
@@ -196,7 +209,7 @@ CURE_DEV bool locate(const Args& a, Work& w, Shared& sh) {
 // The ancestor bits of sequence b's nodes, for a workgroup of at least 256 threads whose work
 // reaches the tree's rows; reports the tree's status. False: malformed.
 CURE_DEV bool build_tree(const Args& a, const Work& w, Shared& sh) {
-  const int n = threadIdx.x, nodes = w.rows / a.group;
+  const int n = threadIdx.x, nodes = a.by_group(w.rows);
   int p = -1;
   if (n < nodes) p = a.parent[w.row0 + n];
   const bool ok = !__syncthreads_or(n < nodes && (p < -1 || p >= n));
@@ -225,7 +238,7 @@ struct Row {
 };
 template <bool kPrefix>
 CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
-  const int t = R / a.group;
+  const int t = a.by_group(R);
   Row r;
   r.head = w.hk * a.group + (R - t * a.group);
   r.token = t;
@@ -872,7 +885,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
 // As in the kernel above, with V read a column per lane: D register r of a wave's block i =
 // column 32 i + 8 (r / 4) + 4 half + r % 4.
 template <int D, bool kPrefix>
-__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
+__global__ __launch_bounds__(64 * kWaves) void seq_attn_f32_shared(Args a) {
   using G = GeoF32<D>;
   constexpr int kJ = D / 8 / kWaves;               // column groups of a wave's scores
   constexpr int kBlk = D / 32;
@@ -1085,9 +1098,9 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
     row = (int64_t)b * a.n_max + i;
   } else {
     // The tile of this row's head decides how many keys its splits covered.
-    const int rows = n * a.group, R = i * a.group + head % a.group;
-    const int end = min((R / a.tile + 1) * a.tile, rows);
-    shared = parts = cut_of(a.cut, ctx + (end - 1) / a.group + 1).n;
+    const int rows = n * a.group, R = i * a.group + (head - a.by_group(head) * a.group);
+    const int end = min(((R >> a.tile_log2) + 1) * a.tile, rows);
+    shared = parts = cut_of(a.cut, ctx + a.by_group(end - 1) + 1).n;
     if (parts == 1) return;                        // written whole
     row = a.row_off[b] + i;
   }
@@ -1286,6 +1299,8 @@ size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int slots) {
 
 void set_plan(Args& a, const Plan& p, void* ws, int64_t rows, int32_t d) {
   a.tile = p.tile;
+  a.tile_log2 = p.tile == kNarrow ? 5 : 7;
+  static_assert(kNarrow == 1 << 5 && kRows == 1 << 7, "tiles of a power of two");
   a.tiles = p.tiles;
   a.own_tiles = p.own_tiles;
   a.cut = p.cut;
@@ -1388,6 +1403,8 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   a.hq = hq;
   a.hkv = hkv;
   a.group = hq / hkv;
+  a.by_group = Div::by(a.group, std::max<int64_t>(longest * a.group, hq));
+  a.by_hkv = Div::by(hkv, (int64_t)p.tiles * hkv);
   a.batch = batch;
   a.n_max = (int32_t)longest;
   a.scale_log2 = scale * kLog2e;
@@ -1455,6 +1472,8 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   a.hq = hq;
   a.hkv = hkv;
   a.group = hq / hkv;
+  a.by_group = Div::by(a.group, std::max<int64_t>((int64_t)batch * n_max * a.group, hq));
+  a.by_hkv = Div::by(hkv, units);
   a.batch = batch;
   a.n_max = n_max;
   a.scale_log2 = scale * kLog2e;
