@@ -50,8 +50,16 @@ CURE_DEV i16x4 lds_read_tr8(uint32_t addr) {
 // land at lds_base + 16 * i (lds_base travels in M0). Out-of-range offsets
 // read as zero. A DMA may follow the write of its M0 after one wait state, which the
 // compiler does not add for an instruction that it cannot see into.
+// dma16 marks the bytes as read once; dma16_shared leaves them to the L2, for
+// workgroups that read the same ones.
 CURE_DEV void dma16(uint32_t lds_base, uint32_t voff, i32x4 rsrc) {
   asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds"
+               :
+               : "v"(voff), "s"(rsrc), "{m0}"(lds_base)
+               : "memory");
+}
+CURE_DEV void dma16_shared(uint32_t lds_base, uint32_t voff, i32x4 rsrc) {
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :
                : "v"(voff), "s"(rsrc), "{m0}"(lds_base)
                : "memory");
