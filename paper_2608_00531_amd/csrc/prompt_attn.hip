@@ -106,11 +106,26 @@ struct Work {
   bool tree;                         // a sequence's own rows, in cure_prefix_attn
 };
 
-struct Shared {
-  int first[kMaxPrefixBatch + 1];    // nodes before each sequence
-  int parent[CURE_MAX_TREE_NODES];
-  unsigned long long anc[CURE_MAX_TREE_NODES][kAncWords];   // a tree's root paths, as bits
+// What cure_prefix_attn keeps in LDS beside the tiles: for the start of a workgroup alone the
+// nodes before each sequence, or a tree's parents; then the root paths of its tile's nodes, as bits.
+template <int kTileRows>
+struct TreeSpace {
+  unsigned long long anc[kTileRows][kAncWords];
 };
+struct StartSpace {
+  int first[kMaxPrefixBatch + 1];
+  int parent[CURE_MAX_TREE_NODES];
+};
+struct Shared {
+  int* first;
+  int* parent;
+  unsigned long long (*anc)[kAncWords];
+};
+struct Nothing {};
+template <class T>
+CURE_DEV Shared shared_of(StartSpace& s, T& t) { return Shared{s.first, s.parent, t.anc}; }
+CURE_DEV Shared shared_of(Nothing&, Nothing&) { return Shared{}; }
+CURE_DEV Shared shared_of(StartSpace&, Nothing&) { return Shared{}; }
 
 // Prompt: grid (kv-heads x tiles, splits, sequences); a sequence's last tiles, which see the
 // most keys, come first. A sequence's tiles stay together, as they share its keys in the L2: dealt
@@ -141,7 +156,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
 // Prefix: kv-heads x (tiles x splits of the prefix, then tiles x splits of each sequence's own
 // rows). The prefix's tiles hold the existing nodes of all sequences in order, whose counts are
 // summed here.
-CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
+CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
   int x = a.by_hkv(blockIdx.x);
   w.hk = blockIdx.x - x * a.hkv;
   const int shared_units = a.tiles * a.cut.most;
@@ -202,13 +217,13 @@ CURE_DEV bool locate_prefix(const Args& a, Work& w, Shared& sh) {
 }
 
 template <bool kPrefix>
-CURE_DEV bool locate(const Args& a, Work& w, Shared& sh) {
+CURE_DEV bool locate(const Args& a, Work& w, const Shared& sh) {
   return kPrefix ? locate_prefix(a, w, sh) : locate_prompt(a, w);
 }
 
-// The ancestor bits of sequence b's nodes, for a workgroup of at least 256 threads whose work
+// The ancestor bits of the tile's nodes, for a workgroup of at least 256 threads whose work
 // reaches the tree's rows; reports the tree's status. False: malformed.
-CURE_DEV bool build_tree(const Args& a, const Work& w, Shared& sh) {
+CURE_DEV bool build_tree(const Args& a, const Work& w, const Shared& sh) {
   const int n = threadIdx.x, nodes = a.by_group(w.rows);
   int p = -1;
   if (n < nodes) p = a.parent[w.row0 + n];
@@ -217,9 +232,10 @@ CURE_DEV bool build_tree(const Args& a, const Work& w, Shared& sh) {
   if (!ok) return false;
   if (n < nodes) sh.parent[n] = p;
   __syncthreads();
-  if (n < nodes) {
+  const int t0 = a.by_group(w.r0), t1 = a.by_group(min(w.r0 + a.tile, w.rows) - 1);
+  if (n <= t1 - t0) {
     unsigned long long bits[kAncWords] = {};
-    for (int j = n; j >= 0; j = sh.parent[j]) {
+    for (int j = t0 + n; j >= 0; j = sh.parent[j]) {
 #pragma unroll
       for (int i = 0; i < kAncWords; ++i) bits[i] |= j >> 6 == i ? 1ull << (j & 63) : 0ull;
     }
@@ -230,18 +246,18 @@ CURE_DEV bool build_tree(const Args& a, const Work& w, Shared& sh) {
   return true;
 }
 
-// Packed row R: its row of q and o, its query head, its token or node, and the last key that it
-// sees with all before it.
+// Packed row R: its row of q and o, its query head, its node within the tile, and the last key
+// that it sees with all before it.
 struct Row {
   int64_t row;
-  int head, token, last;
+  int head, node, last;
 };
 template <bool kPrefix>
 CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
   const int t = a.by_group(R);
   Row r;
   r.head = w.hk * a.group + (R - t * a.group);
-  r.token = t;
+  r.node = kPrefix ? t - a.by_group(w.r0) : 0;
   if (!kPrefix || w.tree) {
     r.row = w.row0 + t;
     r.last = kPrefix ? w.ctx - 1 : w.ctx + t;
@@ -346,8 +362,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   constexpr int kVmWait = waitcnt_vm((kRing - 2) * 2 * G::kDma);
   __shared__ __attribute__((aligned(1024))) unsigned char s_k[kRing * G::kBytes];
   __shared__ __attribute__((aligned(1024))) unsigned char s_v[kRing * G::kBytes];
-  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
-  Shared& sh = reinterpret_cast<Shared&>(s_map);
+  __shared__ typename std::conditional<kPrefix, StartSpace, Nothing>::type s_start;
+  __shared__ typename std::conditional<kPrefix, TreeSpace<kRows>, Nothing>::type s_tree;
+  const Shared sh = shared_of(s_start, s_tree);
 
   Work w;
   if (!locate<kPrefix>(a, w, sh)) return;
@@ -392,7 +409,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const int R = w.r0 + wave * 32 + col;
   const bool row_ok = R < w.rows;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
-  const int node = me.token;
+  const int node = me.node;
   bf16x8 q[kKK];
   {
     const uint16_t* qrow = reinterpret_cast<const uint16_t*>(a.q) + (me.row * a.hq + me.head) * D;
@@ -695,8 +712,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   constexpr int kBlk = D / 32;                     // output blocks
   typedef float vfrag __attribute__((ext_vector_type(D / 32)));
   __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2][2][G::kBytes];   // [buffer][K, V]
-  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
-  Shared& sh = reinterpret_cast<Shared&>(s_map);
+  __shared__ typename std::conditional<kPrefix, StartSpace, Nothing>::type s_start;
+  __shared__ typename std::conditional<kPrefix, TreeSpace<kRows>, Nothing>::type s_tree;
+  const Shared sh = shared_of(s_start, s_tree);
 
   Work w;
   if (!locate<kPrefix>(a, w, sh)) return;
@@ -732,7 +750,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   const int R = w.r0 + wave * 32 + col;
   const bool row_ok = R < w.rows;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
-  const int node = me.token;
+  const int node = me.node;
   f32x4 q[kJ];
   {
     const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D;
@@ -891,16 +909,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
 // As in the kernel above, with V read a column per lane: D register r of a wave's block i =
 // column 32 i + 8 (r / 4) + 4 half + r % 4.
 template <int D, bool kPrefix>
-__global__ __launch_bounds__(64 * kWaves) void seq_attn_f32_shared(Args a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
   using G = GeoF32<D>;
   constexpr int kJ = D / 8 / kWaves;               // column groups of a wave's scores
   constexpr int kBlk = D / 32;
   constexpr int kParts = kWaves / kBlk;            // waves that share a column block's tokens
   constexpr int kRegs = 16 / kParts;               // score registers of a wave's tokens
-  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2][2][G::kBytes];   // [buffer][K, V]
+  // K has one buffer, refilled while its step's probabilities and products are formed, and V two:
+  // so two workgroups fit a CU.
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[G::kBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_v[2][G::kBytes];
   __shared__ f32x4 s_x[kWaves][4][kWave];          // partial scores, at the end partial outputs
-  __shared__ typename std::conditional<kPrefix, Shared, int>::type s_map;
-  Shared& sh = reinterpret_cast<Shared&>(s_map);
+  __shared__ typename std::conditional<kPrefix, TreeSpace<kNarrow>, Nothing>::type s_tree;
+  static_assert(sizeof(StartSpace) <= sizeof(s_x), "the start's space is in s_x, before its use");
+  const Shared sh = kPrefix ? shared_of(reinterpret_cast<StartSpace&>(s_x), s_tree) : Shared{};
 
   Work w;
   if (!locate<kPrefix>(a, w, sh)) return;
@@ -920,23 +942,20 @@ __global__ __launch_bounds__(64 * kWaves) void seq_attn_f32_shared(Args a) {
   const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const int steps = (w.end - w.begin + kStep - 1) / kStep;
-  auto dma = [&](int buf, int h) {
+  auto dma = [&](const char* p, uint32_t lds, int h) {
     const int left = min(w.end - w.begin - h * kStep, kStep);
-    const uint32_t bytes = left > 0 ? (uint32_t)left * tok_bytes : 0u;
-    const int64_t at = (int64_t)h * kStep * tok_bytes;
-    const i32x4 rk = raw_rsrc(kp + at, bytes), rv = raw_rsrc(vp + at, bytes);
+    const i32x4 rsrc = raw_rsrc(p + (int64_t)h * kStep * tok_bytes, left > 0 ? (uint32_t)left * tok_bytes : 0u);
 #pragma unroll
-    for (int j = 0; j < G::kDma; ++j) {
-      const int b = (wave * G::kDma + j) * 1024;
-      dma16_shared(lds_addr(&s_kv[buf][0][b]), src[j], rk);
-      dma16_shared(lds_addr(&s_kv[buf][1][b]), src[j], rv);
-    }
+    for (int j = 0; j < G::kDma; ++j) dma16_shared(lds + j * 1024, src[j], rsrc);
   };
-  dma(0, 0);
+  const uint32_t mine = __builtin_amdgcn_readfirstlane(wave * G::kDma * 1024);
+  const uint32_t k_lds = lds_addr(s_k) + mine, v_lds = lds_addr(s_v) + mine;
+  dma(kp, k_lds, 0);
+  dma(vp, v_lds, 0);
 
   const int R = w.r0 + col;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
-  const int node = me.token;
+  const int node = me.node;
   f32x4 q[kJ];
   {
     const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D + wave * 8 * kJ;
@@ -971,10 +990,10 @@ __global__ __launch_bounds__(64 * kWaves) void seq_attn_f32_shared(Args a) {
   __builtin_amdgcn_s_waitcnt(0);
   for (int h = 0, buf = 0; h < steps; ++h, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(0);                 // this wave's DMA into `buf` has landed
-    __syncthreads();                               // everyone's has; the other buffer and s_x are free
-    dma(buf ^ 1, h + 1);
-    const unsigned char* kt = s_kv[buf][0];
-    const unsigned char* vt = s_kv[buf][1];
+    __syncthreads();                               // everyone's has; the other V buffer and s_x are free
+    dma(vp, v_lds + (buf ^ 1) * G::kBytes, h + 1);
+    const unsigned char* kt = s_k;
+    const unsigned char* vt = s_v[buf];
     f32x16 x;
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = 0.f;
@@ -989,7 +1008,8 @@ __global__ __launch_bounds__(64 * kWaves) void seq_attn_f32_shared(Args a) {
     float f[kRegs];                                // values, on their way meanwhile
 #pragma unroll
     for (int i = 0; i < kRegs; ++i) f[i] = value(vt, row_at(i));
-    __syncthreads();
+    __syncthreads();                               // every wave's partial scores are there, and K is read
+    dma(kp, k_lds, h + 1);
     const bool tail = h * kStep + kStep - 1 > first_last;
     float mt = -INFINITY;
 #pragma unroll
@@ -1277,9 +1297,7 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
       work += (double)t * k;
     }
     const double each = cost.start + cost.part, unit = tps * cost.key + each;
-    double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
-    // The fp32 kernel for few rows leaves room for one workgroup on a CU.
-    if (p.tile == kNarrow) time = std::max(time, (double)((tiles * s * hkv + cus - 1) / cus) * unit);
+    const double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
     if (best == 0 || time < best) {
       if (kv_split == 0) most = s;
       own = (keys + own_tps - 1) / own_tps;
