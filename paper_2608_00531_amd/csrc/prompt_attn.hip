@@ -767,9 +767,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
     return;
   }
 
-  int k_off[kJ];
-#pragma unroll
-  for (int j = 0; j < kJ; ++j) k_off[j] = G::offset(col, 2 * j + half);
+  const int k_off = G::offset(col, half);          // column group j: 32 j XORed onto it
   // V: row 8 (r / 4) + 4 half + r % 4. The swizzle takes a row's low four bits, so registers r
   // and r + 8 are 16 rows apart.
   int v_off[8];
@@ -807,7 +805,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
     for (int r = 0; r < 16; ++r) x[r] = 0.f;
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
-      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + k_off[j]);
+      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + (k_off ^ (32 * j)));
 #pragma unroll
       for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], q[j][i], x, 0, 0, 0);
     }
@@ -915,10 +913,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
   constexpr int kBlk = D / 32;
   constexpr int kParts = kWaves / kBlk;            // waves that share a column block's tokens
   constexpr int kRegs = 16 / kParts;               // score registers of a wave's tokens
-  // K has one buffer, refilled while its step's probabilities and products are formed, and V two:
-  // so two workgroups fit a CU.
-  __shared__ __attribute__((aligned(1024))) unsigned char s_k[G::kBytes];
-  __shared__ __attribute__((aligned(1024))) unsigned char s_v[2][G::kBytes];
+  // Rings of steps in LDS, such that two workgroups fit a CU: at head dim 128 one of K, refilled
+  // while its step's probabilities and products are formed, and two of V. Step h - kV + 1 asks for
+  // V of step h, then step h - kK for K; what has been asked for since may be under way.
+  constexpr int kK = D == 128 ? 1 : 3, kV = D == 128 ? 2 : 3;
+  constexpr int kVmWait = waitcnt_vm(D == 128 ? 0 : 3 * G::kDma);
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[kK][G::kBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_v[kV][G::kBytes];
   __shared__ f32x4 s_x[kWaves][4][kWave];          // partial scores, at the end partial outputs
   __shared__ typename std::conditional<kPrefix, TreeSpace<kNarrow>, Nothing>::type s_tree;
   static_assert(sizeof(StartSpace) <= sizeof(s_x), "the start's space is in s_x, before its use");
@@ -950,8 +951,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
   };
   const uint32_t mine = __builtin_amdgcn_readfirstlane(wave * G::kDma * 1024);
   const uint32_t k_lds = lds_addr(s_k) + mine, v_lds = lds_addr(s_v) + mine;
-  dma(kp, k_lds, 0);
-  dma(vp, v_lds, 0);
+#pragma unroll
+  for (int h = 0; h < kK; ++h) dma(kp, k_lds + h * G::kBytes, h);
+#pragma unroll
+  for (int h = 0; h < kV - 1; ++h) dma(vp, v_lds + h * G::kBytes, h);
 
   const int R = w.r0 + col;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
@@ -988,12 +991,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
   const float c = a.scale_log2;
 
   __builtin_amdgcn_s_waitcnt(0);
-  for (int h = 0, buf = 0; h < steps; ++h, buf ^= 1) {
-    __builtin_amdgcn_s_waitcnt(0);                 // this wave's DMA into `buf` has landed
-    __syncthreads();                               // everyone's has; the other V buffer and s_x are free
-    dma(vp, v_lds + (buf ^ 1) * G::kBytes, h + 1);
-    const unsigned char* kt = s_k;
-    const unsigned char* vt = s_v[buf];
+  for (int h = 0; h < steps; ++h) {
+    __builtin_amdgcn_s_waitcnt(kVmWait);           // this wave's DMA of step h has landed
+    __syncthreads();                               // everyone's has; V of step h - 1 and s_x are free
+    dma(vp, v_lds + (h + kV - 1) % kV * G::kBytes, h + kV - 1);
+    const unsigned char* kt = s_k[h % kK];
+    const unsigned char* vt = s_v[h % kV];
     f32x16 x;
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = 0.f;
@@ -1009,7 +1012,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
 #pragma unroll
     for (int i = 0; i < kRegs; ++i) f[i] = value(vt, row_at(i));
     __syncthreads();                               // every wave's partial scores are there, and K is read
-    dma(kp, k_lds, h + 1);
+    dma(kp, k_lds + h % kK * G::kBytes, h + kK);
     const bool tail = h * kStep + kStep - 1 > first_last;
     float mt = -INFINITY;
 #pragma unroll
@@ -1203,12 +1206,17 @@ constexpr int kCandidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 struct Cost {
   double key, start, part;
   Cost(int32_t dtype, int tile, int32_t d, double rows) {
-    const double step = dtype == CURE_BF16 ? (d == 128 ? 0.45 : 0.28) : (tile == kNarrow ? 2.2 : 3.6) * d / 128;
+    const double step = dtype == CURE_BF16 ? (d == 128 ? 0.45 : 0.28) : tile == kNarrow ? (d == 128 ? 1.9 : 1.0) : 3.6 * d / 128;
     key = step / kStep;
     start = 5;
     part = std::min<double>(tile, rows) * d * 8 / 27e3;
   }
 };
+
+// fp32: narrow tiles where the wide ones would leave CUs idle, or half their rows.
+bool narrow(int32_t dtype, int64_t wide, int64_t rows, int32_t hkv) {
+  return dtype == CURE_F32 && (wide * hkv < device_cu_count() || 2 * rows < wide * kRows);
+}
 
 Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t d, const int32_t* host_n_rows,
                  const int32_t* host_ctx_len, int32_t kv_split) {
@@ -1223,7 +1231,7 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   Plan p{};
-  p.tile = dtype == CURE_F32 && wide * hkv < cus ? kNarrow : kRows;
+  p.tile = narrow(dtype, wide, total * group, hkv) ? kNarrow : kRows;
   p.tiles = (int)tiles_of(longest, p.tile);
   // The merge's grid holds the tokens of a sequence in 16 bits.
   int64_t most = longest > 65535 ? 1 : kv_split;
@@ -1277,7 +1285,7 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   Plan p{};
-  p.tile = dtype == CURE_F32 && (wide + tiles_of(nodes, kRows)) * hkv < cus ? kNarrow : kRows;
+  p.tile = narrow(dtype, wide + tiles_of(nodes, kRows), 2 * nodes * group, hkv) ? kNarrow : kRows;
   const int64_t tiles = tiles_of(nodes, p.tile);
   int64_t most = kv_split, own = 1;
   // As for prompts; own rows are split as the prefix is, and fill the CUs around its
