@@ -78,6 +78,51 @@ def test_splits_and_output_types(dtype, out, kv_split):
     c.check(o, lse, only=lambda n: [0, n // 2, n - 1])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_tiles_that_fill_the_chip(d):
+    """Launches whose tiles of 128 rows number 256 and more and are full take a kernel of their own."""
+    c = Case("f32", 150, [40] * 8, [0, 5, 33, 64, 90, 1, 31, 32], 64, 16, d)
+    o, lse, st = c.run()
+    assert st.tolist() == [0] * 8
+    c.check(o, lse, only=lambda n: [0, 17, n - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes,hq,hkv", [([256, 200], 2, 1), ([256], 5, 5), ([129, 3, 128], 33, 1)])
+def test_large_trees(dtype, nodes, hq, hkv):
+    """Trees of several tiles and of four words of ancestor bits."""
+    c = Case(dtype, 65, nodes, [37, 0, 300][:len(nodes)], hq, hkv, 64)
+    o, lse, st = c.run()
+    assert st.tolist() == [0] * len(nodes)
+    c.check(o, lse, only=lambda n: [0, 63, 64, n // 2, 127, 128, 199, n - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_own_contexts_longer_than_the_prefix(dtype):
+    c = Case(dtype, 40, [9, 17], [3000, 1500], 8, 2, 128)
+    for kv_split in (0, 1, 2):
+        o, lse, _ = c.run(kv_split=kv_split)
+        c.check(o, lse, only=lambda n: [0, n - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nodes_off_a_path_may_be_anything(dtype):
+    """Keys and values of nodes that a node does not descend from: NaN and infinities there leave it its bits."""
+    c = Case(dtype, 50, [20, 12], [33, 0], 4, 2, 64, seed=5)
+    want, want_lse, _ = c.run()
+    anc, _ = oracle.ancestors(c.parents[0], 20)
+    bad = 11                                               # a node of sequence 0
+    at = c.kv_off[0] + c.ctx[0] + bad
+    c.k[at], c.v[at, :, ::2], c.v[at, :, 1::2] = float("nan"), float("inf"), float("nan")
+    o, lse, _ = c.run()
+    for n in range(20):
+        if bad in anc[n]:
+            assert torch.isnan(o[0, n]).all()
+        else:
+            assert torch.equal(o[0, n], want[0, n]) and torch.equal(lse[0, n], want_lse[0, n]), n
+    assert torch.equal(o[1, :12], want[1, :12])
+
+
 def test_many_sequences():
     """More sequences than lanes of a wave, some of them without nodes."""
     c = Case("bf16", 200, [b % 4 for b in range(131)], [b % 7 for b in range(131)], 2, 1, 64)

@@ -85,6 +85,16 @@ def test_long_prompts(dtype, group):
     c.check(*c.run(), only=lambda n: [0, 1, 31, 32, n // 3, n // 2, n - 33, n - 2, n - 1])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,ctx,hq,hkv", [([1111], [70], 32, 8), ([130, 100], [0, 33], 128, 128)])
+def test_fp32_tiles_that_fill_the_chip(d, rows, ctx, hq, hkv):
+    """Launches whose tiles of 128 rows number 256 and more and are full take a kernel of their own."""
+    assert sum(-(-n * hq // hkv // 128) for n in rows) * hkv >= 256
+    c = Case("f32", rows, ctx, hq, hkv, d)
+    c.check(*c.run(), only=lambda n: [0, 31, n // 2, n - 1])
+    c.check(*c.run(kv_split=2), only=lambda n: [0, n - 2])
+
+
 def test_one_token_over_a_long_context():
     c = Case("bf16", [1, 1, 1], [9000, 0, 4097], 8, 2, 128)
     c.check(*c.run())
@@ -92,13 +102,14 @@ def test_one_token_over_a_long_context():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,ctx,kv_split", [([70, 9], [0, 40], 1), ([70, 9], [400, 300], 3), ([1, 1], [33, 5], 1)])
-def test_values_a_row_does_not_see_may_be_anything(dtype, rows, ctx, kv_split):
+@pytest.mark.parametrize("rows,ctx,kv_split,hkv", [([70, 9], [0, 40], 1, 2), ([70, 9], [400, 300], 3, 2), ([1, 1], [33, 5], 1, 2),
+                                                   ([120, 100], [0, 64], 1, 128)])
+def test_values_a_row_does_not_see_may_be_anything(dtype, rows, ctx, kv_split, hkv):
     """Keys and values outside the sequences, and those of later tokens, hold NaN and infinities: rows
     before them keep their bits, rows that see them have none that is finite."""
-    clean = Case(dtype, rows, ctx, 4, 2, 64, seed=3)
+    clean = Case(dtype, rows, ctx, 2 * hkv, hkv, 64, seed=3)
     want, want_lse = clean.run(kv_split=kv_split)
-    dirty = Case(dtype, rows, ctx, 4, 2, 64, seed=3)
+    dirty = Case(dtype, rows, ctx, 2 * hkv, hkv, 64, seed=3)
     inside = np.zeros(len(dirty.k), bool)
     for off, n, c in zip(dirty.kv_off, rows, ctx):
         inside[off:off + n + c] = True
@@ -236,16 +247,16 @@ def test_cache_rows_past_4_gb():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n,group,kv_split", [(1, 1, 1), (33, 1, 1), (7, 5, 1), (1, 1, 2)])
-def test_every_key_counts_once(dtype, d, n, group, kv_split):
+@pytest.mark.parametrize("n,group,kv_split,hkv", [(1, 1, 1, 1), (33, 1, 1, 1), (7, 5, 1, 1), (1, 1, 2, 1), (100, 1, 1, 256)])
+def test_every_key_counts_once(dtype, d, n, group, kv_split, hkv):
     """Equal scores and one-hot values: element t % d of the output, times the number of keys, is how many
     of the visible tokens t counted. Every number of steps around several turns of the tile rings."""
     t = DTYPES[dtype]
     for total in list(range(n, n + 70, 3)) + list(range(n + 90, n + 460, 29)):
         ctx = total - n
-        v = torch.zeros(total, 1, d, dtype=t)
-        v[torch.arange(total), 0, torch.arange(total) % d] = 1
-        q, k = torch.zeros(n, group, d, dtype=t, device="cuda"), torch.zeros(total, 1, d, dtype=t, device="cuda")
+        v = torch.zeros(total, hkv, d, dtype=t)
+        v[torch.arange(total), :, torch.arange(total) % d] = 1
+        q, k = torch.zeros(n, group * hkv, d, dtype=t, device="cuda"), torch.zeros(total, hkv, d, dtype=t, device="cuda")
         zero = ints([0], torch.int64)
         o, lse = pc.cure_prompt_attn(q, k, v.cuda(), zero, ints([n]), zero, ints([ctx]), [n], [ctx], 1.0,
                                      out_dtype=torch.float32, kv_split=kv_split)
