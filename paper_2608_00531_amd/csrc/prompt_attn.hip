@@ -35,6 +35,7 @@ constexpr int kWaves = 4;            // waves per workgroup, 32 query rows each
 constexpr int kRows = 32 * kWaves;   // query rows per tile
 constexpr int kNarrow = 32;          // query rows per tile of the fp32 kernel that shares them
 constexpr int kMaxPrefixBatch = 1024;
+constexpr float kNone = -3e38f;      // reference of a row that has seen nothing
 constexpr int kAncWords = CURE_MAX_TREE_NODES / 64;
 
 // Division by a launch's constant: x / d = the high half of x * (2^32 / d + 1) while x * d < 2^32.
@@ -609,10 +610,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   if (my_steps > 0) {
     scores(x, 0);
     if (full == 0) mask(x, 0);
-    // The first reference: the row's maximum. A row that sees nothing here has no finite
-    // one, and probabilities of zero against any.
+    // The first reference: the row's maximum. A row that sees nothing here (a tree's node whose
+    // path comes later) has no finite one: against kNone hidden scores have probabilities of
+    // zero and the first score that is seen an infinite one, with which the reference moves.
     const float mx = row_max(x);
-    m = mx == -INFINITY ? 0.f : mx;
+    m = mx == -INFINITY ? kNone : mx;
   }
   begin(0, 0, slot_of(kRing - 2));
   int h = 1;
@@ -1376,7 +1378,7 @@ cure_status check(const void* q, const void* k, const void* v, const void* o, in
   if (out_dtype != CURE_F32 && out_dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
   if (hq <= 0 || hkv <= 0 || hq % hkv != 0) return CURE_ERR_INVALID_ARG;
   if (d != 64 && d != 128) return CURE_ERR_UNSUPPORTED;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return CURE_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || !std::isfinite(scale * kLog2e)) return CURE_ERR_INVALID_ARG;
   if ((int64_t)hkv * d * 4 * kStep > INT32_MAX) return CURE_ERR_UNSUPPORTED;
   const uintptr_t in = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) |
                        reinterpret_cast<uintptr_t>(v);
@@ -1492,6 +1494,7 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
     if (host_ctx_len[b] < 0 || host_n_nodes[b] < 0 || host_n_nodes[b] > n_max) return CURE_ERR_INVALID_ARG;
   for (int b = 0; b < batch; ++b)
     if (host_ctx_len[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
+  if ((int64_t)batch * n_max * (hq / hkv) > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
   const Plan p = prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
   if (!workspace || workspace_bytes < part_bytes((int64_t)batch * n_max, hq, d, p.slots())) return CURE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;

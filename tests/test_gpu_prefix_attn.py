@@ -123,6 +123,23 @@ def test_nodes_off_a_path_may_be_anything(dtype):
     assert torch.equal(o[1, :12], want[1, :12])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("low", [-60.0, -300.0])
+def test_low_scores_behind_hidden_nodes(dtype, low):
+    """A row whose first visible token is not among its first 32, with scores whose exponentials are
+    none: a tree of roots, each of which sees itself and a prefix of lower scores yet."""
+    c = Case(dtype, 40, [90, 64], [0, 0], 4, 2, 64)
+    c.parents = [[-1] * 90, [-1] * 64]
+    side = torch.full((64,), 64 ** -0.5)
+    rise = normal(9, c.k.shape[0], 1, 1)
+    c.q = (side * 8 * torch.ones(c.q.shape[:3]).unsqueeze(-1)).to(c.q.dtype)
+    c.k = ((low - 5 + rise) * side).expand(c.k.shape).to(c.k.dtype).contiguous()
+    for off, n in zip(c.kv_off, c.nodes):
+        c.k[off:off + n] += (5 * side).to(c.k.dtype)
+    o, lse, _ = c.run()
+    c.check(o, lse)
+
+
 def test_many_sequences():
     """More sequences than lanes of a wave, some of them without nodes."""
     c = Case("bf16", 200, [b % 4 for b in range(131)], [b % 7 for b in range(131)], 2, 1, 64)

@@ -130,7 +130,7 @@ def test_prompt_argument_errors(L):
         assert prompt(L, **{name: -1}) == E, name
     assert prompt(L, hq=5) == E and prompt(L, hkv=0) == E
     assert prompt(L, d=96) == U and prompt(L, d=256) == U
-    for scale in (0.0, -0.1, math.inf, math.nan):
+    for scale in (0.0, -0.1, math.inf, math.nan, 3e38):
         assert prompt(L, scale=scale) == E, scale
     assert prompt(L, q=4104) == E and prompt(L, k=4104) == E and prompt(L, v=4100) == E and prompt(L, o=4100) == E
     assert prompt(L, o=4104, out_dtype=0) == E
@@ -160,11 +160,12 @@ def test_prefix_argument_errors(L):
     for name in ("batch", "n_max", "kv_split", "prefix_off", "prefix_len"):
         assert prefix(L, **{name: -1}) == E, name
     assert prefix(L, hq=5) == E and prefix(L, d=80) == U
-    for scale in (0.0, -0.1, math.inf, math.nan):
+    for scale in (0.0, -0.1, math.inf, math.nan, 3e38):
         assert prefix(L, scale=scale) == E, scale
     assert prefix(L, q=4104) == E and prefix(L, o=4100) == E
     assert prefix(L, n_max=257) == U and prefix(L, batch=1025) == U and prefix(L, prefix_len=2 ** 31 - 10) == U
     assert prefix(L, nodes=(3, 5)) == E and prefix(L, nodes=(-1, 2)) == E and prefix(L, ctx=(-1, 2)) == E
+    assert prefix(L, nodes=(1,) * 1024, ctx=(0,) * 1024, batch=1024, n_max=256, hq=1 << 13, hkv=1) == U   # 2^31 rows
     assert prefix(L) == pc.CURE_ERR_WORKSPACE
     assert prefix(L, workspace=4104, ws_bytes=1 << 30) == E
     assert prefix(L, batch=0) == OK and prefix(L, n_max=0) == OK
