@@ -48,9 +48,10 @@ struct Div {
   CURE_DEV int operator()(int x) const { return m ? (int)__umulhi((uint32_t)x, m) : d == 1 ? x : x / d; }
 };
 
-// How keys are split: at most `most` splits of about tps tokens, at least one.
+// How keys are split: at most `most` splits of about tps tokens, at least one, which begin at
+// multiples of `quantum`.
 struct Splits {
-  int32_t tps, most;
+  int32_t tps, most, quantum;
 };
 
 struct Args {
@@ -83,15 +84,15 @@ CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int slot) {
   return (row * a.hq + head) * (a.cut.most + a.own.most) + slot;
 }
 
-// The splits of `keys` (at least one) keys: n of `per` tokens, whole steps, the last one shorter
-// (a single one: all).
+// The splits of `keys` (at least one) keys: n of `per` tokens, the last one shorter (a single
+// one: all).
 struct Cut {
   int n, per;
 };
 CURE_DEV Cut cut_of(const Splits& s, int keys) {
   if (s.most == 1) return Cut{1, keys};
   const int n = max(1, min((keys - 1) / s.tps + 1, s.most));
-  const int per = ((keys - 1) / n / kStep + 1) * kStep;
+  const int per = ((keys - 1) / n / s.quantum + 1) * s.quantum;
   return Cut{(keys - 1) / per + 1, per};
 }
 
@@ -126,7 +127,6 @@ struct Nothing {};
 template <class T>
 CURE_DEV Shared shared_of(StartSpace& s, T& t) { return Shared{s.first, s.parent, t.anc}; }
 CURE_DEV Shared shared_of(Nothing&, Nothing&) { return Shared{}; }
-CURE_DEV Shared shared_of(StartSpace&, Nothing&) { return Shared{}; }
 
 // Prompt: grid (kv-heads x tiles, splits, sequences); a sequence's last tiles, which see the
 // most keys, come first. A sequence's tiles stay together, as they share its keys in the L2: dealt
@@ -689,33 +689,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// fp32 kernel: 32 query rows per wave, 32x32x2 fp32 matrix instructions, products and
-// sums in fp32 throughout.
+// fp32 kernel: a tile is 32 query rows, which all four waves share, 32x32x2 fp32 matrix
+// instructions, products and sums in fp32 throughout. Each wave takes every fourth step of the
+// keys, with buffers and sums of its own, joined at the end.
 //
-// Lane l = 32 half + col owns query row col of its wave:
+// Lane l = 32 half + col owns query row col:
 //   S^T: MFMA i of column group j takes k index half for column 8 j + 4 half + i, so one
 //        16-byte read of K (row col, columns 8 j + 4 half .. +3) feeds four; D register r =
 //        score of token 8 (r / 4) + 4 half + r % 4
 //   O^T: MFMA r takes k index half for that token, the probability the lane holds; output
 //        row c' of block i stands for column (D / 32) c' + i, so one read of V (the token's
 //        row, columns (D / 32) col ..) feeds all D / 32 blocks.
+// The scores of a wave's next step are formed together with the probabilities of the present
+// one, whose vector instructions fill the matrix unit's time; then come the present one's products. K of
+// the step after is asked for when the scores have read the buffer, V after the products, so that one
+// buffer of each is enough and no wave waits for another.
 template <int D>
 struct GeoF32 {
   static constexpr int kRowBytes = 4 * D;
   static constexpr int kBytes = kStep * kRowBytes;
-  static constexpr int kDma = kBytes / 1024 / kWaves;
+  static constexpr int kDma = kBytes / 1024;                 // 1 KB blocks per tensor
   static CURE_DEV int offset(int row, int chunk) { return row * kRowBytes + ((chunk ^ (row & 15)) << 4); }
 };
 
 template <int D, bool kPrefix>
-__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void seq_attn_f32(Args a) {
   using G = GeoF32<D>;
   constexpr int kJ = D / 8;                        // column groups of the scores
   constexpr int kBlk = D / 32;                     // output blocks
+  constexpr int kGroups = D / 8;                   // of four columns that a lane ends up with
+  constexpr int kAhead = 2;
   typedef float vfrag __attribute__((ext_vector_type(D / 32)));
-  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[2][2][G::kBytes];   // [buffer][K, V]
+  __shared__ __attribute__((aligned(1024))) unsigned char s_kv[kWaves][2][G::kBytes];   // [wave][K, V]
+  __shared__ float s_m[kWaves][kNarrow], s_l[kWaves][kNarrow];
   __shared__ typename std::conditional<kPrefix, StartSpace, Nothing>::type s_start;
-  __shared__ typename std::conditional<kPrefix, TreeSpace<kRows>, Nothing>::type s_tree;
+  __shared__ typename std::conditional<kPrefix, TreeSpace<kNarrow>, Nothing>::type s_tree;
   const Shared sh = shared_of(s_start, s_tree);
 
   Work w;
@@ -727,30 +735,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
   uint32_t src[G::kDma];
 #pragma unroll
   for (int j = 0; j < G::kDma; ++j) {
-    const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
-    const int row = byte / G::kRowBytes;
+    const int byte = j * 1024 + lane * 16, row = byte / G::kRowBytes;
     src[j] = (uint32_t)row * tok_bytes +
              (uint32_t)(w.hk * G::kRowBytes + ((((byte % G::kRowBytes) >> 4) ^ (row & 15)) << 4));
   }
   const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
   const int steps = (w.end - w.begin + kStep - 1) / kStep;
-  auto dma = [&](int buf, int h) {
+  const unsigned char *const kt = s_kv[wave][0], *const vt = s_kv[wave][1];
+  auto dma = [&](const char* p, const unsigned char* to, int h) {
     const int left = min(w.end - w.begin - h * kStep, kStep);
-    const uint32_t bytes = left > 0 ? (uint32_t)left * tok_bytes : 0u;
-    const int64_t at = (int64_t)h * kStep * tok_bytes;
-    const i32x4 rk = raw_rsrc(kp + at, bytes), rv = raw_rsrc(vp + at, bytes);
+    const i32x4 rsrc = raw_rsrc(p + (int64_t)h * kStep * tok_bytes, left > 0 ? (uint32_t)left * tok_bytes : 0u);
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");     // the reads of the buffer have their data
 #pragma unroll
-    for (int j = 0; j < G::kDma; ++j) {
-      const int blk = (wave * G::kDma + j) * 1024;
-      dma16_shared(lds_addr(&s_kv[buf][0][blk]), src[j], rk);
-      dma16_shared(lds_addr(&s_kv[buf][1][blk]), src[j], rv);
-    }
+    for (int j = 0; j < G::kDma; ++j) dma16_shared(lds_addr(to) + j * 1024, src[j], rsrc);
   };
-  dma(0, 0);
+  // Everything but the last tensor asked for has landed.
+  const auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(G::kDma) : "memory"); };
+  const auto all_landed = [] { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); };
+  dma(kp, kt, wave);
+  dma(vp, vt, wave);
 
-  const int R = w.r0 + wave * 32 + col;
-  const bool row_ok = R < w.rows;
+  const int R = w.r0 + col;
   const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
   const int node = me.node;
   f32x4 q[kJ];
@@ -759,13 +765,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
 #pragma unroll
     for (int j = 0; j < kJ; ++j) q[j] = *reinterpret_cast<const f32x4*>(qrow + 8 * j + 4 * half);
   }
-  const bool wave_ok = w.r0 + wave * 32 < w.rows;
   const int last = me.last - w.begin;
   const int first_last = __builtin_amdgcn_readfirstlane(last);
   const int last_last = __builtin_amdgcn_readlane(last, 31);
-  const int my_steps = !wave_ok ? 0 : kPrefix ? steps : min(steps, max(0, (last_last + kStep) / kStep));
+  const int my_steps = kPrefix ? steps : min(steps, max(0, (last_last + kStep) / kStep));
   if (kPrefix && w.tree && w.end > w.ctx && !build_tree(a, w, sh)) {
-    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land after the workgroup ends
+    all_landed();                                  // no DMA may land after the workgroup ends
     return;
   }
 
@@ -778,80 +783,94 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
     const int byte = col * (D / 32) * 4;
     v_off[r] = G::offset(8 * (r >> 2) + 4 * half + (r & 3), byte >> 4) + (byte & 15);
   }
+  const auto key = [&](int j) { return *reinterpret_cast<const f32x4*>(kt + (k_off ^ (32 * j))); };
+  const auto values = [&](int r) {
+    return *reinterpret_cast<const vfrag*>(vt + (r >> 3) * 16 * G::kRowBytes + v_off[r & 7]);
+  };
 
   f32x16 o[kBlk];
 #pragma unroll
   for (int i = 0; i < kBlk; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m = kNone, l = 0.f;
   const float c = a.scale_log2;
-
-  __builtin_amdgcn_s_waitcnt(0);
-  if (!row_ok) {
+  const auto tail = [&](int h) { return h * kStep + kStep - 1 > first_last; };   // some row sees step h in part
+  const auto mask = [&](f32x16& x, int h) {
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) q[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  for (int h = 0, buf = 0; h < steps; ++h, buf ^= 1) {
-    __builtin_amdgcn_s_waitcnt(0);                 // this wave's DMA into `buf` has landed
-    __syncthreads();                               // everyone's has; the other buffer is free
-    dma(buf ^ 1, h + 1);
-    if (h >= my_steps) continue;
-    const unsigned char* kt = s_kv[buf][0];
-    const unsigned char* vt = s_kv[buf][1];
-    const auto values = [&](int r) {
-      return *reinterpret_cast<const vfrag*>(vt + (r >> 3) * 16 * G::kRowBytes + v_off[r & 7]);
-    };
-    f32x16 x;
+    for (int r = 0; r < 16; ++r)
+      x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
+  };
+  const auto row_max = [&](const f32x16& x) {
+    float mx = x[0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+    return max_halves(mx) * c;
+  };
+  const auto exps = [&](const f32x16& x, f32x16& p, float sum) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = fast_exp2(fmaf(x[r], c, -m));
+      sum += p[r];
+    }
+    return sum;
+  };
+  // Scores of the next step into y, probabilities of this one, whose scores are x, into p; returns
+  // the running sum.
+  const auto scores_and_exps = [&](f32x16& y, const f32x16& x, f32x16& p) {
+    constexpr int kEach = 16 / kJ;                 // probabilities per column group
+    f32x4 f[kJ];
+    float sum = l;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) f[j] = key(j);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = 0.f;
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
-      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + (k_off ^ (32 * j)));
+      if (j + kAhead < kJ) f[j + kAhead] = key(j + kAhead);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], q[j][i], x, 0, 0, 0);
+      for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_32x32x2f32(f[j][i], q[j][i], y, 0, 0, 0);
+#pragma unroll
+      for (int r = kEach * j; r < kEach * (j + 1); ++r) {
+        p[r] = fast_exp2(fmaf(x[r], c, -m));
+        sum += p[r];
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const bool tail = h * kStep + kStep - 1 > first_last;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] *= c;
-      if (tail)
-        x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
-    }
-    float mt = x[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mt = fmaxf(mt, x[r]);
-    const float m_new = fmaxf(m, max_halves(mt));
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    if (__ballot(m_new > m)) {                     // a maximum rose: rescale (factor 1 for the others)
-      const float alpha = fast_exp2(m - m_use);
-      l *= alpha;
+    return sum;
+  };
+  // Takes over a step's sum; the reference moves as in the bf16 kernel.
+  const auto settle = [&](const f32x16& x, f32x16& p, float sum) {
+    if (__builtin_expect(__ballot(!(sum - l <= 256.f)) != 0, 0)) {
+      const float mx = row_max(x);
+      const bool grow = mx > m + kRescaleLog2;
+      const float alpha = grow ? fast_exp2(m - mx) : 1.f;
+      m = grow ? mx : m;
 #pragma unroll
       for (int i = 0; i < kBlk; ++i) o[i] *= alpha;
+      sum = exps(x, p, l * alpha);
     }
-    m = m_new;
+    l = sum;
+  };
+  const auto products = [&](const f32x16& p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      x[r] = fast_exp2(x[r] - m_use);
-      l += x[r];
+      const vfrag f = values(r);
+#pragma unroll
+      for (int i = 0; i < kBlk; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], p[r], o[i], 0, 0, 0);
     }
-    float probe = 0.f;                             // a NaN from a value of a masked step that is not finite
-    if (tail) {
+  };
+  const auto hidden_products = [&](const f32x16& p, int h) {
+    float probe = 0.f;                             // a NaN from the first value that is not finite
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const vfrag f = values(r);
+    for (int r = 0; r < 16; ++r) {
+      const vfrag f = values(r);
 #pragma unroll
-        for (int i = 0; i < kBlk; ++i) probe = fmaf(f[i], 0.f, probe);
-      }
+      for (int i = 0; i < kBlk; ++i) probe = fmaf(f[i], 0.f, probe);
     }
     if (__builtin_expect(__ballot(probe != 0.f) == 0, 1)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const vfrag f = values(r);
-#pragma unroll
-        for (int i = 0; i < kBlk; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], x[r], o[i], 0, 0, 0);
-      }
-      continue;
+      products(p);
+      return;
     }
     // As in the bf16 kernel: zeros for the values that are not finite, which the rows that see
     // them take as they are.
@@ -860,7 +879,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
       const vfrag f = values(r);
 #pragma unroll
       for (int i = 0; i < kBlk; ++i)
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(f[i]) < INFINITY ? f[i] : 0.f, x[r], o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(f[i]) < INFINITY ? f[i] : 0.f, p[r], o[i], 0, 0, 0);
     }
     for (int t = 0; t < kStep; ++t) {
       const bool seen = sees<kPrefix>(a, w, sh, h * kStep + t, last, node);
@@ -873,232 +892,97 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32(Args a) {
           if (seen && !(fabsf(f[i]) < INFINITY)) o[i][r] += f[i];
       }
     }
-  }
-
-  __builtin_amdgcn_s_waitcnt(0);                   // the trailing DMA lands before exit
-  if (!row_ok) return;
-  const float lt = sum_halves(l);
-  const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
-  const float lse = lt == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(lt)) * kLn2;
-  const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
-  const int64_t orow = me.row * a.hq + me.head;
-  // Lane's columns: (D / 32) c' + i for rows c' of the blocks, four consecutive ones at a time.
-#pragma unroll
-  for (int r = 0; r < 16; r += 4 / kBlk) {
-    float x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = o[e % kBlk][r + e / kBlk] * inv;
-    const int d0 = kBlk * (8 * (r >> 2) + 4 * half + (r & 3));
-    if (whole) store4(a, orow * D + d0, x[0], x[1], x[2], x[3]);
-    else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x[0], x[1], x[2], x[3]);
-  }
-  if (half == 0) {
-    if (!whole) a.part_lse[pi] = lse;
-    else if (a.lse) a.lse[orow] = lse;
-  }
-}
-
-// ---------------------------------------------------------------------------
-// fp32 kernel for launches with few rows: a tile is 32 query rows, which all four waves
-// share. A step's scores take 64 matrix instructions at head dim 128 and as many its
-// products; each wave forms the scores of a quarter of the columns, which the waves add
-// through LDS, in one order, so that all hold the same, and the products of its own 32
-// columns (at head dim 64 of half the step's tokens as well; the halves are added at the end).
-//
-// As in the kernel above, with V read a column per lane: D register r of a wave's block i =
-// column 32 i + 8 (r / 4) + 4 half + r % 4.
-template <int D, bool kPrefix>
-__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_f32_shared(Args a) {
-  using G = GeoF32<D>;
-  constexpr int kJ = D / 8 / kWaves;               // column groups of a wave's scores
-  constexpr int kBlk = D / 32;
-  constexpr int kParts = kWaves / kBlk;            // waves that share a column block's tokens
-  constexpr int kRegs = 16 / kParts;               // score registers of a wave's tokens
-  // Rings of steps in LDS, such that two workgroups fit a CU: at head dim 128 one of K, refilled
-  // while its step's probabilities and products are formed, and two of V. Step h - kV + 1 asks for
-  // V of step h, then step h - kK for K; what has been asked for since may be under way.
-  constexpr int kK = D == 128 ? 1 : 3, kV = D == 128 ? 2 : 3;
-  constexpr int kVmWait = waitcnt_vm(D == 128 ? 0 : 3 * G::kDma);
-  __shared__ __attribute__((aligned(1024))) unsigned char s_k[kK][G::kBytes];
-  __shared__ __attribute__((aligned(1024))) unsigned char s_v[kV][G::kBytes];
-  __shared__ f32x4 s_x[kWaves][4][kWave];          // partial scores, at the end partial outputs
-  __shared__ typename std::conditional<kPrefix, TreeSpace<kNarrow>, Nothing>::type s_tree;
-  static_assert(sizeof(StartSpace) <= sizeof(s_x), "the start's space is in s_x, before its use");
-  const Shared sh = kPrefix ? shared_of(reinterpret_cast<StartSpace&>(s_x), s_tree) : Shared{};
-
-  Work w;
-  if (!locate<kPrefix>(a, w, sh)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, col = lane & 31;
-  const int blk = wave % kBlk, r0 = wave / kBlk * kRegs;
-
-  const uint32_t tok_bytes = (uint32_t)(a.hkv * G::kRowBytes);
-  uint32_t src[G::kDma];
-#pragma unroll
-  for (int j = 0; j < G::kDma; ++j) {
-    const int byte = (wave * G::kDma + j) * 1024 + lane * 16;
-    const int row = byte / G::kRowBytes;
-    src[j] = (uint32_t)row * tok_bytes +
-             (uint32_t)(w.hk * G::kRowBytes + ((((byte % G::kRowBytes) >> 4) ^ (row & 15)) << 4));
-  }
-  const char* const kp = reinterpret_cast<const char*>(a.k) + (w.key0 + w.begin) * (int64_t)tok_bytes;
-  const char* const vp = reinterpret_cast<const char*>(a.v) + (w.key0 + w.begin) * (int64_t)tok_bytes;
-  const int steps = (w.end - w.begin + kStep - 1) / kStep;
-  auto dma = [&](const char* p, uint32_t lds, int h) {
-    const int left = min(w.end - w.begin - h * kStep, kStep);
-    const i32x4 rsrc = raw_rsrc(p + (int64_t)h * kStep * tok_bytes, left > 0 ? (uint32_t)left * tok_bytes : 0u);
-#pragma unroll
-    for (int j = 0; j < G::kDma; ++j) dma16_shared(lds + j * 1024, src[j], rsrc);
-  };
-  const uint32_t mine = __builtin_amdgcn_readfirstlane(wave * G::kDma * 1024);
-  const uint32_t k_lds = lds_addr(s_k) + mine, v_lds = lds_addr(s_v) + mine;
-#pragma unroll
-  for (int h = 0; h < kK; ++h) dma(kp, k_lds + h * G::kBytes, h);
-#pragma unroll
-  for (int h = 0; h < kV - 1; ++h) dma(vp, v_lds + h * G::kBytes, h);
-
-  const int R = w.r0 + col;
-  const Row me = row_of<kPrefix>(a, w, sh, min(R, w.rows - 1));
-  const int node = me.node;
-  f32x4 q[kJ];
-  {
-    const float* qrow = reinterpret_cast<const float*>(a.q) + (me.row * a.hq + me.head) * D + wave * 8 * kJ;
-#pragma unroll
-    for (int j = 0; j < kJ; ++j) q[j] = *reinterpret_cast<const f32x4*>(qrow + 8 * j + 4 * half);
-  }
-  const int last = me.last - w.begin;
-  const int first_last = __builtin_amdgcn_readfirstlane(last);
-  if (kPrefix && w.tree && w.end > w.ctx && !build_tree(a, w, sh)) {
-    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land after the workgroup ends
-    return;
-  }
-
-  int k_off[kJ];
-#pragma unroll
-  for (int j = 0; j < kJ; ++j) k_off[j] = G::offset(col, 2 * (wave * kJ + j) + half);
-  // This wave's value of a step's token row, at column 32 blk + col.
-  const auto value = [&](const unsigned char* vt, int row) {
-    return *reinterpret_cast<const float*>(vt + G::offset(row, 8 * blk + (col >> 2)) + (col & 3) * 4);
-  };
-  const auto row_at = [&](int i) {                 // token row of this wave's score register r0 + i
-    const int r = r0 + i;
-    return 8 * (r >> 2) + 4 * half + (r & 3);
   };
 
-  f32x16 o;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) o[r] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  const float c = a.scale_log2;
-
-  __builtin_amdgcn_s_waitcnt(0);
-  for (int h = 0; h < steps; ++h) {
-    __builtin_amdgcn_s_waitcnt(kVmWait);           // this wave's DMA of step h has landed
-    __syncthreads();                               // everyone's has; V of step h - 1 and s_x are free
-    dma(vp, v_lds + (h + kV - 1) % kV * G::kBytes, h + kV - 1);
-    const unsigned char* kt = s_k[h % kK];
-    const unsigned char* vt = s_v[h % kV];
-    f32x16 x;
+  const auto scores = [&](f32x16& x) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = 0.f;
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
-      const f32x4 f = *reinterpret_cast<const f32x4*>(kt + k_off[j]);
+      const f32x4 f = key(j);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], q[j][i], x, 0, 0, 0);
     }
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) s_x[wave][r / 4][lane] = f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
-    float f[kRegs];                                // values, on their way meanwhile
-#pragma unroll
-    for (int i = 0; i < kRegs; ++i) f[i] = value(vt, row_at(i));
-    __syncthreads();                               // every wave's partial scores are there, and K is read
-    dma(kp, k_lds + h % kK * G::kBytes, h + kK);
-    const bool tail = h * kStep + kStep - 1 > first_last;
-    float mt = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      f32x4 sum = s_x[0][b][lane];
-#pragma unroll
-      for (int i = 1; i < kWaves; ++i) sum += s_x[i][b][lane];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * b + i] = sum[i] * c;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (tail)
-        x[r] = sees<kPrefix>(a, w, sh, h * kStep + 8 * (r >> 2) + 4 * half + (r & 3), last, node) ? x[r] : -INFINITY;
-      mt = fmaxf(mt, x[r]);
-    }
-    const float m_new = fmaxf(m, max_halves(mt));
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    if (__ballot(m_new > m)) {                     // a maximum rose: rescale (factor 1 for the others)
-      const float alpha = fast_exp2(m - m_use);
-      l *= alpha;
-      o *= alpha;
-    }
-    m = m_new;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] = fast_exp2(x[r] - m_use);
-      l += x[r];
-    }
-    float probe = 0.f;                             // a NaN from a value of a masked step that is not finite
-    if (tail) {
-#pragma unroll
-      for (int i = 0; i < kRegs; ++i) probe = fmaf(f[i], 0.f, probe);
-    }
-    const bool finite = __ballot(probe != 0.f) == 0;
-    if (__builtin_expect(!finite, 0)) {
-      // As in the bf16 kernel: zeros in the products, and the rows that see a value add it.
-      const int t0 = 2 * r0;                       // first token of this wave's registers
-      for (int t = t0; t < t0 + 2 * kRegs; ++t) {
-        const bool seen = sees<kPrefix>(a, w, sh, h * kStep + t, last, node);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int d = 8 * (r >> 2) + 4 * half + (r & 3);
-          const float v = *reinterpret_cast<const float*>(vt + G::offset(t, 8 * blk + (d >> 2)) + (d & 3) * 4);
-          o[r] += seen && !(fabsf(v) < INFINITY) ? v : 0.f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kRegs; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kRegs; ++i) {
-      float p = x[i];
-      if (kParts > 1) p = r0 ? x[(i + kRegs) % 16] : x[i];
-      o = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i], p, o, 0, 0, 0);
-    }
+  };
+
+  int h = wave;
+  f32x16 x, p;
+  if (h < my_steps) {
+    landed();
+    scores(x);
+    dma(kp, kt, h + kWaves);
+    if (tail(h)) mask(x, h);
+    const float mx = row_max(x);
+    m = mx == -INFINITY ? kNone : mx;
+    all_landed();                                  // asked for in this order: V, the next K
+  }
+  // Steps that every row sees whole, but the last.
+  for (; h + kWaves < my_steps && !tail(h); h += kWaves) {
+    f32x16 y;
+    landed();
+    const float sum = scores_and_exps(y, x, p);
+    dma(kp, kt, h + 2 * kWaves);
+    settle(x, p, sum);
+    landed();
+    products(p);
+    dma(vp, vt, h + kWaves);
+    x = y;
+  }
+  // What is seen in part, and the last.
+  for (; h < my_steps; h += kWaves) {
+    if (tail(h)) mask(x, h);
+    settle(x, p, exps(x, p, l));
+    all_landed();
+    hidden_products(p, h);
+    if (h + kWaves >= my_steps) break;
+    dma(vp, vt, h + kWaves);
+    scores(x);
+    dma(kp, kt, h + 2 * kWaves);
   }
 
-  __builtin_amdgcn_s_waitcnt(0);                   // the trailing DMA lands before exit
-  if (kParts > 1) {                                // the other tokens of this column block
-    static_assert(kParts <= 2, "at most two waves share a column block");
-    __syncthreads();
-    if (r0 > 0) {
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) s_x[blk][r / 4][lane] = f32x4{o[r], o[r + 1], o[r + 2], o[r + 3]};
-    }
-    __syncthreads();
-    if (r0 > 0) return;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[r] += s_x[blk][r / 4][lane][r % 4];
+  // The waves' sums are joined through the buffers, a quarter of the columns by each wave. Group g
+  // of a lane's: columns kBlk c' + i for one or more rows c' of the blocks i, four consecutive ones.
+  all_landed();
+  const auto sums = [&](int i, int g) { return reinterpret_cast<f32x4*>(s_kv[i][0]) + g * kWave + lane; };
+  static_assert(kGroups * kWave * sizeof(f32x4) <= G::kBytes, "a wave's sums fit its K buffer");
+  l = sum_halves(l);
+  if (half == 0) {
+    s_m[wave][col] = m;
+    s_l[wave][col] = l;
   }
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    f32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = o[e % kBlk][4 / kBlk * g + e / kBlk];
+    *sums(wave, g) = y;
+  }
+  __syncthreads();
   if (R >= w.rows) return;
-  const float lt = sum_halves(l);
+  m = kNone;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) m = fmaxf(m, s_m[i][col]);
+  float lt = 0.f, weight[kWaves];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    weight[i] = fast_exp2(s_m[i][col] - m);
+    lt = fmaf(s_l[i][col], weight[i], lt);
+  }
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
-  const float lse = lt == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(lt)) * kLn2;
+  const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
   const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
   const int64_t orow = me.row * a.hq + me.head;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    const int d0 = 32 * blk + 8 * b + 4 * half;
-    const float x0 = o[4 * b] * inv, x1 = o[4 * b + 1] * inv, x2 = o[4 * b + 2] * inv, x3 = o[4 * b + 3] * inv;
-    if (whole) store4(a, orow * D + d0, x0, x1, x2, x3);
-    else *reinterpret_cast<float4*>(a.part_o + pi * D + d0) = make_float4(x0, x1, x2, x3);
+  for (int u = 0; u < kGroups / kWaves; ++u) {
+    const int g = wave * (kGroups / kWaves) + u, r = 4 / kBlk * g;
+    f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) y += *sums(i, g) * weight[i];
+    y *= inv;
+    const int d0 = kBlk * (8 * (r >> 2) + 4 * half + (r & 3));
+    if (whole) store4(a, orow * D + d0, y[0], y[1], y[2], y[3]);
+    else *reinterpret_cast<f32x4*>(a.part_o + pi * D + d0) = y;
   }
   if (wave == 0 && half == 0) {
     if (!whole) a.part_lse[pi] = lse;
@@ -1192,48 +1076,55 @@ struct Plan {
   int slots() const { return cut.most + own.most; }
 };
 
-// `most` splits of `keys`, or as many as there are whole steps.
-Splits splits_of(int64_t keys, int64_t most) {
-  most = std::max<int64_t>(1, std::min<int64_t>({most, (keys + kStep - 1) / kStep, 65535}));
-  const int64_t tps = ((keys + most - 1) / most + kStep - 1) / kStep * kStep;
-  return Splits{(int32_t)std::max<int64_t>(kStep, tps), (int32_t)most};
+// Keys that a workgroup works on at a time: the waves of a narrow tile take a step each.
+int quantum_of(int tile) { return tile == kNarrow ? kStep * kWaves : kStep; }
+
+// At least one whole quantum.
+int64_t rounded(int64_t keys, int tile) {
+  const int64_t quantum = quantum_of(tile);
+  return std::max<int64_t>(1, (keys + quantum - 1) / quantum) * quantum;
+}
+
+// `most` splits of `keys`, or as many as there are quanta.
+Splits splits_of(int64_t keys, int64_t most, int tile) {
+  const int64_t quantum = quantum_of(tile);
+  most = std::max<int64_t>(1, std::min<int64_t>({most, (keys + quantum - 1) / quantum, 65535}));
+  return Splits{(int32_t)rounded((keys + most - 1) / most, tile), (int32_t)most, (int32_t)quantum};
 }
 
 // Splits that a plan considers of the longest keys.
 constexpr int kCandidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
-// Estimated us, from measurements: a step of 32 keys with one workgroup on a CU (two on a CU take
-// turns: together they are no faster), and what a workgroup takes beside its steps, of which
-// the way of its part of `rows` rows to memory and back at a CU's share of the bandwidth.
+// Estimated us, from measurements: a step of 32 keys on a CU (two workgroups there take turns:
+// together they are little faster), and what a workgroup takes beside its steps, of which the way of
+// its part of `rows` rows to memory and back at a CU's share of the bandwidth. At head dim 64 two
+// workgroups of the fp32 kernel hide half of each other's start.
 struct Cost {
   double key, start, part;
   Cost(int32_t dtype, int tile, int32_t d, double rows) {
-    const double step = dtype == CURE_BF16 ? (d == 128 ? 0.45 : 0.28) : tile == kNarrow ? (d == 128 ? 1.9 : 1.0) : 3.6 * d / 128;
-    key = step / kStep;
-    start = 5;
+    const bool bf16 = dtype == CURE_BF16;
+    key = (bf16 ? (d == 128 ? 0.45 : 0.28) : (d == 128 ? 0.95 : 0.53)) / kStep;
+    start = bf16 ? 5 : d == 128 ? 6 : 2.5;
     part = std::min<double>(tile, rows) * d * 8 / 27e3;
   }
 };
 
-// fp32: narrow tiles where the wide ones would leave CUs idle, or half their rows.
-bool narrow(int32_t dtype, int64_t wide, int64_t rows, int32_t hkv) {
-  return dtype == CURE_F32 && (wide * hkv < device_cu_count() || 2 * rows < wide * kRows);
-}
+int tile_of(int32_t dtype) { return dtype == CURE_F32 ? kNarrow : kRows; }
 
 Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t d, const int32_t* host_n_rows,
                  const int32_t* host_ctx_len, int32_t kv_split) {
   const int64_t cus = device_cu_count(), group = hq / hkv;
   const auto tiles_of = [&](int64_t n, int64_t tile) { return (n * group + tile - 1) / tile; };
-  int64_t wide = 0, keys = 0, longest = 0, total = 0;
+  Plan p{};
+  p.tile = tile_of(dtype);
+  int64_t tiles = 0, keys = 0, longest = 0, total = 0;
   for (int b = 0; b < batch; ++b) {
     const int64_t n = host_n_rows[b];
-    wide += tiles_of(n, kRows);
+    tiles += tiles_of(n, p.tile);
     total += n;
     longest = std::max(longest, n);
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
-  Plan p{};
-  p.tile = narrow(dtype, wide, total * group, hkv) ? kNarrow : kRows;
   p.tiles = (int)tiles_of(longest, p.tile);
   // The merge's grid holds the tokens of a sequence in 16 bits.
   int64_t most = longest > 65535 ? 1 : kv_split;
@@ -1242,11 +1133,11 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
     // with the most workgroups, or of the longest workgroup. Measured us a call with 1, 2, 4 and 12
     // splits: one prompt of 2k 52, 72 (two); 4 chunks of 256 - 512 tokens on 2k - 16k, head dim
     // 64, 211, 185, 207, 222; 8 single tokens on 4k - 32k 385, 202, 120, 105.
-    const Cost cost(dtype, p.tile, d, (double)total * group / std::max<int64_t>(1, wide));
+    const Cost cost(dtype, p.tile, d, (double)total * group / std::max<int64_t>(1, tiles));
     double best = 0;
     for (const int s : kCandidates) {
-      const int64_t tps = std::max<int64_t>(kStep, (keys + s - 1) / s);
-      if (s > 1 && tps < (dtype == CURE_BF16 ? 256 : 96)) break;
+      const int64_t tps = rounded((keys + s - 1) / s, p.tile);
+      if (s > 1 && tps < 256) break;
       int64_t units = 0;
       double work = 0;
       for (int b = 0; b < batch; ++b) {
@@ -1271,7 +1162,7 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
       }
     }
   }
-  p.cut = splits_of(keys, most);
+  p.cut = splits_of(keys, most, p.tile);
   return p;
 }
 
@@ -1279,15 +1170,14 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
                  int32_t prefix_len, const int32_t* host_ctx_len, const int32_t* host_n_nodes, int32_t kv_split) {
   const int64_t cus = device_cu_count(), group = hq / hkv;
   const auto tiles_of = [&](int64_t nodes, int64_t tile) { return (nodes * group + tile - 1) / tile; };
-  int64_t nodes = 0, keys = 0, wide = 0;
+  int64_t nodes = 0, keys = 0;
   for (int b = 0; b < batch; ++b) {
     const int64_t n = host_n_nodes[b];
     nodes += n;
-    wide += tiles_of(n, kRows);
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   Plan p{};
-  p.tile = narrow(dtype, wide + tiles_of(nodes, kRows), 2 * nodes * group, hkv) ? kNarrow : kRows;
+  p.tile = tile_of(dtype);
   const int64_t tiles = tiles_of(nodes, p.tile);
   int64_t most = kv_split, own = 1;
   // As for prompts; own rows are split as the prefix is, and fill the CUs around its
@@ -1296,9 +1186,9 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
   double best = 0;
   for (const int s : kCandidates) {
-    const int64_t tps = std::max<int64_t>(kStep, ((kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len) + s - 1) / s);
-    if (s > 1 && (kv_split > 0 || tps < (dtype == CURE_BF16 ? 256 : 64))) break;
-    const int64_t own_tps = std::max<int64_t>(tps, dtype == CURE_BF16 ? 256 : 64);
+    const int64_t tps = rounded(((kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len) + s - 1) / s, p.tile);
+    if (s > 1 && (kv_split > 0 || tps < 256)) break;
+    const int64_t own_tps = std::max<int64_t>(tps, 256);
     int64_t units = tiles * s * hkv;
     double work = (double)tiles * prefix_len;
     for (int b = 0; b < batch; ++b) {
@@ -1314,8 +1204,8 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
       best = time;
     }
   }
-  p.cut = splits_of(prefix_len, most);
-  p.own = splits_of(keys, own);
+  p.cut = splits_of(prefix_len, most, p.tile);
+  p.own = splits_of(keys, own, p.tile);
   // The device may hold other counts than the host's copies: tiles for every node there may
   // be, of which those past the last one end at once.
   p.tiles = (int)std::min<int64_t>(tiles_of((int64_t)batch * n_max, p.tile), INT32_MAX);
@@ -1354,9 +1244,6 @@ void launch_attn(const Args& a, int32_t dtype, int32_t d, dim3 grid, hipStream_t
     else if (once) hipLaunchKernelGGL((seq_attn<64, kPrefix, !kPrefix>), grid, block, 0, st, a);
     else if (d == 128) hipLaunchKernelGGL((seq_attn<128, kPrefix, false>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((seq_attn<64, kPrefix, false>), grid, block, 0, st, a);
-  } else if (a.tile == kNarrow) {
-    if (d == 128) hipLaunchKernelGGL((seq_attn_f32_shared<128, kPrefix>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((seq_attn_f32_shared<64, kPrefix>), grid, block, 0, st, a);
   } else {
     if (d == 128) hipLaunchKernelGGL((seq_attn_f32<128, kPrefix>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((seq_attn_f32<64, kPrefix>), grid, block, 0, st, a);
