@@ -1148,9 +1148,10 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
       }
       units = std::max<int64_t>(1, units * hkv);
       if (longest * group <= 32) {
-        // Single tokens and the like stream the cache once: as many workgroups as two per CU,
+        // Single tokens and the like stream the cache once: as many workgroups as two per CU
+        // (fp32 one: 8 single tokens on 8k, 4 kv-heads, head dim 128, 52 us with one and 60 with two),
         // whose tiles under way cover the memory's latency.
-        if (s == 1 || units <= 2 * cus) most = s;
+        if (s == 1 || units <= (dtype == CURE_BF16 ? 2 : 1) * cus) most = s;
         continue;
       }
       const double each = cost.start + (s > 1 ? cost.part : 0);
