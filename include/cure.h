@@ -403,8 +403,9 @@ cure_status cure_commit(void* k, void* v, int32_t dtype, int32_t n_layers, int64
  *              sequence's parent array is malformed, its sizes are negative,
  *              n_rows exceeds n_max, or its rows or cache rows reach past rows or
  *              cache_rows. Nothing of such a sequence is written.
- * q_out may be q itself where q_ld = hq * d. Cache rows of different sequences
- * must not overlap. Rows that belong to no sequence are not written.
+ * q_out may be q itself where q_ld = hq * d. Rows and cache rows of different
+ * sequences must not overlap, and q, k and v must not overlap the cache rows written.
+ * Rows that belong to no sequence are not written.
  * Supports d a multiple of 16 up to 256, rot a multiple of 16 up to d, n_max <= 256
  * with a tree, batch <= 65535. All row pointers, weights and row distances must be
  * multiples of 16 bytes (else CURE_ERR_INVALID_ARG). No workspace.
@@ -467,7 +468,8 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  *              output. ctx_len may differ either way.
  * The values that a row sees must be finite; keys and values after it (later
  * tokens, and whatever the cache holds behind the sequence) may be anything.
- * Supports d in {64, 128}, hq % hkv == 0, 0 < scale < inf, batch <= 65535.
+ * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite,
+ * batch <= 65535. o may be q where their types are one.
  * kv_split: 0 = automatic, else the number of splits of the longest context.
  * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
  * 16-byte aligned, as q, k, v and o are.
@@ -491,17 +493,20 @@ cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* 
  * begin with the same prefix_len tokens, stored once in cache rows prefix_off ..
  * prefix_off + prefix_len - 1. Node n of sequence b attends to those, to its
  * sequence's own ctx_len[b] rows from kv_off[b] on and to the tree rows on its root
- * path behind them. The prefix is read once for all nodes of all sequences; the own
- * rows take cure_tree_attn, and log-sum-exps join the two.
+ * path behind them. The prefix is read once for all nodes of all sequences, the own
+ * rows by workgroups of the same launch, and log-sum-exps join the two.
  * Arguments, layout and outputs as for cure_tree_attn (ctx_len counts a sequence's
  * own rows only; the position of a node is prefix_len + ctx_len + depth, which
  * cure_rope_append's pos_off = prefix_len gives). prefix_len = 0 is cure_tree_attn.
  * kv_split: splits of the prefix, 0 = automatic.
  * A malformed tree is reported in tree_status, and that sequence's o and lse are then
- * unspecified. Prefix values must be finite.
- * Supports 0 < scale < inf, batch <= 1024 (where prefix_len > 0), and what
- * cure_tree_attn supports. Alignment as for cure_prompt_attn. workspace:
- * cure_prefix_attn_workspace_size(...) bytes for the same arguments.
+ * unspecified. The values that a node sees must be finite; what it does not see may be
+ * anything. The device's n_nodes and ctx_len may differ from the host's copies
+ * (n_nodes up to n_max).
+ * Supports a scale as cure_prompt_attn, batch <= 1024 and batch * n_max * hq/hkv below
+ * 2^31 - 4096 (where prefix_len > 0), and what cure_tree_attn supports. Alignment as for
+ * cure_prompt_attn. workspace: cure_prefix_attn_workspace_size(...) bytes for the same
+ * arguments.
  */
 size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int32_t hkv, int32_t d,
                                        int32_t n_max, int32_t prefix_len,

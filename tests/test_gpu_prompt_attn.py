@@ -95,6 +95,18 @@ def test_fp32_tiles_that_fill_the_chip(d, rows, ctx, hq, hkv):
     c.check(*c.run(kv_split=2), only=lambda n: [0, n - 2])
 
 
+@pytest.mark.parametrize("dtype,rows,ctx,kv_split", [("bf16", [70, 9], [400, 0], 1), ("bf16", [70, 9], [400, 0], 3),
+                                                     ("f32", [70, 9], [400, 0], 1), ("f32", [70, 9], [400, 0], 3)])
+def test_the_output_may_be_the_queries(dtype, rows, ctx, kv_split):
+    c = Case(dtype, rows, ctx, 4, 2, 64)
+    want, want_lse = c.run(kv_split=kv_split)
+    q = c.q.cuda()
+    o, lse = pc.cure_prompt_attn(q, c.k.cuda(), c.v.cuda(), ints(c.row_off, torch.int64), ints(c.rows), ints(c.kv_off, torch.int64),
+                                 ints(c.ctx), c.rows, c.ctx, c.scale, kv_split=kv_split, out=q)
+    live = torch.cat([torch.arange(r, r + n) for r, n in zip(c.row_off, c.rows)]).cuda()
+    assert torch.equal(q[live], want[live]) and torch.equal(lse[live], want_lse[live])
+
+
 def test_one_token_over_a_long_context():
     c = Case("bf16", [1, 1, 1], [9000, 0, 4097], 8, 2, 128)
     c.check(*c.run())
