@@ -61,7 +61,7 @@ CSRC = os.path.join(ROOT, "paper_2608_00531_amd", "csrc")
 # these files are unchanged since the counters were taken.
 CALL_SOURCES = {"margins": ["margins.hip", "common.hpp", "accept_walk.hpp"],
                 "margins_accept": ["margins.hip", "common.hpp", "accept_walk.hpp"],
-                "attn": ["tree_attn.hip", "common.hpp"],
+                "attn": ["tree_attn.hip", "mfma_tile.hpp", "common.hpp"],
                 "accept": ["accept.hip", "common.hpp", "accept_walk.hpp"],
                 "repair": ["repair.hip", "common.hpp"], "commit": ["commit.hip", "common.hpp"]}
 # Layers of the cache the commit runs over (a Llama-3-8B-class target).
