@@ -223,3 +223,39 @@ def test_captured_calls_replay_on_other_trees():
         torch.cuda.synchronize()
         assert torch.equal(out, fresh), new
         c.check(out, None, only=lambda n: [0, n - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_split", [0, 1, 5])
+def test_sizes_other_than_the_hosts_copies(dtype, kv_split):
+    """A captured call is replayed on contexts that grew or shrank and on other trees: the plan is the host's, the sizes
+    are the device's."""
+    c = Case(dtype, 700, [20, 31, 3], [900, 40, 0], 4, 2, 64, n_max=40)
+    for ctx, nodes in (([5, 700, 64], [1, 40, 17]), ([0, 0, 0], [40, 40, 40])):
+        other = Case(dtype, 700, nodes, ctx, 4, 2, 64, n_max=40)
+        q, k, v = other.q.cuda(), other.k.cuda(), other.v.cuda()
+        o, lse, st = pc.cure_prefix_attn(q, k, v, other.prefix_off, 700, ints(other.kv_off, torch.int64), ints(ctx), ints(nodes),
+                                         other.parent(), c.ctx, c.nodes, other.scale, kv_split=kv_split)
+        assert st.tolist() == [0, 0, 0]
+        other.check(o, lse, only=lambda n: [0, n // 2, n - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_streams_at_once(dtype):
+    """Calls under way together on two streams, each with scratch of its own."""
+    cases = [Case(dtype, 900, [30, 12], [64, 300], 8, 2, 128, seed=s) for s in (1, 2)]
+    args = [(c.q.cuda(), c.k.cuda(), c.v.cuda(), c.prefix_off, c.prefix, ints(c.kv_off, torch.int64), ints(c.ctx), ints(c.nodes),
+             c.parent(), c.ctx, c.nodes, c.scale) for c in cases]
+    want = [pc.cure_prefix_attn(*a) for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(10):
+        for i, (st, a) in enumerate(zip(streams, args)):
+            with torch.cuda.stream(st):
+                got[i].append(pc.cure_prefix_attn(*a))
+    torch.cuda.synchronize()
+    for c, w, runs in zip(cases, want, got):
+        for r in runs:
+            for b, n in enumerate(c.nodes):
+                assert torch.equal(r[0][b, :n], w[0][b, :n]) and torch.equal(r[1][b, :n], w[1][b, :n])

@@ -278,3 +278,14 @@ def test_every_key_counts_once(dtype, d, n, group, kv_split, hkv):
         # 1 / n, the sum and the products of ones are exact up to a few fp32 roundings.
         assert float((got - seen[:, None]).abs().max()) <= 8 * 2.0 ** -24 * total, total
         assert float((lse.cpu().double() - keys.log()[:, None]).abs().max()) <= 2e-6, total
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_split", [0, 1, 4])
+def test_contexts_other_than_the_hosts_copies(dtype, kv_split):
+    c = Case(dtype, [40, 7, 1], [600, 30, 0], 4, 2, 64)
+    for ctx, rows in (([10, 900, 33], [40, 40, 1]), ([0, 0, 1500], [38, 0, 1])):
+        other = Case(dtype, rows, ctx, 4, 2, 64)
+        o, lse = pc.cure_prompt_attn(other.q.cuda(), other.k.cuda(), other.v.cuda(), ints(other.row_off, torch.int64), ints(rows),
+                                     ints(other.kv_off, torch.int64), ints(ctx), c.rows, c.ctx, other.scale, kv_split=kv_split)
+        other.check(o, lse, only=lambda n: [0, n // 2, n - 1])
