@@ -1153,6 +1153,8 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
     // with the most workgroups, or of the longest workgroup. Measured us a call with 1, 2, 4 and 12
     // splits: one prompt of 2k 52, 72 (two); 4 chunks of 256 - 512 tokens on 2k - 16k, head dim
     // 64, 211, 185, 207, 222; 8 single tokens on 4k - 32k 385, 202, 120, 105.
+    // Splits of fewer than 256 tokens cost more in starts and parts than they save: 4 x 32 tokens
+    // on 2000 in fp32 69, 46, 53 and (6, 8 and 16 splits) 62, 66 and 94.
     const Cost cost(dtype, p.tile, d, (double)total * group / std::max<int64_t>(1, tiles));
     double best = 0;
     for (const int s : kCandidates) {
@@ -1207,7 +1209,8 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
   double best = 0;
   for (const int s : kCandidates) {
-    const int64_t tps = rounded(((kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len) + s - 1) / s, p.tile);
+    const int64_t len = kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len;
+    const int64_t tps = rounded((len + s - 1) / s, p.tile);
     if (s > 1 && (kv_split > 0 || tps < 256)) break;
     const int64_t own_tps = std::max<int64_t>(tps, 256);
     int64_t units = tiles * s * hkv;
