@@ -401,8 +401,8 @@ cure_status cure_commit(void* k, void* v, int32_t dtype, int32_t n_layers, int64
  *   rows       rows that q, k, v and q_out hold;  cache_rows  rows of the caches
  *   row_status [batch] int32 output: CURE_OK, or CURE_ERR_BAD_TREE when the
  *              sequence's parent array is malformed, its sizes are negative,
- *              n_rows exceeds n_max, or its rows or cache rows reach past rows or
- *              cache_rows. Nothing of such a sequence is written.
+ *              n_rows exceeds n_max, or its rows or (where hkv > 0) cache rows reach past
+ *              rows or cache_rows. Nothing of such a sequence is written.
  * q_out may be q itself where q_ld = hq * d. Rows and cache rows of different
  * sequences must not overlap, and q, k and v must not overlap the cache rows written.
  * Rows that belong to no sequence are not written.

@@ -169,8 +169,8 @@ __global__ __launch_bounds__(kThreads) void rope_append(Args a) {
   const int L = a.ctx_len[b];
   const int64_t off = a.kv_off[b];
   const int64_t base = (int64_t)L + (a.pos_off ? a.pos_off[b] : 0);
-  bool bad = N < 0 || N > a.n_max || L < 0 || off < 0 || off > a.cache_rows - L - N || row0 < 0 ||
-             row0 > a.rows - N;
+  bool bad = N < 0 || N > a.n_max || L < 0 || row0 < 0 || row0 > a.rows - N ||
+             (a.hkv > 0 && (off < 0 || off > a.cache_rows - L - N));
   // Depths by pointer doubling: p becomes the ancestor 2^round up (-1: past the root), depth
   // the steps up to it. Up to 64 nodes every wave does it by itself, with lane exchanges; more
   // (at most 8 rounds for 256) go through LDS.
@@ -330,10 +330,9 @@ extern "C" cure_status cure_rope_append(const void* q, int64_t q_ld, const void*
     return CURE_ERR_INVALID_ARG;
   if (hq == 0 && hkv == 0) return CURE_ERR_INVALID_ARG;
   if (batch == 0) return CURE_OK;
-  if (!n_rows || !kv_off || !ctx_len || !row_status) return CURE_ERR_INVALID_ARG;
+  if (!n_rows || !kv_off || !ctx_len || !row_status || (rot > 0 && !inv_freq)) return CURE_ERR_INVALID_ARG;
   if (n_max > 0) {
-    if ((hq > 0 && (!q || !q_out)) || (hkv > 0 && (!k || !v || !k_cache || !v_cache)) ||
-        (rot > 0 && !inv_freq))
+    if ((hq > 0 && (!q || !q_out)) || (hkv > 0 && (!k || !v || !k_cache || !v_cache)))
       return CURE_ERR_INVALID_ARG;
     if (!row_off && rows / n_max < batch) return CURE_ERR_INVALID_ARG;   // padded rows
   }
@@ -346,12 +345,13 @@ extern "C" cure_status cure_rope_append(const void* q, int64_t q_ld, const void*
   if ((hq > 0 && q_ld < (int64_t)hq * d) ||
       (hkv > 0 && (k_ld < (int64_t)hkv * d || v_ld < (int64_t)hkv * d)))
     return CURE_ERR_INVALID_ARG;
-  if (q && q == q_out && q_ld != (int64_t)hq * d) return CURE_ERR_INVALID_ARG;   // rows would overlap
+  if (hq > 0 && q == q_out && q_ld != (int64_t)hq * d) return CURE_ERR_INVALID_ARG;   // rows would overlap
   // Rows move as 16-byte vectors.
-  const uintptr_t at = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) |
-                       reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(q_out) |
-                       reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache) |
-                       reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight);
+  uintptr_t at = reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight);
+  if (hq > 0) at |= reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out);
+  if (hkv > 0)
+    at |= reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(k_cache) |
+          reinterpret_cast<uintptr_t>(v_cache);
   if (at % 16 != 0) return CURE_ERR_INVALID_ARG;
   if ((hq > 0 && q_ld * elem % 16) || (hkv > 0 && (k_ld * elem % 16 || v_ld * elem % 16)))
     return CURE_ERR_INVALID_ARG;

@@ -144,6 +144,19 @@ def test_keys_without_queries():
     assert torch.equal(vc[3:8], v) and not kc[:3].any() and not kc[8:].any()
 
 
+def test_queries_without_keys():
+    t = torch.bfloat16
+    q = normal(1, 5, 3, 64, dtype=t).cuda()
+    none = torch.empty(5, 0, 64, dtype=t, device="cuda")
+    freq, _ = pc.cure_rope_frequencies(64)
+    got, status = pc.cure_rope_append(q, none, none, none[:0], none[:0], ints([0], torch.int64), ints([3]), ints([5]), freq.cuda(),
+                                      row_off=ints([0], torch.int64))
+    assert status.tolist() == [0]
+    x = wide(q)
+    ref = oracle.rope_append(x, np.zeros((5, 1, 64)), np.zeros((5, 1, 64)), 3 + np.arange(5), freq.double().numpy())[0]
+    assert np.all(np.abs(wide(got) - ref) <= bound(x, ref, 64, 64, False, 1.0, HALF[t]))
+
+
 @pytest.mark.parametrize("what", ["parent", "self", "below", "n_rows", "n_max", "ctx", "kv_off", "cache_end", "rows_end"])
 def test_a_bad_sequence_is_reported_and_left_alone(what):
     t = torch.float32

@@ -66,6 +66,7 @@ def test_append_argument_errors(L):
     assert append(L, n_max=257, rows=514, parent=1) == U
     assert append(L, batch=70000, rows=1 << 20) == U
     assert append(L, batch=0) == OK
+    assert append(L, n_max=0, inv_freq=None) == E           # read whatever the rows are
 
 
 def frequencies(L, rot=8, base=10000.0, scaling=0, factor=1.0, orig=0.0, p0=0.0, p1=0.0):
