@@ -71,14 +71,34 @@ union Pack8 {
   i16x4 h[2];
 };
 
-
 // Three-input maximum as one v_max3_f32. Written as assembly because fmaxf
 // first canonicalises every operand that may be a signalling NaN (an extra
-// instruction per score); scores here are finite dot products or -inf.
+// instruction per score); scores here are finite dot products or -inf. The compiler
+// puts no wait states between a matrix instruction and assembly that reads its
+// result, so no operand may be such a result that nothing else has read: max_scores.
 CURE_DEV float max3_raw(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+// Maximum of the scores of one matrix result (and of m). The canonicalised score is read by an
+// instruction that the compiler sees and delays until the result is there, and every
+// other score's read depends on it: one instruction more than the maxima alone.
+template <class V>
+CURE_DEV float max_scores(const V& x) {
+  constexpr int n = sizeof(V) / sizeof(float);
+  float m = __builtin_canonicalizef(x[0]);
+#pragma unroll
+  for (int r = 1; r < n; r += 2) m = max3_raw(m, x[r], x[r + 1 < n ? r + 1 : r]);
+  return m;
+}
+template <class V>
+CURE_DEV float max_scores(const V& x, float m) {
+  constexpr int n = sizeof(V) / sizeof(float);
+  m = max3_raw(m, __builtin_canonicalizef(x[0]), x[1]);
+#pragma unroll
+  for (int r = 2; r < n; r += 2) m = max3_raw(m, x[r], x[r + 1]);
+  return m;
 }
 constexpr int kTile = 64;            // tokens per K/V tile
 constexpr float kRescaleLog2 = 8.f;       // lazy rescale threshold (log2 units)

@@ -565,11 +565,7 @@ __global__ __launch_bounds__(64 * NW, NBUF > 2 ? 1 : 2) void tree_attn_mfma(A a)
           sacc[blk][r] += mask_bias(t0 + blk * 32 + 8 * (r >> 2) + 4 * half + (r & 3), L, end, n, s_anc);
     }
     // Row maximum: one three-input max per two scores, in two chains.
-    float mb[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) mb[blk] = max3_raw(mb[blk], sacc[blk][r], sacc[blk][r + 1]);
+    const float mb[2] = {max_scores(sacc[0]), max_scores(sacc[1])};
     const float m_tile = max_halves(max3_raw(mb[0], mb[1], mb[1])) * c;
     // Lazy rescale: move the reference only when the maximum rises by > 2^8.
     const bool grow = m_tile > m_run + kRescaleLog2;
@@ -903,12 +899,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
       check = __ballot(!(l0 + l1 <= 256.f)) != 0;
     }
     if (__builtin_expect(check, 0)) {
-      // Row maximum over the lane's 16 scores (eight v_max3), then its 3 partners.
-      float mb = max3_raw(sacc[0][0], sacc[0][1], sacc[0][2]);
+      // Row maximum over the lane's 16 scores, then its 3 partners.
+      float mb = max_scores(sacc[0]);
 #pragma unroll
-      for (int i = 3; i < 15; i += 2)
-        mb = max3_raw(mb, sacc[i >> 2][i & 3], sacc[(i + 1) >> 2][(i + 1) & 3]);
-      mb = max3_raw(mb, sacc[3][3], sacc[3][3]);
+      for (int i = 1; i < 4; ++i) mb = max_scores(sacc[i], mb);
       mb = max3_raw(mb, partner<16>(mb), mb);
       const float m_tile = max_halves(mb) * cs;
       const bool grow = m_tile > m_run + kRescaleLog2;
@@ -1269,11 +1263,9 @@ void tree_attn_rg(A a) {
           bool grow_any = false;
 #pragma unroll
           for (int rg = 0; rg < NG; ++rg) {
-            float mb = max3_raw(sacc[rg][0][0], sacc[rg][0][1], sacc[rg][0][2]);
+            float mb = max_scores(sacc[rg][0]);
 #pragma unroll
-            for (int i = 3; i + 1 < 4 * kTB; i += 2)
-              mb = max3_raw(mb, sacc[rg][i >> 2][i & 3], sacc[rg][(i + 1) >> 2][(i + 1) & 3]);
-            mb = max3_raw(mb, sacc[rg][kTB - 1][3], sacc[rg][kTB - 1][3]);
+            for (int i = 1; i < kTB; ++i) mb = max_scores(sacc[rg][i], mb);
             mb = max3_raw(mb, partner<16>(mb), mb);
             m_tile[rg] = max_halves(mb) * cs;
             grow_any |= m_tile[rg] > m_run[rg] + kRescaleLog2;
