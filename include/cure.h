@@ -465,7 +465,8 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  *   host_n_rows, host_ctx_len  host copies that the launch is planned from. The
  *              device's n_rows may be smaller (a captured call replayed on shorter
  *              prompts), not larger: tokens past the host's longest n_rows may get no
- *              output. ctx_len may differ either way.
+ *              output. ctx_len may differ either way. A sequence whose ctx_len is negative
+ *              or whose rows do not lie within `rows` on the device is taken as empty.
  * The values that a row sees must be finite; keys and values after it (later
  * tokens, and whatever the cache holds behind the sequence) may be anything.
  * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite,
@@ -500,9 +501,10 @@ cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* 
  * cure_rope_append's pos_off = prefix_len gives). prefix_len = 0 is cure_tree_attn.
  * kv_split: splits of the prefix, 0 = automatic.
  * A malformed tree is reported in tree_status, and that sequence's o and lse are then
- * unspecified. The values that a node sees must be finite; what it does not see may be
- * anything. The device's n_nodes and ctx_len may differ from the host's copies
- * (n_nodes up to n_max).
+ * unspecified. Where prefix_len > 0 a ctx_len that is negative on the device is reported as
+ * well, and that sequence's o and lse are not written. The values that a node sees must be
+ * finite; what it does not see may be anything. The device's n_nodes and ctx_len may differ
+ * from the host's copies (n_nodes up to n_max).
  * Supports a scale as cure_prompt_attn, batch <= 1024 and batch * n_max * hq/hkv below
  * 2^31 - 4096 (where prefix_len > 0), and what cure_tree_attn supports. Alignment as for
  * cure_prompt_attn. workspace: cure_prefix_attn_workspace_size(...) bytes for the same

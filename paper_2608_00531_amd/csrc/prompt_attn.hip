@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -66,6 +67,7 @@ struct Args {
   Div by_group, by_hkv;
   int32_t batch, n_max;
   float scale_log2;
+  int64_t rows;                      // rows of q and o
   const int64_t* row_off;            // prompt: first row of q and o per sequence
   const int32_t* n_rows;             // tokens, or nodes, per sequence
   const int64_t* kv_off;
@@ -95,6 +97,14 @@ CURE_DEV Cut cut_of(const Splits& s, int keys) {
   const int n = max(1, min((keys - 1) / s.tps + 1, s.most));
   const int per = ((keys - 1) / n / s.quantum + 1) * s.quantum;
   return Cut{(keys - 1) / per + 1, per};
+}
+
+// A sequence's rows, as the device's sizes have them: none where its context cannot be (the
+// host's checks keep context and rows below 2^31 - 4096) or its rows lie outside those of q and o.
+CURE_DEV int rows_of(const Args& a, int n_raw, int ctx, int64_t row0) {
+  const int n = min(n_raw, a.n_max);
+  const bool ok = ctx >= 0 && ctx <= INT32_MAX - 4096 - max(n, 0) && row0 >= 0 && row0 <= a.rows - n;
+  return ok ? n : 0;
 }
 
 // What a workgroup works on: packed query rows r0 .. of `rows` in all, against cache rows
@@ -140,7 +150,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   w.row0 = a.row_off[b];
   w.key0 = a.kv_off[b];
   asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.row0), "s"(w.key0));
-  const int n = min(n_raw, a.n_max);
+  const int n = rows_of(a, n_raw, w.ctx, w.row0);
   w.rows = n * a.group;
   const int tiles = (w.rows + a.tile - 1) >> a.tile_log2;
   if (n <= 0 || x >= tiles) return false;
@@ -172,12 +182,13 @@ CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
     w.ctx = a.ctx_len[b];
     w.key0 = a.kv_off[b];
     asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.key0));
-    const int n = min(n_raw, a.n_max);
+    w.row0 = (int64_t)b * a.n_max;
+    const int n = rows_of(a, n_raw, w.ctx, w.row0);
     w.rows = n * a.group;
     w.r0 = tile * a.tile;
-    w.row0 = (int64_t)b * a.n_max;
-    if (n <= 0) {                                  // the empty tree is valid
-      if (tile == 0 && s == 0 && w.hk == 0 && threadIdx.x == 0 && a.tree_status) a.tree_status[b] = CURE_OK;
+    if (n <= 0) {                                  // the empty tree is valid, a context that cannot be is not
+      if (tile == 0 && s == 0 && w.hk == 0 && threadIdx.x == 0 && a.tree_status)
+        a.tree_status[b] = n_raw > 0 ? CURE_ERR_BAD_TREE : CURE_OK;
       return false;
     }
     const int keys = w.ctx + n;
@@ -1022,22 +1033,20 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   const int col = (threadIdx.x % kLanes) * 4;
   const int i = blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
-  const int n = min(a.n_rows[b], a.n_max);
-  const int ctx = a.ctx_len[b];
+  const int n_raw = a.n_rows[b], ctx = a.ctx_len[b];
+  const int64_t row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b], row = row0 + i;
+  const int n = rows_of(a, n_raw, ctx, row0);
   if (i >= n) return;
   int shared, parts;                               // parts from slot 0 on, and in all
-  int64_t row;
   if (kPrefix) {
     shared = cut_of(a.cut, a.prefix_len).n;
     parts = shared + cut_of(a.own, ctx + n).n;
-    row = (int64_t)b * a.n_max + i;
   } else {
     // The tile of this row's head decides how many keys its splits covered.
     const int rows = n * a.group, R = i * a.group + (head - a.by_group(head) * a.group);
     const int end = min(((R >> a.tile_log2) + 1) * a.tile, rows);
     shared = parts = cut_of(a.cut, ctx + a.by_group(end - 1) + 1).n;
     if (parts == 1) return;                        // written whole
-    row = a.row_off[b] + i;
   }
   const int64_t p0 = part_index(a, row, head, 0), orow = row * a.hq + head;
   const int gap = a.cut.most - shared;             // slots that no split of the prefix has
@@ -1356,6 +1365,7 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   a.batch = batch;
   a.n_max = (int32_t)longest;
   a.scale_log2 = scale * kLog2e;
+  a.rows = rows;
   a.row_off = row_off;
   a.n_rows = n_rows;
   a.kv_off = kv_off;
@@ -1426,6 +1436,7 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   a.batch = batch;
   a.n_max = n_max;
   a.scale_log2 = scale * kLog2e;
+  a.rows = (int64_t)batch * n_max;
   a.n_rows = n_nodes;
   a.kv_off = kv_off;
   a.ctx_len = ctx_len;
