@@ -1123,6 +1123,8 @@ Splits splits_of(int64_t keys, int64_t most, int tile) {
 
 // Splits that a plan considers of the longest keys.
 constexpr int kCandidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+// Of the own rows behind a prefix: one sequence with one kv-head has a workgroup per CU with the last.
+constexpr int kOwnCandidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
 
 // Estimated us, from measurements: a step of 32 keys on a CU (two workgroups there take turns:
 // together they are little faster), and what a workgroup takes beside its steps, of which the way of
@@ -1211,30 +1213,50 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   Plan p{};
   p.tile = tile_of(dtype);
   const int64_t tiles = tiles_of(nodes, p.tile);
-  int64_t most = kv_split, own = 1;
-  // As for prompts; own rows are split as the prefix is, and fill the CUs around its
-  // workgroups. Measured us a call with 1, 2, 4 and 12 splits: 16 trees of 40 - 48 nodes on 8k 131,
-  // 122, 137, 171; 32 single tokens on 16k, head dim 64, 169, 92, 52, 27 (24 with 24, 26 with 32).
-  const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
-  double best = 0;
-  for (const int s : kCandidates) {
-    const int64_t len = kv_split > 0 ? prefix_len / std::min(kv_split, prefix_len) : prefix_len;
-    const int64_t tps = rounded((len + s - 1) / s, p.tile);
-    if (s > 1 && (kv_split > 0 || tps < 256)) break;
-    const int64_t own_tps = std::max<int64_t>(tps, 256);
-    int64_t units = tiles * s * hkv;
-    double work = (double)tiles * prefix_len;
+  // Own rows are split for themselves, as their number and lengths have nothing to do with the
+  // prefix: workgroups and longest split of every candidate, up to one for each 256 keys or part of them.
+  // us a call behind 200 shared tokens, with the estimate's splits and with one for each 256 keys: 16
+  // trees of 48 nodes on 4000 104 (one) and 208, on 30000 579 (four) and 1245, 64 trees 2043 (two) and
+  // 4969, where the workspace of the latter is 6 GB. 12 trees of 28 on 684 28 (one) and 32.
+  struct Own {
+    int64_t units, longest;
+  };
+  constexpr int kOwn = (int)(sizeof(kOwnCandidates) / sizeof(kOwnCandidates[0]));
+  Own owns[kOwn] = {};
+  int own_count = 0;
+  double work = (double)tiles * prefix_len;
+  for (int b = 0; b < batch; ++b)
+    work += (double)tiles_of(host_n_nodes[b], p.tile) * ((int64_t)host_n_nodes[b] + host_ctx_len[b]);
+  for (const int u : kOwnCandidates) {
+    if (u > 1 && u > (keys + 255) / 256) break;
+    const int64_t tps = rounded((keys + u - 1) / u, p.tile);
+    Own& o = owns[own_count++];
+    o.longest = std::min(tps, keys);
     for (int b = 0; b < batch; ++b) {
-      const int64_t t = tiles_of(host_n_nodes[b], p.tile), k = (int64_t)host_n_nodes[b] + host_ctx_len[b];
-      units += t * std::max<int64_t>(1, (k + own_tps - 1) / own_tps) * hkv;
-      work += (double)t * k;
+      const int64_t k = (int64_t)host_n_nodes[b] + host_ctx_len[b];
+      o.units += tiles_of(host_n_nodes[b], p.tile) * std::max<int64_t>(1, (k + tps - 1) / tps) * hkv;
     }
-    const double each = cost.start + cost.part, unit = tps * cost.key + each;
-    const double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
-    if (best == 0 || time < best) {
-      if (kv_split == 0) most = s;
-      own = (keys + own_tps - 1) / own_tps;
-      best = time;
+  }
+  // As for prompts, but all workgroups are one launch, in which those of own rows fill the CUs
+  // around the prefix's. Measured us a call with 1, 2, 4 and 12 splits: 16 trees of 40 - 48 nodes on 8k
+  // 131, 122, 137, 171; 32 single tokens on 16k, head dim 64, 169, 92, 52, 27 (24 with 24, 26 with 32).
+  int64_t most = kv_split, own = 1;
+  const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
+  const double each = cost.start + cost.part;
+  double best = 0;
+  for (const int c : kCandidates) {
+    const int64_t s = kv_split > 0 ? std::min(kv_split, prefix_len) : c;
+    const int64_t tps = rounded((prefix_len + s - 1) / s, p.tile);
+    if (c > 1 && (kv_split > 0 || tps < 256)) break;
+    for (int i = 0; i < own_count; ++i) {
+      const int64_t units = tiles * s * hkv + owns[i].units;
+      const double unit = std::max(tps, owns[i].longest) * cost.key + each;
+      const double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
+      if (best == 0 || time < best) {
+        most = s;
+        own = kOwnCandidates[i];
+        best = time;
+      }
     }
   }
   p.cut = splits_of(prefix_len, most, p.tile);
