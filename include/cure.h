@@ -406,9 +406,11 @@ cure_status cure_commit(void* k, void* v, int32_t dtype, int32_t n_layers, int64
  * q_out may be q itself where q_ld = hq * d. Rows and cache rows of different
  * sequences must not overlap, and q, k and v must not overlap the cache rows written.
  * Rows that belong to no sequence are not written.
+ * n_max sizes the launch: with row_off, give the longest n_rows rather than all rows.
  * Supports d a multiple of 16 up to 256, rot a multiple of 16 up to d, n_max <= 256
- * with a tree, batch <= 65535. All row pointers, weights and row distances must be
- * multiples of 16 bytes (else CURE_ERR_INVALID_ARG). No workspace.
+ * with a tree, n_max (with row_off: n_max or rows) < 2^26 - 3, batch <= 65535. All row
+ * pointers, weights and row distances must be multiples of 16 bytes (else
+ * CURE_ERR_INVALID_ARG). No workspace.
  */
 #define CURE_ROPE_INTERLEAVED 1u
 

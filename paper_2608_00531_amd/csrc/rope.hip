@@ -362,7 +362,10 @@ extern "C" cure_status cure_rope_append(const void* q, int64_t q_ld, const void*
   // with four: 1024 rows of 32 + 8 heads of 128 8.5 and 12.2, 2048 14.6 and 15.1, 4096 22.3 and 21.6;
   // 2048 of 8 + 1 heads of 64 8.7 and 5.7.
   if ((int64_t)batch * n_max >= 2048) a.rows_per_wg = kMaxRows;
-  const dim3 grid((unsigned)std::max(1, (n_max + a.rows_per_wg - 1) / a.rows_per_wg), (unsigned)batch);
+  const int64_t most = row_off ? std::min<int64_t>(n_max, rows) : n_max;   // rows that a sequence can have
+  const int64_t wgs = std::max<int64_t>(1, (most + a.rows_per_wg - 1) / a.rows_per_wg);
+  if (wgs * kThreads >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;   // a launch counts threads in 32 bits
+  const dim3 grid((unsigned)wgs, (unsigned)batch);
   const bool interleaved = flags & CURE_ROPE_INTERLEAVED;
   hipStream_t st = as_stream(stream);
   if (dtype == CURE_BF16) interleaved ? launch<uint16_t, true>(a, grid, st) : launch<uint16_t, false>(a, grid, st);

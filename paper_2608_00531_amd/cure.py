@@ -270,12 +270,13 @@ def cure_rope_append(q, k, v, k_cache, v_cache, kv_off, ctx_len, n_rows, inv_fre
 
     q [batch, n_max, hq, d] (or None), k, v [batch, n_max, hkv, d]: each sequence's
     rows padded to n_max; or, with row_off int64 [batch], packed [rows, heads, d] with
-    sequence b's rows from row_off[b] on and n_max a bound on n_rows (default: rows). Rows
-    may be slices of a fused projection's output. k_cache, v_cache [cache_rows, hkv, d].
-    kv_off int64, ctx_len, n_rows and pos_off int32 [batch]; parent int32 [batch, n_max]
-    where the rows are a tree's nodes; q_weight, k_weight [d] to normalise by; inv_freq
-    float32 [rot / 2] or None (all on the GPU). out: the queries' result, as q but
-    contiguous. Returns (queries, status [batch]); rows past a sequence's n_rows are
+    sequence b's rows from row_off[b] on and n_max a bound on n_rows (default: rows; for
+    many sequences the longest n_rows is faster, as the launch has room for n_max rows of
+    each). Rows may be slices of a fused projection's output. k_cache, v_cache
+    [cache_rows, hkv, d]. kv_off int64, ctx_len, n_rows and pos_off int32 [batch]; parent
+    int32 [batch, n_max] where the rows are a tree's nodes; q_weight, k_weight [d] to
+    normalise by; inv_freq float32 [rot / 2] or None (all on the GPU). out: the queries'
+    result, as q but contiguous. Returns (queries, status [batch]); rows past a sequence's n_rows are
     not written.
     """
     return _native().rope_append(q, k, v, k_cache, v_cache, kv_off, ctx_len, n_rows, inv_freq, parent,
