@@ -473,7 +473,8 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  * tokens, and whatever the cache holds behind the sequence) may be anything.
  * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite,
  * batch <= 65535. o may be q where their types are one.
- * kv_split: 0 = automatic, else the number of splits of the longest context.
+ * kv_split: 0 = automatic, else the number of splits of the longest context (fewer where
+ * that has not as many steps of keys).
  * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
  * 16-byte aligned, as q, k, v and o are.
  * bf16: probabilities are rounded to bf16 for their product and lse sums the rounded

@@ -81,6 +81,7 @@ struct Args {
   Splits cut, own;                   // of a prompt's keys or the prefix, and of own rows
   float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most
   float* part_lse;                   // [row][hq][slots]
+  int32_t merge0;                    // first token of a merge launch
 };
 
 CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int slot) {
@@ -1031,7 +1032,7 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   constexpr int kLanes = D / 4;
   const int head = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
   const int col = (threadIdx.x % kLanes) * 4;
-  const int i = blockIdx.y, b = blockIdx.z;
+  const int i = a.merge0 + blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
   const int n_raw = a.n_rows[b], ctx = a.ctx_len[b];
   const int64_t row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b], row = row0 + i;
@@ -1157,8 +1158,8 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
     if (n > 0) keys = std::max<int64_t>(keys, n + host_ctx_len[b]);
   }
   p.tiles = (int)tiles_of(longest, p.tile);
-  // The merge's grid holds the tokens of a sequence in 16 bits.
-  int64_t most = longest > 65535 ? 1 : kv_split;
+  // A prompt of more than 65535 tokens has two tiles and more for every CU.
+  int64_t most = kv_split > 0 ? kv_split : longest > 65535;
   if (most == 0) {
     // The splits of the longest keys that are estimated to take least time: that of the CUs
     // with the most workgroups, or of the longest workgroup. Measured us a call with 1, 2, 4 and 12
@@ -1306,11 +1307,16 @@ void launch_attn(const Args& a, int32_t dtype, int32_t d, dim3 grid, hipStream_t
 }
 
 template <bool kPrefix>
-void launch_merge(const Args& a, int32_t d, hipStream_t st) {
+void launch_merge(Args a, int32_t d, hipStream_t st) {
   const int heads = 1024 / d;
-  const dim3 grid((unsigned)((a.hq + heads - 1) / heads), (unsigned)a.n_max, (unsigned)a.batch);
-  if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((seq_merge<64, kPrefix>), grid, dim3(256), 0, st, a);
+  constexpr int kTokens = 65535;                   // of a launch, whose grid holds them in 16 bits
+  for (int64_t t = 0; t < a.n_max; t += kTokens) {
+    a.merge0 = (int32_t)t;
+    const dim3 grid((unsigned)((a.hq + heads - 1) / heads), (unsigned)std::min<int64_t>(a.n_max - t, kTokens),
+                    (unsigned)a.batch);
+    if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((seq_merge<64, kPrefix>), grid, dim3(256), 0, st, a);
+  }
 }
 
 // The checks that both calls make of their operands.
