@@ -334,7 +334,8 @@ CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, f
 // instructions of one wave interleave.
 //
 // 128 rows share a tile of keys, so that 2 workgroups of 4 waves fit a CU's registers (198 of
-// 256 at head dim 128) and each key read from LDS serves 32 rows. Large prompts are bound by the
+// 256 at head dim 128; 235 with a prefix, where the masks of the steps seen in part also keep 82
+// scalar registers in lanes of a vector one, outside the main loop) and each key read from LDS serves 32 rows. Large prompts are bound by the
 // matrix unit and the power it draws: a prompt of 8192 tokens, 32 heads of 128, takes 500 us (1.10
 // PFLOP/s of the 1.20 that a large product reaches), the unit busy 58 % of the cycles at 1.75 GHz;
 // its instructions alone take 386 us. 16 prompts of 1 to 2048 tokens take 240 us, 0.33 GB of
@@ -500,6 +501,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
     }
     return sum;
   };
+  // Not by max3_raw: the compiler would not wait for the scores (max_scores), and here a step's maximum is rare.
   auto row_max = [&](const f32x16& x) {
     float mx = x[0];
 #pragma unroll
