@@ -1242,7 +1242,7 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   }
   // As for prompts, but all workgroups are one launch, in which those of own rows fill the CUs
   // around the prefix's. Measured us a call with 1, 2, 4 and 12 splits: 16 trees of 40 - 48 nodes on 8k
-  // 131, 122, 137, 171; 32 single tokens on 16k, head dim 64, 169, 92, 52, 27 (24 with 24, 26 with 32).
+  // 131, 122, 137, 171; 32 single tokens on 16k, head dim 64, 169, 92, 52, 27 (24 with 16 and with 24, 26 with 32).
   int64_t most = kv_split, own = 1;
   const Cost cost(dtype, p.tile, d, (double)(nodes * group) / std::max<int64_t>(1, tiles));
   const double each = cost.start + cost.part;
