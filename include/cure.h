@@ -476,7 +476,8 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  * kv_split: 0 = automatic, else the number of splits of the longest context (fewer where
  * that has not as many steps of keys).
  * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
- * 16-byte aligned, as q, k, v and o are.
+ * 16-byte aligned, as q, k, v and o are. Beyond 1 GB it has room for the splits of the
+ * host's sizes only; a sequence that is longer on the device is then computed in one split.
  * bf16: probabilities are rounded to bf16 for their product and lse sums the rounded
  * ones (within 2^-8 of the exact sum). float32: float32 throughout.
  */

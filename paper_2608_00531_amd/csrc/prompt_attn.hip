@@ -56,6 +56,19 @@ struct Splits {
   int32_t tps, most, quantum;
 };
 
+// Splits that rows of `keys` (at least one) keys have at most.
+__host__ __device__ inline int32_t slots_of(const Splits& s, int64_t keys) {
+  const int64_t n = (keys - 1) / s.tps + 1;
+  return (int32_t)(n < s.most ? n : s.most);
+}
+
+// Where each sequence's parts lie, in calls whose workspace would be large with one number of
+// slots for all rows: row r, head h, split j at first + (r * hq + h) * splits + j.
+struct Place {
+  int64_t first;
+  int32_t splits;                    // of the sequence's longest rows; 1: written whole
+};
+
 struct Args {
   const void* q;
   const void* k;
@@ -79,13 +92,16 @@ struct Args {
   int32_t tile, tile_log2;           // query rows of a tile
   int32_t tiles, own_tiles;          // prefix: tiles of all nodes, and of a sequence's
   Splits cut, own;                   // of a prompt's keys or the prefix, and of own rows
-  float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most
+  float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most; or by place
   float* part_lse;                   // [row][hq][slots]
+  Place* place;                      // [batch], or null
   int32_t merge0;                    // first token of a merge launch
 };
 
-CURE_DEV int64_t part_index(const Args& a, int64_t row, int head, int slot) {
-  return (row * a.hq + head) * (a.cut.most + a.own.most) + slot;
+// The place of sequence b's parts.
+CURE_DEV Place place_of(const Args& a, int b) { return a.place ? a.place[b] : Place{0, a.cut.most + a.own.most}; }
+CURE_DEV int64_t part_index(const Args& a, const Place& p, int64_t row, int head, int slot) {
+  return p.first + (row * a.hq + head) * p.splits + slot;
 }
 
 // The splits of `keys` (at least one) keys: n of `per` tokens, the last one shorter (a single
@@ -117,6 +133,7 @@ struct Work {
   int64_t row0;                      // first row of the sequence (not for a prefix)
   int ctx;
   int b;
+  Place place;
   bool tree;                         // a sequence's own rows, in cure_prefix_attn
 };
 
@@ -145,6 +162,7 @@ CURE_DEV Shared shared_of(Nothing&, Nothing&) { return Shared{}; }
 // out in turn over the sequences, 16 prompts of 1 to 2048 tokens took 399 us instead of 253.
 CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   const int b = blockIdx.z, x = a.by_hkv(blockIdx.x);
+  w.place = place_of(a, b);
   w.hk = blockIdx.x - x * a.hkv;
   const int n_raw = a.n_rows[b];
   w.ctx = a.ctx_len[b];
@@ -157,7 +175,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   if (n <= 0 || x >= tiles) return false;
   w.r0 = (tiles - 1 - x) * a.tile;
   const int keys = w.ctx + a.by_group(min(w.r0 + a.tile, w.rows) - 1) + 1;
-  const Cut c = cut_of(a.cut, keys);
+  const Cut c = cut_of(Splits{a.cut.tps, w.place.splits, a.cut.quantum}, keys);
   w.tree = false;
   w.slot = blockIdx.y;
   w.splits = c.n;
@@ -172,6 +190,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
 CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
   int x = a.by_hkv(blockIdx.x);
   w.hk = blockIdx.x - x * a.hkv;
+  w.place = Place{0, a.cut.most + a.own.most};
   const int shared_units = a.tiles * a.cut.most;
   w.tree = x >= shared_units;
   if (w.tree) {
@@ -688,7 +707,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);   // a NaN stays one
   const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
+  const int64_t pi = whole ? 0 : part_index(a, w.place, me.row, me.head, w.slot);
   const int64_t orow = me.row * a.hq + me.head;
   // Lanes l and l + 32 hold columns 0 - 3 and 4 - 7 of each eight of one row: they trade, so that each
   // has eight together, of every other eight.
@@ -1003,7 +1022,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void seq_attn_f32(Ar
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
   const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, me.row, me.head, w.slot);
+  const int64_t pi = whole ? 0 : part_index(a, w.place, me.row, me.head, w.slot);
   const int64_t orow = me.row * a.hq + me.head;
 #pragma unroll
   for (int u = 0; u < kGroups / kWaves; ++u) {
@@ -1037,6 +1056,7 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   const int i = a.merge0 + blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
   const int n_raw = a.n_rows[b], ctx = a.ctx_len[b];
+  const Place place = place_of(a, b);
   const int64_t row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b], row = row0 + i;
   const int n = rows_of(a, n_raw, ctx, row0);
   if (i >= n) return;
@@ -1048,11 +1068,11 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
     // The tile of this row's head decides how many keys its splits covered.
     const int rows = n * a.group, R = i * a.group + (head - a.by_group(head) * a.group);
     const int end = min(((R >> a.tile_log2) + 1) * a.tile, rows);
-    shared = parts = cut_of(a.cut, ctx + a.by_group(end - 1) + 1).n;
+    shared = parts = cut_of(Splits{a.cut.tps, place.splits, a.cut.quantum}, ctx + a.by_group(end - 1) + 1).n;
     if (parts == 1) return;                        // written whole
   }
-  const int64_t p0 = part_index(a, row, head, 0), orow = row * a.hq + head;
-  const int gap = a.cut.most - shared;             // slots that no split of the prefix has
+  const int64_t p0 = part_index(a, place, row, head, 0), orow = row * a.hq + head;
+  const int gap = kPrefix ? a.cut.most - shared : 0;   // slots that no split of the prefix has
   // kMerge parts at a time, all of whose loads are under way together. Parts that saw
   // nothing (a log-sum-exp of -inf) weigh nothing.
   float m = -INFINITY, sum = 0.f;
@@ -1096,6 +1116,44 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   store4(a, orow * D + col, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (col == 0 && a.lse) a.lse[orow] = sum == 0.f ? -INFINITY : m + logf(sum);
+}
+
+// ---------------------------------------------------------------------------
+// Places the sequences' parts one after the other, by the device's sizes, in `capacity` slots. Where
+// those exceed the host's, a sequence whose parts do not fit is written whole, in one split.
+constexpr int kPlaceThreads = 1024;  // at most
+
+__global__ __launch_bounds__(kPlaceThreads) void seq_place(Args a, int64_t capacity) {
+  __shared__ int64_t s_sum[kPlaceThreads / kWave];
+  const int threads = blockDim.x, waves = threads / kWave;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int64_t total = 0;                               // slots of the sequences before this turn's
+  for (int b0 = 0; b0 < a.batch; b0 += threads) {
+    const int b = b0 + threadIdx.x;
+    int64_t row0 = 0, need = 0;
+    int splits = 1;
+    if (b < a.batch) {
+      row0 = a.row_off[b];
+      const int ctx = a.ctx_len[b], n = rows_of(a, a.n_rows[b], ctx, row0);
+      if (n > 0) splits = slots_of(a.cut, ctx + n);
+      if (splits > 1) need = (int64_t)n * a.hq * splits;
+    }
+    int64_t sum = need;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int64_t u = __shfl_up((long long)sum, d);
+      if (lane >= d) sum += u;
+    }
+    if (lane == kWave - 1) s_sum[wave] = sum;
+    __syncthreads();
+    int64_t before = total + sum - need;
+    for (int i = 0; i < waves; ++i) {
+      if (i < wave) before += s_sum[i];
+      total += s_sum[i];
+    }
+    __syncthreads();                               // the sums are read before the next turn's
+    if (b < a.batch) a.place[b] = Place{before - row0 * a.hq * splits, before + need <= capacity ? splits : 1};
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1274,12 +1332,39 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
 // Whether a call's parts go through the workspace: a prompt's where there are several.
 bool in_parts(const Plan& p) { return p.slots() > 1; }
 
-size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int slots) {
-  const size_t parts = (size_t)rows * hq * slots;
-  return align_up(parts * d * sizeof(float), 256) + align_up(parts * sizeof(float), 256);
+// A call's workspace: places of the sequences, if it has them, and `slots` parts of d columns and a
+// log-sum-exp.
+struct Space {
+  bool placed;
+  int32_t batch, d;
+  int64_t slots;
+  size_t place_bytes() const { return placed ? align_up((size_t)batch * sizeof(Place), 256) : 0; }
+  size_t o_bytes() const { return align_up((size_t)slots * d * sizeof(float), 256); }
+  size_t bytes() const { return place_bytes() + o_bytes() + align_up((size_t)slots * sizeof(float), 256); }
+};
+
+// Workspace up to which every row has the slots of the longest. Beyond, a launch of its own places the
+// parts of each sequence by its own splits. 16 prompts of 2048 tokens beside one token on 128k, 32
+// heads of 128: 1 MB and 1010 us, even 17 GB and 1140; 8 beside four, 2.2 GB even, 1116 and 1137. One
+// prompt beside one token on 32k, 0.8 GB even, would take 133 us placed, and takes 126.
+constexpr size_t kEvenBytes = size_t(1) << 30;
+
+Space prompt_space(const Plan& p, int32_t batch, int64_t rows, int32_t hq, int32_t d, const int32_t* host_n_rows,
+                   const int32_t* host_ctx_len) {
+  const Space even{false, batch, d, in_parts(p) ? rows * hq * p.slots() : 0};
+  if (even.bytes() <= kEvenBytes) return even;
+  int64_t slots = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_rows[b];
+    const int32_t splits = n > 0 ? slots_of(p.cut, n + host_ctx_len[b]) : 1;
+    if (splits > 1) slots += n * hq * splits;
+  }
+  return Space{true, batch, d, slots};
 }
 
-void set_plan(Args& a, const Plan& p, void* ws, int64_t rows, int32_t d) {
+size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int slots) { return Space{false, 0, d, rows * hq * slots}.bytes(); }
+
+void set_plan(Args& a, const Plan& p, const Space& space, void* ws) {
   a.tile = p.tile;
   a.tile_log2 = p.tile == kNarrow ? 5 : 7;
   static_assert(kNarrow == 1 << 5 && kRows == 1 << 7, "tiles of a power of two");
@@ -1287,10 +1372,12 @@ void set_plan(Args& a, const Plan& p, void* ws, int64_t rows, int32_t d) {
   a.own_tiles = p.own_tiles;
   a.cut = p.cut;
   a.own = p.own;
-  if (!in_parts(p)) return;
-  const size_t parts = (size_t)rows * a.hq * p.slots();
-  a.part_o = static_cast<float*>(ws);
-  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(parts * d * sizeof(float), 256));
+  if (space.bytes() == 0) return;
+  char* at = static_cast<char*>(ws);
+  if (space.placed) a.place = reinterpret_cast<Place*>(at);
+  at += space.place_bytes();
+  a.part_o = reinterpret_cast<float*>(at);
+  a.part_lse = reinterpret_cast<float*>(at + space.o_bytes());
 }
 
 template <bool kPrefix>
@@ -1349,7 +1436,7 @@ extern "C" size_t cure_prompt_attn_workspace_size(int32_t batch, int64_t rows, i
   size_t need = 0;                                 // of whichever type needs more
   for (const int32_t dtype : {CURE_F32, CURE_BF16}) {
     const Plan p = prompt_plan(dtype, batch, hq, hkv, d, host_n_rows, host_ctx_len, kv_split);
-    if (in_parts(p)) need = std::max(need, part_bytes(rows, hq, d, p.slots()));
+    need = std::max(need, prompt_space(p, batch, rows, hq, d, host_n_rows, host_ctx_len).bytes());
   }
   return need;
 }
@@ -1376,7 +1463,8 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   }
   if (longest == 0) return CURE_OK;
   const Plan p = prompt_plan(dtype, batch, hq, hkv, d, host_n_rows, host_ctx_len, kv_split);
-  const size_t need = in_parts(p) ? part_bytes(rows, hq, d, p.slots()) : 0;
+  const Space space = prompt_space(p, batch, rows, hq, d, host_n_rows, host_ctx_len);
+  const size_t need = space.bytes();
   if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
   if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
   if ((int64_t)p.tiles * hkv * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
@@ -1400,8 +1488,13 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   a.n_rows = n_rows;
   a.kv_off = kv_off;
   a.ctx_len = ctx_len;
-  set_plan(a, p, workspace, rows, d);
+  set_plan(a, p, space, workspace);
   hipStream_t st = as_stream(stream);
+  if (space.placed) {
+    const int threads = std::min((batch + kWave - 1) / kWave * kWave, kPlaceThreads);
+    hipLaunchKernelGGL(seq_place, dim3(1), dim3((unsigned)threads), 0, st, a, space.slots);
+    if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
+  }
   launch_attn<false>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.cut.most, (unsigned)batch), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
   if (in_parts(p)) launch_merge<false>(a, d, st);
@@ -1474,7 +1567,7 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   a.tree_status = tree_status;
   a.prefix_off = prefix_off;
   a.prefix_len = prefix_len;
-  set_plan(a, p, workspace, (int64_t)batch * n_max, d);
+  set_plan(a, p, Space{false, batch, d, (int64_t)batch * n_max * hq * p.slots()}, workspace);
   hipStream_t st = as_stream(stream);
   launch_attn<true>(a, dtype, d, dim3((unsigned)units), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
