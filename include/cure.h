@@ -512,7 +512,8 @@ cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* 
  * Supports a scale as cure_prompt_attn, batch <= 1024 and batch * n_max * hq/hkv below
  * 2^31 - 4096 (where prefix_len > 0), and what cure_tree_attn supports. Alignment as for
  * cure_prompt_attn. workspace: cure_prefix_attn_workspace_size(...) bytes for the same
- * arguments.
+ * arguments; as there beyond 1 GB, where a sequence with more nodes or own rows on the device
+ * has its own rows in one split.
  */
 size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int32_t hkv, int32_t d,
                                        int32_t n_max, int32_t prefix_len,

@@ -63,10 +63,12 @@ __host__ __device__ inline int32_t slots_of(const Splits& s, int64_t keys) {
 }
 
 // Where each sequence's parts lie, in calls whose workspace would be large with one number of
-// slots for all rows: row r, head h, split j at first + (r * hq + h) * splits + j.
+// slots for all rows. A prompt: row r, head h, split j at first + (r * hq + h) * splits + j. Own rows
+// behind a prefix: the first split beside the prefix's, split j from 1 on at first + (r * hq + h) *
+// (splits - 1) + j - 1.
 struct Place {
   int64_t first;
-  int32_t splits;                    // of the sequence's longest rows; 1: written whole
+  int32_t splits;                    // of the sequence's longest rows; 1: a prompt is written whole
 };
 
 struct Args {
@@ -92,16 +94,29 @@ struct Args {
   int32_t tile, tile_log2;           // query rows of a tile
   int32_t tiles, own_tiles;          // prefix: tiles of all nodes, and of a sequence's
   Splits cut, own;                   // of a prompt's keys or the prefix, and of own rows
-  float* part_o;                     // [row][hq][slots][d], slots = cut.most + own.most; or by place
+  int32_t slots;                     // of a row: the splits of a prompt, or the prefix's and then the own rows'
+  float* part_o;                     // [row][hq][slots][d], or by place
   float* part_lse;                   // [row][hq][slots]
   Place* place;                      // [batch], or null
   int32_t merge0;                    // first token of a merge launch
 };
 
 // The place of sequence b's parts.
-CURE_DEV Place place_of(const Args& a, int b) { return a.place ? a.place[b] : Place{0, a.cut.most + a.own.most}; }
-CURE_DEV int64_t part_index(const Args& a, const Place& p, int64_t row, int head, int slot) {
-  return p.first + (row * a.hq + head) * p.splits + slot;
+template <bool kPrefix>
+CURE_DEV Place place_of(const Args& a, int b) {
+  return a.place ? a.place[b] : Place{0, kPrefix ? a.own.most : a.cut.most};
+}
+// The part of a row and head for `slot`: rows of a prefix have a.slots together, and the others by place.
+struct Parts {
+  int64_t near, far;
+  int32_t together;
+  CURE_DEV int64_t operator()(int slot) const { return (slot < together ? near : far) + slot; }
+};
+template <bool kPrefix>
+CURE_DEV Parts parts_of(const Args& a, const Place& p, int64_t row, int head) {
+  const int64_t i = row * a.hq + head;
+  if (!kPrefix) return Parts{p.first + i * p.splits, 0, INT32_MAX};
+  return Parts{i * a.slots, p.first + i * (p.splits - 1) - a.slots, a.slots};
 }
 
 // The splits of `keys` (at least one) keys: n of `per` tokens, the last one shorter (a single
@@ -133,7 +148,7 @@ struct Work {
   int64_t row0;                      // first row of the sequence (not for a prefix)
   int ctx;
   int b;
-  Place place;
+  Place place;                       // of a prompt
   bool tree;                         // a sequence's own rows, in cure_prefix_attn
 };
 
@@ -162,7 +177,7 @@ CURE_DEV Shared shared_of(Nothing&, Nothing&) { return Shared{}; }
 // out in turn over the sequences, 16 prompts of 1 to 2048 tokens took 399 us instead of 253.
 CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   const int b = blockIdx.z, x = a.by_hkv(blockIdx.x);
-  w.place = place_of(a, b);
+  w.place = place_of<false>(a, b);
   w.hk = blockIdx.x - x * a.hkv;
   const int n_raw = a.n_rows[b];
   w.ctx = a.ctx_len[b];
@@ -190,7 +205,7 @@ CURE_DEV bool locate_prompt(const Args& a, Work& w) {
 CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
   int x = a.by_hkv(blockIdx.x);
   w.hk = blockIdx.x - x * a.hkv;
-  w.place = Place{0, a.cut.most + a.own.most};
+  w.b = 0;
   const int shared_units = a.tiles * a.cut.most;
   w.tree = x >= shared_units;
   if (w.tree) {
@@ -198,6 +213,7 @@ CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
     const int tile = x % a.own_tiles;
     x /= a.own_tiles;
     const int b = w.b = x % a.batch, s = x / a.batch;
+    const int own_most = place_of<true>(a, b).splits;
     const int n_raw = a.n_rows[b];
     w.ctx = a.ctx_len[b];
     w.key0 = a.kv_off[b];
@@ -212,7 +228,7 @@ CURE_DEV bool locate_prefix(const Args& a, Work& w, const Shared& sh) {
       return false;
     }
     const int keys = w.ctx + n;
-    const Cut c = cut_of(a.own, keys);
+    const Cut c = cut_of(Splits{a.own.tps, own_most, a.own.quantum}, keys);
     w.slot = a.cut.most + s;
     w.splits = c.n;
     w.begin = s * c.per;
@@ -305,6 +321,14 @@ CURE_DEV Row row_of(const Args& a, const Work& w, const Shared& sh, int R) {
   r.row = (int64_t)lo * a.n_max + (t - sh.first[lo]);
   r.last = w.ctx - 1;
   return r;
+}
+
+// The part of a row that this workgroup computes. Own rows read their place again where they need it.
+template <bool kPrefix>
+CURE_DEV int64_t part_at(const Args& a, const Work& w, const Row& me) {
+  if (!kPrefix) return parts_of<false>(a, w.place, me.row, me.head)(w.slot);
+  if (w.slot < a.slots) return (me.row * a.hq + me.head) * a.slots + w.slot;
+  return parts_of<true>(a, a.place[w.b], me.row, me.head)(w.slot);
 }
 
 // Whether a row sees token t of its split: one up to `last`, or in a tree a node on its path.
@@ -707,7 +731,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn(Args a) {
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);   // a NaN stays one
   const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, w.place, me.row, me.head, w.slot);
+  const int64_t pi = whole ? 0 : part_at<kPrefix>(a, w, me);
   const int64_t orow = me.row * a.hq + me.head;
   // Lanes l and l + 32 hold columns 0 - 3 and 4 - 7 of each eight of one row: they trade, so that each
   // has eight together, of every other eight.
@@ -1022,7 +1046,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void seq_attn_f32(Ar
   const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
   const float lse = lt == 0.f ? -INFINITY : (m + log2f(lt)) * kLn2;
   const bool whole = w.splits == 1 && !kPrefix;
-  const int64_t pi = whole ? 0 : part_index(a, w.place, me.row, me.head, w.slot);
+  const int64_t pi = whole ? 0 : part_at<kPrefix>(a, w, me);
   const int64_t orow = me.row * a.hq + me.head;
 #pragma unroll
   for (int u = 0; u < kGroups / kWaves; ++u) {
@@ -1056,14 +1080,14 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   const int i = a.merge0 + blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
   const int n_raw = a.n_rows[b], ctx = a.ctx_len[b];
-  const Place place = place_of(a, b);
+  const Place place = place_of<kPrefix>(a, b);
   const int64_t row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b], row = row0 + i;
   const int n = rows_of(a, n_raw, ctx, row0);
   if (i >= n) return;
   int shared, parts;                               // parts from slot 0 on, and in all
   if (kPrefix) {
     shared = cut_of(a.cut, a.prefix_len).n;
-    parts = shared + cut_of(a.own, ctx + n).n;
+    parts = shared + cut_of(Splits{a.own.tps, place.splits, a.own.quantum}, ctx + n).n;
   } else {
     // The tile of this row's head decides how many keys its splits covered.
     const int rows = n * a.group, R = i * a.group + (head - a.by_group(head) * a.group);
@@ -1071,7 +1095,8 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
     shared = parts = cut_of(Splits{a.cut.tps, place.splits, a.cut.quantum}, ctx + a.by_group(end - 1) + 1).n;
     if (parts == 1) return;                        // written whole
   }
-  const int64_t p0 = part_index(a, place, row, head, 0), orow = row * a.hq + head;
+  const Parts part = parts_of<kPrefix>(a, place, row, head);
+  const int64_t orow = row * a.hq + head;
   const int gap = kPrefix ? a.cut.most - shared : 0;   // slots that no split of the prefix has
   // kMerge parts at a time, all of whose loads are under way together. Parts that saw
   // nothing (a log-sum-exp of -inf) weigh nothing.
@@ -1085,7 +1110,7 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
 #pragma unroll
     for (int u = 0; u < kMerge; ++u) {
       const bool ok = s0 + u < parts;
-      const int64_t at = p0 + s0 + u + (s0 + u < shared ? 0 : gap);
+      const int64_t at = part(s0 + u + (s0 + u < shared ? 0 : gap));
       v[u] = ok ? *reinterpret_cast<const float4*>(a.part_o + at * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
       lse[u] = ok ? a.part_lse[at] : -INFINITY;
     }
@@ -1119,11 +1144,12 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// Places the sequences' parts one after the other, by the device's sizes, in `capacity` slots. Where
-// those exceed the host's, a sequence whose parts do not fit is written whole, in one split.
+// Places the sequences' parts one after the other from `begin` on, by the device's sizes, in `capacity`
+// slots. Where those exceed the host's, a sequence whose parts do not fit has one split.
 constexpr int kPlaceThreads = 1024;  // at most
 
-__global__ __launch_bounds__(kPlaceThreads) void seq_place(Args a, int64_t capacity) {
+template <bool kPrefix>
+__global__ __launch_bounds__(kPlaceThreads) void seq_place(Args a, int64_t begin, int64_t capacity) {
   __shared__ int64_t s_sum[kPlaceThreads / kWave];
   const int threads = blockDim.x, waves = threads / kWave;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -1131,12 +1157,13 @@ __global__ __launch_bounds__(kPlaceThreads) void seq_place(Args a, int64_t capac
   for (int b0 = 0; b0 < a.batch; b0 += threads) {
     const int b = b0 + threadIdx.x;
     int64_t row0 = 0, need = 0;
-    int splits = 1;
+    int splits = 1, stride = 0;
     if (b < a.batch) {
-      row0 = a.row_off[b];
+      row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b];
       const int ctx = a.ctx_len[b], n = rows_of(a, a.n_rows[b], ctx, row0);
-      if (n > 0) splits = slots_of(a.cut, ctx + n);
-      if (splits > 1) need = (int64_t)n * a.hq * splits;
+      if (n > 0) splits = slots_of(kPrefix ? a.own : a.cut, ctx + n);
+      stride = kPrefix ? splits - 1 : splits;
+      if (splits > 1) need = (int64_t)n * a.hq * stride;
     }
     int64_t sum = need;
 #pragma unroll
@@ -1152,7 +1179,7 @@ __global__ __launch_bounds__(kPlaceThreads) void seq_place(Args a, int64_t capac
       total += s_sum[i];
     }
     __syncthreads();                               // the sums are read before the next turn's
-    if (b < a.batch) a.place[b] = Place{before - row0 * a.hq * splits, before + need <= capacity ? splits : 1};
+    if (b < a.batch) a.place[b] = Place{begin + before - row0 * a.hq * stride, before + need <= capacity ? splits : 1};
   }
 }
 
@@ -1333,11 +1360,11 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
 bool in_parts(const Plan& p) { return p.slots() > 1; }
 
 // A call's workspace: places of the sequences, if it has them, and `slots` parts of d columns and a
-// log-sum-exp.
+// log-sum-exp, of which the first `even` are the same for every row.
 struct Space {
   bool placed;
   int32_t batch, d;
-  int64_t slots;
+  int64_t slots, even;
   size_t place_bytes() const { return placed ? align_up((size_t)batch * sizeof(Place), 256) : 0; }
   size_t o_bytes() const { return align_up((size_t)slots * d * sizeof(float), 256); }
   size_t bytes() const { return place_bytes() + o_bytes() + align_up((size_t)slots * sizeof(float), 256); }
@@ -1351,7 +1378,8 @@ constexpr size_t kEvenBytes = size_t(1) << 30;
 
 Space prompt_space(const Plan& p, int32_t batch, int64_t rows, int32_t hq, int32_t d, const int32_t* host_n_rows,
                    const int32_t* host_ctx_len) {
-  const Space even{false, batch, d, in_parts(p) ? rows * hq * p.slots() : 0};
+  const int64_t every = in_parts(p) ? rows * hq * p.slots() : 0;
+  const Space even{false, batch, d, every, every};
   if (even.bytes() <= kEvenBytes) return even;
   int64_t slots = 0;
   for (int b = 0; b < batch; ++b) {
@@ -1359,10 +1387,24 @@ Space prompt_space(const Plan& p, int32_t batch, int64_t rows, int32_t hq, int32
     const int32_t splits = n > 0 ? slots_of(p.cut, n + host_ctx_len[b]) : 1;
     if (splits > 1) slots += n * hq * splits;
   }
-  return Space{true, batch, d, slots};
+  return Space{true, batch, d, slots, 0};
 }
 
-size_t part_bytes(int64_t rows, int32_t hq, int32_t d, int slots) { return Space{false, 0, d, rows * hq * slots}.bytes(); }
+// As for prompts. 256 trees of 48 nodes behind 200 shared tokens, one of them on 131072 of its own and the
+// others on 100: 0.4 GB and 697 us, even 6.7 GB and 780; 64 of them 0.1 GB and 350 us, 1.7 GB and 374.
+Space prefix_space(const Plan& p, int32_t batch, int32_t hq, int32_t d, int32_t n_max, const int32_t* host_ctx_len,
+                   const int32_t* host_n_nodes) {
+  const int64_t rows = (int64_t)batch * n_max * hq;
+  const Space even{false, batch, d, rows * p.slots(), rows * p.slots()};
+  if (even.bytes() <= kEvenBytes) return even;
+  int64_t slots = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = host_n_nodes[b];
+    if (n > 0) slots += n * hq * (slots_of(p.own, n + host_ctx_len[b]) - 1);
+  }
+  const int64_t fixed = rows * (p.cut.most + 1);
+  return Space{true, batch, d, fixed + slots, fixed};
+}
 
 void set_plan(Args& a, const Plan& p, const Space& space, void* ws) {
   a.tile = p.tile;
@@ -1372,12 +1414,20 @@ void set_plan(Args& a, const Plan& p, const Space& space, void* ws) {
   a.own_tiles = p.own_tiles;
   a.cut = p.cut;
   a.own = p.own;
+  a.slots = space.placed ? p.cut.most + 1 : p.slots();
   if (space.bytes() == 0) return;
   char* at = static_cast<char*>(ws);
   if (space.placed) a.place = reinterpret_cast<Place*>(at);
   at += space.place_bytes();
   a.part_o = reinterpret_cast<float*>(at);
   a.part_lse = reinterpret_cast<float*>(at + space.o_bytes());
+}
+
+template <bool kPrefix>
+hipError_t launch_place(const Args& a, const Space& space, hipStream_t st) {
+  const int threads = std::min((a.batch + kWave - 1) / kWave * kWave, kPlaceThreads);
+  hipLaunchKernelGGL(seq_place<kPrefix>, dim3(1), dim3((unsigned)threads), 0, st, a, space.even, space.slots - space.even);
+  return hipGetLastError();
 }
 
 template <bool kPrefix>
@@ -1490,11 +1540,7 @@ extern "C" cure_status cure_prompt_attn(const void* q, const void* k, const void
   a.ctx_len = ctx_len;
   set_plan(a, p, space, workspace);
   hipStream_t st = as_stream(stream);
-  if (space.placed) {
-    const int threads = std::min((batch + kWave - 1) / kWave * kWave, kPlaceThreads);
-    hipLaunchKernelGGL(seq_place, dim3(1), dim3((unsigned)threads), 0, st, a, space.slots);
-    if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
-  }
+  if (space.placed && launch_place<false>(a, space, st) != hipSuccess) return CURE_ERR_HIP;
   launch_attn<false>(a, dtype, d, dim3((unsigned)(hkv * p.tiles), (unsigned)p.cut.most, (unsigned)batch), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
   if (in_parts(p)) launch_merge<false>(a, d, st);
@@ -1508,11 +1554,12 @@ extern "C" size_t cure_prefix_attn_workspace_size(int32_t batch, int32_t hq, int
       !host_n_nodes)
     return 0;
   if (prefix_len == 0) return cure_tree_attn_workspace_size(batch, hq, hkv, d, n_max, host_ctx_len, host_n_nodes, 0);
-  int slots = 0;                                   // of whichever type takes more
-  for (const int32_t dtype : {CURE_F32, CURE_BF16})
-    slots = std::max(slots, prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes,
-                                        kv_split).slots());
-  return part_bytes((int64_t)batch * n_max, hq, d, slots);
+  size_t need = 0;                                 // of whichever type needs more
+  for (const int32_t dtype : {CURE_F32, CURE_BF16}) {
+    const Plan p = prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
+    need = std::max(need, prefix_space(p, batch, hq, d, n_max, host_ctx_len, host_n_nodes).bytes());
+  }
+  return need;
 }
 
 extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* o, float* lse,
@@ -1540,7 +1587,8 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
     if (host_ctx_len[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
   if ((int64_t)batch * n_max * (hq / hkv) > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
   const Plan p = prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
-  if (!workspace || workspace_bytes < part_bytes((int64_t)batch * n_max, hq, d, p.slots())) return CURE_ERR_WORKSPACE;
+  const Space space = prefix_space(p, batch, hq, d, n_max, host_ctx_len, host_n_nodes);
+  if (!workspace || workspace_bytes < space.bytes()) return CURE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
   const int64_t units = ((int64_t)p.tiles * p.cut.most + (int64_t)p.own_tiles * batch * p.own.most) * hkv;
   if (units * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
@@ -1567,8 +1615,9 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   a.tree_status = tree_status;
   a.prefix_off = prefix_off;
   a.prefix_len = prefix_len;
-  set_plan(a, p, Space{false, batch, d, (int64_t)batch * n_max * hq * p.slots()}, workspace);
+  set_plan(a, p, space, workspace);
   hipStream_t st = as_stream(stream);
+  if (space.placed && launch_place<true>(a, space, st) != hipSuccess) return CURE_ERR_HIP;
   launch_attn<true>(a, dtype, d, dim3((unsigned)units), st);
   if (hipGetLastError() != hipSuccess) return CURE_ERR_HIP;
   launch_merge<true>(a, d, st);
