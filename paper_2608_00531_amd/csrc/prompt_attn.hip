@@ -1376,16 +1376,22 @@ struct Space {
 // prompt beside one token on 32k, 0.8 GB even, would take 133 us placed, and takes 126.
 constexpr size_t kEvenBytes = size_t(1) << 30;
 
+// rows * heads * slots, or a number that no workspace holds and whose bytes do not pass 64 bits.
+constexpr int64_t kMostSlots = int64_t(1) << 46;
+int64_t slots_in_all(int64_t rows, int64_t hq, int64_t slots) {
+  return (double)rows * (double)hq * (double)slots < (double)kMostSlots ? rows * hq * slots : kMostSlots;
+}
+
 Space prompt_space(const Plan& p, int32_t batch, int64_t rows, int32_t hq, int32_t d, const int32_t* host_n_rows,
                    const int32_t* host_ctx_len) {
-  const int64_t every = in_parts(p) ? rows * hq * p.slots() : 0;
+  const int64_t every = in_parts(p) ? slots_in_all(rows, hq, p.slots()) : 0;
   const Space even{false, batch, d, every, every};
   if (even.bytes() <= kEvenBytes) return even;
   int64_t slots = 0;
   for (int b = 0; b < batch; ++b) {
     const int64_t n = host_n_rows[b];
     const int32_t splits = n > 0 ? slots_of(p.cut, n + host_ctx_len[b]) : 1;
-    if (splits > 1) slots += n * hq * splits;
+    if (splits > 1) slots = std::min(slots + slots_in_all(n, hq, splits), kMostSlots);
   }
   return Space{true, batch, d, slots, 0};
 }
@@ -1394,15 +1400,15 @@ Space prompt_space(const Plan& p, int32_t batch, int64_t rows, int32_t hq, int32
 // others on 100: 0.4 GB and 697 us, even 6.7 GB and 780; 64 of them 0.1 GB and 350 us, 1.7 GB and 374.
 Space prefix_space(const Plan& p, int32_t batch, int32_t hq, int32_t d, int32_t n_max, const int32_t* host_ctx_len,
                    const int32_t* host_n_nodes) {
-  const int64_t rows = (int64_t)batch * n_max * hq;
-  const Space even{false, batch, d, rows * p.slots(), rows * p.slots()};
+  const int64_t rows = (int64_t)batch * n_max, every = slots_in_all(rows, hq, p.slots());
+  const Space even{false, batch, d, every, every};
   if (even.bytes() <= kEvenBytes) return even;
   int64_t slots = 0;
   for (int b = 0; b < batch; ++b) {
     const int64_t n = host_n_nodes[b];
-    if (n > 0) slots += n * hq * (slots_of(p.own, n + host_ctx_len[b]) - 1);
+    if (n > 0) slots = std::min(slots + slots_in_all(n, hq, slots_of(p.own, n + host_ctx_len[b]) - 1), kMostSlots);
   }
-  const int64_t fixed = rows * (p.cut.most + 1);
+  const int64_t fixed = slots_in_all(rows, hq, p.cut.most + 1);
   return Space{true, batch, d, fixed + slots, fixed};
 }
 
