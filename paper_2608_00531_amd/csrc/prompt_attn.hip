@@ -1072,7 +1072,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void seq_attn_f32(Ar
 // heads of 128, 9.3 us).
 constexpr int kMerge = 8;
 
-template <int D, bool kPrefix>
+template <int D, bool kPrefix, bool kPlaced>
 __global__ __launch_bounds__(256) void seq_merge(Args a) {
   constexpr int kLanes = D / 4;
   const int head = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
@@ -1080,7 +1080,7 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
   const int i = a.merge0 + blockIdx.y, b = blockIdx.z;
   if (head >= a.hq) return;
   const int n_raw = a.n_rows[b], ctx = a.ctx_len[b];
-  const Place place = place_of<kPrefix>(a, b);
+  const Place place = kPlaced ? a.place[b] : Place{0, kPrefix ? a.own.most : a.cut.most};
   const int64_t row0 = kPrefix ? (int64_t)b * a.n_max : a.row_off[b], row = row0 + i;
   const int n = rows_of(a, n_raw, ctx, row0);
   if (i >= n) return;
@@ -1110,7 +1110,8 @@ __global__ __launch_bounds__(256) void seq_merge(Args a) {
 #pragma unroll
     for (int u = 0; u < kMerge; ++u) {
       const bool ok = s0 + u < parts;
-      const int64_t at = part(s0 + u + (s0 + u < shared ? 0 : gap));
+      const int slot = s0 + u + (s0 + u < shared ? 0 : gap);
+      const int64_t at = kPlaced ? part(slot) : part.near + slot;
       v[u] = ok ? *reinterpret_cast<const float4*>(a.part_o + at * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
       lse[u] = ok ? a.part_lse[at] : -INFINITY;
     }
@@ -1459,8 +1460,10 @@ void launch_merge(Args a, int32_t d, hipStream_t st) {
     a.merge0 = (int32_t)t;
     const dim3 grid((unsigned)((a.hq + heads - 1) / heads), (unsigned)std::min<int64_t>(a.n_max - t, kTokens),
                     (unsigned)a.batch);
-    if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((seq_merge<64, kPrefix>), grid, dim3(256), 0, st, a);
+    if (a.place && d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix, true>), grid, dim3(256), 0, st, a);
+    else if (a.place) hipLaunchKernelGGL((seq_merge<64, kPrefix, true>), grid, dim3(256), 0, st, a);
+    else if (d == 128) hipLaunchKernelGGL((seq_merge<128, kPrefix, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((seq_merge<64, kPrefix, false>), grid, dim3(256), 0, st, a);
   }
 }
 
