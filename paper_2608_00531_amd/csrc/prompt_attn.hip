@@ -379,9 +379,10 @@ CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, f
 // 128 rows share a tile of keys, so that 2 workgroups of 4 waves fit a CU's registers (198 of
 // 256 at head dim 128; 235 with a prefix, where the masks of the steps seen in part also keep 82
 // scalar registers in lanes of a vector one, outside the main loop) and each key read from LDS serves 32 rows. Large prompts are bound by the
-// matrix unit and the power it draws: a prompt of 8192 tokens, 32 heads of 128, takes 500 us (1.10
-// PFLOP/s of the 1.20 that a large product reaches), the unit busy 58 % of the cycles at 1.75 GHz;
-// its instructions alone take 386 us. 16 prompts of 1 to 2048 tokens take 240 us, 0.33 GB of
+// matrix unit and the power it draws: a prompt of 8192 tokens, 32 heads of 128, took 488, 515 and
+// 523 us on three cards (1.05 - 1.13 PFLOP/s of the 1.20 that a large product reaches), the unit busy
+// 57 % of the cycles at 1.6 - 1.75 GHz; its instructions alone take 386 us. 16 prompts of 1 to 2048
+// tokens take 236 us, 0.33 GB of
 // queries and outputs among them that move at the workgroups' starts and ends. Single tokens are
 // bound by the cache's way: 8 on 4k - 32k tokens 107 us, 5.9 TB/s of the 6.97 that a read reaches.
 // Measured and slower: 64 rows per wave with one wave to a SIMD (2.4 times), 8 waves per workgroup
