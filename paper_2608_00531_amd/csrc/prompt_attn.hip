@@ -177,13 +177,15 @@ CURE_DEV Shared shared_of(Nothing&, Nothing&) { return Shared{}; }
 // out in turn over the sequences, 16 prompts of 1 to 2048 tokens took 399 us instead of 253.
 CURE_DEV bool locate_prompt(const Args& a, Work& w) {
   const int b = blockIdx.z, x = a.by_hkv(blockIdx.x);
-  w.place = place_of<false>(a, b);
   w.hk = blockIdx.x - x * a.hkv;
   const int n_raw = a.n_rows[b];
   w.ctx = a.ctx_len[b];
   w.row0 = a.row_off[b];
   w.key0 = a.kv_off[b];
   asm volatile("" : : "s"(n_raw), "s"(w.ctx), "s"(w.row0), "s"(w.key0));
+  // A launch of the longest sequence's tiles is mostly workgroups without work: they end here.
+  if (x * a.tile >= min(n_raw, a.n_max) * a.group) return false;
+  w.place = place_of<false>(a, b);
   const int n = rows_of(a, n_raw, w.ctx, w.row0);
   w.rows = n * a.group;
   const int tiles = (w.rows + a.tile - 1) >> a.tile_log2;
@@ -376,7 +378,7 @@ CURE_DEV void store4(const Args& a, int64_t idx, float x0, float x1, float x2, f
 // do not wait for each other, so the matrix instructions and the softmax's vector
 // instructions of one wave interleave.
 //
-// 128 rows share a tile of keys, so that 2 workgroups of 4 waves fit a CU's registers (198 of
+// 128 rows share a tile of keys, so that 2 workgroups of 4 waves fit a CU's registers (200 of
 // 256 at head dim 128; 235 with a prefix, where the masks of the steps seen in part also keep 82
 // scalar registers in lanes of a vector one, outside the main loop) and each key read from LDS serves 32 rows. Large prompts are bound by the
 // matrix unit and the power it draws: a prompt of 8192 tokens, 32 heads of 128, took 488, 515 and
