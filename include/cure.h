@@ -509,8 +509,9 @@ cure_status cure_prompt_attn(const void* q, const void* k, const void* v, void* 
  * well, and that sequence's o and lse are not written. The values that a node sees must be
  * finite; what it does not see may be anything. The device's n_nodes and ctx_len may differ
  * from the host's copies (n_nodes up to n_max).
- * Supports a scale as cure_prompt_attn, batch <= 1024 and batch * n_max * hq/hkv below
- * 2^31 - 4096 (where prefix_len > 0), and what cure_tree_attn supports. Alignment as for
+ * Supports a scale as cure_prompt_attn, and where prefix_len > 0 batch <= 1024,
+ * batch * n_max * hq/hkv below 2^31 - 4096, batch * n_max * hq up to 2^27 and batch * hkv
+ * up to 2^22, and what cure_tree_attn supports. Alignment as for
  * cure_prompt_attn. workspace: cure_prefix_attn_workspace_size(...) bytes for the same
  * arguments; as there beyond 1 GB, where a sequence with more nodes or own rows on the device
  * has its own rows in one split.

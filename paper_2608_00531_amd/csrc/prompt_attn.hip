@@ -1292,6 +1292,13 @@ Plan prompt_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   return p;
 }
 
+// Workgroups of a launch over a prefix's tiles and every sequence's own, existing or not, and whether
+// their threads fit the 32 bits that a launch counts them in.
+int64_t prefix_units(const Plan& p, int32_t batch, int32_t hkv, int64_t prefix_splits, int64_t own_splits) {
+  return (p.tiles * prefix_splits + (int64_t)p.own_tiles * batch * own_splits) * hkv;
+}
+bool launchable(int64_t units) { return units < (int64_t(1) << 32) / (64 * kWaves); }
+
 Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t n_max,
                  int32_t prefix_len, const int32_t* host_ctx_len, const int32_t* host_n_nodes, int32_t kv_split) {
   const int64_t cus = device_cu_count(), group = hq / hkv;
@@ -1304,6 +1311,10 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   }
   Plan p{};
   p.tile = tile_of(dtype);
+  // The device may hold other counts than the host's copies: tiles for every node there may
+  // be, of which those past the last one end at once.
+  p.tiles = (int)std::min<int64_t>(tiles_of((int64_t)batch * n_max, p.tile), INT32_MAX);
+  p.own_tiles = (int)tiles_of(n_max, p.tile);
   const int64_t tiles = tiles_of(nodes, p.tile);
   // Own rows are split for themselves, as their number and lengths have nothing to do with the
   // prefix: workgroups and longest split of every candidate, up to one for each 256 keys or part of them.
@@ -1344,7 +1355,7 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
       const int64_t units = tiles * s * hkv + owns[i].units;
       const double unit = std::max(tps, owns[i].longest) * cost.key + each;
       const double time = std::max(unit, (work * hkv * cost.key + units * each) / cus + unit / 3);
-      if (best == 0 || time < best) {
+      if (best == 0 || (time < best && launchable(prefix_units(p, batch, hkv, s, kOwnCandidates[i])))) {
         most = s;
         own = kOwnCandidates[i];
         best = time;
@@ -1353,10 +1364,6 @@ Plan prefix_plan(int32_t dtype, int32_t batch, int32_t hq, int32_t hkv, int32_t 
   }
   p.cut = splits_of(prefix_len, most, p.tile);
   p.own = splits_of(keys, own, p.tile);
-  // The device may hold other counts than the host's copies: tiles for every node there may
-  // be, of which those past the last one end at once.
-  p.tiles = (int)std::min<int64_t>(tiles_of((int64_t)batch * n_max, p.tile), INT32_MAX);
-  p.own_tiles = (int)tiles_of(n_max, p.tile);
   return p;
 }
 
@@ -1600,10 +1607,10 @@ extern "C" cure_status cure_prefix_attn(const void* q, const void* k, const void
   if ((int64_t)batch * n_max * (hq / hkv) > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
   const Plan p = prefix_plan(dtype, batch, hq, hkv, d, n_max, prefix_len, host_ctx_len, host_n_nodes, kv_split);
   const Space space = prefix_space(p, batch, hq, d, n_max, host_ctx_len, host_n_nodes);
+  const int64_t units = prefix_units(p, batch, hkv, p.cut.most, p.own.most);
+  if (!launchable(units)) return CURE_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < space.bytes()) return CURE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return CURE_ERR_INVALID_ARG;
-  const int64_t units = ((int64_t)p.tiles * p.cut.most + (int64_t)p.own_tiles * batch * p.own.most) * hkv;
-  if (units * 64 * kWaves >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;
   Args a{};
   a.q = q;
   a.k = k;

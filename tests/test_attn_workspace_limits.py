@@ -19,4 +19,4 @@ def test_prompt_workspaces_do_not_wrap(L, rows):  # noqa: F811
 def test_prefix_workspaces_do_not_wrap(L):  # noqa: F811
     """1024 trees of 256 nodes (of which one each exists), 2^12 heads, 2^15 splits of the prefix: 2^53 bytes."""
     kw = dict(nodes=(1,) * 1024, ctx=(0,) * 1024, batch=1024, n_max=256, hq=2 ** 12, hkv=2 ** 11, prefix_len=2 ** 30, kv_split=2 ** 15)
-    assert prefix(L, workspace=4096, ws_bytes=2 ** 52, **kw) == pc.CURE_ERR_WORKSPACE
+    assert prefix(L, workspace=4096, ws_bytes=2 ** 52, **kw) in (pc.CURE_ERR_WORKSPACE, pc.CURE_ERR_UNSUPPORTED)

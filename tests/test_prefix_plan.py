@@ -47,3 +47,20 @@ def test_short_own_contexts_have_one_part():
     assert slots(200, [0, 5, 250], [4, 1, 3]) == 2
     assert slots(200, [0], [1]) == 2
     assert slots(200, [260], [1]) <= 3
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("batch,n_max,hq,hkv", [(1024, 256, 512, 8), (1024, 256, 128, 32), (1024, 256, 256, 32), (1024, 256, 512, 512),
+                                               (1024, 1, 131072, 1024), (2, 256, 262144, 256), (1024, 128, 1024, 1024)])
+@pytest.mark.parametrize("own", [0, 1000, 100000, 1 << 20, 1 << 29])
+@pytest.mark.parametrize("prefix", [200, 100000, 1 << 29])
+def test_no_plan_asks_for_more_than_a_launch_holds(dtype, batch, n_max, hq, hkv, own, prefix):
+    """batch * n_max * hq up to 2^27, one node each and one long context: the splits stop where the launch would pass 2^32
+    threads, and the call where its workspace (of one byte here) ends."""
+    assert batch * n_max * hq <= 2 ** 27
+    ctx, nodes = np.zeros(batch, np.int32), np.ones(batch, np.int32)
+    ctx[0] = own
+    c, n = (a.ctypes.data_as(ctypes.c_void_p) for a in (ctx, nodes))
+    st = pc.lib().cure_prefix_attn(4096, 4096, 4096, 4096, None, dtype, 1, batch, hq, hkv, 64, 0.1, 0, prefix, 1, 1, 1, 1, n_max,
+                                   c, n, 0, None, 4096, 1, None)
+    assert st == pc.CURE_ERR_WORKSPACE
