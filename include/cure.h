@@ -472,7 +472,7 @@ cure_status cure_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
  * The values that a row sees must be finite; keys and values after it (later
  * tokens, and whatever the cache holds behind the sequence) may be anything.
  * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite,
- * batch <= 65535. o may be q where their types are one.
+ * batch <= 65535, n_rows * hq up to 2^28. o may be q where their types are one.
  * kv_split: 0 = automatic, else the number of splits of the longest context (fewer where
  * that has not as many steps of keys).
  * workspace: cure_prompt_attn_workspace_size(...) bytes for the same arguments,
