@@ -24,6 +24,12 @@
  *                   tokens, packed without padding: what fills the context
  *   cure_prefix_attn  cure_tree_attn for sequences that share a prefix, whose
  *                   keys and values are read once for all of them
+ *   cure_kv_pack    committed cache rows made blocks of 64 tokens in 8 bits, with a
+ *                   scale for each block and head; cure_kv_unpack makes rows again
+ *   cure_packed_attn  attention of trees, single tokens or chunks of prompts over a
+ *                   packed context, the rows behind it and themselves
+ *   cure_sample     one token drawn for each logits row, with temperature, top-k,
+ *                   top-p and min-p, from given uniform numbers
  *   cure_margins_noalloc  cure_margins for callers that cannot allocate: its
  *                   scratch is a fixed array inside the library
  *   cure_read_ceiling  not a step of the method: a plain streaming read, the
@@ -529,6 +535,164 @@ cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* 
                              const int32_t* host_ctx_len, const int32_t* host_n_nodes,
                              int32_t kv_split, int32_t* tree_status, void* workspace,
                              size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Packed cache: committed tokens' keys and values in 8 bits.
+ *
+ * A block holds CURE_PACK_TOKENS consecutive tokens of one sequence. For each block and
+ * kv head, keys and values apart, with x the values of the block's tokens in that head:
+ *   a = max |x|,  scale = a / 127 (one fp32 rounding),  c = 127 x / a rounded to the
+ *   nearest integer, ties to even, and x is taken as scale * c from then on.
+ * A block or head of zeros has scale 0. Tokens past the end of a sequence's last block
+ * are zeros. The values packed must be finite.
+ *
+ * Layout of a packed cache, of `blocks` blocks:
+ *   pk, pv     [blocks][hkv][64 * d] int8, 16-byte aligned
+ *   k_scale, v_scale  [blocks][hkv] float32
+ *   Within a block and head the bytes lie in the order in which the attention's matrix
+ *   instructions take them: for each half of 32 tokens and each 32 columns 1 KB, in
+ *   which 64 lanes have 16 bytes each. Token t, column j:
+ *     piece = ((t / 32) * (d / 32) + j / 32) * 1024
+ *     keys   at piece + (j % 32) / 16 * 512 + (t % 32) * 16 + j % 16
+ *     values at piece + (t / 4) % 2 * 512 + (j % 32) * 16 + (t % 32) / 8 * 4 + t % 4
+ *   Sequence b's token t is token t % 64 of block blk_off[b] + t / 64.
+ *
+ * cure_kv_pack packs rows kv_off[b] .. kv_off[b] + n_rows[b] - 1 of the caches k and v as
+ * sequence b's tokens packed_len[b] .. packed_len[b] + n_rows[b] - 1; packed_len[b] must be
+ * a multiple of 64. The rows are left as they are.
+ * cure_kv_unpack is the way back: sequence b's tokens first[b] .. first[b] + n_rows[b] - 1,
+ * from any token on, to rows kv_off[b] .. of k and v (one rounding to dtype) -- for a
+ * sequence whose last block is filled further, or that is copied.
+ *
+ *   k, v       n_layers caches of token rows [hkv][d] dtype, layer l's from element
+ *              l * layer_stride on (ignored when n_layers <= 1), `rows` rows each
+ *   block_stride  blocks between the layers of pk, pv, k_scale and v_scale (ignored when
+ *              n_layers <= 1); each layer has `blocks`
+ *   kv_off, blk_off  [batch] int64;  n_rows, packed_len, first  [batch] int32 (device)
+ *   n_max      the most rows of a sequence: sizes the launch
+ *   row_status [batch] int32 output: CURE_OK, or CURE_ERR_BAD_TREE when the sequence's
+ *              sizes are negative, n_rows exceeds n_max, packed_len is no multiple of 64,
+ *              or its rows or blocks reach past `rows` or `blocks`. Nothing of such a
+ *              sequence is written.
+ * Rows, or blocks, of different sequences that are written must not overlap.
+ * Supports d in {64, 128}, batch <= 65535, n_layers <= 65535, n_max * hkv < 2^30. k, v and
+ * layer_stride in bytes must be multiples of 16. No workspace.
+ */
+#define CURE_PACK_TOKENS 64
+
+cure_status cure_kv_pack(const void* k, const void* v, int32_t dtype, int32_t n_layers,
+                         int64_t layer_stride, int64_t rows, int32_t hkv, int32_t d,
+                         int32_t batch, int32_t n_max, const int64_t* kv_off,
+                         const int32_t* n_rows, int8_t* pk, int8_t* pv, float* k_scale,
+                         float* v_scale, int64_t block_stride, int64_t blocks,
+                         const int64_t* blk_off, const int32_t* packed_len,
+                         int32_t* row_status, void* stream);
+
+cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_scale,
+                           const float* v_scale, int64_t block_stride, int64_t blocks,
+                           const int64_t* blk_off, const int32_t* first, void* k, void* v,
+                           int32_t dtype, int32_t n_layers, int64_t layer_stride, int64_t rows,
+                           int32_t hkv, int32_t d, int32_t batch, int32_t n_max,
+                           const int64_t* kv_off, const int32_t* n_rows, int32_t* row_status,
+                           void* stream);
+
+/* Attention over a packed context: candidate trees, single tokens or chunks of prompts.
+ *
+ * New row n < n_rows[b] of sequence b attends, in every query head h (key/value head
+ * h / (hq/hkv)), to
+ *   - its packed tokens 0 .. packed_len[b] - 1, from block blk_off[b] on, as scale * c,
+ *   - the open rows kv_off[b] .. kv_off[b] + ctx_len[b] - 1 of k and v, which are context
+ *     that is not packed yet, and
+ *   - of the new rows behind them (rows kv_off[b] + ctx_len[b] + m) those of its root path,
+ *     itself included, where parent is given, else those up to itself (m <= n).
+ *   o[r][h] = sum_j softmax_j * v_j,  lse[r][h] = log sum_j exp(scale * <q, k_j>)
+ * A row's position is packed_len + ctx_len + depth or + n (cure_rope_append's
+ * pos_off = packed_len gives it).
+ *
+ * Layout:
+ *   q, o       [rows][hq][d] dtype / out_dtype; sequence b's rows are row_off[b] .., or
+ *              b * n_max .. where row_off is NULL (padded). Other rows are not written
+ *   pk, pv, k_scale, v_scale  one layer's packed cache, as above, of `blocks` blocks
+ *   k, v       one layer's cache rows [hkv][d] dtype, cache_rows of them
+ *   lse        [rows][hq] float32 (may be NULL)
+ *   parent     [batch][n_max] int32 as for cure_tree_attn, or NULL
+ *   row_off, blk_off, kv_off  [batch] int64 (row_off may be NULL);
+ *   n_rows, packed_len, ctx_len  [batch] int32 (device)
+ *   host_*     host copies that the launch is planned from. The device's sizes may differ
+ *              from them (n_rows up to n_max)
+ *   row_status [batch] int32 output (may be NULL): CURE_OK, or CURE_ERR_BAD_TREE when the
+ *              sequence's parent array is malformed (its o and lse are then
+ *              unspecified), or when its sizes are negative, n_rows exceeds n_max, or its
+ *              rows, blocks or cache rows reach past rows, blocks or cache_rows (nothing
+ *              of it is written then).
+ * The values that a row sees must be finite; what it does not see may be anything.
+ * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite, n_max <= 256
+ * with parent, batch <= 65535, n_max * hq up to 2^28. o may be q where their types are one.
+ * kv_split: 0 = automatic, else the number of splits of the longest context.
+ * workspace: cure_packed_attn_workspace_size(...) bytes for the same arguments, 16-byte
+ * aligned, as q, k, v, pk, pv and o are.
+ * bf16: probabilities times the value's scale are rounded to bf16 for their product; their
+ * sum and lse take them before. float32: float32 throughout.
+ */
+size_t cure_packed_attn_workspace_size(int32_t batch, int64_t rows, int32_t n_max, int32_t hq,
+                                       int32_t hkv, int32_t d, const int32_t* host_n_rows,
+                                       const int32_t* host_packed_len,
+                                       const int32_t* host_ctx_len, int32_t kv_split);
+
+cure_status cure_packed_attn(const void* q, const int8_t* pk, const int8_t* pv,
+                             const float* k_scale, const float* v_scale, int64_t blocks,
+                             const void* k, const void* v, int64_t cache_rows, void* o, float* lse,
+                             int32_t dtype, int32_t out_dtype, int32_t batch, int64_t rows,
+                             int32_t n_max, int32_t hq, int32_t hkv, int32_t d, float scale,
+                             const int64_t* row_off, const int32_t* n_rows,
+                             const int64_t* blk_off, const int32_t* packed_len,
+                             const int64_t* kv_off, const int32_t* ctx_len,
+                             const int32_t* parent, const int32_t* host_n_rows,
+                             const int32_t* host_packed_len, const int32_t* host_ctx_len,
+                             int32_t kv_split, int32_t* row_status, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Sampling: one token drawn for each logits row.
+ *
+ * Row n < n_rows[b] of sequence b (logits laid out as for cure_margins), with the
+ * sequence's temperature T, top_k, top_p and min_p and the row's number u. Entries are
+ * taken in the order (value descending, index ascending), m being the first one's value
+ * and an entry's weight w = exp((x - m) / T), or none where m - x > 64 T (T = 0: none
+ * but the first entry's, 1). Kept is a run from the front of what has a weight:
+ *   top_k   the first top_k entries (top_k <= 0: all),
+ *   top_p   of those the fewest whose weights reach top_p of all of theirs, at least
+ *           one (top_p >= 1: all),
+ *   min_p   of those the ones with w >= min_p, at least one (min_p <= 0: all).
+ * With W the kept weights' sum, the token is the first kept entry up to which the weights
+ * exceed u * W (the last one where none does, as for u >= 1; u < 0 counts as 0).
+ *   token    [batch][rows] int32, its index: what cure_accept takes as tgt, where drawing
+ *            every node's token makes the walk sample from the target's distribution
+ *   logprob  [batch][rows] float32, log(w / W) of it (may be NULL)
+ *   kept     [batch][rows] int32, how many entries were kept (may be NULL)
+ * Rows n >= n_rows[b], rows without a finite entry, with a NaN or a +inf, and rows
+ * whose T is negative, infinite or NaN, or whose top_p, min_p or u is NaN get CURE_NO_TOKEN
+ * (which no tree's token equals), -inf and 0.
+ *
+ *   temperature, top_p, min_p  [batch] float32, top_k [batch] int32: NULL for 1, 1, 0, 0
+ *   uniform    [batch][rows] float32, in [0, 1)
+ *   n_rows     [batch] int32, or NULL: all rows
+ * Weights and their sums are held in 64 bits or as integers, so that the result is the
+ * same however the work is split. bf16 values of magnitude below 2^-64 count as 0, those of
+ * 2^64 and more as that.
+ * Requires 1 <= vocab <= 2^20, ld >= vocab, batch * rows < 2^21, logits aligned to their type.
+ * workspace: cure_sample_workspace_size(batch, rows, vocab) bytes, 16-byte aligned.
+ */
+#define CURE_NO_TOKEN (-2)
+
+size_t cure_sample_workspace_size(int32_t batch, int32_t rows, int32_t vocab);
+
+cure_status cure_sample(const void* logits, int32_t dtype, int32_t batch, int32_t rows,
+                        int32_t vocab, int64_t ld, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p,
+                        const float* uniform, const int32_t* n_rows, int32_t* token,
+                        float* logprob, int32_t* kept, void* workspace, size_t workspace_bytes,
+                        void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Read ceiling -- a measurement aid, not a step of the method.

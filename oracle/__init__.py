@@ -35,6 +35,10 @@ unless the paper (or the decision being reproduced) fixes another precision:
                     -- around the verify step: rotary positions of new rows,
                        causal attention over prompts, and tree attention over
                        a prefix that sequences share.
+* ``pack_rows``, ``to_bytes``, ``from_bytes``, ``packed_rows``
+                    -- the packed cache: rows in blocks of 64 tokens with 8 bits a
+                       value, and the order of a block's bytes.
+* ``sample``        -- one token drawn with temperature, top-k, top-p and min-p.
 
 Inputs are the same bytes the GPU path receives: bf16 arrives as raw uint16
 bit patterns and is widened here exactly to float32 by this package's own
@@ -47,10 +51,12 @@ from .accept import accept
 from .repair import topk, branch_budget, repair_tree
 from .commit import commit_kv, commit_tokens
 from .prompt import rope_append, tree_positions, attend, prompt_attention, prefix_attention
+from .packed import key_place, value_place, pack_rows, to_bytes, from_bytes, packed_rows, sample
 
 __all__ = [
     "widen_bf16", "as_float32", "margins", "ufp_select",
     "ancestors", "tree_attention", "accept",
     "topk", "branch_budget", "repair_tree", "commit_kv", "commit_tokens",
     "rope_append", "tree_positions", "attend", "prompt_attention", "prefix_attention",
+    "key_place", "value_place", "pack_rows", "to_bytes", "from_bytes", "packed_rows", "sample",
 ]

@@ -164,7 +164,8 @@ struct Outputs {
 #define CURE_KEYS(X)                                                                     \
   X(top1_val) X(top1_idx) X(top2_val) X(top2_idx) X(lse) X(margin) X(ufp_pos) X(ufp_cnt) \
   X(acc_len) X(path) X(best) X(bonus) X(resync) X(parent) X(token) X(n_nodes)            \
-  X(branch_cnt) X(new_ctx_len) X(emit) X(emit_cnt) X(replay_start) X(status)
+  X(branch_cnt) X(new_ctx_len) X(emit) X(emit_cnt) X(replay_start) X(status) X(logprob)   \
+  X(kept)
 #define X(name) PyObject* k_##name = nullptr;
 CURE_KEYS(X)
 #undef X
@@ -832,6 +833,228 @@ PyObject* py_prefix_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// A cache of one layer [rows, hkv, d] or of several, each contiguous, and the packed cache
+// that goes with it.
+struct PackedLayers {
+  int64_t layers = 1, layer_stride = 0, rows = 0, hkv = 0, d = 0, block_stride = 0, blocks = 0;
+};
+PackedLayers packed_layers(const at::Tensor& k, const at::Tensor& v, const at::Tensor& pk, const at::Tensor& pv,
+                           const at::Tensor& ks, const at::Tensor& vs) {
+  if (k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type() || (k.dim() != 3 && k.dim() != 4))
+    fail("k and v must have the same shape [n_layers,] rows, hkv, d");
+  PackedLayers p;
+  const bool several = k.dim() == 4;
+  p.layers = several ? k.size(0) : 1;
+  p.rows = k.size(-3);
+  p.hkv = k.size(-2);
+  p.d = k.size(-1);
+  const auto together = [](const at::Tensor& x, int64_t dims) {     // the last dims dimensions
+    int64_t want = 1;
+    for (int64_t i = x.dim() - 1; i >= x.dim() - dims; --i) {
+      if (x.size(i) > 1 && x.stride(i) != want) return false;
+      want *= x.size(i);
+    }
+    return true;
+  };
+  if (!together(k, 3) || !together(v, 3)) fail("each layer of k and v must be contiguous");
+  if (pk.scalar_type() != at::kChar || pv.scalar_type() != at::kChar) fail("pk and pv must be int8");
+  if (ks.scalar_type() != at::kFloat || vs.scalar_type() != at::kFloat) fail("k_scale and v_scale must be float32");
+  if (pk.dim() != k.dim() || ks.dim() != k.dim() - 1) fail("the packed cache must have layers as k and v do");
+  p.blocks = pk.size(-3);
+  std::vector<int64_t> bytes, scales;
+  if (several) bytes.push_back(p.layers), scales.push_back(p.layers);
+  bytes.insert(bytes.end(), {p.blocks, p.hkv, CURE_PACK_TOKENS * p.d});
+  scales.insert(scales.end(), {p.blocks, p.hkv});
+  for (const at::Tensor* x : {&pk, &pv})
+    if (x->sizes() != c10::IntArrayRef(bytes)) fail("pk and pv: expected shape " + shape_text(bytes) + ", got " + shape_text(x->sizes()));
+  for (const at::Tensor* x : {&ks, &vs})
+    if (x->sizes() != c10::IntArrayRef(scales)) fail("k_scale and v_scale: expected shape " + shape_text(scales) + ", got " + shape_text(x->sizes()));
+  if (!together(pk, 3) || !together(pv, 3) || !together(ks, 2) || !together(vs, 2))
+    fail("each layer of the packed cache must be contiguous");
+  if (several && p.layers > 1) {
+    p.layer_stride = k.stride(0);
+    const int64_t block = p.hkv * CURE_PACK_TOKENS * p.d;
+    if (v.stride(0) != p.layer_stride) fail("the layers of k and v must be the same distance apart");
+    if (block > 0) {
+      p.block_stride = pk.stride(0) / block;
+      if (pk.stride(0) != p.block_stride * block || pv.stride(0) != pk.stride(0) || ks.stride(0) != p.block_stride * p.hkv ||
+          vs.stride(0) != ks.stride(0))
+        fail("the layers of the packed cache must be the same whole number of blocks apart");
+    }
+  }
+  for (const at::Tensor* x : {&v, &pk, &pv, &ks, &vs}) same_device(*x, k);
+  return p;
+}
+
+// Rows and blocks of kv_pack and kv_unpack: which argument is which.
+PyObject* pack_call(PyObject* const* args, Py_ssize_t n, bool pack) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 11);
+    const at::Tensor k = gpu_tensor(args[pack ? 0 : 6]), v = gpu_tensor(args[pack ? 1 : 7]);
+    const at::Tensor pk = gpu_tensor(args[pack ? 4 : 0]), pv = gpu_tensor(args[pack ? 5 : 1]);
+    const at::Tensor ks = gpu_tensor(args[pack ? 6 : 2]), vs = gpu_tensor(args[pack ? 7 : 3]);
+    at::Tensor blk_off = gpu_tensor(args[pack ? 8 : 4]), from = gpu_tensor(args[pack ? 9 : 5]);
+    at::Tensor kv_off = gpu_tensor(args[pack ? 2 : 8]), rows_of = gpu_tensor(args[pack ? 3 : 9]);
+    const PackedLayers p = packed_layers(k, v, pk, pv, ks, vs);
+    if (rows_of.dim() != 1) fail("n_rows must be [batch]");
+    const int64_t batch = rows_of.size(0);
+    want_ints(rows_of, at::kInt, {batch}, "n_rows");
+    want_ints(from, at::kInt, {batch}, pack ? "packed_len" : "first");
+    want_ints(kv_off, at::kLong, {batch}, "kv_off");
+    want_ints(blk_off, at::kLong, {batch}, "blk_off");
+    for (at::Tensor* x : {&rows_of, &from, &kv_off, &blk_off}) {
+      same_device(*x, k);
+      *x = x->contiguous();
+    }
+    const int64_t n_max = args[10] == Py_None ? std::min<int64_t>(p.rows, INT32_MAX) : as_i32(args[10]);
+    if (p.layers > INT32_MAX || p.hkv > INT32_MAX || p.d > INT32_MAX || batch > INT32_MAX) fail("too large");
+    const int32_t dtype = dtype_code(k);
+    at::Tensor status = empty({batch}, at::kInt, k);
+    const OnDevice on(k);
+    void* s = stream_of(k);
+    void *kp = k.data_ptr(), *vp = v.data_ptr();
+    int8_t *pkp = data<int8_t>(pk), *pvp = data<int8_t>(pv);
+    float *ksp = data<float>(ks), *vsp = data<float>(vs);
+    const int64_t *kop = data<int64_t>(kv_off), *bop = data<int64_t>(blk_off);
+    const int32_t *np = data<int32_t>(rows_of), *fp = data<int32_t>(from);
+    int32_t* stp = data<int32_t>(status);
+    const int32_t layers = (int32_t)p.layers, hkv = (int32_t)p.hkv, d = (int32_t)p.d, nb = (int32_t)batch;
+    check(unlocked([&] {
+            return pack ? cure_kv_pack(kp, vp, dtype, layers, p.layer_stride, p.rows, hkv, d, nb, (int32_t)n_max, kop, np,
+                                       pkp, pvp, ksp, vsp, p.block_stride, p.blocks, bop, fp, stp, s)
+                        : cure_kv_unpack(pkp, pvp, ksp, vsp, p.block_stride, p.blocks, bop, fp, kp, vp, dtype, layers,
+                                         p.layer_stride, p.rows, hkv, d, nb, (int32_t)n_max, kop, np, stp, s);
+          }), pack ? "cure_kv_pack" : "cure_kv_unpack");
+    return THPVariable_Wrap(status);
+  });
+}
+
+// kv_pack(k, v, kv_off, n_rows, pk, pv, k_scale, v_scale, blk_off, packed_len, n_max)
+PyObject* py_kv_pack(PyObject*, PyObject* const* args, Py_ssize_t n) { return pack_call(args, n, true); }
+
+// kv_unpack(pk, pv, k_scale, v_scale, blk_off, first, k, v, kv_off, n_rows, n_max)
+PyObject* py_kv_unpack(PyObject*, PyObject* const* args, Py_ssize_t n) { return pack_call(args, n, false); }
+
+// packed_attn(q, pk, pv, k_scale, v_scale, blk_off, packed_len, k, v, kv_off, ctx_len, n_rows, host_packed_len,
+//             host_ctx_len, host_n_rows, scale, parent, row_off, out_dtype, kv_split, with_lse, out)
+PyObject* py_packed_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 22);
+    at::Tensor t[12];                    // q, pk, pv, k_scale, v_scale, blk_off, packed_len, k, v, kv_off, ctx_len, n_rows
+    for (int i = 0; i < 12; ++i) t[i] = gpu_tensor(args[i]);
+    const at::Tensor &q = t[0], &k = t[7], &v = t[8];
+    at::Tensor parent = optional(args[16]), row_off = optional(args[17]);
+    const bool padded = !row_off.defined();
+    if (q.dim() != (padded ? 4 : 3) || !q.is_contiguous())
+      fail(padded ? "q must be [batch, n_max, hq, d] (or [rows, hq, d] with row_off), contiguous"
+                  : "with row_off, q must be [rows, hq, d], contiguous");
+    const int64_t hq = q.size(-2), d = q.size(-1);
+    want_caches(k, v, q, d);
+    const PackedLayers p = packed_layers(k, v, t[1], t[2], t[3], t[4]);
+    if (t[11].dim() != 1) fail("n_rows must be [batch]");
+    const int64_t batch = t[11].size(0);
+    const std::vector<int32_t> hp = host_sizes(args[12], batch), hc = host_sizes(args[13], batch),
+                               hn = host_sizes(args[14], batch);
+    int64_t rows = q.size(0), n_max = 0;
+    if (padded) {
+      if (q.size(0) != batch) fail("n_rows must have an entry for each sequence of q");
+      n_max = q.size(1);
+      rows = batch * n_max;
+    } else if (parent.defined() && parent.dim() == 2) {
+      n_max = parent.size(1);
+    } else {
+      for (int64_t b = 0; b < batch; ++b) n_max = std::max<int64_t>(n_max, hn[b]);
+    }
+    want_ints(t[5], at::kLong, {batch}, "blk_off");
+    want_ints(t[6], at::kInt, {batch}, "packed_len");
+    want_ints(t[9], at::kLong, {batch}, "kv_off");
+    want_ints(t[10], at::kInt, {batch}, "ctx_len");
+    want_ints(t[11], at::kInt, {batch}, "n_rows");
+    want_ints(row_off, at::kLong, {batch}, "row_off");
+    want_ints(parent, at::kInt, {batch, n_max}, "parent");
+    for (at::Tensor* x : {&t[5], &t[6], &t[9], &t[10], &t[11], &row_off, &parent}) {
+      if (!x->defined()) continue;
+      same_device(*x, q);
+      *x = x->contiguous();
+    }
+    if (n_max > INT32_MAX || batch > INT32_MAX || hq > INT32_MAX || d > INT32_MAX || p.hkv > INT32_MAX) fail("too large");
+    const float scale = as_f32(args[15]);
+    const int32_t split = as_i32(args[19]);
+    const bool with_lse = truth(args[20]);
+    at::Tensor o = output(args[21], q.sizes(), out_dtype(args[18], q), q);
+    at::Tensor lse = with_lse ? empty(q.sizes().slice(0, q.dim() - 1), at::kFloat, q) : at::Tensor();
+    at::Tensor status = empty({batch}, at::kInt, q);
+    const int32_t dt = dtype_code(q), odt = dtype_code(o), hkv = (int32_t)p.hkv;
+    const OnDevice on(q);
+    void* s = stream_of(q);
+    const Scratch ws(q, cure_packed_attn_workspace_size((int32_t)batch, rows, (int32_t)n_max, (int32_t)hq, hkv, (int32_t)d,
+                                                        hn.data(), hp.data(), hc.data(), split));
+    const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
+    const int8_t *pkp = data<int8_t>(t[1]), *pvp = data<int8_t>(t[2]);
+    const float *ksp = data<float>(t[3]), *vsp = data<float>(t[4]);
+    void* op = o.data_ptr();
+    float* lp = data<float>(lse);
+    const int64_t *rop = data<int64_t>(row_off), *bop = data<int64_t>(t[5]), *kop = data<int64_t>(t[9]);
+    const int32_t *pp = data<int32_t>(t[6]), *cp = data<int32_t>(t[10]), *np = data<int32_t>(t[11]),
+                  *parp = data<int32_t>(parent);
+    int32_t* stp = data<int32_t>(status);
+    const int64_t cache_rows = k.size(0);
+    check(unlocked([&] {
+            return cure_packed_attn(qp, pkp, pvp, ksp, vsp, p.blocks, kp, vp, cache_rows, op, lp, dt, odt, (int32_t)batch,
+                                    rows, (int32_t)n_max, (int32_t)hq, hkv, (int32_t)d, scale, rop, np, bop, pp, kop, cp,
+                                    parp, hn.data(), hp.data(), hc.data(), split, stp, ws.ptr, ws.bytes, s);
+          }), "cure_packed_attn");
+    return attn_result(o, lse, status);
+  });
+}
+
+// sample(logits, uniform, temperature, top_k, top_p, min_p, n_rows)
+PyObject* py_sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 7);
+    const at::Tensor x = logits_of(args[0]);
+    at::Tensor u = gpu_tensor(args[1]);
+    at::Tensor t = optional(args[2]), k = optional(args[3]), p = optional(args[4]), m = optional(args[5]),
+               rows_of = optional(args[6]);
+    const int64_t batch = x.size(0), rows = x.size(1), vocab = x.size(2);
+    if (u.dim() == 1) u = u.unsqueeze(0);
+    const auto want = [&](at::Tensor& a, c10::IntArrayRef shape, const char* name) {
+      if (!a.defined()) return;
+      if (a.scalar_type() != at::kFloat) fail(std::string(name) + " must be float32");
+      if (a.sizes() != shape) fail(std::string(name) + ": expected shape " + shape_text(shape) + ", got " + shape_text(a.sizes()));
+    };
+    want(u, {batch, rows}, "uniform");
+    want(t, {batch}, "temperature");
+    want(p, {batch}, "top_p");
+    want(m, {batch}, "min_p");
+    want_ints(k, at::kInt, {batch}, "top_k");
+    want_ints(rows_of, at::kInt, {batch}, "n_rows");
+    for (at::Tensor* a : {&u, &t, &k, &p, &m, &rows_of}) {
+      if (!a->defined()) continue;
+      same_device(*a, x);
+      *a = a->contiguous();
+    }
+    if (batch > INT32_MAX || rows > INT32_MAX || vocab > INT32_MAX) fail("too large");
+    const int32_t dtype = dtype_code(x);
+    Outputs out;
+    int32_t* token = out.add<int32_t>(k_token, empty({batch, rows}, at::kInt, x));
+    float* logprob = out.add<float>(k_logprob, empty({batch, rows}, at::kFloat, x));
+    int32_t* kept = out.add<int32_t>(k_kept, empty({batch, rows}, at::kInt, x));
+    const OnDevice on(x);
+    void* s = stream_of(x);
+    const Scratch ws(x, cure_sample_workspace_size((int32_t)batch, (int32_t)rows, (int32_t)vocab));
+    const void* lp = x.data_ptr();
+    const int64_t ld = rows > 1 || batch > 1 ? x.stride(1) : std::max<int64_t>(x.stride(1), vocab);
+    const float *up = data<float>(u), *tp = data<float>(t), *pp = data<float>(p), *mp = data<float>(m);
+    const int32_t *kp = data<int32_t>(k), *np = data<int32_t>(rows_of);
+    check(unlocked([&] {
+            return cure_sample(lp, dtype, (int32_t)batch, (int32_t)rows, (int32_t)vocab, ld, tp, kp, pp, mp, up, np, token,
+                               logprob, kept, ws.ptr, ws.bytes, s);
+          }), "cure_sample");
+    return out.take();
+  });
+}
+
 // setup(CureError, host_i32)
 PyObject* py_setup(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -847,7 +1070,8 @@ PyObject* py_setup(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup),       FAST(margins),     FAST(tree_attn),   FAST(accept),
                          FAST(repair_tree), FAST(commit),      FAST(rope_append), FAST(prompt_attn),
-                         FAST(prefix_attn), {nullptr, nullptr, 0, nullptr}};
+                         FAST(prefix_attn), FAST(kv_pack),     FAST(kv_unpack),   FAST(packed_attn),
+                         FAST(sample),      {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

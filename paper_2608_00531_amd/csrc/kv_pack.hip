@@ -1,0 +1,289 @@
+// cure_kv_pack: cache rows made blocks of 64 tokens in 8 bits with one scale for each
+// block and kv head; cure_kv_unpack: blocks made rows.
+//
+//   a = max |x|,  scale = a / 127,  c = rint(127 x / a)
+//
+// The integer is the exact quotient's nearest, ties to even: c0 = rint(x * (127 / a)) is at
+// most one off, and the remainder 127 x - c0 a, which fp32 holds exactly for bf16 values (15
+// bits) and fp64 for fp32 ones (31 bits), says which.
+//
+// Bound by memory. One wave takes one block and head of K or of V, whole, in registers: all
+// its loads (16 KB of bf16 at head dim 128) are in flight together, and the maximum is a wave's
+// reduction, without LDS or barriers. A row's vectors lie in neighbouring lanes; the 16 tokens
+// that a lane of V's layout holds are its own 16 loads, so that its bytes come together
+// without exchange.
+#include <hip/hip_runtime.h>
+
+#include "common.hpp"
+#include "host_util.hpp"
+#include "packed.hpp"
+
+namespace cure {
+namespace {
+
+struct Args {
+  void* k;
+  void* v;
+  int64_t layer_stride, rows;
+  int32_t n_max, hkv;
+  const int64_t* kv_off;
+  const int32_t* n_rows;
+  int8_t* pk;
+  int8_t* pv;
+  float* k_scale;
+  float* v_scale;
+  int64_t block_stride, blocks;
+  const int64_t* blk_off;
+  const int32_t* from;               // first token of the sequence
+  int32_t* row_status;
+};
+
+// What a workgroup takes of a sequence: tokens t0 .. of block `block`, n of them wanted, the
+// first of which is row `row`; a head of it.
+struct Part {
+  int64_t row, block;
+  int n, skip, head;                 // skip: the block's tokens before the first one wanted
+};
+
+// False: nothing to do.
+CURE_DEV bool part_of(const Args& a, bool whole_blocks, Part& p) {
+  const int b = blockIdx.y, index = blockIdx.x / a.hkv;
+  const int n = a.n_rows[b], from = a.from[b];
+  const int64_t row0 = a.kv_off[b], block0 = a.blk_off[b];
+  const bool ok = n >= 0 && n <= a.n_max && from >= 0 && row0 >= 0 && row0 <= a.rows - n && block0 >= 0 &&
+                  block0 <= a.blocks - blocks_of((int64_t)from + n) && !(whole_blocks && from % kBlockTokens);
+  if (blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0) a.row_status[b] = ok ? CURE_OK : CURE_ERR_BAD_TREE;
+  if (!ok || n == 0) return false;
+  const int64_t t0 = ((int64_t)(from / kBlockTokens) + index) * kBlockTokens;      // the block's first token
+  const int64_t begin = t0 > from ? t0 : from, end = min(t0 + kBlockTokens, (int64_t)from + n);
+  if (begin >= end) return false;
+  p.head = blockIdx.x % a.hkv;
+  p.skip = (int)(begin - t0);
+  p.n = (int)(end - begin);
+  p.row = row0 + (begin - from);
+  p.block = block0 + t0 / kBlockTokens;
+  return true;
+}
+
+// rint(127 x / a), ties to even; inv is near 127 / a.
+CURE_DEV float to_int(float x, float a, float inv, uint16_t) {
+  float c = rintf(x * inv);
+  const float r = 2.f * fmaf(-c, a, 127.f * x), m = fabsf(r);
+  if (m > a || (m == a && ((int)c & 1))) c += copysignf(1.f, r);
+  return c;
+}
+CURE_DEV float to_int(float x, float a, float inv, float) {
+  float c = rintf(x * inv);
+  const double r = 2.0 * fma(-(double)c, (double)a, 127.0 * (double)x), m = fabs(r);
+  if (m > (double)a || (m == (double)a && ((int)c & 1))) c += copysignf(1.f, (float)r);
+  return c;
+}
+
+// Four integers of magnitude up to 127 as bytes.
+CURE_DEV uint32_t bytes_of(float a, float b, float c, float d) {
+  return ((uint32_t)(int)a & 255u) | ((uint32_t)(int)b & 255u) << 8 | ((uint32_t)(int)c & 255u) << 16 | (uint32_t)(int)d << 24;
+}
+
+// Lanes and pieces. K: unit i is 16 columns of a token, and 16 bytes of the block. V: a lane has
+// D / 16 columns of the 16 tokens 8 a + 4 h + c of a half, each column 16 bytes of the block.
+template <int D>
+struct Lanes {
+  static constexpr int kUnits = D / 16;            // of K, per lane
+  static constexpr int kCols = D / 16;             // of V, per lane
+  static CURE_DEV int k_token(int lane, int i) { return (i * kWave + lane) / (D / 16); }
+  static CURE_DEV int k_col(int lane) { return lane % (D / 16) * 16; }
+  static CURE_DEV int k_byte(int t, int j) { return ((t / 32) * (D / 32) + j / 32) * 1024 + j % 32 / 16 * 512 + t % 32 * 16; }
+  static CURE_DEV int v_token(int lane, int i) { return lane / 32 * 32 + lane / 16 % 2 * 4 + i / 4 * 8 + i % 4; }
+  static CURE_DEV int v_col(int lane) { return lane % 16 * kCols; }
+  static CURE_DEV int v_byte(int lane, int j) { return (lane / 32 * (D / 32) + j / 32) * 1024 + lane / 16 % 2 * 512 + j % 32 * 16; }
+};
+
+// A power of two by which a block is scaled first where 127 / a or 127 x would overflow: what it
+// rounds off is far below a / 254.
+CURE_DEV float scaled_by(float a) { return a < 0x1p-100f ? 0x1p100f : a > 0x1p100f ? 0x1p-100f : 1.f; }
+
+template <typename E, int D>
+__global__ __launch_bounds__(2 * kWave) void kv_pack(Args a) {
+  using L = Lanes<D>;
+  Part p;
+  if (!part_of(a, true, p)) return;
+  const int lane = threadIdx.x % kWave;
+  const bool values = threadIdx.x >= kWave;
+  const int64_t pitch = (int64_t)a.hkv * D, layer = blockIdx.z;
+  const E* src = static_cast<const E*>(values ? a.v : a.k) + layer * a.layer_stride + p.row * pitch + (int64_t)p.head * D;
+  const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
+  float* scale = (values ? a.v_scale : a.k_scale) + block;
+  int8_t* dst = (values ? a.pv : a.pk) + block * (kBlockTokens * D);
+  float high = 0.f;
+  if (!values) {
+    RowVec<E, 16> x[L::kUnits];
+#pragma unroll
+    for (int i = 0; i < L::kUnits; ++i) {
+      const int t = L::k_token(lane, i);
+      if (t < p.n) x[i].load(src + t * pitch + L::k_col(lane));
+      else x[i].clear();
+    }
+#pragma unroll
+    for (int i = 0; i < L::kUnits; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
+    high = wave_max(high);
+    if (lane == 0) *scale = high / 127.f;
+    const float up = scaled_by(high), top = high * up, inv = top > 0.f ? 127.f / top : 0.f;
+#pragma unroll
+    for (int i = 0; i < L::kUnits; ++i) {
+      u32x4 out;
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        float c[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) c[u] = to_int(x[i].get(j + u) * up, top, inv, E());
+        out[j / 4] = bytes_of(c[0], c[1], c[2], c[3]);
+      }
+      *reinterpret_cast<u32x4*>(dst + L::k_byte(L::k_token(lane, i), L::k_col(lane))) = out;
+    }
+    return;
+  }
+  RowVec<E, L::kCols> x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int t = L::v_token(lane, i);
+    if (t < p.n) x[i].load(src + t * pitch + L::v_col(lane));
+    else x[i].clear();
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int j = 0; j < L::kCols; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
+  high = wave_max(high);
+  if (lane == 0) *scale = high / 127.f;
+  const float up = scaled_by(high), top = high * up, inv = top > 0.f ? 127.f / top : 0.f;
+#pragma unroll
+  for (int j = 0; j < L::kCols; ++j) {
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      float c[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) c[u] = to_int(x[i + u].get(j) * up, top, inv, E());
+      out[i / 4] = bytes_of(c[0], c[1], c[2], c[3]);
+    }
+    *reinterpret_cast<u32x4*>(dst + L::v_byte(lane, L::v_col(lane) + j)) = out;
+  }
+}
+
+// The same pieces the other way.
+template <typename E, int D>
+__global__ __launch_bounds__(2 * kWave) void kv_unpack(Args a) {
+  using L = Lanes<D>;
+  Part p;
+  if (!part_of(a, false, p)) return;
+  const int lane = threadIdx.x % kWave;
+  const bool values = threadIdx.x >= kWave;
+  const int64_t pitch = (int64_t)a.hkv * D, layer = blockIdx.z;
+  E* dst = static_cast<E*>(values ? a.v : a.k) + layer * a.layer_stride + (p.row - p.skip) * pitch + (int64_t)p.head * D;
+  const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
+  const float scale = (values ? a.v_scale : a.k_scale)[block];
+  const int8_t* src = (values ? a.pv : a.pk) + block * (kBlockTokens * D);
+  const auto value = [&](const u32x4& w, int i) { return scale * (float)(int8_t)(w[i / 4] >> (i % 4 * 8)); };
+  const auto wanted = [&](int t) { return t >= p.skip && t < p.skip + p.n; };
+  if (!values) {
+    u32x4 w[L::kUnits];
+#pragma unroll
+    for (int i = 0; i < L::kUnits; ++i)
+      w[i] = *reinterpret_cast<const u32x4*>(src + L::k_byte(L::k_token(lane, i), L::k_col(lane)));
+#pragma unroll
+    for (int i = 0; i < L::kUnits; ++i) {
+      const int t = L::k_token(lane, i);
+      RowVec<E, 16> x;
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) x.put2(j, value(w[i], j), value(w[i], j + 1));
+      if (wanted(t)) x.store(dst + t * pitch + L::k_col(lane));
+    }
+    return;
+  }
+  u32x4 w[L::kCols];
+#pragma unroll
+  for (int j = 0; j < L::kCols; ++j) w[j] = *reinterpret_cast<const u32x4*>(src + L::v_byte(lane, L::v_col(lane) + j));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int t = L::v_token(lane, i);
+    RowVec<E, L::kCols> x;
+#pragma unroll
+    for (int j = 0; j < L::kCols; j += 2) x.put2(j, value(w[j], i), value(w[j + 1], i));
+    if (wanted(t)) x.store(dst + t * pitch + L::v_col(lane));
+  }
+}
+
+// The checks that both calls make, and the launch. *nothing: there is nothing to do.
+cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int32_t batch, bool* nothing) {
+  *nothing = false;
+  if (dtype != CURE_F32 && dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
+  if (n_layers < 1 || a.rows < 0 || a.hkv <= 0 || d <= 0 || batch < 0 || a.n_max < 0 || a.blocks < 0)
+    return CURE_ERR_INVALID_ARG;
+  if (n_layers > 1 && (a.layer_stride < 0 || a.block_stride < 0)) return CURE_ERR_INVALID_ARG;
+  if (d != 64 && d != 128) return CURE_ERR_UNSUPPORTED;
+  if (batch > 65535 || n_layers > 65535 || (int64_t)a.n_max * a.hkv >= (int64_t(1) << 30)) return CURE_ERR_UNSUPPORTED;
+  *nothing = batch == 0;
+  if (batch == 0) return CURE_OK;
+  if (!a.kv_off || !a.n_rows || !a.blk_off || !a.from || !a.row_status) return CURE_ERR_INVALID_ARG;
+  if (a.n_max > 0) {
+    if (!a.k || !a.v || !a.pk || !a.pv || !a.k_scale || !a.v_scale) return CURE_ERR_INVALID_ARG;
+    const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    if ((at(a.k) | at(a.v) | at(a.pk) | at(a.pv)) % 16 || (at(a.k_scale) | at(a.v_scale)) % 4) return CURE_ERR_INVALID_ARG;
+    if (n_layers > 1 && a.layer_stride * (dtype == CURE_BF16 ? 2 : 4) % 16) return CURE_ERR_INVALID_ARG;
+  }
+  return CURE_OK;
+}
+
+// Workgroups: blocks that a sequence's rows can touch (one more where they need not begin with
+// one) x heads, sequences, layers.
+template <bool kPack>
+cure_status launch(Args a, int32_t dtype, int32_t n_layers, int32_t d, int32_t batch, void* stream) {
+  bool nothing;
+  const cure_status st = check(a, dtype, n_layers, d, batch, &nothing);
+  if (st != CURE_OK || nothing) return st;
+  if (n_layers <= 1) a.layer_stride = a.block_stride = 0;
+  const int64_t touched = a.n_max == 0 ? 1 : blocks_of(a.n_max) + (kPack ? 0 : 1);
+  const dim3 grid((unsigned)(touched * a.hkv), (unsigned)batch, (unsigned)n_layers), block(2 * kWave);
+  hipStream_t s = as_stream(stream);
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+  if (kPack) {
+    if (dtype == CURE_BF16) d == 128 ? run(kv_pack<uint16_t, 128>) : run(kv_pack<uint16_t, 64>);
+    else d == 128 ? run(kv_pack<float, 128>) : run(kv_pack<float, 64>);
+  } else {
+    if (dtype == CURE_BF16) d == 128 ? run(kv_unpack<uint16_t, 128>) : run(kv_unpack<uint16_t, 64>);
+    else d == 128 ? run(kv_unpack<float, 128>) : run(kv_unpack<float, 64>);
+  }
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace cure
+
+using namespace cure;
+
+extern "C" cure_status cure_kv_pack(const void* k, const void* v, int32_t dtype, int32_t n_layers,
+                                    int64_t layer_stride, int64_t rows, int32_t hkv, int32_t d,
+                                    int32_t batch, int32_t n_max, const int64_t* kv_off,
+                                    const int32_t* n_rows, int8_t* pk, int8_t* pv, float* k_scale,
+                                    float* v_scale, int64_t block_stride, int64_t blocks,
+                                    const int64_t* blk_off, const int32_t* packed_len,
+                                    int32_t* row_status, void* stream) {
+  return launch<true>(Args{const_cast<void*>(k), const_cast<void*>(v), layer_stride, rows, n_max, hkv, kv_off, n_rows, pk, pv,
+                           k_scale, v_scale, block_stride, blocks, blk_off, packed_len, row_status},
+                      dtype, n_layers, d, batch, stream);
+}
+
+extern "C" cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_scale,
+                                      const float* v_scale, int64_t block_stride, int64_t blocks,
+                                      const int64_t* blk_off, const int32_t* first, void* k, void* v,
+                                      int32_t dtype, int32_t n_layers, int64_t layer_stride, int64_t rows,
+                                      int32_t hkv, int32_t d, int32_t batch, int32_t n_max,
+                                      const int64_t* kv_off, const int32_t* n_rows, int32_t* row_status,
+                                      void* stream) {
+  return launch<false>(Args{k, v, layer_stride, rows, n_max, hkv, kv_off, n_rows, const_cast<int8_t*>(pk),
+                            const_cast<int8_t*>(pv), const_cast<float*>(k_scale), const_cast<float*>(v_scale), block_stride,
+                            blocks, blk_off, first, row_status},
+                       dtype, n_layers, d, batch, stream);
+}

@@ -30,6 +30,8 @@ CURE_BF16 = 1
 CURE_ATTN_FORCE_VALU = 1
 CURE_MAX_TREE_NODES = 256
 CURE_ROPE_INTERLEAVED = 1
+CURE_PACK_TOKENS = 64
+CURE_NO_TOKEN = -2
 _ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 _lock = threading.Lock()
@@ -83,6 +85,17 @@ _SIGNATURES = {
     "cure_prefix_attn": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
                                         _f32, _i64, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32,
                                         _vp, _vp, _sz, _vp]),
+    "cure_kv_pack": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i64, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp,
+                                    _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "cure_kv_unpack": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _i64,
+                                      _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "cure_packed_attn_workspace_size": (_sz, [_i32, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32]),
+    "cure_packed_attn": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i32, _i32,
+                                        _i64, _i32, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                        _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "cure_sample_workspace_size": (_sz, [_i32, _i32, _i32]),
+    "cure_sample": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                   _vp, _sz, _vp]),
 }
 
 
@@ -307,6 +320,60 @@ def cure_prefix_attn(q, k, v, prefix_off, prefix_len, kv_off, ctx_len, n_nodes, 
     """
     return _native().prefix_attn(q, k, v, prefix_off, prefix_len, kv_off, ctx_len, n_nodes, parent,
                                  host_ctx_len, host_n_nodes, scale, out_dtype, kv_split, with_lse, out)
+
+
+def cure_kv_pack(k, v, kv_off, n_rows, pk, pv, k_scale, v_scale, blk_off, packed_len, n_max=None):
+    """Pack rows of the cache into blocks of CURE_PACK_TOKENS tokens with 8 bits a value.
+
+    k, v: one layer's cache [rows, hkv, d], or n_layers caches [n_layers, rows, hkv, d], as for
+    cure_commit. pk, pv int8 [(n_layers,) blocks, hkv, 64 * d] and k_scale, v_scale float32
+    [(n_layers,) blocks, hkv]: the packed cache. kv_off, blk_off int64, n_rows, packed_len
+    int32 [batch] (all on the GPU): rows kv_off[b] .. kv_off[b] + n_rows[b] - 1 become sequence b's
+    tokens from packed_len[b] (a multiple of 64) on. n_max: a bound on n_rows (default: the
+    cache's rows; the longest n_rows is faster, as the launch has room for n_max of each).
+    Returns the status [batch].
+    """
+    return _native().kv_pack(k, v, kv_off, n_rows, pk, pv, k_scale, v_scale, blk_off, packed_len, n_max)
+
+
+def cure_kv_unpack(pk, pv, k_scale, v_scale, blk_off, first, k, v, kv_off, n_rows, n_max=None):
+    """Make packed tokens rows of the cache again: sequence b's tokens first[b] .. first[b] + n_rows[b] - 1
+    go to rows kv_off[b] .. of k and v. Arguments as for cure_kv_pack, first int32 [batch].
+    Returns the status [batch].
+    """
+    return _native().kv_unpack(pk, pv, k_scale, v_scale, blk_off, first, k, v, kv_off, n_rows, n_max)
+
+
+def cure_packed_attn(q, pk, pv, k_scale, v_scale, blk_off, packed_len, k, v, kv_off, ctx_len, n_rows,
+                     host_packed_len, host_ctx_len, host_n_rows, scale, parent=None, row_off=None, out_dtype=None,
+                     kv_split=0, with_lse=True, out=None):
+    """Attention over a packed context, the open rows behind it and the new rows themselves.
+
+    q [batch, n_max, hq, d], each sequence's rows padded to n_max; or, with row_off int64 [batch],
+    packed [rows, hq, d] with sequence b's n_rows[b] from row_off[b] on. pk, pv int8
+    [blocks, hkv, 64 * d], k_scale, v_scale float32 [blocks, hkv]: a layer's packed cache, in
+    which sequence b's packed_len[b] tokens lie from block blk_off[b] on; k, v [cache_rows, hkv, d]:
+    its ctx_len[b] open rows and then its new ones from kv_off[b] on. parent int32 [batch, n_max]
+    where the rows are a tree's nodes, else they see each other causally. blk_off, kv_off int64,
+    packed_len, ctx_len, n_rows int32 [batch] (all on the GPU); host_*: host copies (numpy or
+    lists). Returns (o as q, lse [..., hq] or None, status [batch]); rows past a sequence's n_rows
+    are not written.
+    """
+    return _native().packed_attn(q, pk, pv, k_scale, v_scale, blk_off, packed_len, k, v, kv_off, ctx_len, n_rows,
+                                 host_packed_len, host_ctx_len, host_n_rows, scale, parent, row_off, out_dtype,
+                                 kv_split, with_lse, out)
+
+
+def cure_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, n_rows=None):
+    """Draw one token for each row of logits [batch, rows, vocab] (or [rows, vocab]).
+
+    uniform float32 [batch, rows] (or [rows]): numbers in [0, 1). temperature, top_p, min_p float32 and top_k
+    int32 [batch]: each sequence's settings, None for none; n_rows int32 [batch]: rows of
+    each, None for all (all on the GPU). Returns a dict of tensors [batch, rows]: token (as
+    cure_accept's tgt), logprob (under the distribution that it was drawn from) and kept;
+    rows past n_rows, or without a distribution, have CURE_NO_TOKEN, -inf and 0.
+    """
+    return _native().sample(logits, uniform, temperature, top_k, top_p, min_p, n_rows)
 
 
 def cure_read_ceiling(buf):
