@@ -677,22 +677,16 @@ cure_status cure_packed_attn(const void* q, const int8_t* pk, const int8_t* pv,
  *   temperature, top_p, min_p  [batch] float32, top_k [batch] int32: NULL for 1, 1, 0, 0
  *   uniform    [batch][rows] float32, in [0, 1)
  *   n_rows     [batch] int32, or NULL: all rows
- * Weights and their sums are held in 64 bits or as integers, so that the result is the
- * same however the work is split. bf16 values of magnitude below 2^-64 count as 0, those of
- * 2^64 and more as that.
- * Requires 1 <= vocab <= 2^20, ld >= vocab, batch * rows < 2^21, logits aligned to their type.
- * workspace: cure_sample_workspace_size(batch, rows, vocab) bytes, 16-byte aligned.
+ * Weights and their sums are held in 64 bits or as integers and added in one order.
+ * Requires 1 <= vocab <= 2^20, ld >= vocab, batch * rows < 2^21, logits aligned to their type. No workspace.
  */
 #define CURE_NO_TOKEN (-2)
-
-size_t cure_sample_workspace_size(int32_t batch, int32_t rows, int32_t vocab);
 
 cure_status cure_sample(const void* logits, int32_t dtype, int32_t batch, int32_t rows,
                         int32_t vocab, int64_t ld, const float* temperature,
                         const int32_t* top_k, const float* top_p, const float* min_p,
                         const float* uniform, const int32_t* n_rows, int32_t* token,
-                        float* logprob, int32_t* kept, void* workspace, size_t workspace_bytes,
-                        void* stream);
+                        float* logprob, int32_t* kept, void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Read ceiling -- a measurement aid, not a step of the method.

@@ -1042,14 +1042,13 @@ PyObject* py_sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
     int32_t* kept = out.add<int32_t>(k_kept, empty({batch, rows}, at::kInt, x));
     const OnDevice on(x);
     void* s = stream_of(x);
-    const Scratch ws(x, cure_sample_workspace_size((int32_t)batch, (int32_t)rows, (int32_t)vocab));
     const void* lp = x.data_ptr();
     const int64_t ld = rows > 1 || batch > 1 ? x.stride(1) : std::max<int64_t>(x.stride(1), vocab);
     const float *up = data<float>(u), *tp = data<float>(t), *pp = data<float>(p), *mp = data<float>(m);
     const int32_t *kp = data<int32_t>(k), *np = data<int32_t>(rows_of);
     check(unlocked([&] {
             return cure_sample(lp, dtype, (int32_t)batch, (int32_t)rows, (int32_t)vocab, ld, tp, kp, pp, mp, up, np, token,
-                               logprob, kept, ws.ptr, ws.bytes, s);
+                               logprob, kept, s);
           }), "cure_sample");
     return out.take();
   });

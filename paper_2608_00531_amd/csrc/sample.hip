@@ -3,17 +3,17 @@
 //
 // In the order (value descending, index ascending), with w_j = exp((x_j - m) / T) or nothing
 // past 64 T below the maximum m, what each filter keeps is a run from the front, and the
-// token is the entry at which the kept weights' running sum passes u W. So a row needs
-// three places in its order: by a count (top-k), by a sum of weights (top-p, and the token) and by
-// a value (min-p). All are found alike, without sorting: a histogram over bins of the
-// logits holds each bin's count and weight, a scan over the bins says in which one the place
-// lies, and that bin is divided again until it holds a single value, whose entries differ
-// by index alone.
+// token is the entry at which the kept weights' running sum passes u W. So a row needs a few
+// places in its order: by a count (top-k), by a sum of weights (top-p, and the token) and by
+// a value (min-p). They are found alike, without sorting: a histogram over bins of the values
+// holds what each bin has, sums over groups of 64 bins say in which group a place lies, and
+// a scan of that group's bins in which bin.
 //
-// Whether an entry is kept or drawn must not depend on how the work is split, so weights
-// are summed in bins as integers: relative to the upper edge of a bin of width T / 64 a weight
-// is in (exp(-1/64), 1], and 2^44 times it, rounded, leaves room for 2^20 of them. Over the bins
-// the sums are formed in fp64, in one order.
+// Whether an entry is kept or drawn must not depend on how the work is split. Counts are
+// integers, weights are formed in fp64 once for each bin or summed as integers, and the bins' sums
+// are added in one order.
+//
+// One workgroup takes a row, so that every bin is in one LDS.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -24,11 +24,11 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kBins = 4096;
-constexpr int kPer = kBins / kThreads;             // bins of a thread
 constexpr double kRange = 64.0;                    // weights reach 64 T below the maximum
-constexpr double kUnit = 0x1p44;
 constexpr int kMaxVocab = 1 << 20;
+constexpr int kList = 2048;                        // entries of a bin that are put in order in a list, at most
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 struct Args {
   const void* logits;
@@ -45,8 +45,154 @@ struct Args {
   int32_t* kept;
 };
 
-CURE_DEV float widen(uint16_t x) { return bf16_to_f32(x); }
-CURE_DEV float widen(float x) { return x; }
+// A row's settings. none: no token can be drawn by them.
+struct Settings {
+  float t, top_p, min_p, u;
+  int top_k;
+  bool none;
+};
+CURE_DEV Settings settings_of(const Args& a, int64_t r) {
+  const int b = (int)(r / a.rows), n = (int)(r % a.rows);
+  Settings s;
+  s.t = a.temperature ? a.temperature[b] : 1.f;
+  s.top_p = a.top_p ? a.top_p[b] : 1.f;
+  s.min_p = a.min_p ? a.min_p[b] : 0.f;
+  s.top_k = a.top_k ? a.top_k[b] : 0;
+  s.u = a.uniform[r];
+  s.none = (a.n_rows && n >= a.n_rows[b]) || !(s.t >= 0.f) || s.t == INFINITY || s.top_p != s.top_p || s.min_p != s.min_p ||
+           s.u != s.u;
+  return s;
+}
+CURE_DEV void answer(const Args& a, int64_t r, int token, float logprob, int kept) {
+  a.token[r] = token;
+  if (a.logprob) a.logprob[r] = logprob;
+  if (a.kept) a.kept[r] = kept;
+}
+CURE_DEV void no_answer(const Args& a, int64_t r) { answer(a, r, CURE_NO_TOKEN, -INFINITY, 0); }
+
+// A row's map from values to weights.
+struct Scale {
+  double m, inv_t, limit;            // limit: 64 T
+  CURE_DEV double below(float x) const { return m - (double)x; }
+  CURE_DEV bool has(float x) const { return below(x) <= limit; }
+  CURE_DEV double weight(float x) const { return exp(-below(x) * inv_t); }
+};
+CURE_DEV Scale scale_of(float high, float t) {
+  const double td = t == 0.f ? 1.0 : (double)t;    // T = 0: only what equals the maximum
+  return Scale{(double)high, 1.0 / td, t == 0.f ? 0.0 : kRange * td};
+}
+
+// Sums over the wave.
+template <int kStage>
+CURE_DEV double with_partner(double v) {
+  return v + __hiloint2double(cure::partner<kStage>(__double2hiint(v)), cure::partner<kStage>(__double2loint(v)));
+}
+CURE_DEV double wave_sum(double x) {
+  x = with_partner<1>(x);
+  x = with_partner<2>(x);
+  x = with_partner<4>(x);
+  x = with_partner<8>(x);
+  x = with_partner<16>(x);
+  return with_partner<32>(x);
+}
+CURE_DEV int wave_sum(int x) {
+  x += cure::partner<1>(x);
+  x += cure::partner<2>(x);
+  x += cure::partner<4>(x);
+  x += cure::partner<8>(x);
+  x += cure::partner<16>(x);
+  return x + cure::partner<32>(x);
+}
+
+// Entries and their weight.
+struct Amount {
+  int n;
+  double w;
+};
+CURE_DEV Amount operator+(Amount a, Amount b) { return Amount{a.n + b.n, a.w + b.w}; }
+CURE_DEV Amount lane_of(Amount a, int lane) { return Amount{__shfl(a.n, lane), __shfl(a.w, lane)}; }
+// Sum over the lanes up to this one.
+CURE_DEV Amount wave_scan(Amount a) {
+  for (int d = 1; d < kWave; d *= 2) {
+    const Amount up{__shfl_up(a.n, d), __shfl_up(a.w, d)};
+    if (lane_id() >= d) a = a + up;
+  }
+  return a;
+}
+
+// A bin in the order: what lies before it, and what it holds.
+struct Found {
+  int pos;
+  Amount before, in;
+};
+
+// The bins of a row for one wave: kGroups groups of 64 positions in descending order of value, whose
+// sums lie in LDS; bin(pos) gives what a position holds.
+template <int kGroups, typename Bin>
+struct Order {
+  static constexpr int kEach = kGroups / kWave;    // groups of a lane
+  Bin bin;
+  Amount group[kEach], before, upto;               // of the lane
+
+  CURE_DEV Order(const int* n, const double* w, Bin b) : bin(b) {
+    Amount mine{0, 0.0};
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      group[j] = Amount{n[lane_id() * kEach + j], w[lane_id() * kEach + j]};
+      mine = mine + group[j];
+    }
+    upto = wave_scan(mine);
+    const Amount up{__shfl_up(upto.n, 1), __shfl_up(upto.w, 1)};
+    before = lane_id() ? up : Amount{0, 0.0};
+  }
+  CURE_DEV Amount all() const { return lane_of(upto, kWave - 1); }
+
+  // The first position that holds something and up to which hit(amount) is true; where rounding
+  // keeps it from being so, the last one that holds something. There has to be one.
+  template <typename Hit>
+  CURE_DEV Found find(const Hit& hit) const {
+    const bool any = upto.n > before.n;
+    unsigned long long is = __ballot(any && hit(upto));
+    const int lane = is ? __ffsll(is) - 1 : 63 - __clzll(__ballot(any));
+    int at = -1;
+    bool sure = false;
+    Amount run = before, base = before;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const Amount next = run + group[j];
+      if (group[j].n > 0 && !sure) {
+        at = j;
+        base = run;
+        sure = hit(next);
+      }
+      run = next;
+    }
+    const int g = lane * kEach + __shfl(at, lane);
+    base = lane_of(base, lane);
+    const Amount in = bin(g * kWave + lane_id());
+    const Amount sum = wave_scan(in);
+    is = __ballot(in.n > 0 && hit(base + sum));
+    const int l = is ? __ffsll(is) - 1 : 63 - __clzll(__ballot(in.n > 0));
+    const Amount here = lane_of(in, l), up{__shfl_up(sum.n, 1), __shfl_up(sum.w, 1)};
+    return Found{g * kWave + l, l ? base + lane_of(up, l) : base, here};
+  }
+};
+
+// How many of n entries of weight `each` behind `before` reach (or pass) a target.
+CURE_DEV int ties_to(double target, Amount before, Amount in, bool pass) {
+  const double each = in.w / in.n, x = (target - before.w) / each;
+  return (int)fmin((double)in.n, fmax(1.0, pass ? floor(x) + 1.0 : ceil(x)));
+}
+
+// ---------------------------------------------------------------------------
+// Any values, and fp32 in general: bins of width T / 64 below the maximum. Relative to its upper edge an entry of a
+// bin has a weight in (exp(-1/64), 1], and 2^44 times it, rounded, leaves room for 2^20 of them
+// in an integer. The bin of a place is gathered and put in order; where it holds too many entries
+// it is divided by their keys until it holds a single value.
+constexpr int kBins = 4096;
+constexpr int kPer = kBins / kThreads;             // bins of a thread
+constexpr int kGroups = kBins / kWave;
+constexpr double kUnit = 0x1p44;
 
 // Order-preserving integer of a finite value; both zeros alike.
 CURE_DEV uint32_t key_of(float x) {
@@ -66,6 +212,15 @@ CURE_DEV double exp_small(double y) {
   return fma(-y, p, 1.0);
 }
 
+struct Binned : Scale {
+  CURE_DEV int bin(float x) const { return min((int)(below(x) * inv_t * kRange), kBins - 1); }
+  // Units of exp(-bin / 64) that an entry of the bin has.
+  CURE_DEV unsigned long long units(float x, int bin) const {
+    return (unsigned long long)rint(kUnit * exp_small(fmax(fma(below(x), inv_t, -bin * (1.0 / kRange)), 0.0)));
+  }
+};
+CURE_DEV double edge(int bin) { return exp(-bin * (1.0 / kRange)) / kUnit; }
+
 // A place in the order: the entries before it, their weight.
 struct Place {
   int count;
@@ -83,7 +238,6 @@ enum Query { kCount, kMass, kDraw, kValue };       // entries, weight reached, w
 struct Shared {
   uint32_t cnt[kBins];
   unsigned long long mass[kBins];
-  // Saved scan of the first histogram.
   uint32_t sum_cnt[kWaves];
   double sum_mass[kWaves];
   uint32_t found_bin;
@@ -91,21 +245,21 @@ struct Shared {
   uint32_t lo, hi;
   uint32_t seg[kWaves];
   float max[kWaves];
+  // For places found in the first histogram.
+  int group_n[kGroups];
+  double group_w[kGroups];
+  Found at;
+  int query;
+  double target;
+  Amount run;
+  int listed;
+  uint32_t key[kList];
+  int index[kList];
+  int order[kList];
 };
 
-// A row's map from values to weights and bins.
-struct Scale {
-  double m, inv_t, limit;            // 64 T
-  CURE_DEV double below(float x) const { return m - (double)x; }
-  CURE_DEV bool has(float x) const { return below(x) <= limit; }
-  CURE_DEV int bin(float x) const { return min((int)(below(x) * inv_t * kRange), kBins - 1); }
-  CURE_DEV double weight(float x) const { return exp(-below(x) * inv_t); }
-  // Units of exp(-bin / 64) that an entry of the bin has.
-  CURE_DEV unsigned long long units(float x, int bin) const {
-    return (unsigned long long)rint(kUnit * exp_small(fmax(fma(below(x), inv_t, -bin * (1.0 / kRange)), 0.0)));
-  }
-};
-CURE_DEV double edge(int bin) { return exp(-bin * (1.0 / kRange)) / kUnit; }
+CURE_DEV float widen(uint16_t x) { return bf16_to_f32(x); }
+CURE_DEV float widen(float x) { return x; }
 
 template <typename E>
 struct Row {
@@ -113,7 +267,28 @@ struct Row {
   int vocab;
   template <typename F>
   CURE_DEV void each(F&& f) const {
-    for (int i = threadIdx.x; i < vocab; i += kThreads) f(widen(x[i]), i);
+    each_at([&](float v, int) { f(v); });
+  }
+  template <typename F>
+  CURE_DEV void each_at(F&& f) const {
+    constexpr int kAhead = 4;
+    if (sizeof(E) == 2) {
+      for (int i = threadIdx.x; i < vocab; i += kThreads) f(widen(x[i]), i);
+      return;
+    }
+    int i = threadIdx.x * 4;
+    for (; i + (kAhead - 1) * 4 * kThreads + 4 <= vocab; i += kAhead * 4 * kThreads) {
+      u32x4 w[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) __builtin_memcpy(&w[u], x + i + u * 4 * kThreads, 16);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f(__uint_as_float(w[u][j]), i + u * 4 * kThreads + j);
+    }
+    for (; i < vocab; i += 4 * kThreads)
+      for (int j = 0; j < 4; ++j)
+        if (i + j < vocab) f(widen(x[i + j]), i + j);
   }
 };
 
@@ -207,7 +382,7 @@ CURE_DEV int find_bin(Shared& sh, const Place& base, W&& weight, Hit&& hit) {
 // The run of `query`: count entries, or weight `target`, or values from key `from` on, at most
 // `most` entries. sh holds the first histogram, which is made again where it was replaced.
 template <typename E>
-CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Scale& sc, Query query, int count, double target, uint32_t from) {
+CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Binned& sc, Query query, int count, double target, uint32_t from) {
   const int tid = threadIdx.x;
   const auto hit = [&](const Place& upto) {
     return query == kCount ? upto.count >= count : query == kMass ? upto.mass >= target : upto.mass > target;
@@ -219,7 +394,7 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Scale& sc, Query quer
     sh.mass[i] = 0;
   }
   __syncthreads();
-  row.each([&](float x, int) {
+  row.each([&](float x) {
     if (!sc.has(x)) return;
     const int bin = sc.bin(x);
     atomicAdd(&sh.cnt[bin], 1u);
@@ -237,7 +412,7 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Scale& sc, Query quer
     sh.hi = 0;
   }
   __syncthreads();
-  row.each([&](float x, int) {
+  row.each([&](float x) {
     if (!sc.has(x) || sc.bin(x) != bin) return;
     atomicMin(&sh.lo, key_of(x));
     atomicMax(&sh.hi, key_of(x));
@@ -256,7 +431,7 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Scale& sc, Query quer
       sh.mass[i] = 0;
     }
     __syncthreads();
-    row.each([&](float x, int) {
+    row.each([&](float x) {
       if (!sc.has(x) || sc.bin(x) != bin) return;
       const uint32_t k = key_of(x);
       if (k < lo || k > hi) return;
@@ -289,28 +464,104 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Scale& sc, Query quer
   }
 }
 
+// The entry up to which the row's order has `count` entries, or weight `target`: found in the first
+// histogram, whose groups are summed, by gathering its bin. False: the bin holds too many.
+struct Entry {
+  uint32_t key;
+  int index;
+  Amount upto;
+};
 template <typename E>
-__global__ __launch_bounds__(kThreads) void sample_rows(Args a) {
-  __shared__ Shared sh;
+CURE_DEV bool find_entry(Shared& sh, const Row<E>& row, const Binned& sc, Query query, int count, double target, Entry& out) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int b = blockIdx.x / a.rows, n = blockIdx.x % a.rows;
-  const int64_t r = blockIdx.x;
-  const float t = a.temperature ? a.temperature[b] : 1.f, top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
-  const int top_k = a.top_k ? a.top_k[b] : 0;
-  const float u = a.uniform[r];
-  const auto answer = [&](int token, float logprob, int kept) {
-    a.token[r] = token;
-    if (a.logprob) a.logprob[r] = logprob;
-    if (a.kept) a.kept[r] = kept;
-  };
-  if ((a.n_rows && n >= a.n_rows[b]) || !(t >= 0.f) || t == INFINITY || top_p != top_p || min_p != min_p || u != u) {
-    if (tid == 0) answer(CURE_NO_TOKEN, -INFINITY, 0);
-    return;
+  const auto hit = [&](Amount x) { return query == kCount ? x.n >= count : query == kMass ? x.w >= target : x.w > target; };
+  __syncthreads();
+  if (wave == 0) {
+    const auto holds = [&](int pos) {
+      const int n = (int)sh.cnt[pos];
+      return Amount{n, n ? (double)sh.mass[pos] * edge(pos) : 0.0};
+    };
+    const Order<kGroups, decltype(holds)> order(sh.group_n, sh.group_w, holds);
+    const Found f = order.find(hit);
+    if (lane == 0) {
+      sh.at = f;
+      sh.listed = 0;
+    }
   }
+  __syncthreads();
+  const Found f = sh.at;
+  if (f.in.n > kList) return false;
+  row.each_at([&](float x, int i) {
+    if (!sc.has(x) || sc.bin(x) != f.pos) return;
+    const int k = atomicAdd(&sh.listed, 1);
+    sh.key[k] = key_of(x);
+    sh.index[k] = i;
+  });
+  __syncthreads();
+  const int n = f.in.n;
+  for (int i = tid; i < n; i += kThreads) {
+    const uint32_t k = sh.key[i];
+    const int at = sh.index[i];
+    int before = 0;
+    for (int j = 0; j < n; ++j) before += sh.key[j] > k || (sh.key[j] == k && sh.index[j] < at);
+    sh.order[before] = i;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const double unit = edge(f.pos);
+    int found = n - 1;
+    Amount upto = f.before;
+    unsigned long long sum = 0;
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+      const int i = min(i0 + lane, n - 1);
+      unsigned long long u = i0 + lane < n ? sc.units(value_of(sh.key[sh.order[i]]), f.pos) : 0;
+      for (int d = 1; d < kWave; d *= 2) {
+        const unsigned long long up = __shfl_up(u, d);
+        if (lane >= d) u += up;
+      }
+      const Amount here{f.before.n + i + 1, f.before.w + (double)(sum + u) * unit};
+      const unsigned long long is = __ballot(i0 + lane < n && hit(here));
+      const int l = is ? __ffsll(is) - 1 : min(kWave, n - i0) - 1;
+      upto = lane_of(here, l);
+      if (is) {
+        found = i0 + l;
+        break;
+      }
+      sum += __shfl(u, kWave - 1);
+    }
+    if (lane == 0) {
+      sh.lo = sh.key[sh.order[found]];
+      sh.query = sh.index[sh.order[found]];
+      sh.run = upto;
+    }
+  }
+  __syncthreads();
+  out = Entry{sh.lo, sh.query, sh.run};
+  return true;
+}
+
+// The smallest key whose weight reaches min_p, which is at most 1.
+CURE_DEV uint32_t key_from(const Binned& sc, float min_p) {
+  uint32_t lo = key_of((float)(sc.m - sc.limit)), hi = key_of((float)sc.m);
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (sc.weight(value_of(mid)) >= (double)min_p) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+template <typename E>
+CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const Row<E> row{static_cast<const E*>(a.logits) + r * a.ld, a.vocab};
   float high = -INFINITY;
   bool bad = false;
-  row.each([&](float x, int) {
+  for (int i = tid; i < kBins; i += kThreads) {
+    sh.cnt[i] = 0;
+    sh.mass[i] = 0;
+  }
+  row.each([&](float x) {
     bad = bad || !(x < INFINITY);
     high = fmaxf(high, x);
   });
@@ -319,55 +570,391 @@ __global__ __launch_bounds__(kThreads) void sample_rows(Args a) {
   bad = __syncthreads_or(bad);
   for (int w = 0; w < kWaves; ++w) high = fmaxf(high, sh.max[w]);
   if (bad || high == -INFINITY) {
-    if (tid == 0) answer(CURE_NO_TOKEN, -INFINITY, 0);
+    if (tid == 0) no_answer(a, r);
     return;
   }
-  const double td = t == 0.f ? 1.0 : (double)t;
-  const Scale sc{(double)high, 1.0 / td, t == 0.f ? 0.0 : kRange * td};
-  Run run, drawn;
-  if (t == 0.f) {
-    run = drawn = Run{key_of(high), 1, 1, 1.0};
+  const Binned sc{scale_of(high, s.t)};
+  const double u = fmax(0.0, (double)s.u), top_p = fmax(0.0, (double)s.top_p);
+  // The first histogram, and its groups' sums.
+  row.each([&](float x) {
+    if (!sc.has(x)) return;
+    const int bin = sc.bin(x);
+    atomicAdd(&sh.cnt[bin], 1u);
+    atomicAdd(&sh.mass[bin], sc.units(x, bin));
+  });
+  __syncthreads();
+  for (int g = wave; g < kGroups; g += kWaves) {
+    const int pos = g * kWave + lane, n = (int)sh.cnt[pos];
+    Amount sum{0, 0.0};
+    if (__ballot(n > 0)) sum = Amount{wave_sum(n), wave_sum(n ? (double)sh.mass[pos] * edge(pos) : 0.0)};
+    if (lane == 0) {
+      sh.group_n[g] = sum.n;
+      sh.group_w[g] = sum.w;
+    }
+  }
+  __syncthreads();
+  Amount run{0, 0.0};
+  for (int g = 0; g < kGroups; ++g) run = run + Amount{sh.group_n[g], sh.group_w[g]};
+  const Amount whole = run;
+  const bool by_k = s.t > 0.f && s.top_k > 0 && s.top_k < run.n, by_p = s.t > 0.f && s.top_p < 1.f, by_min = s.t > 0.f && s.min_p > 0.f;
+  Entry e;
+  bool quick = true;
+  if (s.t == 0.f) {
+    run = Amount{1, 1.0};
+    quick = find_entry(sh, row, sc, kCount, 1, 0.0, e);
   } else {
-    run = find_run(sh, row, sc, kCount, top_k > 0 ? min(top_k, a.vocab) : a.vocab, 0.0, 0);
-    if (top_p < 1.f) {
-      const Run p = find_run(sh, row, sc, kMass, 0, fmax(0.0, (double)top_p) * run.mass, 0);
-      if (p.count < run.count) run = p;
-    }
-    if (min_p > 0.f) {
-      // The smallest key whose weight reaches min_p (the maximum's does, or is kept all the same).
-      uint32_t lo = key_of((float)(sc.m - sc.limit)), hi = key_of(high);
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (sc.weight(value_of(mid)) >= (double)min_p) hi = mid;
-        else lo = mid + 1;
+    if (by_k && (quick = find_entry(sh, row, sc, kCount, s.top_k, 0.0, e))) run = e.upto;
+    if (quick && by_p && (quick = find_entry(sh, row, sc, kMass, 0, top_p * run.w, e)) && e.upto.n < run.n) run = e.upto;
+    if (quick && by_min) {
+      if (s.min_p > 1.f) {
+        run = Amount{1, 1.0};
+      } else {
+        // How many reach min_p; then as a count.
+        const float from = value_of(key_from(sc, s.min_p));
+        int n = 0;
+        row.each([&](float x) { n += x >= from; });
+        n = wave_sum(n);
+        __syncthreads();
+        if (lane == 0) sh.seg[wave] = n;
+        __syncthreads();
+        n = 0;
+        for (int w = 0; w < kWaves; ++w) n += sh.seg[w];
+        n = max(1, min(n, whole.n));
+        if (n < run.n && (quick = find_entry(sh, row, sc, kCount, n, 0.0, e))) run = e.upto;
       }
-      const bool one = !(1.f >= min_p);
-      const Run v = one ? Run{key_of(high), 1, 1, 1.0} : find_run(sh, row, sc, kValue, 0, 0.0, lo);
-      if (v.count < run.count) run = v;
     }
-    drawn = find_run(sh, row, sc, kDraw, 0, fmax(0.0, (double)u) * run.mass, 0);
+    if (quick) quick = find_entry(sh, row, sc, kDraw, 0, u * run.w, e);
+    if (quick && e.upto.n > run.n) quick = find_entry(sh, row, sc, kCount, run.n, 0.0, e);
+  }
+  if (quick) {
+    if (tid == 0) answer(a, r, e.index, (float)(-sc.below(value_of(e.key)) * sc.inv_t - log(run.w)), run.n);
+    return;
+  }
+  // A bin that holds too many: by keys.
+  Run kept{key_of(high), 1, 1, 1.0}, drawn = kept;
+  if (s.t > 0.f) {
+    kept = Run{0, 0, whole.n, whole.w};
+    if (by_k) kept = find_run(sh, row, sc, kCount, s.top_k, 0.0, 0);
+    if (by_p) {
+      const Run p = find_run(sh, row, sc, kMass, 0, top_p * kept.mass, 0);
+      if (p.count < kept.count) kept = p;
+    }
+    if (by_min) {
+      const Run v = s.min_p > 1.f ? Run{key_of(high), 1, 1, 1.0} : find_run(sh, row, sc, kValue, 0, 0.0, key_from(sc, s.min_p));
+      if (v.count < kept.count) kept = v;
+    }
+    drawn = find_run(sh, row, sc, kDraw, 0, u * kept.mass, 0);
     // Rounding, or a number of one and more: the last entry kept.
-    if (drawn.count > run.count) drawn = find_run(sh, row, sc, kCount, run.count, 0.0, 0);
+    if (drawn.count > kept.count) drawn = find_run(sh, row, sc, kCount, kept.count, 0.0, 0);
   }
   // The drawn.ties-th entry of that value, by index: waves count in parts of the row.
   const int part = ((a.vocab + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
   const int i0 = wave * part, i1 = min(i0 + part, a.vocab);
+  const auto is_it = [&](int i) {
+    const float x = widen(row.x[min(i, a.vocab - 1)]);
+    return i < i1 && x > -INFINITY && key_of(x) == drawn.key;
+  };
   int found = 0;
-  for (int i = i0 + lane; i - lane < i1; i += kWave)
-    found += __popcll(__ballot(i < i1 && widen(row.x[min(i, a.vocab - 1)]) > -INFINITY && key_of(widen(row.x[min(i, a.vocab - 1)])) == drawn.key));
+  for (int i = i0; i < i1; i += kWave) found += __popcll(__ballot(is_it(i + lane)));
+  __syncthreads();
   if (lane == 0) sh.seg[wave] = found;
   __syncthreads();
   int before = 0;
   for (int w = 0; w < wave; ++w) before += sh.seg[w];
-  if (before < drawn.ties && before + found >= drawn.ties) {
-    for (int i = i0 + lane; i - lane < i1; i += kWave) {
-      const bool is = i < i1 && key_of(widen(row.x[min(i, a.vocab - 1)])) == drawn.key;
-      const unsigned long long hits = __ballot(is);
-      const int here = __popcll(hits & ((1ull << lane) - 1));
-      if (is && before + here + 1 == drawn.ties)
-        answer(i, (float)(-sc.below(value_of(drawn.key)) * sc.inv_t - log(run.mass)), run.count);
-      before += __popcll(hits);
+  if (before >= drawn.ties || before + found < drawn.ties) return;
+  for (int i = i0; i < i1; i += kWave) {
+    const bool is = is_it(i + lane);
+    const unsigned long long hits = __ballot(is);
+    const int here = __popcll(hits & ((1ull << lane) - 1));
+    if (is && before + here + 1 == drawn.ties)
+      answer(a, r, i + lane, (float)(-sc.below(value_of(drawn.key)) * sc.inv_t - log(kept.mass)), kept.count);
+    before += __popcll(hits);
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void sample_f32(Args a) {
+  __shared__ Shared sh;
+  const int64_t r = blockIdx.x;
+  const Settings s = settings_of(a, r);
+  if (!s.none) sample_any<float>(sh, a, r, s);
+  else if (threadIdx.x == 0) no_answer(a, r);
+}
+
+// ---------------------------------------------------------------------------
+// bf16: a bin is a value, of which [2^-32, 2^32) has 64 octaves of 128 to either sign, and zero. Weights
+// are formed once for each bin in use, so that an entry costs a few packed integer instructions
+// and one LDS addition. Rows with other magnitudes that count go the general way.
+constexpr int kOctaves = 64 * 128;                 // bins of one sign
+constexpr int kBins16 = 2 * kOctaves;
+constexpr uint32_t kFirst16 = (127 - 32) << 7;     // bits of 2^-32
+constexpr int kLowest = 1, kHighest = kBins16 - 1; // the bins of the largest magnitudes
+constexpr uint32_t kMinusInf2 = 0xff80ff80u;
+constexpr int kGroups16 = kBins16 / kWave;
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+CURE_DEV u16x2 both(uint32_t x) { return __builtin_bit_cast(u16x2, x * 0x10001u); }
+// Bins of two values.
+CURE_DEV u16x2 bins_of(uint32_t w) {
+  const u16x2 mag = __builtin_bit_cast(u16x2, w & 0x7fff7fffu);
+  const u16x2 t = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, both(kFirst16)), both(kOctaves - 1));
+  const i16x2 sign = __builtin_bit_cast(i16x2, w) >> 15;
+  const i16x2 x = (__builtin_bit_cast(i16x2, t) ^ sign) - sign;
+  return __builtin_bit_cast(u16x2, x) + both(kOctaves);
+}
+CURE_DEV float value_of_bin(int bin) {
+  const int t = abs(bin - kOctaves);
+  const float x = __uint_as_float(t ? (uint32_t)(t + kFirst16) << 16 : 0u);
+  return bin < kOctaves ? -x : x;
+}
+
+struct Shared16 {
+  int cnt[kBins16];
+  int idle[kWave];                   // takes what lies in the lowest bin, as masked entries do: no bin in use
+  int group_n[kGroups16];
+  double group_w[kGroups16];
+  int list[kList];
+  int listed, bad, lowest, high, reach, other;
+  int bin, ties, kept;
+  float logprob;
+  int seg[kWaves];
+};
+
+// A row's entries as 16-byte vectors: vector i * kThreads + thread for i < n, entries past the end
+// as -inf.
+struct Row16 {
+  const uint16_t* x;
+  int vocab, n;
+
+  // Index of the vector's first entry: the last vectors overlap, and what they repeat is -inf.
+  CURE_DEV int first(int i) const { return max(min((i * kThreads + (int)threadIdx.x) * 8, vocab - 8), 0); }
+  CURE_DEV u32x4 load(int i) const {
+    u32x4 w;
+    if (vocab >= 8) {
+      __builtin_memcpy(&w, x + first(i), 16);      // rows need not begin with 16 bytes
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = x[min(2 * j, vocab - 1)] | (uint32_t)x[min(2 * j + 1, vocab - 1)] << 16;
     }
+    return w;
+  }
+  CURE_DEV u32x4 masked(u32x4 w, int i) const {
+    const int at = (i * kThreads + (int)threadIdx.x) * 8, f = first(i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool is = f + j >= at && f + j < vocab;
+      if (!is) w[j / 2] = j % 2 ? (w[j / 2] & 0xffffu) | (kMinusInf2 & 0xffff0000u) : (w[j / 2] & 0xffff0000u) | (kMinusInf2 & 0xffffu);
+    }
+    return w;
+  }
+  // f(vector, i) for each, kAhead of whose loads are under way at a time.
+  static constexpr int kAhead = 4;
+  // Entries past the end that it goes over.
+  CURE_DEV int padding() const { return (n + kAhead - 1) / kAhead * kAhead * kThreads * 8 - vocab; }
+  template <typename F>
+  CURE_DEV void each(const F& f) const {
+#pragma unroll 1
+    for (int i = 0; i < n; i += kAhead) {
+      u32x4 w[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) w[u] = load(min(i + u, n - 1));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) f(i + u < n - 1 ? w[u] : masked(w[u], i + u), i + u);
+    }
+  }
+};
+
+__global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
+  __shared__ union {
+    Shared16 own;
+    Shared any;
+  } space;
+  Shared16& sh = space.own;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int64_t r = blockIdx.x;
+  const Settings s = settings_of(a, r);
+  if (s.none) {
+    if (tid == 0) no_answer(a, r);
+    return;
+  }
+  const Row16 row{static_cast<const uint16_t*>(a.logits) + r * a.ld, a.vocab, (a.vocab + 8 * kThreads - 1) / (8 * kThreads)};
+  for (int i = tid; i < kBins16 / 4; i += kThreads) reinterpret_cast<u32x4*>(sh.cnt)[i] = u32x4{0, 0, 0, 0};
+  if (tid < kWave) sh.idle[tid] = 0;
+  if (tid == 0) {
+    sh.listed = sh.bad = sh.lowest = sh.reach = sh.other = 0;
+    sh.high = -1;
+  }
+  __syncthreads();
+  row.each([&](const u32x4& w, int) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u16x2 b = bins_of(w[j]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) atomicAdd(b[e] == kLowest ? &sh.idle[lane] : &sh.cnt[b[e]], 1);
+    }
+  });
+  __syncthreads();
+  // Bins that stand for more than one value, rare but for -inf: NaNs and +inf, how many are
+  // finite in the lowest, and whether others have magnitudes that have no bins.
+  bool odd = sh.cnt[kHighest] > 0 || sh.cnt[kOctaves] > 0;
+  if (wave == 0) odd = odd || wave_sum(sh.idle[lane]) != row.padding();
+  if (__syncthreads_or(odd)) {
+    int low = 0;
+    bool bad = false, other = false;
+    row.each([&](const u32x4& w, int) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t v = w[j / 2] >> (j % 2 * 16) & 0xffffu, mag = v & 0x7fffu;
+        const int bin = bins_of(v)[0];
+        bad = bad || mag > 0x7f80u || v == 0x7f80u;
+        low += v < 0xff80u && bin == kLowest;
+        other = other || bin == kHighest || (bin == kOctaves && mag != 0);
+      }
+    });
+    low = wave_sum(low);
+    if (lane == 0 && low) atomicAdd(&sh.lowest, low);
+    if (bad) sh.bad = 1;
+    if (other) sh.other = 1;
+    __syncthreads();
+  }
+  // The highest bin in use: a wave's first group that has any.
+  for (int g = wave; g < kGroups16; g += kWaves) {
+    const int bin = kBins16 - 1 - (g * kWave + lane);
+    const unsigned long long used = __ballot(sh.cnt[bin] > 0);
+    if (!used) continue;
+    if (lane == 0) atomicMax(&sh.high, kBins16 - 1 - (g * kWave + __ffsll(used) - 1));
+    break;
+  }
+  __syncthreads();
+  if (sh.bad || (sh.high < 0 && sh.lowest == 0)) {
+    if (tid == 0) no_answer(a, r);
+    return;
+  }
+  const Scale sc = scale_of(value_of_bin(max(sh.high, kLowest)), s.t);
+  if (sh.other || (sh.lowest > 0 && (sh.high < 0 || sc.has(value_of_bin(kLowest))))) {
+    __syncthreads();
+    sample_any<uint16_t>(space.any, a, r, s);
+    return;
+  }
+  // What position `pos` of the order holds: bins from the top down.
+  const auto holds = [&](int pos) {
+    const int bin = kBins16 - 1 - pos, n = sh.cnt[bin];
+    const float x = value_of_bin(bin);
+    if (n == 0 || !sc.has(x)) return Amount{0, 0.0};
+    return Amount{n, n * sc.weight(x)};
+  };
+  int reach = 0;                                   // entries whose weight is at least min_p
+#pragma unroll 1
+  for (int g = wave; g < kGroups16; g += kWaves) {
+    const Amount in = holds(g * kWave + lane);
+    Amount sum{0, 0.0};
+    if (__ballot(in.n > 0)) {
+      if (in.w >= in.n * (double)s.min_p) reach += in.n;
+      sum = Amount{wave_sum(in.n), wave_sum(in.w)};
+    }
+    if (lane == 0) {
+      sh.group_n[g] = sum.n;
+      sh.group_w[g] = sum.w;
+    }
+  }
+  reach = wave_sum(reach);
+  if (lane == 0 && reach) atomicAdd(&sh.reach, reach);
+  __syncthreads();
+  if (wave == 0) {
+    const Order<kGroups16, decltype(holds)> order(sh.group_n, sh.group_w, holds);
+    Amount run = s.t == 0.f ? Amount{1, 1.0} : order.all();    // what is kept so far
+    Found f{0, {0, 0.0}, {0, 0.0}};
+    int ties = 0;
+    // top-k, top-p, min-p, the token; and the last entry kept, where rounding or a number of one
+    // and more lead past it.
+#pragma unroll 1
+    for (int q = s.t == 0.f ? 3 : 0; q < 5; ++q) {
+      int n = 0;                                   // so many entries, or (0) a weight
+      double target = 0.0;
+      if (q == 0) {
+        if (s.top_k <= 0 || s.top_k >= run.n) continue;
+        n = s.top_k;
+      } else if (q == 1) {
+        if (!(s.top_p < 1.f)) continue;
+        target = fmax(0.0, (double)s.top_p) * run.w;
+      } else if (q == 2) {
+        n = max(1, sh.reach);
+        if (!(s.min_p > 0.f) || n >= run.n) continue;
+      } else if (q == 3) {
+        target = fmax(0.0, (double)s.u) * run.w;
+      } else {
+        if (f.before.n + ties <= run.n) break;
+        n = run.n;
+      }
+      f = order.find([&](Amount x) { return n ? x.n >= n : q == 1 ? x.w >= target : x.w > target; });
+      ties = n ? min(n - f.before.n, f.in.n) : ties_to(target, f.before, f.in, q == 3);
+      const Amount upto = f.before + Amount{ties, ties * (f.in.w / f.in.n)};
+      if (q < 3 && upto.n < run.n) run = upto;
+    }
+    if (lane == 0) {
+      const int bin = kBins16 - 1 - f.pos;
+      sh.bin = bin;
+      sh.ties = ties;
+      sh.kept = run.n;
+      sh.logprob = (float)(-sc.below(value_of_bin(bin)) * sc.inv_t - log(run.w));
+    }
+  }
+  __syncthreads();
+  // The ties-th entry of that value, by index.
+  const int bin = sh.bin, n = sh.cnt[bin];
+  // Zero where a word's entries have the bin's value.
+  const bool zero = bin == kOctaves;
+  const u16x2 bits = both(__float_as_uint(value_of_bin(bin)) >> 16);
+  const auto off = [&](uint32_t w) { return (u16x2)(__builtin_bit_cast(u16x2, zero ? w & 0x7fff7fffu : w) ^ bits); };
+  if (n <= kList) {
+    row.each([&](const u32x4& w, int i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u16x2 x = off(w[j]);
+        if (x[0] == 0) sh.list[atomicAdd(&sh.listed, 1)] = row.first(i) + 2 * j;
+        if (x[1] == 0) sh.list[atomicAdd(&sh.listed, 1)] = row.first(i) + 2 * j + 1;
+      }
+    });
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+      const int me = sh.list[i];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += sh.list[j] < me;
+      if (before == sh.ties - 1) answer(a, r, me, sh.logprob, sh.kept);
+    }
+    return;
+  }
+  // Many: counted by vectors, waves and lanes, in the entries' order.
+  int left = sh.ties;
+  for (int i = 0; i < row.n; ++i) {
+    const u32x4 w = row.masked(row.load(i), i);
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u16x2 x = off(w[j]);
+      mine += (x[0] == 0) + (x[1] == 0);
+    }
+    const int upto = wave_scan(Amount{mine, 0.0}).n;
+    if (lane == kWave - 1) sh.seg[wave] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int k = 0; k < kWaves; ++k) {
+      before += k < wave ? sh.seg[k] : 0;
+      all += sh.seg[k];
+    }
+    before += upto - mine;
+    if (before < left && before + mine >= left) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u16x2 x = off(w[j]);
+        if (x[0] == 0 && ++before == left) answer(a, r, row.first(i) + 2 * j, sh.logprob, sh.kept);
+        if (x[1] == 0 && ++before == left) answer(a, r, row.first(i) + 2 * j + 1, sh.logprob, sh.kept);
+      }
+    }
+    left -= all;
+    __syncthreads();
+    if (left <= 0) return;
   }
 }
 
@@ -376,21 +963,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows(Args a) {
 
 using namespace cure;
 
-extern "C" size_t cure_sample_workspace_size(int32_t batch, int32_t rows, int32_t vocab) {
-  (void)batch;
-  (void)rows;
-  (void)vocab;
-  return 0;
-}
-
 extern "C" cure_status cure_sample(const void* logits, int32_t dtype, int32_t batch, int32_t rows,
                                    int32_t vocab, int64_t ld, const float* temperature,
                                    const int32_t* top_k, const float* top_p, const float* min_p,
                                    const float* uniform, const int32_t* n_rows, int32_t* token,
-                                   float* logprob, int32_t* kept, void* workspace, size_t workspace_bytes,
-                                   void* stream) {
-  (void)workspace;
-  (void)workspace_bytes;
+                                   float* logprob, int32_t* kept, void* stream) {
   if (dtype != CURE_F32 && dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
   if (batch < 0 || rows < 0 || vocab < 1 || ld < vocab) return CURE_ERR_INVALID_ARG;
   if (vocab > kMaxVocab) return CURE_ERR_UNSUPPORTED;
@@ -401,7 +978,8 @@ extern "C" cure_status cure_sample(const void* logits, int32_t dtype, int32_t ba
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == CURE_BF16 ? 2 : 4)) return CURE_ERR_INVALID_ARG;
   const Args a{logits, rows, vocab, ld, temperature, top_k, top_p, min_p, uniform, n_rows, token, logprob, kept};
   const dim3 grid((unsigned)total), block(kThreads);
-  if (dtype == CURE_BF16) hipLaunchKernelGGL((sample_rows<uint16_t>), grid, block, 0, as_stream(stream), a);
-  else hipLaunchKernelGGL((sample_rows<float>), grid, block, 0, as_stream(stream), a);
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, as_stream(stream), a); };
+  if (dtype == CURE_F32) run(sample_f32);
+  else run(sample_bf16);
   return launch_status();
 }

@@ -93,9 +93,8 @@ _SIGNATURES = {
     "cure_packed_attn": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i32, _i32,
                                         _i64, _i32, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                         _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
-    "cure_sample_workspace_size": (_sz, [_i32, _i32, _i32]),
     "cure_sample": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
-                                   _vp, _sz, _vp]),
+                                   _vp]),
 }
 
 
