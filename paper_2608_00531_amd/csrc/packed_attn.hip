@@ -10,7 +10,7 @@
 // whose values are small both have P in the range of 16 bits where they count at all.
 //
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
-// a power of two for each row: what that loses is below 2^-40 of the row's largest. P is rounded
+// a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
 // to fp16 for its product, 2^-12 where bf16 would take 2^-9 and add half as much again to the error that the
 // output's own rounding makes. Open rows keep bf16's range: their products take P as two bf16 values.
 // fp32: fp32 throughout.
@@ -23,7 +23,11 @@
 //        registers 8 t .. 8 t + 7, B = those; D register r of block i = column 32 i + 8 (r / 4)
 //        + 4 half + r % 4 of query row col.
 // A packed block lies in memory as A wants it, 16 bytes to a lane: packed steps need no
-// exchange between lanes.
+// exchange between lanes. Many rows share what is widened through LDS, by 16x16x32 instructions and 16
+// rows per wave, which leaves room for four waves to a SIMD:
+//   lane l = 16 quad + col owns query row col and the scores of tokens 16 i + 4 quad + r;
+//   S^T: A = token col's columns 32 s + 8 quad .. +7;  O^T: A = column 16 i + col of the lane's
+//        eight tokens, D register r of block i = column 16 i + 4 quad + r.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -42,9 +46,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 32;            // tokens per step of the key loop
-constexpr int kWaves = 4;            // waves per workgroup
-constexpr int kRows = 32;            // query rows of a wave
-constexpr int kMaxGroups = 4;        // row groups of a workgroup at most
+constexpr int kWaves = 4;            // waves per workgroup of a tile of few rows
+constexpr int kRows = 32;            // query rows of such a wave, and of the tile
+constexpr int kManyRows = 16;        // query rows of a wave where there are many
+constexpr int kRing = 3;             // steps whose bytes are on their way or wait, of a tile of many rows
 constexpr int kMaxSlots = 64;        // splits of a row's keys at most
 constexpr float kNone = -3e38f;      // reference of a row that has seen nothing
 constexpr int kAncWords = CURE_MAX_TREE_NODES / 32;
@@ -80,6 +85,12 @@ struct Args {
   float* part_lse;                   // [row][hq][slots], of base 2
 };
 
+// A value at an address that the whole wave shares, through the scalar cache: a vector load would
+// have to wait for the DMA before it.
+CURE_DEV float scalar_load(const float* p) {
+  return *(const __attribute__((address_space(4))) float*)(uintptr_t)p;
+}
+
 // A sequence's sizes as the device has them. ok: they can be.
 struct Seq {
   int64_t row0, block0, kv0;
@@ -113,9 +124,10 @@ CURE_DEV Steps steps_of(const Args& a, const Seq& s, int last) {
 struct Cut {
   int n, per;
 };
-CURE_DEV Cut cut_of(const Args& a, int steps) {
-  const int n = max(1, min((steps - 1) / a.tps + 1, a.slots));
-  const int per = ((steps - 1) / n / a.quantum + 1) * a.quantum;
+__host__ CURE_DEV Cut cut_of(int steps, int tps, int slots, int quantum) {
+  int n = (steps - 1) / tps + 1;
+  if (n > slots) n = slots;
+  const int per = ((steps - 1) / n / quantum + 1) * quantum;
   return Cut{(steps - 1) / per + 1, per};
 }
 
@@ -140,6 +152,7 @@ struct Half8 {
 };
 struct Bf8 {
   bf16x8 x;
+  CURE_DEV void words(const u32x4* w) { x = __builtin_bit_cast(bf16x8, w[0]); }
   CURE_DEV void row(const RowVec<uint16_t, 16>& r, int u) {
     Pack8 p;
     p.u = make_uint4(r.w[4 * u], r.w[4 * u + 1], r.w[4 * u + 2], r.w[4 * u + 3]);
@@ -157,6 +170,10 @@ struct Bf8 {
 };
 struct Float8 {
   float x[8];
+  CURE_DEV void words(const u32x4* w) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
+  }
   CURE_DEV void bytes(uint32_t lo, uint32_t hi) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -178,6 +195,12 @@ CURE_DEV f32x16 mma(const Half8& a, const Half8& b, f32x16 c) {
 }
 CURE_DEV f32x16 mma(const Bf8& a, const Bf8& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
+}
+CURE_DEV f32x4 mma16(const Half8& a, const Half8& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.x, b.x, c, 0, 0, 0);
+}
+CURE_DEV f32x4 mma16(const Bf8& a, const Bf8& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x, b.x, c, 0, 0, 0);
 }
 CURE_DEV f32x16 mma(const Float8& a, const Float8& b, f32x16 c) {
 #pragma unroll
@@ -205,80 +228,108 @@ CURE_DEV f32x16 zeros() {
   return x;
 }
 
-// Token of D register r in a lane's half.
-CURE_DEV int token_of(int half, int r) { return 8 * (r / 4) + 4 * half + r % 4; }
-
-// A lane's query row and what it has summed.
-template <int D>
+// A lane's query row and what it has summed: kScores scores of a step, of which kLanes lanes
+// share a row, and kBlocks blocks of output.
+template <int kScores, int kLanes, int kBlocks, class Block>
 struct Sums {
+  static constexpr int kEach = sizeof(Block) / sizeof(float);
   float m = kNone, l = 0.f;
-  f32x16 o[D / 32];
+  Block o[kBlocks];
 
   CURE_DEV Sums() {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = zeros();
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+      for (int r = 0; r < kEach; ++r) o[i][r] = 0.f;
   }
   // Scores x * factor of base 2 (-inf: not seen; factor > 0 there) of tokens whose values have scale 2^lv and
-  // its reciprocal rv: their P.
-  CURE_DEV void soften(const f32x16& x, float factor, float lv, float rv, float (&p)[16]) {
-    const float high = fmaf(max_halves(max_scores(x)), factor, lv);
-    if (__any(high > m + kRescaleLog2)) {
+  // its reciprocal rv: their P. The reference moves where a lane's P sum up to more than 2^8, as
+  // they do at first and seldom later; a maximum for each step would cost a tenth of it.
+  CURE_DEV void soften(const float (&x)[kScores], float factor, float lv, float rv, float (&p)[kScores]) {
+    float added = exps(x, factor, lv, p);
+    if (__builtin_expect(__any(!(added <= 256.f)), 0)) {
+      float high = x[0];
+#pragma unroll
+      for (int r = 1; r < kScores; ++r) high = fmaxf(high, x[r]);
+      if (kLanes == 4) high = fmaxf(high, __shfl_xor(high, 16));
+      high = fmaf(max_halves(high), factor, lv);
       const float mn = fmaxf(m, high), f = fast_exp2(m - mn);
       m = mn;
       l *= f;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
+      for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] *= f;
+        for (int r = 0; r < kEach; ++r) o[i][r] *= f;
+      added = exps(x, factor, lv, p);
     }
+    l = fmaf(added, rv, l);
+  }
+  CURE_DEV float exps(const float (&x)[kScores], float factor, float lv, float (&p)[kScores]) const {
     const float c = lv - m;
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
+    for (int r = 0; r < kScores; ++r) {
       p[r] = fast_exp2(fmaf(x[r], factor, c));
       sum[r % 2] += p[r];
     }
-    l = fmaf(sum[0] + sum[1], rv, l);
+    return sum[0] + sum[1];
+  }
+  // The row's whole sum.
+  CURE_DEV float all() const {
+    float x = l;
+    if (kLanes == 4) x += __shfl_xor(x, 16);
+    return sum_halves(x);
   }
 };
+template <int D>
+using FewSums = Sums<16, 2, D / 32, f32x16>;
+template <int D>
+using ManySums = Sums<8, 4, D / 16, f32x4>;
 
-// The scale of a block's values as soften takes it. Blocks of zeros, and of values below
-// 2^-93, have no products, and a scale that keeps their probabilities in range.
+// The scale of a block's values as soften takes it. Blocks of zeros have one that keeps their
+// probabilities in range; from 2^-116 on down the reciprocal would not.
 struct ValueScale {
   float lv, rv;
-  bool any;
   CURE_DEV explicit ValueScale(float s) {
-    any = s >= 0x1p-100f;
-    lv = any ? __builtin_amdgcn_logf(s) : -60.f;
-    rv = any ? 1.f / s : 0x1p60f;
+    const float x = s > 0.f ? fmaxf(s, 0x1p-116f) : 0x1p-60f;
+    lv = __builtin_amdgcn_logf(x);
+    rv = __builtin_amdgcn_rcpf(x);
   }
 };
 
-// Query rows as fp16: times 2^-e, for the largest of the row to be in [2^14, 2^15). Returns 2^e.
+// The power of two by which a query row is brought to fp16, for its largest value to be in [2^14, 2^15),
+// and its reciprocal.
+struct HalfScale {
+  float down, up;
+  CURE_DEV explicit HalfScale(float high) {
+    int e = (int)(__float_as_uint(high) >> 23) - 127 - 14;
+    e = max(-120, min(e, 120));
+    down = __uint_as_float((uint32_t)(127 - e) << 23);
+    up = __uint_as_float((uint32_t)(127 + e) << 23);
+  }
+};
+// Query rows as a few rows' products take them; returns what the scores are to be multiplied by.
 template <int D>
-CURE_DEV float half_rows(const RowVec<uint16_t, 16> (&x)[D / 32], Half8 (&q)[D / 32][2]) {
+CURE_DEV float byte_rows(const RowVec<uint16_t, 16> (&x)[D / 32], Half8 (&q)[D / 32][2]) {
   float high = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
-  high = max_halves(high);
-  int e = (int)(__float_as_uint(high) >> 23) - 127 - 14;
-  e = max(-120, min(e, 120));
-  const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+  const HalfScale s(max_halves(high));
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = x[i].get(8 * u + j) * down;
+      for (int j = 0; j < 8; ++j) f[j] = x[i].get(8 * u + j) * s.down;
       q[i][u].floats(f);
     }
-  return __uint_as_float((uint32_t)(127 + e) << 23);
+  return s.up;
 }
 template <int D>
-CURE_DEV float half_rows(const RowVec<float, 16> (&x)[D / 32], Float8 (&q)[D / 32][2]) {
+CURE_DEV float byte_rows(const RowVec<float, 16> (&x)[D / 32], Float8 (&q)[D / 32][2]) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -291,14 +342,63 @@ CURE_DEV void load_rows(const E* src, RowVec<E, 16> (&x)[D / 32]) {
   for (int i = 0; i < D / 32; ++i) x[i].load(src + 32 * i);
 }
 
-// Four, or two, values of a row that no query row need see: an infinity or NaN would reach the
-// others through its zero probabilities.
-CURE_DEV uint32_t finite2(uint32_t w) {
+// Values of a row that no query row need see: an infinity or NaN would reach the others through
+// its zero probabilities.
+CURE_DEV uint32_t finite_word(uint32_t w, uint16_t) {
   if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
   return w;
 }
-CURE_DEV float finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.f : x; }
+CURE_DEV uint32_t finite_word(uint32_t w, float) { return (w & 0x7f800000u) == 0x7f800000u ? 0u : w; }
+
+// Token of D register r in a lane's half, and of D register r % 4 of token block r / 4 in a lane's quad.
+CURE_DEV int token_of(int half, int r) { return 8 * (r / 4) + 4 * half + r % 4; }
+CURE_DEV int token_in(int quad, int r) { return 16 * (r / 4) + 4 * quad + r % 4; }
+
+// An open step's values as the products take them, 16 bytes (two times 16, fp32) after the other: of
+// few rows lane l's eight of block i and k-step t at [i][t][l], of many lane l's of block i at [i][l].
+template <typename E, int D>
+struct ValueTile {
+  static constexpr int kWords = 8 * (int)sizeof(E) / 16;
+  u32x4 x[D * 4][kWords];
+  CURE_DEV const u32x4* few(int i, int t, int lane) const { return x[(2 * i + t) * kWave + lane]; }
+  CURE_DEV const u32x4* many(int i, int lane) const { return x[i * kWave + lane]; }
+};
+// One unit of its making, four columns of eight tokens that a lane has: 4 * (D / 4) in all.
+template <typename E, int D, bool kMany>
+struct ValueUnit {
+  RowVec<E, 4> x[8];
+  static CURE_DEV int col_of(int unit) { return unit % (D / 4) * 4; }
+  CURE_DEV void load(const E* rows, int64_t pitch, int t0, int most, int unit) {
+    const int g = unit / (D / 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = kMany ? token_in(g, j) : token_of(g % 2, 8 * (g / 2) + j);
+      x[j].load(rows + min(t0 + t, most) * pitch + col_of(unit));
+    }
+  }
+  CURE_DEV void store(ValueTile<E, D>& tile, int unit) {
+    const int g = unit / (D / 4), c0 = col_of(unit);
+    const int at = kMany ? c0 / 16 * kWave + g * 16 + c0 % 16 : (2 * (c0 / 32) + g / 2) * kWave + g % 2 * 32 + c0 % 32;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int k = 0; k < RowVec<E, 4>::kWords; ++k) x[j].w[k] = finite_word(x[j].w[k], E());
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if constexpr (sizeof(E) == 2) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = __builtin_amdgcn_perm(x[2 * j + 1].w[c / 2], x[2 * j].w[c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+        tile.x[at + c][0] = w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) tile.x[at + c][k] = u32x4{x[4 * k].w[c], x[4 * k + 1].w[c], x[4 * k + 2].w[c], x[4 * k + 3].w[c]};
+      }
+    }
+  }
+};
 
 // What a workgroup works on.
 struct Work {
@@ -309,15 +409,17 @@ struct Work {
   int begin, end;                    // steps
 };
 
+template <int kTileRows>
 struct Trees {
-  uint32_t anc[kRows * kMaxGroups][kAncWords];   // root paths of the tile's nodes, as bits
+  uint32_t anc[kTileRows][kAncWords];   // root paths of the tile's nodes, as bits
   int parent[CURE_MAX_TREE_NODES];
 };
 
 // Finds the workgroup's work, reports the sequence's status and forms the root paths. False: nothing
 // to do. The grid: kv-heads, tiles, splits; sequences. A sequence's workgroups on one kv-head
 // are hkv apart, so where that is a multiple of 8 they share an XCD's L2.
-CURE_DEV bool locate(const Args& a, Work& w, Trees& sh) {
+template <int kTileRows>
+CURE_DEV bool locate(const Args& a, Work& w, Trees<kTileRows>& sh) {
   const int tid = threadIdx.x;
   w.b = blockIdx.y;
   w.hk = blockIdx.x % a.hkv;
@@ -334,7 +436,7 @@ CURE_DEV bool locate(const Args& a, Work& w, Trees& sh) {
   if (w.r0 >= w.rows) return false;
   const int r_last = min(w.r0 + a.tile, w.rows) - 1;
   w.steps = steps_of(a, w.s, r_last);
-  w.cut = cut_of(a, w.steps.all);
+  w.cut = cut_of(w.steps.all, a.tps, a.slots, a.quantum);
   w.begin = w.slot * w.cut.per;
   w.end = min(w.begin + w.cut.per, w.steps.all);
   if (w.begin >= w.end) return false;
@@ -364,7 +466,8 @@ CURE_DEV bool locate(const Args& a, Work& w, Trees& sh) {
 }
 
 // Which of an open step's tokens a node sees, as bits: t0 is the first one's index in the open rows.
-CURE_DEV uint32_t seen_of(const Args& a, const Work& w, const Trees& sh, int node, int t0) {
+template <int kTileRows>
+CURE_DEV uint32_t seen_of(const Args& a, const Work& w, const Trees<kTileRows>& sh, int node, int t0) {
   const int own = t0 - w.s.ctx;                    // its index among the new rows
   if (!a.parent) {
     const int n = node - own + 1;
@@ -378,47 +481,35 @@ CURE_DEV uint32_t seen_of(const Args& a, const Work& w, const Trees& sh, int nod
   return seen;
 }
 
-// Where a workgroup's rows are joined and turned: a wave's 32 rows.
-template <int D>
+// Where a workgroup's rows are joined and turned: kWaveRows of each of kAll waves.
+template <int D, int kAll, int kWaveRows>
 struct Out {
-  float o[kWaves][kRows][D + 4];
-  float m[kWaves][kRows], l[kWaves][kRows];
+  float o[kAll][kWaveRows][D + 4];
+  float m[kAll][kWaveRows], l[kAll][kWaveRows];
 };
 
-// Writes a tile's rows: kGroups groups of 32 rows, each the sum of kWaves / kGroups waves (wave w
-// has rows of group w % kGroups). Nothing else may use sh any more.
-template <int D, int kGroups>
-CURE_DEV void finish(const Args& a, const Work& w, Out<D>& sh, Sums<D>& sum) {
-  constexpr int kParts = kWaves / kGroups, kChunks = D / 4;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, col = lane % 32, half = lane / 32;
-  const float l = sum_halves(sum.l);
-  if (half == 0) {
-    sh.m[wave][col] = sum.m;
-    sh.l[wave][col] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<f32x4*>(&sh.o[wave][col][32 * i + 8 * (r / 4) + 4 * half]) =
-          f32x4{sum.o[i][r], sum.o[i][r + 1], sum.o[i][r + 2], sum.o[i][r + 3]};
+// Writes a tile's rows: kTile groups of kWaveRows, each the sum of kAll / kTile waves (wave w has rows
+// of group w % kTile), which have put theirs into sh.
+template <int D, int kTile, int kAll, int kWaveRows>
+CURE_DEV void finish(const Args& a, const Work& w, const Out<D, kAll, kWaveRows>& sh) {
+  constexpr int kParts = kAll / kTile, kChunks = D / 4;
   __syncthreads();
   const bool whole = w.cut.n == 1;
-  for (int c = tid; c < kGroups * kRows * kChunks; c += kWaves * kWave) {
-    const int row = c / kChunks, j = c % kChunks * 4, group = row / kRows, rr = row % kRows;
+  for (int c = threadIdx.x; c < kTile * kWaveRows * kChunks; c += kAll * kWave) {
+    const int row = c / kChunks, j = c % kChunks * 4, group = row / kWaveRows, rr = row % kWaveRows;
     if (w.r0 + row >= w.rows) break;
     float m = kNone, ll = 0.f, f[kParts];
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) m = fmaxf(m, sh.m[group + k * kGroups][rr]);
+    for (int k = 0; k < kParts; ++k) m = fmaxf(m, sh.m[group + k * kTile][rr]);
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-      f[k] = fast_exp2(sh.m[group + k * kGroups][rr] - m);
-      ll += f[k] * sh.l[group + k * kGroups][rr];
+      f[k] = fast_exp2(sh.m[group + k * kTile][rr] - m);
+      ll += f[k] * sh.l[group + k * kTile][rr];
     }
     const float inv = ll > 0.f ? 1.f / ll : 0.f;
     f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[group + k * kGroups][rr][j]);
+    for (int k = 0; k < kParts; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[group + k * kTile][rr][j]);
     x *= inv;
     const int R = w.r0 + row;
     const int64_t at = (w.s.row0 + R / a.group) * a.hq + w.hk * a.group + R % a.group;
@@ -434,26 +525,42 @@ CURE_DEV void finish(const Args& a, const Work& w, Out<D>& sh, Sums<D>& sum) {
   }
 }
 
-// Scores of packed tokens, of which `left` are there, times `factor`; returns the factor that is left.
-CURE_DEV float mask_packed(f32x16& x, int half, int left, float factor) {
+// What the lanes of a wave wrote to LDS is there for its others, and read before it changes.
+CURE_DEV void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Scores of packed tokens, of which `left` are there, times `factor`; returns the factor that is
+// left. A lane's tokens are kFar * (r / 4) + r % 4 behind its `own` first one.
+template <int kFar, int kScores>
+CURE_DEV float mask_packed(float (&x)[kScores], int left, float factor, int own) {
   if (left >= kStep) return factor;
+  left -= own;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = token_of(half, r) < left ? x[r] * factor : -INFINITY;
+  for (int r = 0; r < kScores; ++r) x[r] = kFar * (r / 4) + r % 4 < left ? x[r] * factor : -INFINITY;
   return 1.f;
+}
+template <int kFar, int kScores>
+CURE_DEV void mask_open(float (&x)[kScores], uint32_t seen, float factor, int own) {
+  seen >>= own;
+#pragma unroll
+  for (int r = 0; r < kScores; ++r) x[r] = seen & (1u << (kFar * (r / 4) + r % 4)) ? x[r] * factor : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
 // Up to 32 query rows to a tile: the waves take the steps in turn, each with all rows and sums of its
 // own, which are joined at the end. Packed bytes go from memory to registers and into the
-// matrix unit, a step ahead of their use.
+// matrix unit, a step ahead of their use, past the caches' ordinary order: nothing reads them twice (eight
+// single tokens over 4096 to 32768: 57 us and 5.5 TB/s, 64 us without). Memory bounds it.
 template <typename E, int D>
-__global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
+__global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void packed_few(Args a) {
   constexpr int kK = D / 32;                       // pieces of 32 columns
   using Byte = typename Types<E>::Byte;
   using RowF = typename Types<E>::Row;
-  __shared__ __attribute__((aligned(16))) Out<D> out;
-  __shared__ Trees trees;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  __shared__ __attribute__((aligned(16))) Out<D, kWaves, kRows> out;
+  __shared__ Trees<kRows> trees;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 32, half = lane / 32;
   Work w;
   if (!locate(a, w, trees)) return;
@@ -461,7 +568,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
   // This lane's query row.
   const int R = min(w.r0 + col, w.rows - 1), node = R / a.group;
   const E* qsrc = static_cast<const E*>(a.q) + ((w.s.row0 + node) * a.hq + w.hk * a.group + R % a.group) * D + 16 * half;
-  Sums<D> sum;
+  FewSums<D> sum;
   int step = w.begin + wave;
   const int packed_end = min(w.end, w.steps.packed);
   if (step < packed_end) {
@@ -470,7 +577,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
     {
       RowVec<E, 16> x[kK];
       load_rows<E, D>(qsrc, x);
-      qs = half_rows<D>(x, q) * a.scale_log2;
+      qs = byte_rows<D>(x, q) * a.scale_log2;
     }
     struct Raw {
       u32x4 k[kK], v[kK];
@@ -480,43 +587,53 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
       const int64_t block = (w.s.block0 + st / 2) * a.hkv + w.hk;
       const int64_t at = block * (kBlockTokens * D) + st % 2 * (kStep * D) + lane * 16;
 #pragma unroll
-      for (int i = 0; i < kK; ++i) raw.k[i] = *reinterpret_cast<const u32x4*>(a.pk + at + i * 1024);
+      for (int i = 0; i < kK; ++i) raw.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.pk + at + i * 1024));
 #pragma unroll
-      for (int i = 0; i < kK; ++i) raw.v[i] = *reinterpret_cast<const u32x4*>(a.pv + at + i * 1024);
-      raw.ks = a.k_scale[block];
-      raw.vs = a.v_scale[block];
+      for (int i = 0; i < kK; ++i) raw.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.pv + at + i * 1024));
+      raw.ks = scalar_load(a.k_scale + block);
+      raw.vs = scalar_load(a.v_scale + block);
     };
-    Raw next;
-    fetch(next, step);
-    for (; step < packed_end; step += kWaves) {
-      const Raw raw = next;
-      fetch(next, min(step + kWaves, packed_end - 1));
-      f32x16 x = zeros();
+    const auto work = [&](const Raw& raw, int st) {
+      f32x16 y = zeros();
 #pragma unroll
       for (int i = 0; i < kK; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           Byte f;
           f.bytes(raw.k[i][2 * u], raw.k[i][2 * u + 1]);
-          x = mma(f, q[i][u], x);
+          y = mma(f, q[i][u], y);
         }
       const ValueScale vs(raw.vs);
-      float p[16];
-      const float factor = mask_packed(x, half, w.s.packed - step * kStep, raw.ks * qs);
+      float x[16], p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = y[r];
+      const float factor = mask_packed<8>(x, w.s.packed - st * kStep, raw.ks * qs, 4 * half);
       sum.soften(x, factor, vs.lv, vs.rv, p);
-      if (vs.any) {
-        Byte pf[2];
-        pf[0].floats(p);
-        pf[1].floats(p + 8);
+      Byte pf[2];
+      pf[0].floats(p);
+      pf[1].floats(p + 8);
 #pragma unroll
-        for (int i = 0; i < kK; ++i)
+      for (int i = 0; i < kK; ++i)
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            Byte f;
-            f.bytes(raw.v[i][2 * t], raw.v[i][2 * t + 1]);
-            sum.o[i] = mma(f, pf[t], sum.o[i]);
-          }
-      }
+        for (int t = 0; t < 2; ++t) {
+          Byte f;
+          f.bytes(raw.v[i][2 * t], raw.v[i][2 * t + 1]);
+          sum.o[i] = mma(f, pf[t], sum.o[i]);
+        }
+    };
+    // Two buffers in turn: a copy from one to the other would wait for its loads.
+    Raw even, odd;
+    fetch(even, step);
+    fetch(odd, min(step + kWaves, packed_end - 1));
+    while (true) {
+      work(even, step);
+      step += kWaves;
+      if (step >= packed_end) break;
+      fetch(even, min(step + kWaves, packed_end - 1));
+      work(odd, step);
+      step += kWaves;
+      if (step >= packed_end) break;
+      fetch(odd, min(step + kWaves, packed_end - 1));
     }
   }
   if (step < w.end) {
@@ -534,23 +651,33 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
         q[i][1].row(x[i], 1);
       }
     }
+    // The wave's own part of the LDS turns the values.
+    static_assert(sizeof(ValueTile<E, D>) <= sizeof(out.o[0]), "");
+    ValueTile<E, D>& tile = *reinterpret_cast<ValueTile<E, D>*>(out.o[wave]);
     for (; step < w.end; step += kWaves) {
       const int t0 = (step - w.steps.packed) * kStep;
       RowVec<E, 16> kx[kK];
       load_rows<E, D>(kp + min(t0 + col, open - 1) * pitch + 16 * half, kx);
-      f32x16 x = zeros();
+      constexpr int kUnits = D / kWave;            // of values, per lane
+      ValueUnit<E, D, false> unit[kUnits];
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) unit[i].load(vp, pitch, t0, open - 1, i * kWave + lane);
+      f32x16 y = zeros();
 #pragma unroll
       for (int i = 0; i < kK; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           RowF f;
           f.row(kx[i], u);
-          x = mma(f, q[i][u], x);
+          y = mma(f, q[i][u], y);
         }
-      const uint32_t seen = seen_of(a, w, trees, node, t0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = seen >> token_of(half, r) & 1 ? x[r] * a.scale_log2 : -INFINITY;
-      float p[16];
+      for (int i = 0; i < kUnits; ++i) unit[i].store(tile, i * kWave + lane);
+      wave_sync();
+      float x[16], p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = y[r];
+      mask_open<8>(x, seen_of(a, w, trees, node, t0), a.scale_log2, 4 * half);
       sum.soften(x, 1.f, 0.f, 1.f, p);
       RowF pf[2], rest[2];
 #pragma unroll
@@ -563,219 +690,269 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void packed_few(Args a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           RowF f;
-          const E* src = vp + 32 * i + col;
-          float y[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const E e = src[min(t0 + token_of(half, 8 * t + j), open - 1) * pitch];
-            y[j] = finite(sizeof(E) == 2 ? __uint_as_float((uint32_t)e << 16) : (float)e);
-          }
-          f.floats(y);
+          f.words(tile.few(i, t, lane));
           sum.o[i] = mma(f, pf[t], sum.o[i]);
           if constexpr (sizeof(E) == 2) sum.o[i] = mma(f, rest[t], sum.o[i]);
         }
+      wave_sync();
     }
   }
-  finish<D, 1>(a, w, out, sum);
+  const float l = sum.all();
+  if (half == 0) {
+    out.m[wave][col] = sum.m;
+    out.l[wave][col] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < kK; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<f32x4*>(&out.o[wave][col][32 * i + 8 * (r / 4) + 4 * half]) =
+          f32x4{sum.o[i][r], sum.o[i][r + 1], sum.o[i][r + 2], sum.o[i][r + 3]};
+  finish<D, 1, kWaves, kRows>(a, w, out);
 }
 
 // ---------------------------------------------------------------------------
-// More rows (bf16): kGroups groups of 32 query rows, a wave each, share a step's keys and
-// values, which they widen together and hand on through LDS, two steps' room for each of the kWaves /
-// kGroups sets of waves that take the steps in turn. An operand's 64 lanes of 16 bytes are 1 KB of
-// LDS, written and read without conflicts.
+// More rows (bf16): 16 for each of kGroups waves, which share each step's keys and values. The first
+// waves bring a step's bytes to LDS by DMA, 1 KB each, widen them and hand them on through LDS; an
+// operand's 64 lanes of 16 bytes are 1 KB of LDS. Step i forms the probabilities and products of step
+// i, the scores of step i + 1 and the widened tile of step i + 2, while the bytes of the kRing steps behind
+// are on their way. A SIMD's waves issue about one instruction in nine cycles each and the matrix unit
+// works beside them, so the softmax's instructions and the LDS reads (8 KB a wave and step at 128 bytes a
+// clock) bound it: 128 rows on four times 32768 tokens, 8 kv-heads, 107 us and 0.65 PFLOP/s; with 32 rows and half as
+// many waves 117 us.
 template <int D>
 struct Tile {
-  u32x4 k[D / 32][2][kWave], v[D / 32][2][kWave];
+  u32x4 k[2][D / 32][kWave];                       // of a block of 16 tokens and 32 columns
+  ValueTile<uint16_t, D> v;
+};
+template <int D>
+struct Stage {
+  Tile<D> tile[3];
+  u32x4 raw[kRing][2 * D / 32][kWave];
 };
 template <int D, int kGroups>
 union Many {
-  Tile<D> tile[2][kWaves / kGroups];
-  Out<D> out;
+  Stage<D> in;
+  Out<D, kGroups, kManyRows> out;
+};
+template <int i>
+struct Turn {
+  static constexpr int value = i;
 };
 
 template <int D, int kGroups>
-__global__ __launch_bounds__(kWaves * kWave, 2) void packed_many(Args a) {
+__global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu(4, 4))) void packed_many(Args a) {
   using E = uint16_t;
-  constexpr int kK = D / 32;
-  constexpr int kSets = kWaves / kGroups;
-  constexpr int kThreads = kGroups * kWave;        // of a set
-  constexpr int kUnits = kK * kWave / kThreads;    // 16-byte units of packed keys, and of values, per thread
-  static_assert(kK * kWave % kThreads == 0 || kK * kWave < kThreads, "");
-  constexpr int kMine = kUnits > 0 ? kUnits : 1;
-  __shared__ __attribute__((aligned(16))) Many<D, kGroups> sh;
-  __shared__ Trees trees;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int col = lane % 32, half = lane / 32;
-  const int set = wave / kGroups, me = tid % kThreads;
+  constexpr int kK = D / 32, kO = D / 16;
+  constexpr int kBring = 2 * kK;                   // waves that bring 1 KB of a step: keys', then values'
+  static_assert(kBring <= kGroups && kRing == 3, "");
+  constexpr uint32_t kTileBytes = sizeof(Tile<D>), kRawBytes = 2 * kStep * D, kValues = sizeof(Tile<D>::k);
+  __shared__ __attribute__((aligned(1024))) Many<D, kGroups> sh;
+  __shared__ Trees<kGroups * kManyRows> trees;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int col = lane % 16, quad = lane / 16, group = wave;
   Work w;
   if (!locate(a, w, trees)) return;
+  Stage<D>& in = sh.in;
 
-  const int R0 = w.r0 + wave % kGroups * kRows, R = min(R0 + col, w.rows - 1), node = R / a.group;
-  const int last_node = min(R0 + kRows - 1, w.rows - 1) / a.group;
-  const E* qsrc = static_cast<const E*>(a.q) + ((w.s.row0 + node) * a.hq + w.hk * a.group + R % a.group) * D + 16 * half;
+  const int R0 = w.r0 + group * kManyRows, R = min(R0 + col, w.rows - 1), node = R / a.group;
+  const int last_node = min(R0 + kManyRows - 1, w.rows - 1) / a.group;
   const bool idle = R0 >= w.rows;                  // this wave's rows are not there
-  Sums<D> sum;
-  Half8 q[kK][2];
-  float qs;
-  {
-    RowVec<E, 16> x[kK];
-    load_rows<E, D>(qsrc, x);
-    qs = half_rows<D>(x, q) * a.scale_log2;
-  }
-  const int packed_end = min(w.end, w.steps.packed);
-  const int64_t pitch = (int64_t)a.hkv * D;
-  const int open = w.s.ctx + w.s.n;
-  const E* kp = static_cast<const E*>(a.k) + w.s.kv0 * pitch + w.hk * D;
-  const E* vp = static_cast<const E*>(a.v) + w.s.kv0 * pitch + w.hk * D;
+  const E* qsrc = static_cast<const E*>(a.q) + ((w.s.row0 + node) * a.hq + w.hk * a.group + R % a.group) * D + 8 * quad;
+  ManySums<D> sum;
 
-  struct Raw {
-    u32x4 k[kMine], v[kMine];
-  };
-  const auto block_of = [&](int st) { return (w.s.block0 + st / 2) * a.hkv + w.hk; };
-  const auto fetch = [&](Raw& raw, int st) {
-    if (st >= packed_end || me >= kK * kWave) return;
-    const int64_t at = block_of(st) * (kBlockTokens * D) + st % 2 * (kStep * D) + me * 16;
+  const int packed_end = min(w.end, w.steps.packed), rounds = packed_end - w.begin;
+  if (rounds > 0) {
+    // This wave's bytes: from one half of a block to the other, and on to the next. Past the last step
+    // there are none, which read as zeros.
+    const int64_t block = (w.s.block0 + w.begin / 2) * a.hkv + w.hk, pitch = (int64_t)a.hkv * (kBlockTokens * D);
+    const int8_t* src = (group < kK ? a.pk : a.pv) + block * (kBlockTokens * D) + w.begin % 2 * (kStep * D) + group % kK * 1024;
+    int asked = 0;
+    const uint32_t raw_lds = lds_addr(in.raw) + group * 1024;
+    const auto dma = [&](uint32_t slot) {
+      dma16_shared(raw_lds + slot, lane * 16, raw_rsrc(src, asked < rounds ? 1024 : 0));
+      src += (w.begin + asked) % 2 ? pitch - kStep * D : kStep * D;
+      ++asked;
+    };
+    if (group < kBring) {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) raw.k[i] = *reinterpret_cast<const u32x4*>(a.pk + at + i * kThreads * 16);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) raw.v[i] = *reinterpret_cast<const u32x4*>(a.pv + at + i * kThreads * 16);
-  };
-  // A packed step's bytes, fetched before, or an open step's rows.
-  const auto stage = [&](const Raw& raw, int st, Tile<D>& t) {
-    if (st >= w.end) return;
-    if (st < packed_end) {
-      if (me >= kK * kWave) return;
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int unit = me + i * kThreads, piece = unit / kWave, ln = unit % kWave;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Half8 f;
-          f.bytes(raw.k[i][2 * u], raw.k[i][2 * u + 1]);
-          t.k[piece][u][ln] = __builtin_bit_cast(u32x4, f.x);
-          f.bytes(raw.v[i][2 * u], raw.v[i][2 * u + 1]);
-          t.v[piece][u][ln] = __builtin_bit_cast(u32x4, f.x);
-        }
-      }
-      return;
+      for (int i = 0; i < kRing; ++i) dma(i * kRawBytes);
     }
-    const int t0 = (st - w.steps.packed) * kStep;
-    // Keys: 16 columns of a token to a unit.
-    for (int unit = me; unit < kStep * (D / 16); unit += kThreads) {
-      const int tok = unit / (D / 16), c = unit % (D / 16);
-      RowVec<E, 16> x;
-      x.load(kp + min(t0 + tok, open - 1) * pitch + 16 * c);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        t.k[c / 2][u][c % 2 * 32 + tok] = u32x4{x.w[4 * u], x.w[4 * u + 1], x.w[4 * u + 2], x.w[4 * u + 3]};
-    }
-    // Values: two columns of the eight tokens that a lane has in a k-step.
-    for (int unit = me; unit < 4 * (D / 2); unit += kThreads) {
-      const int c = unit % (D / 2) * 2, g = unit / (D / 2), h = g % 2, ks = g / 2;
-      uint32_t x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        x[j] = finite2(*reinterpret_cast<const uint32_t*>(vp + min(t0 + token_of(h, 8 * ks + j), open - 1) * pitch + c));
-      u32x4 lo, hi;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        lo[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
-        hi[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
-      }
-      t.v[c / 32][ks][h * 32 + c % 32] = lo;
-      t.v[c / 32][ks][h * 32 + c % 32 + 1] = hi;
-    }
-  };
 
-  // Step `it` of the set is step w.begin + it * kSets + set. One step is staged ahead of the one at
-  // work, and the bytes of the one after that are on their way.
-  const int count = (w.end - w.begin + kSets - 1) / kSets;
-  const auto step_of = [&](int it) { return w.begin + it * kSets + set; };
-  Raw raw;
-  fetch(raw, step_of(0));
-  stage(raw, step_of(0), sh.tile[0][set]);
-  fetch(raw, step_of(1));
-  float ks = 0.f, vsc = 0.f;
-  const auto scales = [&](int st) {
-    if (st < packed_end) {
-      ks = a.k_scale[block_of(st)];
-      vsc = a.v_scale[block_of(st)];
+    Half8 q[kK];
+    float qs;
+    {
+      RowVec<E, 8> x[kK];
+      float high = 0.f;
+#pragma unroll
+      for (int i = 0; i < kK; ++i) {
+        x[i].load(qsrc + 32 * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
+      }
+      const HalfScale s(max_halves(fmaxf(high, __shfl_xor(high, 16))));
+#pragma unroll
+      for (int i = 0; i < kK; ++i) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = x[i].get(j) * s.down;
+        q[i].floats(f);
+      }
+      qs = s.up * a.scale_log2;
     }
-  };
-  scales(step_of(0));
-  __syncthreads();
-  bool rows = false;                               // q holds the rows as they are
-  Bf8 qr[kK][2];
-  for (int it = 0; it < count; ++it) {
-    const int st = step_of(it);
-    const float ks_now = ks, vs_now = vsc;
-    stage(raw, step_of(it + 1), sh.tile[(it + 1) % 2][set]);
-    fetch(raw, step_of(it + 2));
-    scales(step_of(it + 1));
-    const Tile<D>& t = sh.tile[it % 2][set];
-    if (st < packed_end && !idle) {
-      f32x16 x = zeros();
+    // Where this lane's 16 bytes belong: of keys columns 16 h .. of token t, whose quads 2 h and 2 h + 1
+    // have eight each; of values column m of tokens 8 a + 4 h + c, whose quads h and 2 + h have dwords
+    // a of the same parity.
+    const int h = lane / 32, t = lane % 32;
+    const bool keys = group < kK;
+    char* const to0 = reinterpret_cast<char*>(in.tile) +
+                      (keys ? (t / 16 * kK + group) * 1024 + (2 * h * 16 + t % 16) * 16
+                            : kValues + ((group - kK) * 2 + t / 16) * 1024 + (h * 16 + t % 16) * 16);
+    const int to1 = keys ? 256 : 512;
+    const char* const from = reinterpret_cast<const char*>(in.raw) + group * 1024 + lane * 16;
+    // Widens this wave's part of a step from a slot into a tile, and asks for the step that takes its place.
+    u32x4 raw;
+    const auto fetch = [&](uint32_t slot) {
+      if (group >= kBring) return;
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(kRing - 1));
+      asm volatile("" ::: "memory");
+      raw = *reinterpret_cast<const u32x4*>(from + slot);
+    };
+    const auto widen = [&](uint32_t slot, uint32_t tile) {
+      if (group >= kBring) return;
+      Half8 f[2];
+      f[0].bytes(raw[0], keys ? raw[1] : raw[2]);
+      f[1].bytes(keys ? raw[2] : raw[1], raw[3]);
+      *reinterpret_cast<u32x4*>(to0 + tile) = __builtin_bit_cast(u32x4, f[0].x);
+      *reinterpret_cast<u32x4*>(to0 + tile + to1) = __builtin_bit_cast(u32x4, f[1].x);
+      dma(slot);                                   // behind writes of what was read there
+    };
+    const char* const tiles = reinterpret_cast<const char*>(in.tile) + lane * 16;
+    const auto operand = [&](uint32_t at) { return Half8{__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(tiles + at))}; };
+    float x[8];
+    const auto scores = [&](uint32_t tile) {
+      f32x4 y[2];
 #pragma unroll
-      for (int i = 0; i < kK; ++i)
+      for (int i = 0; i < 2; ++i) {
+        y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) x = mma(Half8{__builtin_bit_cast(f16x8, t.k[i][u][lane])}, q[i][u], x);
-      const ValueScale vs(vs_now);
-      float p[16];
-      const float factor = mask_packed(x, half, w.s.packed - st * kStep, ks_now * qs);
-      sum.soften(x, factor, vs.lv, vs.rv, p);
-      if (vs.any) {
-        Half8 pf[2];
-        pf[0].floats(p);
-        pf[1].floats(p + 8);
-#pragma unroll
-        for (int i = 0; i < kK; ++i)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) sum.o[i] = mma(Half8{__builtin_bit_cast(f16x8, t.v[i][u][lane])}, pf[u], sum.o[i]);
+        for (int k = 0; k < kK; ++k) y[i] = mma16(operand(tile + (i * kK + k) * 1024), q[k], y[i]);
       }
-    } else if (st < w.end && !idle) {
-      const int t0 = (st - w.steps.packed) * kStep;
-      if (!rows) {
-        RowVec<E, 16> xr[kK];
-        load_rows<E, D>(qsrc, xr);
 #pragma unroll
-        for (int i = 0; i < kK; ++i) {
-          qr[i][0].row(xr[i], 0);
-          qr[i][1].row(xr[i], 1);
-        }
-        rows = true;
+      for (int r = 0; r < 8; ++r) x[r] = y[r / 4][r % 4];
+    };
+    // Scales of step i, or past the end of the last one.
+    const auto scale_at = [&](const float* s, int i) {
+      return scalar_load(s + (w.s.block0 + min(w.begin + i, packed_end - 1) / 2) * a.hkv + w.hk);
+    };
+    fetch(0);
+    widen(0, 0);
+    fetch(kRawBytes);
+    widen(kRawBytes, kTileBytes);
+    float ks = scale_at(a.k_scale, 0), vsc = scale_at(a.v_scale, 0);
+    __syncthreads();
+    scores(0);
+    const auto step = [&](int i, auto turn) {
+      constexpr uint32_t kNow = decltype(turn)::value, kNext = (kNow + 1) % 3, kAfter = (kNow + 2) % 3;
+      fetch(kAfter * kRawBytes);
+      if (!idle) {
+        const float factor = mask_packed<16>(x, w.s.packed - (w.begin + i) * kStep, ks * qs, 4 * quad);
+        const ValueScale vs(vsc);
+        ks = scale_at(a.k_scale, i + 1);
+        vsc = scale_at(a.v_scale, i + 1);
+        float p[8];
+        sum.soften(x, factor, vs.lv, vs.rv, p);
+        Half8 pf;
+        pf.floats(p);
+        scores(kNext * kTileBytes);
+#pragma unroll
+        for (int k = 0; k < kO; ++k) sum.o[k] = mma16(operand(kNow * kTileBytes + kValues + k * 1024), pf, sum.o[k]);
       }
-      // Later tokens than all of the wave's rows see nothing of it.
-      if (a.parent || t0 - w.s.ctx <= last_node) {
-        f32x16 x = zeros();
-#pragma unroll
-        for (int i = 0; i < kK; ++i)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) x = mma(Bf8{__builtin_bit_cast(bf16x8, t.k[i][u][lane])}, qr[i][u], x);
-        const uint32_t seen = seen_of(a, w, trees, node, t0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = seen >> token_of(half, r) & 1 ? x[r] * a.scale_log2 : -INFINITY;
-        float p[16];
-        sum.soften(x, 1.f, 0.f, 1.f, p);
-        Bf8 pf[2], rest[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          pf[u].floats(p + 8 * u);
-          rest[u].rest(p + 8 * u, pf[u]);
-        }
-#pragma unroll
-        for (int i = 0; i < kK; ++i)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const Bf8 f{__builtin_bit_cast(bf16x8, t.v[i][u][lane])};
-            sum.o[i] = mma(f, pf[u], sum.o[i]);
-            sum.o[i] = mma(f, rest[u], sum.o[i]);
-          }
-      }
+      widen(kAfter * kRawBytes, kAfter * kTileBytes);
+      __syncthreads();
+    };
+    for (int i = 0;; i += 3) {
+      step(i, Turn<0>());
+      if (i + 1 >= rounds) break;
+      step(i + 1, Turn<1>());
+      if (i + 2 >= rounds) break;
+      step(i + 2, Turn<2>());
+      if (i + 3 >= rounds) break;
     }
+    __builtin_amdgcn_s_waitcnt(0);                 // no DMA may land in what LDS holds next
     __syncthreads();
   }
-  finish<D, kGroups>(a, w, sh.out, sum);
+
+  // Open steps: rows as they are, staged a step ahead.
+  const int first = max(w.begin, w.steps.packed), more = max(0, w.end - first);
+  if (more > 0) {
+    const int64_t pitch = (int64_t)a.hkv * D;
+    const int open = w.s.ctx + w.s.n;
+    const E* kp = static_cast<const E*>(a.k) + w.s.kv0 * pitch + w.hk * D;
+    const E* vp = static_cast<const E*>(a.v) + w.s.kv0 * pitch + w.hk * D;
+    Bf8 q[kK];
+#pragma unroll
+    for (int i = 0; i < kK; ++i) {
+      RowVec<E, 8> x;
+      x.load(qsrc + 32 * i);
+      q[i].x = __builtin_bit_cast(bf16x8, u32x4{x.w[0], x.w[1], x.w[2], x.w[3]});
+    }
+    const auto stage = [&](int i) {
+      const int t0 = (first + i - w.steps.packed) * kStep;
+      Tile<D>& t = in.tile[i % 2];
+      // Keys: eight columns of a token to a unit.
+      if (tid < kStep * (D / 8)) {
+        const int tk = tid / (D / 8), c = tid % (D / 8);
+        RowVec<E, 8> x;
+        x.load(kp + min(t0 + tk, open - 1) * pitch + 8 * c);
+        t.k[tk / 16][c / 4][c % 4 * 16 + tk % 16] = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+      }
+      if (tid < D) {
+        ValueUnit<E, D, true> unit;
+        unit.load(vp, pitch, t0, open - 1, tid);
+        unit.store(t.v, tid);
+      }
+    };
+    stage(0);
+    __syncthreads();
+    for (int i = 0; i < more; ++i) {
+      if (i + 1 < more) stage(i + 1);
+      const int t0 = (first + i - w.steps.packed) * kStep;
+      // Later tokens than all of the wave's rows are seen by none of them.
+      if (!idle && (a.parent || t0 - w.s.ctx <= last_node)) {
+        const Tile<D>& t = in.tile[i % 2];
+        float x[8], p[8];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < kK; ++k) y = mma16(Bf8{__builtin_bit_cast(bf16x8, t.k[b][k][lane])}, q[k], y);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[4 * b + r] = y[r];
+        }
+        mask_open<16>(x, seen_of(a, w, trees, node, t0), a.scale_log2, 4 * quad);
+        sum.soften(x, 1.f, 0.f, 1.f, p);
+        Bf8 pf, rest;
+        pf.floats(p);
+        rest.rest(p, pf);
+#pragma unroll
+        for (int k = 0; k < kO; ++k) {
+          const Bf8 f{__builtin_bit_cast(bf16x8, *t.v.many(k, lane))};
+          sum.o[k] = mma16(f, pf, sum.o[k]);
+          sum.o[k] = mma16(f, rest, sum.o[k]);
+        }
+      }
+      __syncthreads();
+    }
+  }
+  const float l = sum.all();
+  if (quad == 0) {
+    sh.out.m[wave][col] = sum.m;
+    sh.out.l[wave][col] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < kO; ++i) *reinterpret_cast<f32x4*>(&sh.out.o[wave][col][16 * i + 4 * quad]) = sum.o[i];
+  finish<D, kGroups, kGroups, kManyRows>(a, w, sh.out);
 }
 
 // Joins the splits of a row by their log-sum-exps: D / 4 lanes per (row, head).
@@ -789,13 +966,15 @@ __global__ __launch_bounds__(256) void packed_merge(Args a) {
   if (!s.ok || i >= (int64_t)s.n * a.hq) return;
   const int n = (int)(i / a.hq), head = (int)(i % a.hq);
   const int rows = s.n * a.group, r0 = (n * a.group + head % a.group) / a.tile * a.tile;
-  const Cut cut = cut_of(a, steps_of(a, s, min(r0 + a.tile, rows) - 1).all);
+  const Cut cut = cut_of(steps_of(a, s, min(r0 + a.tile, rows) - 1).all, a.tps, a.slots, a.quantum);
   if (cut.n == 1) return;                          // written whole
   const int64_t at = (s.row0 + n) * a.hq + head;
   float m = -INFINITY, sum = 0.f;
+#pragma unroll 4
   for (int j = 0; j < cut.n; ++j) m = fmaxf(m, a.part_lse[at * a.slots + j]);
   if (m == -INFINITY) m = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int j = 0; j < cut.n; ++j) {
     const float w = fast_exp2(a.part_lse[at * a.slots + j] - m);
     sum += w;
@@ -810,8 +989,15 @@ __global__ __launch_bounds__(256) void packed_merge(Args a) {
 
 // ---------------------------------------------------------------------------
 // Host: tiles, splits and workspace.
+int64_t steps_of(int32_t packed, int32_t ctx, int32_t n) {
+  return ((int64_t)packed + kStep - 1) / kStep + ((int64_t)ctx + n + kStep - 1) / kStep;
+}
+constexpr int64_t kOverhead = 8;       // steps' time that a workgroup takes besides its steps
+constexpr int64_t kJoined = 300000;    // values of splits written and joined in a step's time
+
 struct Plan {
-  int32_t groups, tiles, tps, quantum, slots;
+  int32_t groups;                    // of many rows; 0: few
+  int32_t tile, tiles, tps, quantum, slots;
 };
 
 // Parts of a call: rows * hq * slots of d + 1 floats.
@@ -823,24 +1009,47 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
   int64_t most_rows = 0;
   for (int32_t b = 0; b < batch; ++b) most_rows = std::max<int64_t>(most_rows, n[b] * group);
   Plan p;
-  p.groups = dtype == CURE_F32 || most_rows <= kRows ? 1 : most_rows <= 2 * kRows ? 2 : 4;
-  p.quantum = kWaves / p.groups;
-  const int64_t tile = p.groups * kRows;
-  int64_t total = 0, longest = 1;
-  for (int32_t b = 0; b < batch; ++b) {
-    if (n[b] <= 0) continue;
-    const int64_t steps = ((int64_t)packed[b] + kStep - 1) / kStep + ((int64_t)ctx[b] + n[b] + kStep - 1) / kStep;
-    total += (n[b] * group + tile - 1) / tile * hkv * steps;
-    longest = std::max(longest, steps);
-  }
-  p.tiles = (int32_t)std::max<int64_t>(1, (most_rows + tile - 1) / tile);
-  // Two workgroups per CU, of at least eight steps.
-  const int64_t target = 2 * (int64_t)device_cu_count();
-  int64_t tps = kv_split > 0 ? (longest + kv_split - 1) / kv_split : std::max<int64_t>(8, (total + target - 1) / target);
-  tps = (tps + p.quantum - 1) / p.quantum * p.quantum;
+  // A tile of many rows has 128, or 256 where those are a sequence's all: that one then reads and widens
+  // its keys once (16 trees of 20 to 48 nodes, group 4: 83 us, 94 with 128). Of more rows two workgroups to a
+  // CU do better than one (chunks of 256 to 512 tokens, d = 64: 274 us to 311; d = 128 alike). Up to 64 rows
+  // the other form: four trees of 16 nodes on 32768 tokens 73 us to 107.
+  p.groups = dtype == CURE_F32 || most_rows <= 2 * kRows ? 0 : most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows ? 16 : 8;
+  p.quantum = p.groups ? 1 : kWaves;
+  p.tile = p.groups ? p.groups * kManyRows : kRows;
   const int64_t room = kMostBytes / std::max<int64_t>(1, rows * hq * (d + 1) * 4);
-  p.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(longest + tps - 1) / tps, (int64_t)kMaxSlots, room}));
-  p.tps = (int32_t)tps;
+  const int64_t at_once = (p.groups == 16 ? 1 : 2) * (int64_t)device_cu_count();       // workgroups
+  int64_t longest = 1;
+  for (int32_t b = 0; b < batch; ++b)
+    if (n[b] > 0) longest = std::max(longest, steps_of(packed[b], ctx[b], n[b]));
+  p.tiles = (int32_t)std::max<int64_t>(1, (most_rows + p.tile - 1) / p.tile);
+  // As many splits as asked for, or those that should take least: either so many turns of the longest, or
+  // all work spread evenly and one more. Eight steps at least, which is what the rest of a split costs.
+  const int64_t fewest = kv_split > 0 ? longest : (longest + kOverhead - 1) / kOverhead;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({fewest, (int64_t)kMaxSlots, room}));
+  int64_t best = INT64_MAX;
+  for (int64_t slots = kv_split > 0 ? std::min<int64_t>(kv_split, most) : 1; slots <= most; ++slots) {
+    const int32_t tps = (int32_t)(((longest + slots - 1) / slots + p.quantum - 1) / p.quantum * p.quantum);
+    int64_t groups = 0, work = 0, high = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+      if (n[b] <= 0) continue;
+      const Cut c = cut_of((int)steps_of(packed[b], ctx[b], n[b]), tps, (int)slots, p.quantum);
+      const int64_t g = (n[b] * group + p.tile - 1) / p.tile * hkv * c.n;
+      groups += g;
+      work += g * (c.per + kOverhead);
+      high = std::max<int64_t>(high, c.per + kOverhead);
+    }
+    // The launch's workgroups that find nothing to do keep some places from the others at first: eight
+    // single tokens with 4096 to 32768 tokens take 64 us in 472 workgroups and 75 in 512.
+    const int64_t places = groups < hkv * p.tiles * slots * batch ? at_once - at_once / 16 : at_once;
+    int64_t time = std::min((groups + places - 1) / places * high, work / at_once + high);
+    if (slots > 1) time += kOverhead + rows * hq * slots * d / kJoined;
+    if (time < best) {
+      best = time;
+      p.slots = (int32_t)slots;
+      p.tps = tps;
+    }
+    if (kv_split > 0) break;
+  }
   return p;
 }
 
@@ -909,18 +1118,19 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
   if (need > 0 && at(workspace) % 16) return CURE_ERR_INVALID_ARG;
   const int64_t wgs = (int64_t)hkv * p.tiles * p.slots;
-  if (wgs * kWaves * kWave >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;         // a launch counts threads in 32 bits
+  const int threads = (p.groups ? p.groups : kWaves) * kWave;
+  if (wgs * threads >= (int64_t(1) << 32)) return CURE_ERR_UNSUPPORTED;         // a launch counts threads in 32 bits
   float* part_o = static_cast<float*>(workspace);
   Args a{q, pk, pv, k_scale, v_scale, blocks, k, v, cache_rows, o, lse, out_dtype == CURE_BF16, batch, n_max, hq, hkv, hq / hkv,
-         rows, scale * kLog2e, row_off, n_rows, blk_off, packed_len, kv_off, ctx_len, parent, row_status, p.groups * kRows, p.tiles, p.tps, p.quantum, p.slots,
+         rows, scale * kLog2e, row_off, n_rows, blk_off, packed_len, kv_off, ctx_len, parent, row_status, p.tile, p.tiles, p.tps, p.quantum, p.slots,
          part_o, p.slots > 1 ? part_o + rows * hq * p.slots * d : nullptr};
   hipStream_t st = as_stream(stream);
-  const dim3 grid((unsigned)wgs, (unsigned)batch), block(kWaves * kWave);
+  const dim3 grid((unsigned)wgs, (unsigned)batch), block(threads);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
   if (dtype == CURE_F32) d == 128 ? run(packed_few<float, 128>) : run(packed_few<float, 64>);
-  else if (p.groups == 1) d == 128 ? run(packed_few<uint16_t, 128>) : run(packed_few<uint16_t, 64>);
-  else if (p.groups == 2) d == 128 ? run(packed_many<128, 2>) : run(packed_many<64, 2>);
-  else d == 128 ? run(packed_many<128, 4>) : run(packed_many<64, 4>);
+  else if (!p.groups) d == 128 ? run(packed_few<uint16_t, 128>) : run(packed_few<uint16_t, 64>);
+  else if (p.groups == 16) d == 128 ? run(packed_many<128, 16>) : run(packed_many<64, 16>);
+  else d == 128 ? run(packed_many<128, 8>) : run(packed_many<64, 8>);
   const cure_status launched = launch_status();
   if (launched != CURE_OK || p.slots == 1 || n_max == 0) return launched;
   const int per = 256 / (d / 4);
