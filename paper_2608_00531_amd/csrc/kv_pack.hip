@@ -3,15 +3,15 @@
 //
 //   a = max |x|,  scale = a / 127,  c = rint(127 x / a)
 //
-// The integer is the exact quotient's nearest, ties to even: c0 = rint(x * (127 / a)) is at
-// most one off, and the remainder 127 x - c0 a, which fp32 holds exactly for bf16 values (15
-// bits) and fp64 for fp32 ones (31 bits), says which.
+// The integer is the exact quotient's nearest, ties to even. x * (127 / a) is within 2^-16 of the
+// quotient, so its nearest is right unless it lies between 0.4999 and 0.5 away; there the
+// remainder 127 x - c a, which fp32 holds exactly for bf16 values (15 bits) and fp64 for fp32 ones
+// (31 bits), says which.
 //
-// Bound by memory. One wave takes one block and head of K or of V, whole, in registers: all
-// its loads (16 KB of bf16 at head dim 128) are in flight together, and the maximum is a wave's
-// reduction, without LDS or barriers. A row's vectors lie in neighbouring lanes; the 16 tokens
-// that a lane of V's layout holds are its own 16 loads, so that its bytes come together
-// without exchange.
+// Bound by memory. Two waves take one block and head of K, two of V, 32 tokens each, whole, in
+// registers: all their loads (8 KB of bf16 at head dim 128 each) are in flight together. A row's vectors lie
+// in neighbouring lanes; the 16 tokens that a lane of V's layout holds are its own 16 loads, so that its
+// bytes come together without exchange.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -79,68 +79,111 @@ CURE_DEV float to_int(float x, float a, float inv, float) {
   return c;
 }
 
-// Four integers of magnitude up to 127 as bytes.
-CURE_DEV uint32_t bytes_of(float a, float b, float c, float d) {
-  return ((uint32_t)(int)a & 255u) | ((uint32_t)(int)b & 255u) << 8 | ((uint32_t)(int)c & 255u) << 16 | (uint32_t)(int)d << 24;
+// Words' low bytes.
+CURE_DEV uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
-// Lanes and pieces. K: unit i is 16 columns of a token, and 16 bytes of the block. V: a lane has
-// D / 16 columns of the 16 tokens 8 a + 4 h + c of a half, each column 16 bytes of the block.
-template <int D>
-struct Lanes {
-  static constexpr int kUnits = D / 16;            // of K, per lane
-  static constexpr int kCols = D / 16;             // of V, per lane
-  static CURE_DEV int k_token(int lane, int i) { return (i * kWave + lane) / (D / 16); }
-  static CURE_DEV int k_col(int lane) { return lane % (D / 16) * 16; }
-  static CURE_DEV int k_byte(int t, int j) { return ((t / 32) * (D / 32) + j / 32) * 1024 + j % 32 / 16 * 512 + t % 32 * 16; }
-  static CURE_DEV int v_token(int lane, int i) { return lane / 32 * 32 + lane / 16 % 2 * 4 + i / 4 * 8 + i % 4; }
-  static CURE_DEV int v_col(int lane) { return lane % 16 * kCols; }
-  static CURE_DEV int v_byte(int lane, int j) { return (lane / 32 * (D / 32) + j / 32) * 1024 + lane / 16 % 2 * 512 + j % 32 * 16; }
+// How a block's values become integers. Where 127 / a or 127 x would overflow they are scaled by a power of
+// two first: what that rounds off is far below a / 254.
+struct Quant {
+  float up, top, inv;
+  CURE_DEV explicit Quant(float a) {
+    up = a < 0x1p-100f ? 0x1p100f : a > 0x1p100f ? 0x1p-100f : 1.f;
+    top = a * up;
+    inv = top > 0.f ? 127.f / top : 0.f;
+  }
+  // 16 values as bytes; E: the type they came in.
+  template <typename E>
+  CURE_DEV u32x4 bytes(const float (&x)[16]) const {
+    constexpr float kMagic = 12582912.f;           // 1.5 * 2^23: a sum's low bits are the integer
+    uint32_t y[16];
+    float off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float f = fmaf(x[i], inv, kMagic);
+      off = fmaxf(off, fabsf(fmaf(x[i], inv, kMagic - f)));
+      y[i] = __float_as_uint(f);
+    }
+    if (__builtin_expect(__any(up != 1.f || !(off <= 0.4999f)), 0)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = (uint32_t)(int)to_int(x[i] * up, top, inv, E());
+    }
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = bytes_of(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+    return out;
+  }
 };
 
-// A power of two by which a block is scaled first where 127 / a or 127 x would overflow: what it
-// rounds off is far below a / 254.
-CURE_DEV float scaled_by(float a) { return a < 0x1p-100f ? 0x1p100f : a > 0x1p100f ? 0x1p-100f : 1.f; }
+// What a wave's lanes take of a half of a block. K: unit i is 16 columns of a token, and 16 bytes of the
+// block. V: D / 32 columns of the 16 tokens 8 a + 4 h + c, each column 16 bytes of the block.
+template <int D>
+struct Lanes {
+  static constexpr int kUnits = D / 32;            // of K, per lane
+  static constexpr int kCols = D / 32;             // of V, per lane
+  static CURE_DEV int k_token(int lane, int i) { return (i * kWave + lane) / (D / 16); }
+  static CURE_DEV int k_col(int lane) { return lane % (D / 16) * 16; }
+  static CURE_DEV int k_byte(int t, int j) { return j / 32 * 1024 + j % 32 / 16 * 512 + t * 16; }
+  static CURE_DEV int v_token(int lane, int i) { return i / 4 * 8 + lane / 32 * 4 + i % 4; }
+  static CURE_DEV int v_col(int lane) { return lane % 32 * kCols; }
+  static CURE_DEV int v_byte(int lane, int j) { return j / 32 * 1024 + lane / 32 * 512 + j % 32 * 16; }
+};
+
+// The wave's part of a workgroup's: keys or values, and the tokens of a half.
+struct Role {
+  int lane, half;
+  bool values;
+  CURE_DEV Role() {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    lane = threadIdx.x % kWave;
+    half = wave % 2;
+    values = wave >= 2;
+  }
+};
 
 template <typename E, int D>
-__global__ __launch_bounds__(2 * kWave) void kv_pack(Args a) {
+__global__ __launch_bounds__(4 * kWave) void kv_pack(Args a) {
   using L = Lanes<D>;
+  __shared__ float highs[4];
   Part p;
   if (!part_of(a, true, p)) return;
-  const int lane = threadIdx.x % kWave;
-  const bool values = threadIdx.x >= kWave;
+  const Role r;
+  const int lane = r.lane, n = p.n - 32 * r.half;  // tokens of this half, or fewer than none
   const int64_t pitch = (int64_t)a.hkv * D, layer = blockIdx.z;
-  const E* src = static_cast<const E*>(values ? a.v : a.k) + layer * a.layer_stride + p.row * pitch + (int64_t)p.head * D;
+  const E* src = static_cast<const E*>(r.values ? a.v : a.k) + layer * a.layer_stride + (p.row + 32 * r.half) * pitch +
+                 (int64_t)p.head * D;
   const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
-  float* scale = (values ? a.v_scale : a.k_scale) + block;
-  int8_t* dst = (values ? a.pv : a.pk) + block * (kBlockTokens * D);
+  int8_t* dst = (r.values ? a.pv : a.pk) + block * (kBlockTokens * D) + r.half * (kBlockTokens / 2 * D);
+  // The block's largest, of both halves.
+  const auto highest = [&](float high) {
+    high = wave_max(high);
+    if (lane == 0) highs[threadIdx.x / kWave] = high;
+    __syncthreads();
+    high = fmaxf(highs[2 * r.values], highs[2 * r.values + 1]);
+    if (lane == 0 && r.half == 0) (r.values ? a.v_scale : a.k_scale)[block] = high / 127.f;
+    return high;
+  };
   float high = 0.f;
-  if (!values) {
+  if (!r.values) {
     RowVec<E, 16> x[L::kUnits];
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i) {
       const int t = L::k_token(lane, i);
-      if (t < p.n) x[i].load(src + t * pitch + L::k_col(lane));
+      if (t < n) x[i].load(src + t * pitch + L::k_col(lane));
       else x[i].clear();
     }
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
-    high = wave_max(high);
-    if (lane == 0) *scale = high / 127.f;
-    const float up = scaled_by(high), top = high * up, inv = top > 0.f ? 127.f / top : 0.f;
+    const Quant q(highest(high));
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i) {
-      u32x4 out;
+      float f[16];
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        float c[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) c[u] = to_int(x[i].get(j + u) * up, top, inv, E());
-        out[j / 4] = bytes_of(c[0], c[1], c[2], c[3]);
-      }
-      *reinterpret_cast<u32x4*>(dst + L::k_byte(L::k_token(lane, i), L::k_col(lane))) = out;
+      for (int j = 0; j < 16; ++j) f[j] = x[i].get(j);
+      *reinterpret_cast<u32x4*>(dst + L::k_byte(L::k_token(lane, i), L::k_col(lane))) = q.template bytes<E>(f);
     }
     return;
   }
@@ -148,46 +191,39 @@ __global__ __launch_bounds__(2 * kWave) void kv_pack(Args a) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int t = L::v_token(lane, i);
-    if (t < p.n) x[i].load(src + t * pitch + L::v_col(lane));
+    if (t < n) x[i].load(src + t * pitch + L::v_col(lane));
     else x[i].clear();
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i)
 #pragma unroll
     for (int j = 0; j < L::kCols; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
-  high = wave_max(high);
-  if (lane == 0) *scale = high / 127.f;
-  const float up = scaled_by(high), top = high * up, inv = top > 0.f ? 127.f / top : 0.f;
+  const Quant q(highest(high));
 #pragma unroll
   for (int j = 0; j < L::kCols; ++j) {
-    u32x4 out;
+    float f[16];
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      float c[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) c[u] = to_int(x[i + u].get(j) * up, top, inv, E());
-      out[i / 4] = bytes_of(c[0], c[1], c[2], c[3]);
-    }
-    *reinterpret_cast<u32x4*>(dst + L::v_byte(lane, L::v_col(lane) + j)) = out;
+    for (int i = 0; i < 16; ++i) f[i] = x[i].get(j);
+    *reinterpret_cast<u32x4*>(dst + L::v_byte(lane, L::v_col(lane) + j)) = q.template bytes<E>(f);
   }
 }
 
 // The same pieces the other way.
 template <typename E, int D>
-__global__ __launch_bounds__(2 * kWave) void kv_unpack(Args a) {
+__global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
   using L = Lanes<D>;
   Part p;
   if (!part_of(a, false, p)) return;
-  const int lane = threadIdx.x % kWave;
-  const bool values = threadIdx.x >= kWave;
+  const Role r;
+  const int lane = r.lane, skip = p.skip - 32 * r.half;
   const int64_t pitch = (int64_t)a.hkv * D, layer = blockIdx.z;
-  E* dst = static_cast<E*>(values ? a.v : a.k) + layer * a.layer_stride + (p.row - p.skip) * pitch + (int64_t)p.head * D;
+  E* dst = static_cast<E*>(r.values ? a.v : a.k) + layer * a.layer_stride + (p.row - skip) * pitch + (int64_t)p.head * D;
   const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
-  const float scale = (values ? a.v_scale : a.k_scale)[block];
-  const int8_t* src = (values ? a.pv : a.pk) + block * (kBlockTokens * D);
+  const float scale = (r.values ? a.v_scale : a.k_scale)[block];
+  const int8_t* src = (r.values ? a.pv : a.pk) + block * (kBlockTokens * D) + r.half * (kBlockTokens / 2 * D);
   const auto value = [&](const u32x4& w, int i) { return scale * (float)(int8_t)(w[i / 4] >> (i % 4 * 8)); };
-  const auto wanted = [&](int t) { return t >= p.skip && t < p.skip + p.n; };
-  if (!values) {
+  const auto wanted = [&](int t) { return t >= skip && t < skip + p.n; };
+  if (!r.values) {
     u32x4 w[L::kUnits];
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i)
@@ -245,7 +281,7 @@ cure_status launch(Args a, int32_t dtype, int32_t n_layers, int32_t d, int32_t b
   if (st != CURE_OK || nothing) return st;
   if (n_layers <= 1) a.layer_stride = a.block_stride = 0;
   const int64_t touched = a.n_max == 0 ? 1 : blocks_of(a.n_max) + (kPack ? 0 : 1);
-  const dim3 grid((unsigned)(touched * a.hkv), (unsigned)batch, (unsigned)n_layers), block(2 * kWave);
+  const dim3 grid((unsigned)(touched * a.hkv), (unsigned)batch, (unsigned)n_layers), block(4 * kWave);
   hipStream_t s = as_stream(stream);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
   if (kPack) {

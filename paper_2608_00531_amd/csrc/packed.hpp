@@ -18,7 +18,7 @@ constexpr int kBlockTokens = CURE_PACK_TOKENS;
 __host__ __device__ inline int64_t blocks_of(int64_t n) { return (n + kBlockTokens - 1) / kBlockTokens; }
 
 // N values of a row, consecutive, as the dwords that hold them; widened to fp32, and back
-// with one rounding, to nearest even. N * sizeof(E) is 8 or a multiple of 16.
+// with one rounding, to nearest even. N * sizeof(E) is 4, 8 or a multiple of 16.
 template <typename E, int N>
 struct RowVec {
   static constexpr int kWords = N * (int)sizeof(E) / 4;
@@ -29,10 +29,14 @@ struct RowVec {
     for (int i = 0; i < kWords; ++i) w[i] = 0;
   }
   CURE_DEV void load(const E* p) {
+    if (kWords == 1) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+      return;
+    }
     if (kWords == 2) {
       const u32x2 x = *reinterpret_cast<const u32x2*>(p);
       w[0] = x[0];
-      w[1] = x[1];
+      w[1 % kWords] = x[1];
       return;
     }
 #pragma unroll
@@ -43,8 +47,12 @@ struct RowVec {
     }
   }
   CURE_DEV void store(E* p) const {
+    if (kWords == 1) {
+      *reinterpret_cast<uint32_t*>(p) = w[0];
+      return;
+    }
     if (kWords == 2) {
-      *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+      *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1 % kWords]};
       return;
     }
 #pragma unroll
