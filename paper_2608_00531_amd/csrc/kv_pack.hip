@@ -3,10 +3,12 @@
 //
 //   a = max |x|,  scale = a / 127,  c = rint(127 x / a)
 //
-// The integer is the exact quotient's nearest, ties to even. x * (127 / a) is within 2^-16 of the
-// quotient, so its nearest is right unless it lies between 0.4999 and 0.5 away; there the
-// remainder 127 x - c a, which fp32 holds exactly for bf16 values (15 bits) and fp64 for fp32 ones
-// (31 bits), says which.
+// The integer is the exact quotient's nearest, ties to even; ties are common in bf16, where x = a / 2
+// is one. With 127 x exact (15 bits), q0 = x * (127 / a) and the exact remainder r = 127 x - q0 a,
+// q0 + r / a is the quotient to fp32's last bit and a tie itself where it is one; no other quotient of
+// two 8-bit integers times 127 lies near enough to a tie to round to it. For fp32 values x * (127 / a)
+// is within 2^-16 of the quotient, so its nearest is right unless it lies between 0.49998 and 0.5 away;
+// there the remainder 127 x - c a, which fp64 holds exactly (31 bits), says which.
 //
 // Bound by memory. Two waves take one block and head of K, two of V, 32 tokens each, whole, in
 // registers: all their loads (8 KB of bf16 at head dim 128 each) are in flight together. A row's vectors lie
@@ -66,13 +68,7 @@ CURE_DEV bool part_of(const Args& a, bool whole_blocks, Part& p) {
 }
 
 // rint(127 x / a), ties to even; inv is near 127 / a.
-CURE_DEV float to_int(float x, float a, float inv, uint16_t) {
-  float c = rintf(x * inv);
-  const float r = 2.f * fmaf(-c, a, 127.f * x), m = fabsf(r);
-  if (m > a || (m == a && ((int)c & 1))) c += copysignf(1.f, r);
-  return c;
-}
-CURE_DEV float to_int(float x, float a, float inv, float) {
+CURE_DEV float to_int(float x, float a, float inv) {
   float c = rintf(x * inv);
   const double r = 2.0 * fma(-(double)c, (double)a, 127.0 * (double)x), m = fabs(r);
   if (m > (double)a || (m == (double)a && ((int)c & 1))) c += copysignf(1.f, (float)r);
@@ -86,28 +82,39 @@ CURE_DEV uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
 
 // How a block's values become integers. Where 127 / a or 127 x would overflow they are scaled by a power of
 // two first: what that rounds off is far below a / 254.
+template <typename E>
 struct Quant {
-  float up, top, inv;
+  static constexpr float kMagic = 12582912.f;      // 1.5 * 2^23: a sum's low bits are the integer
+  float up, top, inv, unit;
   CURE_DEV explicit Quant(float a) {
     up = a < 0x1p-100f ? 0x1p100f : a > 0x1p100f ? 0x1p-100f : 1.f;
     top = a * up;
     inv = top > 0.f ? 127.f / top : 0.f;
+    unit = inv * (1.f / 127.f);
   }
-  // 16 values as bytes; E: the type they came in.
-  template <typename E>
-  CURE_DEV u32x4 bytes(const float (&x)[16]) const {
-    constexpr float kMagic = 12582912.f;           // 1.5 * 2^23: a sum's low bits are the integer
+  // 16 values as bytes.
+  CURE_DEV u32x4 bytes(float (&x)[16]) const {
+    if (up != 1.f) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] *= up;
+    }
     uint32_t y[16];
     float off = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float f = fmaf(x[i], inv, kMagic);
-      off = fmaxf(off, fabsf(fmaf(x[i], inv, kMagic - f)));
+      float f;
+      if (sizeof(E) == 2) {
+        const float q = x[i] * inv;
+        f = fmaf(fmaf(-q, top, 127.f * x[i]), unit, q) + kMagic;
+      } else {
+        f = fmaf(x[i], inv, kMagic);
+        off = fmaxf(off, fabsf(fmaf(x[i], inv, kMagic - f)));
+      }
       y[i] = __float_as_uint(f);
     }
-    if (__builtin_expect(__any(up != 1.f || !(off <= 0.4999f)), 0)) {
+    if (sizeof(E) == 4 && __builtin_expect(__any(!(off <= 0.49998f)), 0)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = (uint32_t)(int)to_int(x[i] * up, top, inv, E());
+      for (int i = 0; i < 16; ++i) y[i] = (uint32_t)(int)to_int(x[i], top, inv);
     }
     u32x4 out;
 #pragma unroll
@@ -122,10 +129,13 @@ template <int D>
 struct Lanes {
   static constexpr int kUnits = D / 32;            // of K, per lane
   static constexpr int kCols = D / 32;             // of V, per lane
-  static CURE_DEV int k_token(int lane, int i) { return (i * kWave + lane) / (D / 16); }
+  // Token of unit i or of V's load i, the part that all lanes share and the lane's own, and the lane's column.
+  static CURE_DEV int k_token(int i) { return i * (kWave * 16 / D); }
+  static CURE_DEV int k_own(int lane) { return lane / (D / 16); }
   static CURE_DEV int k_col(int lane) { return lane % (D / 16) * 16; }
   static CURE_DEV int k_byte(int t, int j) { return j / 32 * 1024 + j % 32 / 16 * 512 + t * 16; }
-  static CURE_DEV int v_token(int lane, int i) { return i / 4 * 8 + lane / 32 * 4 + i % 4; }
+  static CURE_DEV int v_token(int i) { return i / 4 * 8 + i % 4; }
+  static CURE_DEV int v_own(int lane) { return lane / 32 * 4; }
   static CURE_DEV int v_col(int lane) { return lane % 32 * kCols; }
   static CURE_DEV int v_byte(int lane, int j) { return j / 32 * 1024 + lane / 32 * 512 + j % 32 * 16; }
 };
@@ -142,10 +152,20 @@ struct Role {
   }
 };
 
+// Has the values widened anew: kept in fp32 from the maximum on, they would take twice the registers.
+template <class Row, int kRows>
+CURE_DEV void forget(Row (&x)[kRows]) {
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+#pragma unroll
+    for (int j = 0; j < Row::kWords; ++j) asm volatile("" : "+v"(x[i].w[j]));
+}
+
 template <typename E, int D>
-__global__ __launch_bounds__(4 * kWave) void kv_pack(Args a) {
+__global__ __launch_bounds__(4 * kWave, sizeof(E) == 2 ? 7 : 5) void kv_pack(Args a) {
   using L = Lanes<D>;
   __shared__ float highs[4];
+  __shared__ __attribute__((aligned(16))) u32x4 turn[4][D * 2];
   Part p;
   if (!part_of(a, true, p)) return;
   const Role r;
@@ -167,45 +187,63 @@ __global__ __launch_bounds__(4 * kWave) void kv_pack(Args a) {
   float high = 0.f;
   if (!r.values) {
     RowVec<E, 16> x[L::kUnits];
+    const int own = L::k_own(lane);
+    const uint32_t at = own * (uint32_t)pitch + L::k_col(lane);
+    if (n >= kBlockTokens / 2) {
 #pragma unroll
-    for (int i = 0; i < L::kUnits; ++i) {
-      const int t = L::k_token(lane, i);
-      if (t < n) x[i].load(src + t * pitch + L::k_col(lane));
-      else x[i].clear();
+      for (int i = 0; i < L::kUnits; ++i) x[i].load(src + L::k_token(i) * pitch + at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L::kUnits; ++i) {
+        x[i].clear();
+        if (L::k_token(i) + own < n) x[i].load(src + L::k_token(i) * pitch + at);
+      }
     }
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
-    const Quant q(highest(high));
+    const Quant<E> q(highest(high));
+    forget(x);
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i) {
       float f[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) f[j] = x[i].get(j);
-      *reinterpret_cast<u32x4*>(dst + L::k_byte(L::k_token(lane, i), L::k_col(lane))) = q.template bytes<E>(f);
+      *reinterpret_cast<u32x4*>(dst + L::k_byte(L::k_token(i) + own, L::k_col(lane))) = q.bytes(f);
     }
     return;
   }
   RowVec<E, L::kCols> x[16];
+  const int own = L::v_own(lane);
+  const uint32_t at = own * (uint32_t)pitch + L::v_col(lane);
+  if (n >= kBlockTokens / 2) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int t = L::v_token(lane, i);
-    if (t < n) x[i].load(src + t * pitch + L::v_col(lane));
-    else x[i].clear();
+    for (int i = 0; i < 16; ++i) x[i].load(src + L::v_token(i) * pitch + at);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i].clear();
+      if (L::v_token(i) + own < n) x[i].load(src + L::v_token(i) * pitch + at);
+    }
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i)
 #pragma unroll
     for (int j = 0; j < L::kCols; ++j) high = fmaxf(high, fabsf(x[i].get(j)));
-  const Quant q(highest(high));
+  const Quant<E> q(highest(high));
+  forget(x);
 #pragma unroll
   for (int j = 0; j < L::kCols; ++j) {
     float f[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) f[i] = x[i].get(j);
-    *reinterpret_cast<u32x4*>(dst + L::v_byte(lane, L::v_col(lane) + j)) = q.template bytes<E>(f);
+    turn[threadIdx.x / kWave][L::v_byte(lane, L::v_col(lane) + j) / 16] = q.bytes(f);
   }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < L::kCols; ++j) reinterpret_cast<u32x4*>(dst)[j * kWave + lane] = turn[threadIdx.x / kWave][j * kWave + lane];
 }
 
 // The same pieces the other way.
@@ -219,35 +257,42 @@ __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
   const int64_t pitch = (int64_t)a.hkv * D, layer = blockIdx.z;
   E* dst = static_cast<E*>(r.values ? a.v : a.k) + layer * a.layer_stride + (p.row - skip) * pitch + (int64_t)p.head * D;
   const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
+  const bool all = skip <= 0 && skip + p.n >= kBlockTokens / 2;
   const float scale = (r.values ? a.v_scale : a.k_scale)[block];
   const int8_t* src = (r.values ? a.pv : a.pk) + block * (kBlockTokens * D) + r.half * (kBlockTokens / 2 * D);
-  const auto value = [&](const u32x4& w, int i) { return scale * (float)(int8_t)(w[i / 4] >> (i % 4 * 8)); };
+  // scale * c as (c + 128) * scale - 128 * scale, rounded once.
+  const float less = -128.f * scale;
+  const auto value = [&](const u32x4& w, int i) {
+    return fmaf((float)(((w[i / 4] ^ 0x80808080u) >> (i % 4 * 8)) & 255u), scale, less);
+  };
   const auto wanted = [&](int t) { return t >= skip && t < skip + p.n; };
   if (!r.values) {
+    const int own = L::k_own(lane);
+    const uint32_t at = own * (uint32_t)pitch + L::k_col(lane);
     u32x4 w[L::kUnits];
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i)
-      w[i] = *reinterpret_cast<const u32x4*>(src + L::k_byte(L::k_token(lane, i), L::k_col(lane)));
+      w[i] = *reinterpret_cast<const u32x4*>(src + L::k_byte(L::k_token(i) + own, L::k_col(lane)));
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i) {
-      const int t = L::k_token(lane, i);
       RowVec<E, 16> x;
 #pragma unroll
       for (int j = 0; j < 16; j += 2) x.put2(j, value(w[i], j), value(w[i], j + 1));
-      if (wanted(t)) x.store(dst + t * pitch + L::k_col(lane));
+      if (all || wanted(L::k_token(i) + own)) x.store(dst + L::k_token(i) * pitch + at);
     }
     return;
   }
+  const int own = L::v_own(lane);
+  const uint32_t at = own * (uint32_t)pitch + L::v_col(lane);
   u32x4 w[L::kCols];
 #pragma unroll
   for (int j = 0; j < L::kCols; ++j) w[j] = *reinterpret_cast<const u32x4*>(src + L::v_byte(lane, L::v_col(lane) + j));
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int t = L::v_token(lane, i);
     RowVec<E, L::kCols> x;
 #pragma unroll
     for (int j = 0; j < L::kCols; j += 2) x.put2(j, value(w[j], i), value(w[j + 1], i));
-    if (wanted(t)) x.store(dst + t * pitch + L::v_col(lane));
+    if (all || wanted(L::v_token(i) + own)) x.store(dst + L::v_token(i) * pitch + at);
   }
 }
 
