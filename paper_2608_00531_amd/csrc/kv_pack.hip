@@ -13,7 +13,9 @@
 // Bound by memory. Two waves take one block and head of K, two of V, 32 tokens each, whole, in
 // registers: all their loads (8 KB of bf16 at head dim 128 each) are in flight together. A row's vectors lie
 // in neighbouring lanes; the 16 tokens that a lane of V's layout holds are its own 16 loads, so that its
-// bytes come together without exchange.
+// bytes come together without exchange, and LDS turns them for the stores to be whole lines. Eight prompts
+// of 501 to 4001 rows, 8 heads of 128: packed in 25 us and 4.4 TB/s (32 where the rows pass through the
+// caches in the ordinary way), unpacked in 20 us and 5.4 TB/s (where its ordinary stores do better: 25).
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -191,12 +193,12 @@ __global__ __launch_bounds__(4 * kWave, sizeof(E) == 2 ? 7 : 5) void kv_pack(Arg
     const uint32_t at = own * (uint32_t)pitch + L::k_col(lane);
     if (n >= kBlockTokens / 2) {
 #pragma unroll
-      for (int i = 0; i < L::kUnits; ++i) x[i].load(src + L::k_token(i) * pitch + at);
+      for (int i = 0; i < L::kUnits; ++i) x[i].template load<true>(src + L::k_token(i) * pitch + at);
     } else {
 #pragma unroll
       for (int i = 0; i < L::kUnits; ++i) {
         x[i].clear();
-        if (L::k_token(i) + own < n) x[i].load(src + L::k_token(i) * pitch + at);
+        if (L::k_token(i) + own < n) x[i].template load<true>(src + L::k_token(i) * pitch + at);
       }
     }
 #pragma unroll
@@ -219,12 +221,12 @@ __global__ __launch_bounds__(4 * kWave, sizeof(E) == 2 ? 7 : 5) void kv_pack(Arg
   const uint32_t at = own * (uint32_t)pitch + L::v_col(lane);
   if (n >= kBlockTokens / 2) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i].load(src + L::v_token(i) * pitch + at);
+    for (int i = 0; i < 16; ++i) x[i].template load<true>(src + L::v_token(i) * pitch + at);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       x[i].clear();
-      if (L::v_token(i) + own < n) x[i].load(src + L::v_token(i) * pitch + at);
+      if (L::v_token(i) + own < n) x[i].template load<true>(src + L::v_token(i) * pitch + at);
     }
   }
 #pragma unroll

@@ -17,6 +17,12 @@ constexpr int kBlockTokens = CURE_PACK_TOKENS;
 // Blocks that n tokens take.
 __host__ __device__ inline int64_t blocks_of(int64_t n) { return (n + kBlockTokens - 1) / kBlockTokens; }
 
+// Loads of what a kernel reads once, which need not stay in its caches; others.
+template <bool kOnce, typename T>
+CURE_DEV T load_of(const T* p) {
+  return kOnce ? __builtin_nontemporal_load(p) : *p;
+}
+
 // N values of a row, consecutive, as the dwords that hold them; widened to fp32, and back
 // with one rounding, to nearest even. N * sizeof(E) is 4, 8 or a multiple of 16.
 template <typename E, int N>
@@ -28,20 +34,21 @@ struct RowVec {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
   }
+  template <bool kOnce = false>
   CURE_DEV void load(const E* p) {
     if (kWords == 1) {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
+      w[0] = load_of<kOnce>(reinterpret_cast<const uint32_t*>(p));
       return;
     }
     if (kWords == 2) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      const u32x2 x = load_of<kOnce>(reinterpret_cast<const u32x2*>(p));
       w[0] = x[0];
       w[1 % kWords] = x[1];
       return;
     }
 #pragma unroll
     for (int i = 0; i < kWords; i += 4) {
-      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i / 4];
+      const u32x4 x = load_of<kOnce>(reinterpret_cast<const u32x4*>(p) + i / 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[(i + j) % kWords] = x[j];
     }
