@@ -13,7 +13,10 @@
 // integers, weights are formed in fp64 once for each bin or summed as integers, and the bins' sums
 // are added in one order.
 //
-// One workgroup takes a row, so that every bin is in one LDS.
+// One workgroup takes a row, so that every bin is in one LDS. A row is read twice, for its histogram and for the
+// drawn value's entries: 544 bf16 rows of 128256 take 59 us, of which the LDS additions (about 8
+// cycles for a wave's 64, by their conflicts) are a half and the reads another third; one row 25 us, fifteen
+// of them latency of the steps between.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -22,11 +25,10 @@
 namespace cure {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / kWave;
 constexpr double kRange = 64.0;                    // weights reach 64 T below the maximum
+constexpr int kMostWaves = 16;                     // of a workgroup
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kList = 2048;                        // entries of a bin that are put in order in a list, at most
+constexpr int kList = 1024;                        // entries of a bin that are put in order in a list, at most
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -70,12 +72,25 @@ CURE_DEV void answer(const Args& a, int64_t r, int token, float logprob, int kep
 }
 CURE_DEV void no_answer(const Args& a, int64_t r) { answer(a, r, CURE_NO_TOKEN, -INFINITY, 0); }
 
+// exp(y) for -709 < y <= 0: 2^k e^f with |f| <= ln 2 / 2, whose series' next term is below 2^-57.
+CURE_DEV double exp_of(double y) {
+  const double k = rint(y * 1.4426950408889634074);
+  const double f = fma(k, -2.3190468138462996e-17, fma(k, -0.6931471805599453094, y));      // ln 2 in two parts
+  const double f2 = f * f, f4 = f2 * f2;
+  const auto pair = [&](double a, double b) { return fma(f, b, a); };
+  const double low = fma(f2, pair(0.5, 1.0 / 6), pair(1.0, 1.0));
+  const double mid = fma(f2, pair(1.0 / 720, 1.0 / 5040), pair(1.0 / 24, 1.0 / 120));
+  const double high = fma(f2, pair(1.0 / 3628800, 1.0 / 39916800), pair(1.0 / 40320, 1.0 / 362880));
+  const double top = pair(1.0 / 479001600, 1.0 / 6227020800);
+  return ldexp(fma(f4, fma(f4, fma(f4, top, high), mid), low), (int)k);
+}
+
 // A row's map from values to weights.
 struct Scale {
   double m, inv_t, limit;            // limit: 64 T
   CURE_DEV double below(float x) const { return m - (double)x; }
   CURE_DEV bool has(float x) const { return below(x) <= limit; }
-  CURE_DEV double weight(float x) const { return exp(-below(x) * inv_t); }
+  CURE_DEV double weight(float x) const { return exp_of(-below(x) * inv_t); }
 };
 CURE_DEV Scale scale_of(float high, float t) {
   const double td = t == 0.f ? 1.0 : (double)t;    // T = 0: only what equals the maximum
@@ -110,14 +125,32 @@ struct Amount {
   double w;
 };
 CURE_DEV Amount operator+(Amount a, Amount b) { return Amount{a.n + b.n, a.w + b.w}; }
-CURE_DEV Amount lane_of(Amount a, int lane) { return Amount{__shfl(a.n, lane), __shfl(a.w, lane)}; }
-// Sum over the lanes up to this one.
+// Of one lane, the same for all.
+CURE_DEV Amount lane_of(Amount a, int lane) {
+  const auto read = [&](int x) { return __builtin_amdgcn_readlane(x, lane); };
+  return Amount{read(a.n), __hiloint2double(read(__double2hiint(a.w)), read(__double2loint(a.w)))};
+}
+// Of the lane below, nothing for the first.
+CURE_DEV Amount lower(Amount a) {
+  const auto move = [](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x138, 0xf, 0xf, false); };
+  return Amount{move(a.n), __hiloint2double(move(__double2hiint(a.w)), move(__double2loint(a.w)))};
+}
+// One step of a scan: what a DPP pattern brings from a lower lane is added in the rows of kRows, and
+// nothing where it brings none.
+template <int kPattern, int kRows>
+CURE_DEV Amount with_lower(Amount a) {
+  const auto move = [](int x) { return __builtin_amdgcn_update_dpp(0, x, kPattern, kRows, 0xf, false); };
+  return a + Amount{move(a.n), __hiloint2double(move(__double2hiint(a.w)), move(__double2loint(a.w)))};
+}
+// Sum over the lanes up to this one: in rows of 16, then row 0's last lane to row 1 and 2's to 3, then
+// lane 31 to the upper half.
 CURE_DEV Amount wave_scan(Amount a) {
-  for (int d = 1; d < kWave; d *= 2) {
-    const Amount up{__shfl_up(a.n, d), __shfl_up(a.w, d)};
-    if (lane_id() >= d) a = a + up;
-  }
-  return a;
+  a = with_lower<0x111, 0xf>(a);
+  a = with_lower<0x112, 0xf>(a);
+  a = with_lower<0x114, 0xf>(a);
+  a = with_lower<0x118, 0xf>(a);
+  a = with_lower<0x142, 0xa>(a);
+  return with_lower<0x143, 0xc>(a);
 }
 
 // A bin in the order: what lies before it, and what it holds.
@@ -130,7 +163,7 @@ struct Found {
 // sums lie in LDS; bin(pos) gives what a position holds.
 template <int kGroups, typename Bin>
 struct Order {
-  static constexpr int kEach = kGroups / kWave;    // groups of a lane
+  static constexpr int kEach = (kGroups + kWave - 1) / kWave;      // groups of a lane
   Bin bin;
   Amount group[kEach], before, upto;               // of the lane
 
@@ -142,8 +175,7 @@ struct Order {
       mine = mine + group[j];
     }
     upto = wave_scan(mine);
-    const Amount up{__shfl_up(upto.n, 1), __shfl_up(upto.w, 1)};
-    before = lane_id() ? up : Amount{0, 0.0};
+    before = lower(upto);
   }
   CURE_DEV Amount all() const { return lane_of(upto, kWave - 1); }
 
@@ -167,14 +199,13 @@ struct Order {
       }
       run = next;
     }
-    const int g = lane * kEach + __shfl(at, lane);
+    const int g = lane * kEach + __builtin_amdgcn_readlane(at, lane);
     base = lane_of(base, lane);
     const Amount in = bin(g * kWave + lane_id());
     const Amount sum = wave_scan(in);
     is = __ballot(in.n > 0 && hit(base + sum));
     const int l = is ? __ffsll(is) - 1 : 63 - __clzll(__ballot(in.n > 0));
-    const Amount here = lane_of(in, l), up{__shfl_up(sum.n, 1), __shfl_up(sum.w, 1)};
-    return Found{g * kWave + l, l ? base + lane_of(up, l) : base, here};
+    return Found{g * kWave + l, base + lane_of(lower(sum), l), lane_of(in, l)};
   }
 };
 
@@ -185,12 +216,12 @@ CURE_DEV int ties_to(double target, Amount before, Amount in, bool pass) {
 }
 
 // ---------------------------------------------------------------------------
-// Any values, and fp32 in general: bins of width T / 64 below the maximum. Relative to its upper edge an entry of a
-// bin has a weight in (exp(-1/64), 1], and 2^44 times it, rounded, leaves room for 2^20 of them
+// Any values, and fp32 in general: bins of width T / 32 below the maximum. Relative to its upper edge an entry of a
+// bin has a weight in (exp(-1/32), 1], and 2^44 times it, rounded, leaves room for 2^20 of them
 // in an integer. The bin of a place is gathered and put in order; where it holds too many entries
 // it is divided by their keys until it holds a single value.
-constexpr int kBins = 4096;
-constexpr int kPer = kBins / kThreads;             // bins of a thread
+constexpr int kBins = 2048;
+constexpr double kPerT = 32.0;                     // bins of a width T
 constexpr int kGroups = kBins / kWave;
 constexpr double kUnit = 0x1p44;
 
@@ -201,9 +232,10 @@ CURE_DEV uint32_t key_of(float x) {
 }
 CURE_DEV float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// exp(-y) for 0 <= y <= 1/64: the series' next term is below 2^-54.
+// exp(-y) for 0 <= y <= 1/32: the series' next term is below 2^-55.
 CURE_DEV double exp_small(double y) {
-  double p = 1.0 / 720;
+  double p = 1.0 / 5040;
+  p = fma(-y, p, 1.0 / 720);
   p = fma(-y, p, 1.0 / 120);
   p = fma(-y, p, 1.0 / 24);
   p = fma(-y, p, 1.0 / 6);
@@ -213,13 +245,13 @@ CURE_DEV double exp_small(double y) {
 }
 
 struct Binned : Scale {
-  CURE_DEV int bin(float x) const { return min((int)(below(x) * inv_t * kRange), kBins - 1); }
-  // Units of exp(-bin / 64) that an entry of the bin has.
+  CURE_DEV int bin(float x) const { return min((int)(below(x) * inv_t * kPerT), kBins - 1); }
+  // Units of exp(-bin / 32) that an entry of the bin has.
   CURE_DEV unsigned long long units(float x, int bin) const {
-    return (unsigned long long)rint(kUnit * exp_small(fmax(fma(below(x), inv_t, -bin * (1.0 / kRange)), 0.0)));
+    return (unsigned long long)rint(kUnit * exp_small(fmax(fma(below(x), inv_t, -bin * (1.0 / kPerT)), 0.0)));
   }
 };
-CURE_DEV double edge(int bin) { return exp(-bin * (1.0 / kRange)) / kUnit; }
+CURE_DEV double edge(int bin) { return exp_of(-bin * (1.0 / kPerT)) / kUnit; }
 
 // A place in the order: the entries before it, their weight.
 struct Place {
@@ -233,21 +265,21 @@ struct Run {
   double mass;
 };
 
-enum Query { kCount, kMass, kDraw, kValue };       // entries, weight reached, weight passed, values from a key on
+enum Query { kCount, kMass, kDraw };               // entries, weight reached, weight passed
 
 struct Shared {
   uint32_t cnt[kBins];
   unsigned long long mass[kBins];
-  uint32_t sum_cnt[kWaves];
-  double sum_mass[kWaves];
+  uint32_t sum_cnt[kMostWaves];
+  double sum_mass[kMostWaves];
   uint32_t found_bin;
   Place found;
   uint32_t lo, hi;
-  uint32_t seg[kWaves];
-  float max[kWaves];
+  uint32_t seg[kMostWaves];
+  float max[kMostWaves];
   // For places found in the first histogram.
-  int group_n[kGroups];
-  double group_w[kGroups];
+  int group_n[kWave];                // of groups, and zeros
+  double group_w[kWave];
   Found at;
   int query;
   double target;
@@ -261,7 +293,7 @@ struct Shared {
 CURE_DEV float widen(uint16_t x) { return bf16_to_f32(x); }
 CURE_DEV float widen(float x) { return x; }
 
-template <typename E>
+template <typename E, int kThreads>
 struct Row {
   const E* x;
   int vocab;
@@ -294,8 +326,9 @@ struct Row {
 
 // Finds in the histogram the first bin, in order, at which the place lies: its index (or -1),
 // and what is before it. weight(bin) is one unit's worth; bins are in descending order of value.
-template <typename W, typename Hit>
+template <int kThreads, typename W, typename Hit>
 CURE_DEV int find_bin(Shared& sh, const Place& base, W&& weight, Hit&& hit) {
+  constexpr int kPer = kBins / kThreads;           // bins of a thread
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   uint32_t c = 0;
   double w = 0.0;
@@ -340,7 +373,7 @@ CURE_DEV int find_bin(Shared& sh, const Place& base, W&& weight, Hit&& hit) {
     const int bin = tid * kPer + i;
     const int n = sh.cnt[bin];
     const double mass = n ? (double)sh.mass[bin] * weight(bin) : 0.0;
-    if (hit(bin, n, Place{p.count + n, p.mass + mass})) {
+    if (hit(n, Place{p.count + n, p.mass + mass})) {
       mine = bin;
       at = p;
     }
@@ -379,10 +412,10 @@ CURE_DEV int find_bin(Shared& sh, const Place& base, W&& weight, Hit&& hit) {
   return found;
 }
 
-// The run of `query`: count entries, or weight `target`, or values from key `from` on, at most
-// `most` entries. sh holds the first histogram, which is made again where it was replaced.
-template <typename E>
-CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Binned& sc, Query query, int count, double target, uint32_t from) {
+// The run of `query`: count entries, or weight `target`. sh holds the first histogram, which is made
+// again where it was replaced.
+template <typename E, int kThreads>
+CURE_DEV Run find_run(Shared& sh, const Row<E, kThreads>& row, const Binned& sc, Query query, int count, double target) {
   const int tid = threadIdx.x;
   const auto hit = [&](const Place& upto) {
     return query == kCount ? upto.count >= count : query == kMass ? upto.mass >= target : upto.mass > target;
@@ -401,9 +434,7 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Binned& sc, Query que
     atomicAdd(&sh.mass[bin], sc.units(x, bin));
   });
   __syncthreads();
-  const int from_bin = query == kValue ? sc.bin(value_of(from)) : 0;
-  const int bin = find_bin(sh, Place{0, 0.0}, edge,
-                           [&](int b, int n, const Place& upto) { return query == kValue ? b == from_bin : n > 0 && hit(upto); });
+  const int bin = find_bin<kThreads>(sh, Place{0, 0.0}, edge, [&](int n, const Place& upto) { return n > 0 && hit(upto); });
   Place base = sh.found;
   // The keys of the bin's entries.
   __syncthreads();
@@ -419,10 +450,8 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Binned& sc, Query que
   });
   __syncthreads();
   uint32_t lo = sh.lo, hi = sh.hi;
-  if (lo > hi) return Run{from, 0, base.count, base.mass};         // by value, and none in that bin
   const double unit = edge(bin);
   while (true) {
-    if (query == kValue && from > hi) return Run{from, 0, base.count, base.mass};
     // Bins of keys, the largest first.
     const uint32_t width = (hi - lo) / kBins + 1;
     __syncthreads();
@@ -440,17 +469,12 @@ CURE_DEV Run find_run(Shared& sh, const Row<E>& row, const Binned& sc, Query que
       atomicAdd(&sh.mass[i], sc.units(x, bin));
     });
     __syncthreads();
-    // By value: the bin that holds `from`, or the first one below the run.
-    const int at = find_bin(sh, base, [&](int) { return unit; }, [&](int b, int n, const Place& upto) {
-      return query == kValue ? (from <= lo ? b == kBins - 1 : b == (int)((hi - from) / width)) : n > 0 && hit(upto);
-    });
+    const int at = find_bin<kThreads>(sh, base, [&](int) { return unit; }, [&](int n, const Place& upto) { return n > 0 && hit(upto); });
     base = sh.found;
     const int n = sh.cnt[at];
     const double mass = n ? (double)sh.mass[at] * unit : 0.0;
-    if (query == kValue && from <= lo) return Run{lo, n, base.count + n, base.mass + mass};     // all of them: none equals it below
     const uint32_t top = hi - (uint32_t)at * width, bottom = top - lo < width ? lo : top - width + 1;
     if (width == 1 || n == 0) {
-      if (query == kValue) return Run{top, n, base.count + n, base.mass + mass};
       // One value: so many of its entries.
       const double each = mass / n;
       int ties = query == kCount ? count - base.count
@@ -471,8 +495,8 @@ struct Entry {
   int index;
   Amount upto;
 };
-template <typename E>
-CURE_DEV bool find_entry(Shared& sh, const Row<E>& row, const Binned& sc, Query query, int count, double target, Entry& out) {
+template <typename E, int kThreads>
+CURE_DEV bool find_entry(Shared& sh, const Row<E, kThreads>& row, const Binned& sc, Query query, int count, double target, Entry& out) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const auto hit = [&](Amount x) { return query == kCount ? x.n >= count : query == kMass ? x.w >= target : x.w > target; };
   __syncthreads();
@@ -491,8 +515,10 @@ CURE_DEV bool find_entry(Shared& sh, const Row<E>& row, const Binned& sc, Query 
   __syncthreads();
   const Found f = sh.at;
   if (f.in.n > kList) return false;
+  // Values somewhat beyond the bin's, by which to tell most entries without 64-bit arithmetic.
+  const float low = (float)(sc.m - (f.pos + 1.001) / (sc.inv_t * kPerT)), high = (float)(sc.m - (f.pos - 0.001) / (sc.inv_t * kPerT));
   row.each_at([&](float x, int i) {
-    if (!sc.has(x) || sc.bin(x) != f.pos) return;
+    if (!(x >= low && x <= high) || !sc.has(x) || sc.bin(x) != f.pos) return;
     const int k = atomicAdd(&sh.listed, 1);
     sh.key[k] = key_of(x);
     sh.index[k] = i;
@@ -551,10 +577,11 @@ CURE_DEV uint32_t key_from(const Binned& sc, float min_p) {
   return lo;
 }
 
-template <typename E>
+template <typename E, int kThreads>
 CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s) {
+  constexpr int kWaves = kThreads / kWave;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const Row<E> row{static_cast<const E*>(a.logits) + r * a.ld, a.vocab};
+  const Row<E, kThreads> row{static_cast<const E*>(a.logits) + r * a.ld, a.vocab};
   float high = -INFINITY;
   bool bad = false;
   for (int i = tid; i < kBins; i += kThreads) {
@@ -583,8 +610,8 @@ CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s
     atomicAdd(&sh.mass[bin], sc.units(x, bin));
   });
   __syncthreads();
-  for (int g = wave; g < kGroups; g += kWaves) {
-    const int pos = g * kWave + lane, n = (int)sh.cnt[pos];
+  for (int g = wave; g < kWave; g += kWaves) {
+    const int pos = g * kWave + lane, n = g < kGroups ? (int)sh.cnt[pos] : 0;
     Amount sum{0, 0.0};
     if (__ballot(n > 0)) sum = Amount{wave_sum(n), wave_sum(n ? (double)sh.mass[pos] * edge(pos) : 0.0)};
     if (lane == 0) {
@@ -597,55 +624,60 @@ CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s
   for (int g = 0; g < kGroups; ++g) run = run + Amount{sh.group_n[g], sh.group_w[g]};
   const Amount whole = run;
   const bool by_k = s.t > 0.f && s.top_k > 0 && s.top_k < run.n, by_p = s.t > 0.f && s.top_p < 1.f, by_min = s.t > 0.f && s.min_p > 0.f;
+  int reach = 1;                                   // entries whose weight is at least min_p
+  if (by_min && s.min_p <= 1.f) {
+    const float from = value_of(key_from(sc, s.min_p));
+    int n = 0;
+    row.each([&](float x) { n += x >= from; });
+    n = wave_sum(n);
+    if (lane == 0) sh.seg[wave] = n;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < kWaves; ++w) n += sh.seg[w];
+    reach = max(1, min(n, whole.n));
+  }
+  // Place q of the order that a row needs, if it does: top-k, top-p, min-p, the token; and the last
+  // entry kept, where rounding or a number of one and more lead past it. One loop, for the search to be in
+  // the code once.
+  struct Wanted {
+    bool is;
+    Query query;
+    int count;
+    double target;
+  };
+  const auto wanted = [&](int q, const Amount& kept, int drawn) {
+    if (q == 0) return Wanted{by_k, kCount, s.top_k, 0.0};
+    if (q == 1) return Wanted{by_p, kMass, 0, top_p * kept.w};
+    if (q == 2) return Wanted{by_min && reach < kept.n, kCount, reach, 0.0};
+    if (q == 3) return s.t == 0.f ? Wanted{true, kCount, 1, 0.0} : Wanted{true, kDraw, 0, u * kept.w};
+    return Wanted{drawn > kept.n, kCount, kept.n, 0.0};
+  };
+  const int q0 = s.t == 0.f ? 3 : 0;
+  if (s.t == 0.f) run = Amount{1, 1.0};
+  const Amount start = run;
   Entry e;
   bool quick = true;
-  if (s.t == 0.f) {
-    run = Amount{1, 1.0};
-    quick = find_entry(sh, row, sc, kCount, 1, 0.0, e);
-  } else {
-    if (by_k && (quick = find_entry(sh, row, sc, kCount, s.top_k, 0.0, e))) run = e.upto;
-    if (quick && by_p && (quick = find_entry(sh, row, sc, kMass, 0, top_p * run.w, e)) && e.upto.n < run.n) run = e.upto;
-    if (quick && by_min) {
-      if (s.min_p > 1.f) {
-        run = Amount{1, 1.0};
-      } else {
-        // How many reach min_p; then as a count.
-        const float from = value_of(key_from(sc, s.min_p));
-        int n = 0;
-        row.each([&](float x) { n += x >= from; });
-        n = wave_sum(n);
-        __syncthreads();
-        if (lane == 0) sh.seg[wave] = n;
-        __syncthreads();
-        n = 0;
-        for (int w = 0; w < kWaves; ++w) n += sh.seg[w];
-        n = max(1, min(n, whole.n));
-        if (n < run.n && (quick = find_entry(sh, row, sc, kCount, n, 0.0, e))) run = e.upto;
-      }
-    }
-    if (quick) quick = find_entry(sh, row, sc, kDraw, 0, u * run.w, e);
-    if (quick && e.upto.n > run.n) quick = find_entry(sh, row, sc, kCount, run.n, 0.0, e);
+#pragma unroll 1
+  for (int q = q0; q < 5 && quick; ++q) {
+    const Wanted w = wanted(q, run, q > 3 ? e.upto.n : 0);
+    if (!w.is) continue;
+    quick = find_entry(sh, row, sc, w.query, w.count, w.target, e);
+    if (quick && q < 3 && e.upto.n < run.n) run = e.upto;
   }
   if (quick) {
     if (tid == 0) answer(a, r, e.index, (float)(-sc.below(value_of(e.key)) * sc.inv_t - log(run.w)), run.n);
     return;
   }
   // A bin that holds too many: by keys.
-  Run kept{key_of(high), 1, 1, 1.0}, drawn = kept;
-  if (s.t > 0.f) {
-    kept = Run{0, 0, whole.n, whole.w};
-    if (by_k) kept = find_run(sh, row, sc, kCount, s.top_k, 0.0, 0);
-    if (by_p) {
-      const Run p = find_run(sh, row, sc, kMass, 0, top_p * kept.mass, 0);
-      if (p.count < kept.count) kept = p;
-    }
-    if (by_min) {
-      const Run v = s.min_p > 1.f ? Run{key_of(high), 1, 1, 1.0} : find_run(sh, row, sc, kValue, 0, 0.0, key_from(sc, s.min_p));
-      if (v.count < kept.count) kept = v;
-    }
-    drawn = find_run(sh, row, sc, kDraw, 0, u * kept.mass, 0);
-    // Rounding, or a number of one and more: the last entry kept.
-    if (drawn.count > kept.count) drawn = find_run(sh, row, sc, kCount, kept.count, 0.0, 0);
+  Amount kept = start;
+  Run drawn{key_of(high), 1, 1, 1.0};
+#pragma unroll 1
+  for (int q = q0; q < 5; ++q) {
+    const Wanted w = wanted(q, kept, drawn.count);
+    if (!w.is) continue;
+    const Run found = find_run(sh, row, sc, w.query, w.count, w.target);
+    if (q >= 3) drawn = found;
+    else if (found.count < kept.n) kept = Amount{found.count, found.mass};
   }
   // The drawn.ties-th entry of that value, by index: waves count in parts of the row.
   const int part = ((a.vocab + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
@@ -667,76 +699,89 @@ CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s
     const unsigned long long hits = __ballot(is);
     const int here = __popcll(hits & ((1ull << lane) - 1));
     if (is && before + here + 1 == drawn.ties)
-      answer(a, r, i + lane, (float)(-sc.below(value_of(drawn.key)) * sc.inv_t - log(kept.mass)), kept.count);
+      answer(a, r, i + lane, (float)(-sc.below(value_of(drawn.key)) * sc.inv_t - log(kept.w)), kept.n);
     before += __popcll(hits);
   }
 }
 
-__global__ __launch_bounds__(kThreads) void sample_f32(Args a) {
+constexpr int kThreads32 = 1024;
+
+__global__ __launch_bounds__(kThreads32) void sample_f32(Args a) {
   __shared__ Shared sh;
   const int64_t r = blockIdx.x;
   const Settings s = settings_of(a, r);
-  if (!s.none) sample_any<float>(sh, a, r, s);
+  if (!s.none) sample_any<float, kThreads32>(sh, a, r, s);
   else if (threadIdx.x == 0) no_answer(a, r);
 }
 
 // ---------------------------------------------------------------------------
-// bf16: a bin is a value, of which [2^-32, 2^32) has 64 octaves of 128 to either sign, and zero. Weights
-// are formed once for each bin in use, so that an entry costs a few packed integer instructions
-// and one LDS addition. Rows with other magnitudes that count go the general way.
-constexpr int kOctaves = 64 * 128;                 // bins of one sign
-constexpr int kBins16 = 2 * kOctaves;
-constexpr uint32_t kFirst16 = (127 - 32) << 7;     // bits of 2^-32
-constexpr int kLowest = 1, kHighest = kBins16 - 1; // the bins of the largest magnitudes
+// bf16: a bin is a value, of which [2^-30, 2^10) has 40 octaves of 128 to either sign, and zero. Weights
+// are formed once for each bin in use, so that an entry costs four packed integer instructions
+// and one LDS addition. Eight waves take a row and three rows share a CU, which hide each other's latency: 768
+// rows take 72 us, and 90 with 16 waves to a row and two to a CU; a single row 27 and 27. Rows with other magnitudes that count go the general way.
+constexpr int kOctaves = 40 * 128;                 // bins of one sign
+constexpr int kSign = 8192;                        // a negative value's, whose byte offset has its sign bit
+constexpr int kPlaces = 2 * kOctaves;              // in a row's order
+constexpr uint32_t kFirst16 = ((127 - 30) << 7) - 1;      // bits of the value below 2^-30
+constexpr int kLowest = kSign + kOctaves - 1, kHighest = kOctaves - 1; // the bins of the largest magnitudes
+constexpr int kZero = 0, kMinusZero = kSign;    // behind either, of the smallest
 constexpr uint32_t kMinusInf2 = 0xff80ff80u;
-constexpr int kGroups16 = kBins16 / kWave;
+constexpr int kGroups16 = kPlaces / kWave;
+constexpr int kGroupSlots = (kGroups16 + kWave - 1) / kWave * kWave;   // of groups, and zeros
+constexpr int kTies = 2048;                        // entries of one value that are put in order in a list, at most
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x2 __attribute__((ext_vector_type(2)));
+
 
 CURE_DEV u16x2 both(uint32_t x) { return __builtin_bit_cast(u16x2, x * 0x10001u); }
-// Bins of two values.
-CURE_DEV u16x2 bins_of(uint32_t w) {
+// Bins of two values, times 4.
+CURE_DEV uint32_t bins_of(uint32_t w) {
   const u16x2 mag = __builtin_bit_cast(u16x2, w & 0x7fff7fffu);
-  const u16x2 t = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, both(kFirst16)), both(kOctaves - 1));
-  const i16x2 sign = __builtin_bit_cast(i16x2, w) >> 15;
-  const i16x2 x = (__builtin_bit_cast(i16x2, t) ^ sign) - sign;
-  return __builtin_bit_cast(u16x2, x) + both(kOctaves);
+  u16x2 t = __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, both(kFirst16)), both(kOctaves - 1));
+  uint32_t one = 0x10001u;
+  asm("" : "+s"(one));                             // a minimum with a known 1 would become comparisons
+  t = __builtin_elementwise_max(t, __builtin_elementwise_min(mag, __builtin_bit_cast(u16x2, one))) << 2;
+  return (w & 0x80008000u) | __builtin_bit_cast(uint32_t, t);
 }
+constexpr uint32_t kLowest4 = 4 * kLowest;
+static_assert(kLowest4 < 0x10000 && 4 * kSign == 0x8000, "");
 CURE_DEV float value_of_bin(int bin) {
-  const int t = abs(bin - kOctaves);
-  const float x = __uint_as_float(t ? (uint32_t)(t + kFirst16) << 16 : 0u);
-  return bin < kOctaves ? -x : x;
+  const int t = bin % kSign;
+  return __uint_as_float(t ? (uint32_t)(t + kFirst16) << 16 | (bin >= kSign ? 0x80000000u : 0u) : 0u);
 }
+// The bin at a place of the order: positive values from the top down, zero, negative ones. The last
+// place is that of minus zero, whose entries are counted with zero's.
+CURE_DEV int bin_at(int pos) { return pos < kOctaves ? kOctaves - 1 - pos : kSign + (pos + 1) % kOctaves; }
 
 struct Shared16 {
-  int cnt[kBins16];
-  int idle[kWave];                   // takes what lies in the lowest bin, as masked entries do: no bin in use
-  int group_n[kGroups16];
-  double group_w[kGroups16];
-  int list[kList];
-  int listed, bad, lowest, high, reach, other;
+  union {
+    int cnt[kSign + kOctaves];
+    struct {                                       // between the two signs' bins
+      int positive[kOctaves];
+      double group_w[kGroupSlots];
+      int group_n[kGroupSlots];
+      int list[kTies];
+    };
+  };
+  int listed, bad, lowest, first, reach, other, odd;
   int bin, ties, kept;
   float logprob;
-  int seg[kWaves];
+  int seg[kMostWaves];
 };
+static_assert(sizeof(Shared16) <= 53760 && kOctaves + 3 * kGroupSlots + kTies <= kSign, "three to a CU");
 
-// A row's entries as 16-byte vectors: vector i * kThreads + thread for i < n, entries past the end
-// as -inf.
+// A row's entries, eight at least, as 16-byte vectors: vector i * kThreads + thread for i < n, entries
+// past the end as -inf.
+template <int kThreads>
 struct Row16 {
   const uint16_t* x;
   int vocab, n;
 
   // Index of the vector's first entry: the last vectors overlap, and what they repeat is -inf.
-  CURE_DEV int first(int i) const { return max(min((i * kThreads + (int)threadIdx.x) * 8, vocab - 8), 0); }
+  CURE_DEV int first(int i) const { return min((i * kThreads + (int)threadIdx.x) * 8, vocab - 8); }
   CURE_DEV u32x4 load(int i) const {
     u32x4 w;
-    if (vocab >= 8) {
-      __builtin_memcpy(&w, x + first(i), 16);      // rows need not begin with 16 bytes
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = x[min(2 * j, vocab - 1)] | (uint32_t)x[min(2 * j + 1, vocab - 1)] << 16;
-    }
+    __builtin_memcpy(&w, x + first(i), 16);        // rows need not begin with 16 bytes
     return w;
   }
   CURE_DEV u32x4 masked(u32x4 w, int i) const {
@@ -748,111 +793,159 @@ struct Row16 {
     }
     return w;
   }
-  // f(vector, i) for each, kAhead of whose loads are under way at a time.
+  // f(vector, i) for each, kAhead of whose loads are under way at a time beside the last ones'.
   static constexpr int kAhead = 4;
-  // Entries past the end that it goes over.
-  CURE_DEV int padding() const { return (n + kAhead - 1) / kAhead * kAhead * kThreads * 8 - vocab; }
   template <typename F>
   CURE_DEV void each(const F& f) const {
-#pragma unroll 1
-    for (int i = 0; i < n; i += kAhead) {
+    struct Ahead {
       u32x4 w[kAhead];
+    };
+    const auto fetch = [&](Ahead& a, int i) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) w[u] = load(min(i + u, n - 1));
+      for (int u = 0; u < kAhead; ++u) a.w[u] = load(min(i * kAhead + u, n - 1));
+    };
+    const auto take = [&](const Ahead& a, int i) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) f(i + u < n - 1 ? w[u] : masked(w[u], i + u), i + u);
+      for (int u = 0; u < kAhead; ++u) f(a.w[u], i * kAhead + u);
+    };
+    const int whole = (n - 1) / kAhead;            // so many times kAhead that have no end among them
+    Ahead even, odd;                               // in turn: a copy would wait for its loads
+    fetch(even, 0);
+    for (int i = 0; i < whole; i += 2) {
+      fetch(odd, i + 1);
+      take(even, i);
+      if (i + 1 == whole) {
+        even = odd;
+        break;
+      }
+      fetch(even, i + 2);
+      take(odd, i + 1);
+    }
+#pragma unroll 1
+    for (int i = whole * kAhead; i < n; ++i) {
+      f(masked(even.w[0], i), i);
+#pragma unroll
+      for (int u = 0; u + 1 < kAhead; ++u) even.w[u] = even.w[u + 1];
     }
   }
 };
 
-__global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
-  __shared__ union {
-    Shared16 own;
-    Shared any;
-  } space;
-  Shared16& sh = space.own;
+// False, once all threads have left sh: the row has to go the general way.
+template <int kThreads>
+CURE_DEV bool sample_exact(Shared16& sh, const Args& a, int64_t r, const Settings& s) {
+  constexpr int kWaves = kThreads / kWave, kWaveGroups = kGroups16 / kWaves;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int64_t r = blockIdx.x;
-  const Settings s = settings_of(a, r);
-  if (s.none) {
-    if (tid == 0) no_answer(a, r);
-    return;
-  }
-  const Row16 row{static_cast<const uint16_t*>(a.logits) + r * a.ld, a.vocab, (a.vocab + 8 * kThreads - 1) / (8 * kThreads)};
-  for (int i = tid; i < kBins16 / 4; i += kThreads) reinterpret_cast<u32x4*>(sh.cnt)[i] = u32x4{0, 0, 0, 0};
-  if (tid < kWave) sh.idle[tid] = 0;
+  if (a.vocab < 8) return false;
+  const Row16<kThreads> row{static_cast<const uint16_t*>(a.logits) + r * a.ld, a.vocab, (a.vocab + 8 * kThreads - 1) / (8 * kThreads)};
+  for (int i = tid; i < (kSign + kOctaves) / 4; i += kThreads) reinterpret_cast<u32x4*>(sh.cnt)[i] = u32x4{0, 0, 0, 0};
   if (tid == 0) {
     sh.listed = sh.bad = sh.lowest = sh.reach = sh.other = 0;
-    sh.high = -1;
+    sh.first = kPlaces;
   }
   __syncthreads();
+  const auto count = [&](uint32_t bin4) { atomicAdd(reinterpret_cast<int*>(reinterpret_cast<char*>(sh.cnt) + bin4), 1); };
+  // What lies in the lowest bin is not counted there: -inf, as masked entries are, would have the lanes
+  // of a wave wait for each other.
+  int low = 0;                                     // finite ones
+  bool bad = false;
   row.each([&](const u32x4& w, int) {
+    uint32_t b[4];
+    u16x2 high = both(0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const u16x2 b = bins_of(w[j]);
+      b[j] = bins_of(w[j]);
+      high = __builtin_elementwise_max(high, __builtin_bit_cast(u16x2, b[j]));
+    }
+    if (__builtin_expect(__any(high[0] == kLowest4 || high[1] == kLowest4), 0)) {
+      // One word after the other, in a loop that is short.
+      u32x4 left = w;
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) atomicAdd(b[e] == kLowest ? &sh.idle[lane] : &sh.cnt[b[e]], 1);
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t v = e ? left[0] >> 16 : left[0] & 0xffffu, bin4 = bins_of(v) & 0xffffu;
+          if (bin4 != kLowest4) count(bin4);
+          else low += v < 0xff80u;
+          bad = bad || v > 0xff80u;
+        }
+        left = u32x4{left[1], left[2], left[3], left[0]};
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      count(b[j] & 0xffffu);
+      count(b[j] >> 16);
     }
   });
+  if (__any(low > 0)) {
+    low = wave_sum(low);
+    if (lane == 0) atomicAdd(&sh.lowest, low);
+  }
+  if (bad) sh.bad = 1;
   __syncthreads();
-  // Bins that stand for more than one value, rare but for -inf: NaNs and +inf, how many are
-  // finite in the lowest, and whether others have magnitudes that have no bins.
-  bool odd = sh.cnt[kHighest] > 0 || sh.cnt[kOctaves] > 0;
-  if (wave == 0) odd = odd || wave_sum(sh.idle[lane]) != row.padding();
-  if (__syncthreads_or(odd)) {
-    int low = 0;
-    bool bad = false, other = false;
+  // Other bins that stand for more than one value: +inf and NaNs, and magnitudes that have no bins.
+  if (tid == 0) {
+    sh.odd = sh.cnt[kHighest] > 0 || sh.cnt[kZero + 1] > 0 || sh.cnt[kMinusZero + 1] > 0;
+    sh.cnt[kZero] += sh.cnt[kMinusZero];
+    sh.cnt[kMinusZero] = 0;
+  }
+  __syncthreads();
+  if (sh.odd) {
+    bool other = false;
     row.each([&](const u32x4& w, int) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint32_t v = w[j / 2] >> (j % 2 * 16) & 0xffffu, mag = v & 0x7fffu;
-        const int bin = bins_of(v)[0];
         bad = bad || mag > 0x7f80u || v == 0x7f80u;
-        low += v < 0xff80u && bin == kLowest;
-        other = other || bin == kHighest || (bin == kOctaves && mag != 0);
+        other = other || (mag > 0 && mag <= kFirst16) || (v < 0x8000u && mag >= kFirst16 + kOctaves - 1);
       }
     });
-    low = wave_sum(low);
-    if (lane == 0 && low) atomicAdd(&sh.lowest, low);
     if (bad) sh.bad = 1;
     if (other) sh.other = 1;
     __syncthreads();
   }
-  // The highest bin in use: a wave's first group that has any.
-  for (int g = wave; g < kGroups16; g += kWaves) {
-    const int bin = kBins16 - 1 - (g * kWave + lane);
-    const unsigned long long used = __ballot(sh.cnt[bin] > 0);
-    if (!used) continue;
-    if (lane == 0) atomicMax(&sh.high, kBins16 - 1 - (g * kWave + __ffsll(used) - 1));
-    break;
+  // A wave's groups of 64 places, every kWaves-th one: which are used, and the first place that is.
+  const auto group_of = [&](int i) { return i * kWaves + wave; };
+  uint32_t used = 0;
+  int mine = kPlaces;
+#pragma unroll
+  for (int i = kWaveGroups - 1; i >= 0; --i) {
+    const int pos = group_of(i) * kWave + lane, n = sh.cnt[bin_at(pos)];
+    if (n > 0) mine = pos;
+    used |= __any(n > 0) ? 1u << i : 0u;
   }
+  if (lane < kGroupSlots / kWaves) {
+    sh.group_n[group_of(lane)] = 0;
+    sh.group_w[group_of(lane)] = 0.0;
+  }
+  mine = -wave_max(-mine);
+  if (lane == 0 && mine < kPlaces) atomicMin(&sh.first, mine);
   __syncthreads();
-  if (sh.bad || (sh.high < 0 && sh.lowest == 0)) {
+  const bool empty = sh.first == kPlaces;          // but for the lowest bin
+  if (sh.bad || (empty && sh.lowest == 0)) {
     if (tid == 0) no_answer(a, r);
-    return;
+    return true;
   }
-  const Scale sc = scale_of(value_of_bin(max(sh.high, kLowest)), s.t);
-  if (sh.other || (sh.lowest > 0 && (sh.high < 0 || sc.has(value_of_bin(kLowest))))) {
+  const Scale sc = scale_of(value_of_bin(empty ? kLowest : bin_at(sh.first)), s.t);
+  if (sh.other || (sh.lowest > 0 && (empty || sc.has(value_of_bin(kLowest))))) {
     __syncthreads();
-    sample_any<uint16_t>(space.any, a, r, s);
-    return;
+    return false;
   }
-  // What position `pos` of the order holds: bins from the top down.
+  // What a place of the order holds.
   const auto holds = [&](int pos) {
-    const int bin = kBins16 - 1 - pos, n = sh.cnt[bin];
+    const int bin = bin_at(pos), n = sh.cnt[bin];
     const float x = value_of_bin(bin);
     if (n == 0 || !sc.has(x)) return Amount{0, 0.0};
     return Amount{n, n * sc.weight(x)};
   };
   int reach = 0;                                   // entries whose weight is at least min_p
 #pragma unroll 1
-  for (int g = wave; g < kGroups16; g += kWaves) {
+  for (; used; used &= used - 1) {
+    const int g = group_of(__ffs(used) - 1);
     const Amount in = holds(g * kWave + lane);
-    Amount sum{0, 0.0};
-    if (__ballot(in.n > 0)) {
-      if (in.w >= in.n * (double)s.min_p) reach += in.n;
-      sum = Amount{wave_sum(in.n), wave_sum(in.w)};
-    }
+    if (in.w >= in.n * (double)s.min_p) reach += in.n;
+    const Amount sum{wave_sum(in.n), wave_sum(in.w)};
     if (lane == 0) {
       sh.group_n[g] = sum.n;
       sh.group_w[g] = sum.w;
@@ -893,7 +986,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
       if (q < 3 && upto.n < run.n) run = upto;
     }
     if (lane == 0) {
-      const int bin = kBins16 - 1 - f.pos;
+      const int bin = bin_at(f.pos);
       sh.bin = bin;
       sh.ties = ties;
       sh.kept = run.n;
@@ -904,17 +997,18 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
   // The ties-th entry of that value, by index.
   const int bin = sh.bin, n = sh.cnt[bin];
   // Zero where a word's entries have the bin's value.
-  const bool zero = bin == kOctaves;
-  const u16x2 bits = both(__float_as_uint(value_of_bin(bin)) >> 16);
-  const auto off = [&](uint32_t w) { return (u16x2)(__builtin_bit_cast(u16x2, zero ? w & 0x7fff7fffu : w) ^ bits); };
-  if (n <= kList) {
+  const uint32_t mask = bin == kZero ? 0x7fff7fffu : ~0u, bits = (__float_as_uint(value_of_bin(bin)) >> 16) * 0x10001u;
+  const auto off = [&](uint32_t w) { return __builtin_bit_cast(u16x2, (w & mask) ^ bits); };
+  if (n <= kTies) {
     row.each([&](const u32x4& w, int i) {
+      u16x2 x[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u16x2 x = off(w[j]);
-        if (x[0] == 0) sh.list[atomicAdd(&sh.listed, 1)] = row.first(i) + 2 * j;
-        if (x[1] == 0) sh.list[atomicAdd(&sh.listed, 1)] = row.first(i) + 2 * j + 1;
-      }
+      for (int j = 0; j < 4; ++j) x[j] = off(w[j]);
+      const u16x2 low = __builtin_elementwise_min(__builtin_elementwise_min(x[0], x[1]), __builtin_elementwise_min(x[2], x[3]));
+      if (low[0] && low[1]) return;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (x[j / 2][j % 2] == 0) sh.list[atomicAdd(&sh.listed, 1)] = row.first(i) + j;
     });
     __syncthreads();
     for (int i = tid; i < n; i += kThreads) {
@@ -923,7 +1017,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
       for (int j = 0; j < n; ++j) before += sh.list[j] < me;
       if (before == sh.ties - 1) answer(a, r, me, sh.logprob, sh.kept);
     }
-    return;
+    return true;
   }
   // Many: counted by vectors, waves and lanes, in the entries' order.
   int left = sh.ties;
@@ -954,7 +1048,24 @@ __global__ __launch_bounds__(kThreads, 8) void sample_bf16(Args a) {
     }
     left -= all;
     __syncthreads();
-    if (left <= 0) return;
+    if (left <= 0) break;
+  }
+  return true;
+}
+
+constexpr int kThreads16 = 512;
+
+__global__ __launch_bounds__(kThreads16, 6) void sample_bf16(Args a) {
+  __shared__ union {
+    Shared16 own;
+    Shared any;
+  } space;
+  const int64_t r = blockIdx.x;
+  const Settings s = settings_of(a, r);
+  if (s.none) {
+    if (threadIdx.x == 0) no_answer(a, r);
+  } else if (!sample_exact<kThreads16>(space.own, a, r, s)) {
+    sample_any<uint16_t, kThreads16>(space.any, a, r, s);
   }
 }
 
@@ -972,14 +1083,15 @@ extern "C" cure_status cure_sample(const void* logits, int32_t dtype, int32_t ba
   if (batch < 0 || rows < 0 || vocab < 1 || ld < vocab) return CURE_ERR_INVALID_ARG;
   if (vocab > kMaxVocab) return CURE_ERR_UNSUPPORTED;
   const int64_t total = (int64_t)batch * rows;
-  if (total >= (int64_t(1) << 31) / kThreads) return CURE_ERR_UNSUPPORTED;
+  if (total >= (int64_t(1) << 31) / 1024) return CURE_ERR_UNSUPPORTED;
   if (total == 0) return CURE_OK;
   if (!logits || !uniform || !token) return CURE_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == CURE_BF16 ? 2 : 4)) return CURE_ERR_INVALID_ARG;
   const Args a{logits, rows, vocab, ld, temperature, top_k, top_p, min_p, uniform, n_rows, token, logprob, kept};
-  const dim3 grid((unsigned)total), block(kThreads);
-  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, as_stream(stream), a); };
-  if (dtype == CURE_F32) run(sample_f32);
-  else run(sample_bf16);
+  const auto run = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(threads), 0, as_stream(stream), a);
+  };
+  if (dtype == CURE_F32) run(sample_f32, kThreads32);
+  else run(sample_bf16, kThreads16);
   return launch_status();
 }
