@@ -232,24 +232,27 @@ CURE_DEV uint32_t key_of(float x) {
 }
 CURE_DEV float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// exp(-y) for 0 <= y <= 1/32: the series' next term is below 2^-55.
-CURE_DEV double exp_small(double y) {
-  double p = 1.0 / 5040;
-  p = fma(-y, p, 1.0 / 720);
-  p = fma(-y, p, 1.0 / 120);
-  p = fma(-y, p, 1.0 / 24);
-  p = fma(-y, p, 1.0 / 6);
-  p = fma(-y, p, 0.5);
-  p = fma(-y, p, 1.0);
-  return fma(-y, p, 1.0);
+// 2^44 exp(-f / 32) for 0 <= f <= 1, rounded: the series' next term is below 2^-55, and 1.5 * 2^52 added leaves
+// the integer in the low bits.
+CURE_DEV unsigned long long units_of(double f) {
+  constexpr double u = -1.0 / kPerT;
+  constexpr double c2 = u * u / 2, c3 = c2 * u / 3, c4 = c3 * u / 4, c5 = c4 * u / 5, c6 = c5 * u / 6, c7 = c6 * u / 7;
+  double p = fma(f, kUnit * c7, kUnit * c6);
+  p = fma(f, p, kUnit * c5);
+  p = fma(f, p, kUnit * c4);
+  p = fma(f, p, kUnit * c3);
+  p = fma(f, p, kUnit * c2);
+  p = fma(f, p, kUnit * u);
+  p = fma(f, p, kUnit) + 0x1.8p52;
+  return (unsigned long long)__double_as_longlong(p) & ((1ull << 51) - 1);
 }
 
 struct Binned : Scale {
-  CURE_DEV int bin(float x) const { return min((int)(below(x) * inv_t * kPerT), kBins - 1); }
+  double per;                        // bins of a unit
+  CURE_DEV explicit Binned(const Scale& s) : Scale(s), per(s.inv_t * kPerT) {}
+  CURE_DEV int bin(float x) const { return min((int)(below(x) * per), kBins - 1); }
   // Units of exp(-bin / 32) that an entry of the bin has.
-  CURE_DEV unsigned long long units(float x, int bin) const {
-    return (unsigned long long)rint(kUnit * exp_small(fmax(fma(below(x), inv_t, -bin * (1.0 / kPerT)), 0.0)));
-  }
+  CURE_DEV unsigned long long units(float x, int bin) const { return units_of(below(x) * per - bin); }
 };
 CURE_DEV double edge(int bin) { return exp_of(-bin * (1.0 / kPerT)) / kUnit; }
 
@@ -516,7 +519,7 @@ CURE_DEV bool find_entry(Shared& sh, const Row<E, kThreads>& row, const Binned& 
   const Found f = sh.at;
   if (f.in.n > kList) return false;
   // Values somewhat beyond the bin's, by which to tell most entries without 64-bit arithmetic.
-  const float low = (float)(sc.m - (f.pos + 1.001) / (sc.inv_t * kPerT)), high = (float)(sc.m - (f.pos - 0.001) / (sc.inv_t * kPerT));
+  const float low = (float)(sc.m - (f.pos + 1.001) / sc.per), high = (float)(sc.m - (f.pos - 0.001) / sc.per);
   row.each_at([&](float x, int i) {
     if (!(x >= low && x <= high) || !sc.has(x) || sc.bin(x) != f.pos) return;
     const int k = atomicAdd(&sh.listed, 1);
@@ -600,7 +603,7 @@ CURE_DEV void sample_any(Shared& sh, const Args& a, int64_t r, const Settings& s
     if (tid == 0) no_answer(a, r);
     return;
   }
-  const Binned sc{scale_of(high, s.t)};
+  const Binned sc(scale_of(high, s.t));
   const double u = fmax(0.0, (double)s.u), top_p = fmax(0.0, (double)s.top_p);
   // The first histogram, and its groups' sums.
   row.each([&](float x) {
