@@ -992,8 +992,8 @@ __global__ __launch_bounds__(256) void packed_merge(Args a) {
 int64_t steps_of(int32_t packed, int32_t ctx, int32_t n) {
   return ((int64_t)packed + kStep - 1) / kStep + ((int64_t)ctx + n + kStep - 1) / kStep;
 }
-constexpr int64_t kOverhead = 8;       // steps' time that a workgroup takes besides its steps
-constexpr int64_t kJoined = 300000;    // values of splits written and joined in a step's time
+constexpr int kOverhead = 8;           // steps' time that a workgroup takes besides its steps
+constexpr double kJoined = 300000;     // values of splits written and joined in a step's time
 
 struct Plan {
   int32_t groups;                    // of many rows; 0: few
@@ -1019,36 +1019,55 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
   const int64_t room = kMostBytes / std::max<int64_t>(1, rows * hq * (d + 1) * 4);
   const int64_t at_once = (p.groups == 16 ? 1 : 2) * (int64_t)device_cu_count();       // workgroups
   int64_t longest = 1;
-  for (int32_t b = 0; b < batch; ++b)
-    if (n[b] > 0) longest = std::max(longest, steps_of(packed[b], ctx[b], n[b]));
+  double total = 1;                                // steps of all workgroups
+  for (int32_t b = 0; b < batch; ++b) {
+    if (n[b] <= 0) continue;
+    const int64_t steps = steps_of(packed[b], ctx[b], n[b]);
+    longest = std::max(longest, steps);
+    total += (double)((n[b] * group + p.tile - 1) / p.tile * hkv) * (double)steps;
+  }
   p.tiles = (int32_t)std::max<int64_t>(1, (most_rows + p.tile - 1) / p.tile);
-  // As many splits as asked for, or those that should take least: either so many turns of the longest, or
-  // all work spread evenly and one more. Eight steps at least, which is what the rest of a split costs.
-  const int64_t fewest = kv_split > 0 ? longest : (longest + kOverhead - 1) / kOverhead;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({fewest, (int64_t)kMaxSlots, room}));
-  int64_t best = INT64_MAX;
-  for (int64_t slots = kv_split > 0 ? std::min<int64_t>(kv_split, most) : 1; slots <= most; ++slots) {
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({longest, (int64_t)kMaxSlots, room}));
+  double best = -1;
+  const auto consider = [&](int64_t slots) {
+    slots = std::max<int64_t>(1, std::min(slots, most));
     const int32_t tps = (int32_t)(((longest + slots - 1) / slots + p.quantum - 1) / p.quantum * p.quantum);
-    int64_t groups = 0, work = 0, high = 0;
+    int64_t groups = 0, high = 0;
+    double work = 0;
     for (int32_t b = 0; b < batch; ++b) {
       if (n[b] <= 0) continue;
       const Cut c = cut_of((int)steps_of(packed[b], ctx[b], n[b]), tps, (int)slots, p.quantum);
       const int64_t g = (n[b] * group + p.tile - 1) / p.tile * hkv * c.n;
       groups += g;
-      work += g * (c.per + kOverhead);
+      work += (double)g * (c.per + kOverhead);
       high = std::max<int64_t>(high, c.per + kOverhead);
     }
     // The launch's workgroups that find nothing to do keep some places from the others at first: eight
     // single tokens with 4096 to 32768 tokens take 64 us in 472 workgroups and 75 in 512.
-    const int64_t places = groups < hkv * p.tiles * slots * batch ? at_once - at_once / 16 : at_once;
-    int64_t time = std::min((groups + places - 1) / places * high, work / at_once + high);
-    if (slots > 1) time += kOverhead + rows * hq * slots * d / kJoined;
-    if (time < best) {
-      best = time;
-      p.slots = (int32_t)slots;
-      p.tps = tps;
-    }
-    if (kv_split > 0) break;
+    const int64_t places = groups < (int64_t)hkv * p.tiles * slots * batch ? at_once - at_once / 16 : at_once;
+    double time = std::min((double)((groups + places - 1) / places) * high, work / at_once + high);
+    if (slots > 1) time += kOverhead + (double)rows * hq * slots * d / kJoined;
+    if (best >= 0 && time >= best) return;
+    best = time;
+    p.slots = (int32_t)slots;
+    p.tps = tps;
+  };
+  // As many splits as asked for, or those that should take least: either so many turns of the longest, or
+  // all work spread evenly and one more. Tried are one, those about which every place has one, and twice as
+  // many, of kOverhead steps at least.
+  if (kv_split > 0) {
+    consider(kv_split);
+    return p;
+  }
+  const int64_t useful = (longest + kOverhead - 1) / kOverhead;
+  const int64_t even = (int64_t)std::min(std::ceil((double)longest * at_once / total), (double)kMaxSlots);
+  int64_t last = 1;
+  consider(1);
+  for (int64_t slots : {even - 2, even - 1, even, 2 * even}) {
+    slots = std::min(slots, useful);
+    if (slots <= last) continue;
+    consider(slots);
+    last = slots;
   }
   return p;
 }
