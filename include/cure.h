@@ -575,7 +575,7 @@ cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* 
  *              or its rows or blocks reach past `rows` or `blocks`. Nothing of such a
  *              sequence is written.
  * Rows, or blocks, of different sequences that are written must not overlap.
- * Supports d in {64, 128}, batch <= 65535, n_layers <= 65535, n_max * hkv < 2^30. k, v and
+ * Supports d in {64, 128}, batch <= 65535, n_layers <= 65535, hkv <= 2^20, n_max * hkv < 2^30. k, v and
  * layer_stride in bytes must be multiples of 16. No workspace.
  */
 #define CURE_PACK_TOKENS 64
@@ -631,8 +631,11 @@ cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_sc
  * kv_split: 0 = automatic, else the number of splits of the longest context.
  * workspace: cure_packed_attn_workspace_size(...) bytes for the same arguments, 16-byte
  * aligned, as q, k, v, pk, pv and o are.
- * bf16: probabilities times the value's scale are rounded to bf16 for their product; their
- * sum and lse take them before. float32: float32 throughout.
+ * bf16: query rows meet the bytes as fp16 times a power of two for each row (off by at most 2^-39 of
+ * the row's largest value), and probabilities times the value's scale are rounded to fp16 for their
+ * product, 2^-12, but for the open rows, whose products take them to 2^-17; their sum and lse take
+ * them before. float32: float32 throughout. A scale of values below 2^-116 counts as 2^-116; one of
+ * zero needs bytes of zero, as packing makes them.
  */
 size_t cure_packed_attn_workspace_size(int32_t batch, int64_t rows, int32_t n_max, int32_t hq,
                                        int32_t hkv, int32_t d, const int32_t* host_n_rows,

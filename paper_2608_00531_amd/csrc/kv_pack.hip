@@ -306,7 +306,8 @@ cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int
     return CURE_ERR_INVALID_ARG;
   if (n_layers > 1 && (a.layer_stride < 0 || a.block_stride < 0)) return CURE_ERR_INVALID_ARG;
   if (d != 64 && d != 128) return CURE_ERR_UNSUPPORTED;
-  if (batch > 65535 || n_layers > 65535 || (int64_t)a.n_max * a.hkv >= (int64_t(1) << 30)) return CURE_ERR_UNSUPPORTED;
+  if (batch > 65535 || n_layers > 65535 || a.hkv > 1 << 20 || (int64_t)a.n_max * a.hkv >= (int64_t(1) << 30))
+    return CURE_ERR_UNSUPPORTED;                   // offsets within some rows are of 32 bits
   *nothing = batch == 0;
   if (batch == 0) return CURE_OK;
   if (!a.kv_off || !a.n_rows || !a.blk_off || !a.from || !a.row_status) return CURE_ERR_INVALID_ARG;

@@ -1,0 +1,87 @@
+"""Packed context: every length around a step's, a block's and a ring's end, against every number of rows that
+changes how rows are shared out; far offsets; calls at once on two streams."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_00531_amd as pc
+from packed_util import Case
+from prompt_util import ints, random_parents
+
+pytestmark = pytest.mark.gpu
+
+LENGTHS = [0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 160, 193, 225]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [64, 68, 128, 132, 252, 256, 260])
+@pytest.mark.parametrize("form", ["tree", "packed"])
+def test_lengths(d, rows, form):
+    """Rows of a kv-head: few, one tile of 128 or of 256, and several; the last waves have none, or some of theirs."""
+    n, batch = rows // 4, len(LENGTHS)
+    rng = np.random.default_rng(rows)
+    parents = [random_parents(rng, n) for _ in LENGTHS] if form == "tree" else None
+    for split, ctx in ((1, [0] * batch), (0, [(7 * i) % 45 for i in range(batch)]), (3, [33] * batch)):
+        c = Case("bf16", [n] * batch, LENGTHS, ctx, 4, 1, d, form=form, seed=split, parents=parents)
+        c.check(c.call(kv_split=split), every=9)
+
+
+@pytest.mark.parametrize("nodes", [40, 64, 100])
+def test_far_offsets_of_many_rows(nodes):
+    """As for few rows: blocks and cache rows more than 2^31 elements into their buffers."""
+    hkv, d = 8, 128
+    blocks, rows = (1 << 31) // (hkv * 64 * d) + 40, (1 << 31) // (hkv * d) + 400
+    c = Case("bf16", [nodes], [150], [20], 4 * hkv, hkv, d)
+    pk, pv = (torch.zeros(blocks, hkv, 64 * d, dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros(blocks, hkv, device="cuda") for _ in range(2))
+    k, v = (torch.zeros(rows, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    b0, r0 = blocks - c.blocks, rows - c.cache_rows
+    for big, x in ((pk, c.pk), (pv, c.pv), (ks, c.ks), (vs, c.vs)):
+        big[b0:] = x.cuda()
+    for big, x in ((k, c.k), (v, c.v)):
+        big[r0:] = x.cuda()
+    c.check(c.call(pk=pk, pv=pv, k_scale=ks, v_scale=vs, k=k, v=v, blk_off=ints([b0 + c.blk_off[0]], torch.int64),
+                   kv_off=ints([r0 + c.kv_off[0]], torch.int64)), every=5)
+
+
+def test_scales_and_masks_of_many_rows():
+    """Blocks whose scales lie far apart, a block of zeros, and infinities and NaN in rows and scales that nobody sees."""
+    c = Case("bf16", [33, 40], [300, 64], [30, 0], 8, 2, 128)
+    c.ks[:, 0] *= 2.0 ** -10
+    c.vs[::2] *= 2.0 ** 20
+    c.vs[1::2] *= 2.0 ** -40
+    first = c.blk_off[0]
+    c.vs[first + 1, 1], c.pv[first + 1, 1] = 0.0, 0
+    c.ks[first + 2, 0], c.pk[first + 2, 0] = 0.0, 0
+    used = {c.blk_off[b] + i for b in range(2) for i in range((c.packed[b] + 63) // 64)}
+    rows = {c.kv_off[b] + i for b in range(2) for i in range(c.ctx[b] + c.rows[b])}
+    for i in range(c.blocks):
+        if i not in used:
+            c.ks[i], c.vs[i] = float("nan"), float("inf")
+    for i in range(c.cache_rows):
+        if i not in rows:
+            c.k[i], c.v[i] = float("nan"), float("inf")
+    c.check(c.call())
+
+
+def test_two_streams_at_once():
+    """Calls of one shape on two streams, each with a workspace of its own, give what they give alone."""
+    cases = [Case("bf16", [n, 3], [900, 4000], [10, 0], 8, 2, 128, seed=n) for n in (2, 20, 50)]
+    alone = [c.call() for c in cases]
+    torch.cuda.synchronize()
+    args = [dict(c.args) for c in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(4):
+        for i, a in enumerate(args):
+            for s in streams:
+                with torch.cuda.stream(s):
+                    got.append((i, pc.cure_packed_attn(**a)))
+    torch.cuda.synchronize()
+    for i, (o, lse, status) in got:
+        for b, n in enumerate(cases[i].rows):
+            assert torch.equal(o[b, :n], alone[i][0][b, :n]) and torch.equal(lse[b, :n], alone[i][1][b, :n]), i
+        assert status.tolist() == [0, 0]
