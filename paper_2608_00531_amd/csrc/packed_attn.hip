@@ -5,14 +5,14 @@
 // Query row R of a kv-head is query head R % group of token R / group, so the heads that
 // share keys share a tile. With C the bytes and s_k, s_v the scales of a token's block,
 //   S = s_k (C_k Q^T),  P = s_v 2^(S - m),  l += P / s_v,  O^T += C_v^T P^T,  o = O / l
-// in one pass over the keys with the reference m, a running maximum of S + log2 s_v, and l in fp32.
+// in one pass over the keys with the reference m, near a running maximum of S + log2 s_v, and l in fp32.
 // The value's scale is part of the exponent, so a block whose values are large and one
 // whose values are small both have P in the range of 16 bits where they count at all.
 //
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
 // a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
 // to fp16 for its product, 2^-12 where bf16 would take 2^-9 and add half as much again to the error that the
-// output's own rounding makes. Open rows keep bf16's range: their products take P as two bf16 values.
+// output's own rounding makes; what lies 2^-21 below the largest P has fewer bits, down to 2^-32 of it. Open rows keep bf16's range: their products take P as two bf16 values.
 // fp32: fp32 throughout.
 //
 // 32x32 matrix instructions (x16 for 16 bits, x2 eight times for fp32), 32 query rows per wave. Lane
@@ -243,17 +243,18 @@ struct Sums {
       for (int r = 0; r < kEach; ++r) o[i][r] = 0.f;
   }
   // Scores x * factor of base 2 (-inf: not seen; factor > 0 there) of tokens whose values have scale 2^lv and
-  // its reciprocal rv: their P. The reference moves where a lane's P sum up to more than 2^8, as
-  // they do at first and seldom later; a maximum for each step would cost a tenth of it.
+  // its reciprocal rv: their P. The reference moves to where the largest P is 2^7, which leaves small ones of a
+  // million tokens precise in fp16, and does so where a lane's P sum up to more than 2^15, which fp16
+  // holds: at first, and seldom later. A maximum for each step would cost a tenth of it.
   CURE_DEV void soften(const float (&x)[kScores], float factor, float lv, float rv, float (&p)[kScores]) {
     float added = exps(x, factor, lv, p);
-    if (__builtin_expect(__any(!(added <= 256.f)), 0)) {
+    if (__builtin_expect(__any(!(added <= 0x1p15f)), 0)) {
       float high = x[0];
 #pragma unroll
       for (int r = 1; r < kScores; ++r) high = fmaxf(high, x[r]);
       if (kLanes == 4) high = fmaxf(high, __shfl_xor(high, 16));
       high = fmaf(max_halves(high), factor, lv);
-      const float mn = fmaxf(m, high), f = fast_exp2(m - mn);
+      const float mn = fmaxf(m, high - 7.f), f = fast_exp2(m - mn);
       m = mn;
       l *= f;
 #pragma unroll

@@ -85,3 +85,30 @@ def test_two_streams_at_once():
         for b, n in enumerate(cases[i].rows):
             assert torch.equal(o[b, :n], alone[i][0][b, :n]) and torch.equal(lse[b, :n], alone[i][1][b, :n]), i
         assert status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("heads", [1, 128])
+def test_many_small_probabilities_beside_a_large_one(heads):
+    """A million tokens of one score, each of 2^-21 of the first one's weight: together they are a third of the
+    row, and their roundings to 16 bits would all be alike. In 64 bits by hand; the bound is 2^-8 of the whole
+    for the probabilities, as of the other tests, and half a step of the output."""
+    n, d = 1 << 20, 64
+    bits = 21 - np.log2(1.0625)
+    pk = torch.ones(n // 64, 1, 64 * d, dtype=torch.int8, device="cuda")
+    pv = torch.full_like(pk, 100)
+    at = torch.arange(d)
+    pk[0, 0, (at // 32 * 1024 + at % 32 // 16 * 512 + at % 16).cuda()] = 25      # token 0's keys
+    pv[0, 0, (at // 32 * 1024 + at % 32 * 16).cuda()] = 0                        # and values
+    ks = torch.full((n // 64, 1), float(np.float32(bits * np.log(2) / (24 * 8))), device="cuda")
+    vs = torch.full((n // 64, 1), 0.01, device="cuda")
+    q = torch.ones(1, 1, heads, d, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros(2, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    zero = ints([0], torch.int64)
+    k[0] = -300.0                                                                # the new token's own row: no weight
+    o, lse, _ = pc.cure_packed_attn(q, pk, pv, ks, vs, zero, ints([n]), k, v, zero, ints([0]), ints([1]), [n], [0], [1], 0.125,
+                                    kv_split=1)
+    one = float(ks[0, 0]) * 8.0                                                  # a token's score
+    w = (n - 1) * np.exp(-24 * one)
+    want, want_lse = w * 100 * float(vs[0, 0]) / (1 + w), 25 * one + np.log1p(w)
+    assert np.all(np.abs(o.double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -8) * want)
+    assert np.all(np.abs(lse.double().cpu().numpy() - want_lse) <= ((d + 6) * 25 * one + n + 16) * 2.0 ** -24)
