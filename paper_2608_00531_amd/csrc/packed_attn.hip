@@ -49,6 +49,10 @@ constexpr int kStep = 32;            // tokens per step of the key loop
 constexpr int kWaves = 4;            // waves per workgroup of a tile of few rows
 constexpr int kRows = 32;            // query rows of such a wave, and of the tile
 constexpr int kManyRows = 16;        // query rows of a wave where there are many
+// Waves of such a tile on a SIMD. At d = 64 registers and LDS leave room for three workgroups (chunks of
+// 256 to 512 tokens: 243 us, 281 with two).
+template <int D>
+constexpr int kPerSimd = D == 64 ? 6 : 4;
 constexpr int kRing = 3;             // steps whose bytes are on their way or wait, of a tile of many rows
 constexpr int kMaxSlots = 64;        // splits of a row's keys at most
 constexpr float kNone = -3e38f;      // reference of a row that has seen nothing
@@ -742,7 +746,7 @@ struct Turn {
 };
 
 template <int D, int kGroups>
-__global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu(4, 4))) void packed_many(Args a) {
+__global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu(kPerSimd<D>, kPerSimd<D>))) void packed_many(Args a) {
   using E = uint16_t;
   constexpr int kK = D / 32, kO = D / 16;
   constexpr int kBring = 2 * kK;                   // waves that bring 1 KB of a step: keys', then values'
@@ -1010,15 +1014,15 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
   int64_t most_rows = 0;
   for (int32_t b = 0; b < batch; ++b) most_rows = std::max<int64_t>(most_rows, n[b] * group);
   Plan p;
-  // A tile of many rows has 128, or 256 where those are a sequence's all: that one then reads and widens
-  // its keys once (16 trees of 20 to 48 nodes, group 4: 83 us, 94 with 128). Of more rows two workgroups to a
-  // CU do better than one (chunks of 256 to 512 tokens, d = 64: 274 us to 311; d = 128 alike). Up to 64 rows
-  // the other form: four trees of 16 nodes on 32768 tokens 73 us to 107.
-  p.groups = dtype == CURE_F32 || most_rows <= 2 * kRows ? 0 : most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows ? 16 : 8;
+  // A tile of many rows has 128, or 256 where those are a sequence's all and d is 128: that one then reads and
+  // widens its keys once (16 trees of 20 to 48 nodes, group 4: 83 us, 94 with 128; at d = 64 60 with either).
+  // Of more rows two workgroups to a CU do as well as one and balance better (chunks of 256 to 512 tokens: 414
+  // us and 409). Up to 64 rows the other form: four trees of 16 nodes on 32768 tokens 73 us to 107.
+  p.groups = dtype == CURE_F32 || most_rows <= 2 * kRows ? 0 : d == 128 && most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows ? 16 : 8;
   p.quantum = p.groups ? 1 : kWaves;
   p.tile = p.groups ? p.groups * kManyRows : kRows;
   const int64_t room = kMostBytes / std::max<int64_t>(1, rows * hq * (d + 1) * 4);
-  const int64_t at_once = (p.groups == 16 ? 1 : 2) * (int64_t)device_cu_count();       // workgroups
+  const int64_t at_once = (p.groups == 16 ? 1 : p.groups == 8 && d == 64 ? 3 : 2) * (int64_t)device_cu_count();      // workgroups
   int64_t longest = 1;
   double total = 1;                                // steps of all workgroups
   for (int32_t b = 0; b < batch; ++b) {
@@ -1149,7 +1153,7 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
   if (dtype == CURE_F32) d == 128 ? run(packed_few<float, 128>) : run(packed_few<float, 64>);
   else if (!p.groups) d == 128 ? run(packed_few<uint16_t, 128>) : run(packed_few<uint16_t, 64>);
-  else if (p.groups == 16) d == 128 ? run(packed_many<128, 16>) : run(packed_many<64, 16>);
+  else if (p.groups == 16) run(packed_many<128, 16>);
   else d == 128 ? run(packed_many<128, 8>) : run(packed_many<64, 8>);
   const cure_status launched = launch_status();
   if (launched != CURE_OK || p.slots == 1 || n_max == 0) return launched;
