@@ -486,47 +486,50 @@ CURE_DEV uint32_t seen_of(const Args& a, const Work& w, const Trees<kTileRows>& 
   return seen;
 }
 
-// Where a workgroup's rows are joined and turned: kWaveRows of each of kAll waves.
-template <int D, int kAll, int kWaveRows>
-struct Out {
-  float o[kAll][kWaveRows][D + 4];
-  float m[kAll][kWaveRows], l[kAll][kWaveRows];
-};
+// Four columns from column j on of the tile's output row `at`, and the log-sum-exp of base 2 of a row.
+template <int D>
+CURE_DEV void write(const Args& a, const Work& w, int64_t at, int j, const f32x4& x) {
+  if (w.cut.n > 1) *reinterpret_cast<f32x4*>(a.part_o + (at * a.slots + w.slot) * D + j) = x;
+  else if (a.out_bf16)
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + at * D + j) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+  else *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + at * D + j) = x;
+}
+CURE_DEV void write_lse(const Args& a, const Work& w, int64_t at, float m, float l) {
+  const float lse2 = l > 0.f ? m + log2f(l) : -INFINITY;
+  if (w.cut.n > 1) a.part_lse[at * a.slots + w.slot] = lse2;
+  else if (a.lse) a.lse[at] = lse2 * kLn2;
+}
 
-// Writes a tile's rows: kTile groups of kWaveRows, each the sum of kAll / kTile waves (wave w has rows
-// of group w % kTile), which have put theirs into sh.
-template <int D, int kTile, int kAll, int kWaveRows>
-CURE_DEV void finish(const Args& a, const Work& w, const Out<D, kAll, kWaveRows>& sh) {
-  constexpr int kParts = kAll / kTile, kChunks = D / 4;
+// Where a tile of few rows is joined: the same rows of each wave.
+template <int D>
+struct Out {
+  float o[kWaves][kRows][D + 4];
+  float m[kWaves][kRows], l[kWaves][kRows];
+};
+// Writes the tile's rows, the sums of what the waves have put into sh.
+template <int D>
+CURE_DEV void finish(const Args& a, const Work& w, const Out<D>& sh) {
+  constexpr int kChunks = D / 4;
   __syncthreads();
-  const bool whole = w.cut.n == 1;
-  for (int c = threadIdx.x; c < kTile * kWaveRows * kChunks; c += kAll * kWave) {
-    const int row = c / kChunks, j = c % kChunks * 4, group = row / kWaveRows, rr = row % kWaveRows;
+  for (int c = threadIdx.x; c < kRows * kChunks; c += kWaves * kWave) {
+    const int row = c / kChunks, j = c % kChunks * 4;
     if (w.r0 + row >= w.rows) break;
-    float m = kNone, ll = 0.f, f[kParts];
+    float m = kNone, l = 0.f, f[kWaves];
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) m = fmaxf(m, sh.m[group + k * kTile][rr]);
+    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, sh.m[k][row]);
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      f[k] = fast_exp2(sh.m[group + k * kTile][rr] - m);
-      ll += f[k] * sh.l[group + k * kTile][rr];
+    for (int k = 0; k < kWaves; ++k) {
+      f[k] = fast_exp2(sh.m[k][row] - m);
+      l += f[k] * sh.l[k][row];
     }
-    const float inv = ll > 0.f ? 1.f / ll : 0.f;
     f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[group + k * kTile][rr][j]);
-    x *= inv;
+    for (int k = 0; k < kWaves; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[k][row][j]);
+    x *= l > 0.f ? 1.f / l : 0.f;
     const int R = w.r0 + row;
     const int64_t at = (w.s.row0 + R / a.group) * a.hq + w.hk * a.group + R % a.group;
-    if (j == 0) {
-      const float lse2 = ll > 0.f ? m + log2f(ll) : -INFINITY;
-      if (!whole) a.part_lse[at * a.slots + w.slot] = lse2;
-      else if (a.lse) a.lse[at] = lse2 * kLn2;
-    }
-    if (!whole) *reinterpret_cast<f32x4*>(a.part_o + (at * a.slots + w.slot) * D + j) = x;
-    else if (a.out_bf16)
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + at * D + j) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-    else *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + at * D + j) = x;
+    if (j == 0) write_lse(a, w, at, m, l);
+    write<D>(a, w, at, j, x);
   }
 }
 
@@ -563,7 +566,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
   constexpr int kK = D / 32;                       // pieces of 32 columns
   using Byte = typename Types<E>::Byte;
   using RowF = typename Types<E>::Row;
-  __shared__ __attribute__((aligned(16))) Out<D, kWaves, kRows> out;
+  __shared__ __attribute__((aligned(16))) Out<D> out;
   __shared__ Trees<kRows> trees;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 32, half = lane / 32;
@@ -713,7 +716,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
     for (int r = 0; r < 16; r += 4)
       *reinterpret_cast<f32x4*>(&out.o[wave][col][32 * i + 8 * (r / 4) + 4 * half]) =
           f32x4{sum.o[i][r], sum.o[i][r + 1], sum.o[i][r + 2], sum.o[i][r + 3]};
-  finish<D, 1, kWaves, kRows>(a, w, out);
+  finish<D>(a, w, out);
 }
 
 // ---------------------------------------------------------------------------
@@ -735,11 +738,6 @@ struct Stage {
   Tile<D> tile[3];
   u32x4 raw[kRing][2 * D / 32][kWave];
 };
-template <int D, int kGroups>
-union Many {
-  Stage<D> in;
-  Out<D, kGroups, kManyRows> out;
-};
 template <int i>
 struct Turn {
   static constexpr int value = i;
@@ -752,13 +750,12 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
   constexpr int kBring = 2 * kK;                   // waves that bring 1 KB of a step: keys', then values'
   static_assert(kBring <= kGroups && kRing == 3, "");
   constexpr uint32_t kTileBytes = sizeof(Tile<D>), kRawBytes = 2 * kStep * D, kValues = sizeof(Tile<D>::k);
-  __shared__ __attribute__((aligned(1024))) Many<D, kGroups> sh;
+  __shared__ __attribute__((aligned(1024))) Stage<D> in;
   __shared__ Trees<kGroups * kManyRows> trees;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 16, quad = lane / 16, group = wave;
   Work w;
   if (!locate(a, w, trees)) return;
-  Stage<D>& in = sh.in;
 
   const int R0 = w.r0 + group * kManyRows, R = min(R0 + col, w.rows - 1), node = R / a.group;
   const int last_node = min(R0 + kManyRows - 1, w.rows - 1) / a.group;
@@ -950,14 +947,14 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
       __syncthreads();
     }
   }
+  // A row's quads have neighbouring columns: 64 bytes of it to a store.
   const float l = sum.all();
-  if (quad == 0) {
-    sh.out.m[wave][col] = sum.m;
-    sh.out.l[wave][col] = l;
-  }
+  if (R0 + col >= w.rows) return;
+  const int64_t at = (w.s.row0 + node) * a.hq + w.hk * a.group + (R - node * a.group);
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (quad == 0) write_lse(a, w, at, sum.m, l);
 #pragma unroll
-  for (int i = 0; i < kO; ++i) *reinterpret_cast<f32x4*>(&sh.out.o[wave][col][16 * i + 4 * quad]) = sum.o[i];
-  finish<D, kGroups, kGroups, kManyRows>(a, w, sh.out);
+  for (int i = 0; i < kO; ++i) write<D>(a, w, at, 16 * i + 4 * quad, sum.o[i] * inv);
 }
 
 // Joins the splits of a row by their log-sum-exps: D / 4 lanes per (row, head).
