@@ -724,10 +724,11 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
 // waves bring a step's bytes to LDS by DMA, 1 KB each, widen them and hand them on through LDS; an
 // operand's 64 lanes of 16 bytes are 1 KB of LDS. Step i forms the probabilities and products of step
 // i, the scores of step i + 1 and the widened tile of step i + 2, while the bytes of the kRing steps behind
-// are on their way. A SIMD's waves issue about one instruction in nine cycles each and the matrix unit
-// works beside them, so the softmax's instructions and the LDS reads (8 KB a wave and step at 128 bytes a
-// clock) bound it: 128 rows on four times 32768 tokens, 8 kv-heads, 107 us and 0.65 PFLOP/s; with 32 rows and half as
-// many waves 117 us.
+// are on their way. Bound by issue: at
+// 128 rows on four times 32768 tokens, 8 kv-heads, the kernel takes 89 us of the call's 107 (0.65 PFLOP/s), of
+// which counters give the vector unit 46 % and the matrix unit 31 %, one seldom beside the other, and LDS 42 %. Tried
+// and no faster: 32 rows and half as many waves (113 us), bytes brought through registers (108), the scores'
+// products ahead of the softmax (108).
 template <int D>
 struct Tile {
   u32x4 k[2][D / 32][kWave];                       // of a block of 16 tokens and 32 columns
@@ -843,27 +844,37 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
       for (int r = 0; r < 8; ++r) x[r] = y[r / 4][r % 4];
     };
-    // Scales of step i, or past the end of the last one.
-    const auto scale_at = [&](const float* s, int i) {
-      return scalar_load(s + (w.s.block0 + min(w.begin + i, packed_end - 1) / 2) * a.hkv + w.hk);
+    // Scales of 64 blocks, a lane each: the keys' as factors of the scores, the values' as soften takes them.
+    float key_of_block = 0.f, lv_of_block = 0.f, rv_of_block = 0.f;
+    int block_of_lane0 = 0;                        // from the sequence's first one on
+    const auto load_scales = [&](int step) {
+      block_of_lane0 = step / 2;
+      const int64_t at = (w.s.block0 + min(block_of_lane0 + lane, (packed_end - 1) / 2)) * a.hkv + w.hk;
+      key_of_block = a.k_scale[at];
+      const ValueScale v(a.v_scale[at]);
+      lv_of_block = v.lv;
+      rv_of_block = v.rv;
+      // Waited for here, and not at each step's use.
+      asm volatile("" : "+v"(key_of_block), "+v"(lv_of_block), "+v"(rv_of_block));
     };
+    const auto of_block = [&](float x, int at) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)); };
     fetch(0);
     widen(0, 0);
     fetch(kRawBytes);
     widen(kRawBytes, kTileBytes);
-    float ks = scale_at(a.k_scale, 0), vsc = scale_at(a.v_scale, 0);
+    load_scales(w.begin);
     __syncthreads();
     scores(0);
     const auto step = [&](int i, auto turn) {
       constexpr uint32_t kNow = decltype(turn)::value, kNext = (kNow + 1) % 3, kAfter = (kNow + 2) % 3;
       fetch(kAfter * kRawBytes);
       if (!idle) {
-        const float factor = mask_packed<16>(x, w.s.packed - (w.begin + i) * kStep, ks * qs, 4 * quad);
-        const ValueScale vs(vsc);
-        ks = scale_at(a.k_scale, i + 1);
-        vsc = scale_at(a.v_scale, i + 1);
+        const int st = w.begin + i;
+        if (st / 2 - block_of_lane0 == kWave) load_scales(st);
+        const int at = st / 2 - block_of_lane0;
+        const float factor = mask_packed<16>(x, w.s.packed - st * kStep, of_block(key_of_block, at) * qs, 4 * quad);
         float p[8];
-        sum.soften(x, factor, vs.lv, vs.rv, p);
+        sum.soften(x, factor, of_block(lv_of_block, at), of_block(rv_of_block, at), p);
         Half8 pf;
         pf.floats(p);
         scores(kNext * kTileBytes);
