@@ -315,7 +315,7 @@ cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int
     if (!a.k || !a.v || !a.pk || !a.pv || !a.k_scale || !a.v_scale) return CURE_ERR_INVALID_ARG;
     const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
     if ((at(a.k) | at(a.v) | at(a.pk) | at(a.pv)) % 16 || (at(a.k_scale) | at(a.v_scale)) % 4) return CURE_ERR_INVALID_ARG;
-    if (n_layers > 1 && a.layer_stride * (dtype == CURE_BF16 ? 2 : 4) % 16) return CURE_ERR_INVALID_ARG;
+    if (n_layers > 1 && a.layer_stride % (dtype == CURE_BF16 ? 8 : 4)) return CURE_ERR_INVALID_ARG;
   }
   return CURE_OK;
 }

@@ -1029,7 +1029,7 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
   p.groups = dtype == CURE_F32 || most_rows <= 2 * kRows ? 0 : d == 128 && most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows ? 16 : 8;
   p.quantum = p.groups ? 1 : kWaves;
   p.tile = p.groups ? p.groups * kManyRows : kRows;
-  const int64_t room = kMostBytes / std::max<int64_t>(1, rows * hq * (d + 1) * 4);
+  const double room = kMostBytes / ((double)std::max<int64_t>(1, rows) * hq * (d + 1) * 4);
   const int64_t at_once = (p.groups == 16 ? 1 : p.groups == 8 && d == 64 ? 3 : 2) * (int64_t)device_cu_count();      // workgroups
   int64_t longest = 1;
   double total = 1;                                // steps of all workgroups
@@ -1040,7 +1040,7 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
     total += (double)((n[b] * group + p.tile - 1) / p.tile * hkv) * (double)steps;
   }
   p.tiles = (int32_t)std::max<int64_t>(1, (most_rows + p.tile - 1) / p.tile);
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({longest, (int64_t)kMaxSlots, room}));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(longest, (int64_t)std::min((double)kMaxSlots, room)));
   double best = -1;
   const auto consider = [&](int64_t slots) {
     slots = std::max<int64_t>(1, std::min(slots, most));
