@@ -559,9 +559,10 @@ CURE_DEV void mask_open(float (&x)[kScores], uint32_t seen, float factor, int ow
 // ---------------------------------------------------------------------------
 // Up to 32 query rows to a tile: the waves take the steps in turn, each with all rows and sums of its
 // own, which are joined at the end. Packed bytes go from memory to registers and into the
-// matrix unit, a step ahead of their use, past the caches' ordinary order: nothing reads them twice (eight
-// single tokens over 4096 to 32768: 57 us and 5.5 TB/s, 64 us without). Memory bounds it.
-template <typename E, int D>
+// matrix unit, a step ahead of their use; past the caches where one tile is all (kOnce), for nothing reads
+// them twice (eight single tokens over 4096 to 32768: 57 us and 5.5 TB/s, 64 us without; 16 trees of 20 to 48
+// nodes 63 us, 67 with). Memory bounds it for one tile, issue for several.
+template <typename E, int D, bool kOnce>
 __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void packed_few(Args a) {
   constexpr int kK = D / 32;                       // pieces of 32 columns
   using Byte = typename Types<E>::Byte;
@@ -595,9 +596,9 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
       const int64_t block = (w.s.block0 + st / 2) * a.hkv + w.hk;
       const int64_t at = block * (kBlockTokens * D) + st % 2 * (kStep * D) + lane * 16;
 #pragma unroll
-      for (int i = 0; i < kK; ++i) raw.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.pk + at + i * 1024));
+      for (int i = 0; i < kK; ++i) raw.k[i] = load_of<kOnce>(reinterpret_cast<const u32x4*>(a.pk + at + i * 1024));
 #pragma unroll
-      for (int i = 0; i < kK; ++i) raw.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.pv + at + i * 1024));
+      for (int i = 0; i < kK; ++i) raw.v[i] = load_of<kOnce>(reinterpret_cast<const u32x4*>(a.pv + at + i * 1024));
       raw.ks = scalar_load(a.k_scale + block);
       raw.vs = scalar_load(a.v_scale + block);
     };
@@ -1005,84 +1006,103 @@ __global__ __launch_bounds__(256) void packed_merge(Args a) {
 int64_t steps_of(int32_t packed, int32_t ctx, int32_t n) {
   return ((int64_t)packed + kStep - 1) / kStep + ((int64_t)ctx + n + kStep - 1) / kStep;
 }
-constexpr int kOverhead = 8;           // steps' time that a workgroup takes besides its steps
-constexpr double kJoined = 300000;     // values of splits written and joined in a step's time
 
+// How a call is shared out: waves of a tile of many rows (0: few rows) and its rows, and splits.
 struct Plan {
-  int32_t groups;                    // of many rows; 0: few
-  int32_t tile, tiles, tps, quantum, slots;
+  int32_t groups, tile, tiles, tps, quantum, slots;
 };
+
+// A form of tile, and what its workgroup takes in us: a step alone on a CU, and at least, as a share of
+// the CU; and besides its steps. Fitted to trees of 20 to 48 nodes (d = 128; few rows: 0.27 and 0.21 for
+// 32 rows, many: 0.77 and 0.7 for 128, 1.05 for 256). Few rows do better where a workgroup has few steps (16 trees
+// on 1024 to 4096 tokens 62 us, 81 with many), as more and smaller ones spread better, many rows where it has
+// many (four trees of 32 nodes on 32768 tokens 108 us, 118 with few; prompts of 2048 on 4000 290 and 365).
+struct Form {
+  int32_t groups, tile, quantum, per_cu;             // per_cu workgroups fit on a CU
+  double alone, least, start;
+};
+constexpr double kJoin = 5;                          // of the launch that joins splits
+constexpr double kJoined = 1200000;                  // values of splits written and joined in a microsecond
+constexpr double kStream = 5900000;                  // bytes read in one
+constexpr int kFewest = 8;                           // steps of a split
 
 // Parts of a call: rows * hq * slots of d + 1 floats.
 constexpr int64_t kMostBytes = int64_t(1) << 30;
 
 Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv, int32_t d, const int32_t* n,
              const int32_t* packed, const int32_t* ctx, int32_t kv_split) {
-  const int64_t group = hq / hkv;
-  int64_t most_rows = 0;
-  for (int32_t b = 0; b < batch; ++b) most_rows = std::max<int64_t>(most_rows, n[b] * group);
-  Plan p;
-  // A tile of many rows has 128, or 256 where those are a sequence's all and d is 128: that one then reads and
-  // widens its keys once (16 trees of 20 to 48 nodes, group 4: 83 us, 94 with 128; at d = 64 60 with either).
-  // Of more rows two workgroups to a CU do as well as one and balance better (chunks of 256 to 512 tokens: 414
-  // us and 409). Up to 64 rows the other form: four trees of 16 nodes on 32768 tokens 73 us to 107.
-  p.groups = dtype == CURE_F32 || most_rows <= 2 * kRows ? 0 : d == 128 && most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows ? 16 : 8;
-  p.quantum = p.groups ? 1 : kWaves;
-  p.tile = p.groups ? p.groups * kManyRows : kRows;
-  const double room = kMostBytes / ((double)std::max<int64_t>(1, rows) * hq * (d + 1) * 4);
-  const int64_t at_once = (p.groups == 16 ? 1 : p.groups == 8 && d == 64 ? 3 : 2) * (int64_t)device_cu_count();      // workgroups
-  int64_t longest = 1;
-  double total = 1;                                // steps of all workgroups
+  const int64_t group = hq / hkv, cus = device_cu_count();
+  int64_t most_rows = 0, longest = 1;
   for (int32_t b = 0; b < batch; ++b) {
-    if (n[b] <= 0) continue;
-    const int64_t steps = steps_of(packed[b], ctx[b], n[b]);
-    longest = std::max(longest, steps);
-    total += (double)((n[b] * group + p.tile - 1) / p.tile * hkv) * (double)steps;
+    most_rows = std::max<int64_t>(most_rows, n[b] * group);
+    if (n[b] > 0) longest = std::max(longest, steps_of(packed[b], ctx[b], n[b]));
   }
-  p.tiles = (int32_t)std::max<int64_t>(1, (most_rows + p.tile - 1) / p.tile);
+  const double room = kMostBytes / ((double)std::max<int64_t>(1, rows) * hq * (d + 1) * 4);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(longest, (int64_t)std::min((double)kMaxSlots, room)));
-  double best = -1;
-  const auto consider = [&](int64_t slots) {
-    slots = std::max<int64_t>(1, std::min(slots, most));
-    const int32_t tps = (int32_t)(((longest + slots - 1) / slots + p.quantum - 1) / p.quantum * p.quantum);
+  double stream = 0;                                 // what the bytes of all sequences take
+  for (int32_t b = 0; b < batch; ++b)
+    if (n[b] > 0) stream += (double)steps_of(packed[b], ctx[b], n[b]) * hkv * (2 * kStep * d) / kStream;
+  Plan best{};
+  double best_time = -1;
+  // As many splits as asked for, or those that should take least: as many turns of the longest, or all work
+  // spread evenly and a quarter of one more. Tried are one, and half of, about and twice those with which
+  // every place has one.
+  const auto consider = [&](const Form& f, int64_t slots) {
+    Plan p{f.groups, f.tile, (int32_t)std::max<int64_t>(1, (most_rows + f.tile - 1) / f.tile), 0, f.quantum,
+           (int32_t)std::max<int64_t>(1, std::min(slots, most))};
+    p.tps = (int32_t)(((longest + p.slots - 1) / p.slots + f.quantum - 1) / f.quantum * f.quantum);
     int64_t groups = 0, high = 0;
     double work = 0;
     for (int32_t b = 0; b < batch; ++b) {
       if (n[b] <= 0) continue;
-      const Cut c = cut_of((int)steps_of(packed[b], ctx[b], n[b]), tps, (int)slots, p.quantum);
-      const int64_t g = (n[b] * group + p.tile - 1) / p.tile * hkv * c.n;
+      const Cut c = cut_of((int)steps_of(packed[b], ctx[b], n[b]), p.tps, p.slots, f.quantum);
+      const int64_t g = (n[b] * group + f.tile - 1) / f.tile * hkv * c.n;
       groups += g;
-      work += (double)g * (c.per + kOverhead);
-      high = std::max<int64_t>(high, c.per + kOverhead);
+      work += (double)g * c.per;
+      high = std::max<int64_t>(high, c.per);
     }
     // The launch's workgroups that find nothing to do keep some places from the others at first: eight
     // single tokens with 4096 to 32768 tokens take 64 us in 472 workgroups and 75 in 512.
-    const int64_t places = groups < (int64_t)hkv * p.tiles * slots * batch ? at_once - at_once / 16 : at_once;
-    double time = std::min((double)((groups + places - 1) / places) * high, work / at_once + high);
-    if (slots > 1) time += kOverhead + (double)rows * hq * slots * d / kJoined;
-    if (best >= 0 && time >= best) return;
-    best = time;
-    p.slots = (int32_t)slots;
-    p.tps = tps;
+    const int64_t at_once = f.per_cu * cus;
+    const int64_t places = groups < (int64_t)hkv * p.tiles * p.slots * batch ? at_once - at_once / 16 : at_once;
+    const int64_t beside = std::min<int64_t>(f.per_cu, (groups + cus - 1) / cus);
+    const double step = std::max(f.alone, f.least * beside), start = f.start * (0.75 + 0.25 * beside), one = high * step + start;
+    double time = std::min((double)((groups + places - 1) / places) * one,
+                           std::max(one, (work * f.least + groups * start / f.per_cu) / cus + one / 4));
+    time = std::max(time, stream);
+    if (p.slots > 1) time += kJoin + (double)rows * hq * p.slots * d / kJoined;
+    if (best_time >= 0 && time >= best_time) return;
+    best_time = time;
+    best = p;
   };
-  // As many splits as asked for, or those that should take least: either so many turns of the longest, or
-  // all work spread evenly and one more. Tried are one, those about which every place has one, and twice as
-  // many, of kOverhead steps at least.
-  if (kv_split > 0) {
-    consider(kv_split);
-    return p;
+  const auto consider_all = [&](const Form& f) {
+    if (kv_split > 0) return consider(f, kv_split);
+    double total = 1;                                // steps of all workgroups
+    for (int32_t b = 0; b < batch; ++b)
+      if (n[b] > 0) total += (double)((n[b] * group + f.tile - 1) / f.tile * hkv) * steps_of(packed[b], ctx[b], n[b]);
+    const int64_t useful = (longest + kFewest - 1) / kFewest;
+    const int64_t even = (int64_t)std::min(std::ceil((double)longest * f.per_cu * cus / total), (double)kMaxSlots);
+    int64_t last = 1;
+    consider(f, 1);
+    for (int64_t slots : {even / 2, even - 2, even - 1, even, 2 * even}) {
+      slots = std::min(slots, useful);
+      if (slots <= last) continue;
+      consider(f, slots);
+      last = slots;
+    }
+  };
+  const double half = d == 128 ? 1 : 0.5;
+  if (dtype == CURE_F32) {
+    consider_all(Form{0, kRows, kWaves, 2, 0.9 * half, 0.9 * half, 8});
+    return best;
   }
-  const int64_t useful = (longest + kOverhead - 1) / kOverhead;
-  const int64_t even = (int64_t)std::min(std::ceil((double)longest * at_once / total), (double)kMaxSlots);
-  int64_t last = 1;
-  consider(1);
-  for (int64_t slots : {even - 2, even - 1, even, 2 * even}) {
-    slots = std::min(slots, useful);
-    if (slots <= last) continue;
-    consider(slots);
-    last = slots;
+  consider_all(d == 128 ? Form{0, kRows, kWaves, 2, 0.27, 0.21, 8} : Form{0, kRows, kWaves, 2, 0.2, 0.18, 8});
+  if (most_rows > 2 * kRows) {
+    consider_all(d == 128 ? Form{8, 8 * kManyRows, 1, 2, 0.77, 0.7, 12} : Form{8, 8 * kManyRows, 1, 3, 0.55, 0.545, 12});
+    // 256 rows where they are a sequence's all: its keys are then read and widened once.
+    if (d == 128 && most_rows > 8 * kManyRows && most_rows <= 16 * kManyRows) consider_all(Form{16, 16 * kManyRows, 1, 1, 1.05, 1.05, 12});
   }
-  return p;
+  return best;
 }
 
 size_t space_of(const Plan& p, int64_t rows, int32_t hq, int32_t d) {
@@ -1159,8 +1179,11 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   hipStream_t st = as_stream(stream);
   const dim3 grid((unsigned)wgs, (unsigned)batch), block(threads);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  if (dtype == CURE_F32) d == 128 ? run(packed_few<float, 128>) : run(packed_few<float, 64>);
-  else if (!p.groups) d == 128 ? run(packed_few<uint16_t, 128>) : run(packed_few<uint16_t, 64>);
+  const bool once = p.tiles == 1;
+  if (dtype == CURE_F32 && once) d == 128 ? run(packed_few<float, 128, true>) : run(packed_few<float, 64, true>);
+  else if (dtype == CURE_F32) d == 128 ? run(packed_few<float, 128, false>) : run(packed_few<float, 64, false>);
+  else if (!p.groups && once) d == 128 ? run(packed_few<uint16_t, 128, true>) : run(packed_few<uint16_t, 64, true>);
+  else if (!p.groups) d == 128 ? run(packed_few<uint16_t, 128, false>) : run(packed_few<uint16_t, 64, false>);
   else if (p.groups == 16) run(packed_many<128, 16>);
   else d == 128 ? run(packed_many<128, 8>) : run(packed_many<64, 8>);
   const cure_status launched = launch_status();
