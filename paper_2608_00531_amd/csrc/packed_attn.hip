@@ -1029,7 +1029,8 @@ constexpr int kFewest = 8;                           // steps of a split
 // Parts of a call: rows * hq * slots of d + 1 floats.
 constexpr int64_t kMostBytes = int64_t(1) << 30;
 
-Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv, int32_t d, const int32_t* n,
+// Planned from the host's sizes, with tiles for the n_max rows that the device's may reach.
+Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t n_max, int32_t hq, int32_t hkv, int32_t d, const int32_t* n,
              const int32_t* packed, const int32_t* ctx, int32_t kv_split) {
   const int64_t group = hq / hkv, cus = device_cu_count();
   int64_t most_rows = 0, longest = 1;
@@ -1048,7 +1049,7 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t hq, int32_t hkv
   // spread evenly and a quarter of one more. Tried are one, and half of, about and twice those with which
   // every place has one.
   const auto consider = [&](const Form& f, int64_t slots) {
-    Plan p{f.groups, f.tile, (int32_t)std::max<int64_t>(1, (most_rows + f.tile - 1) / f.tile), 0, f.quantum,
+    Plan p{f.groups, f.tile, (int32_t)std::max<int64_t>(1, (std::min<int64_t>(n_max, rows) * group + f.tile - 1) / f.tile), 0, f.quantum,
            (int32_t)std::max<int64_t>(1, std::min(slots, most))};
     p.tps = (int32_t)(((longest + p.slots - 1) / p.slots + f.quantum - 1) / f.quantum * f.quantum);
     int64_t groups = 0, high = 0;
@@ -1130,7 +1131,7 @@ extern "C" size_t cure_packed_attn_workspace_size(int32_t batch, int64_t rows, i
     return 0;
   size_t most = 0;
   for (int32_t dtype : {CURE_F32, CURE_BF16})
-    most = std::max(most, space_of(plan_of(dtype, batch, rows, hq, hkv, d, host_n_rows, host_packed_len, host_ctx_len, kv_split), rows, hq, d));
+    most = std::max(most, space_of(plan_of(dtype, batch, rows, n_max, hq, hkv, d, host_n_rows, host_packed_len, host_ctx_len, kv_split), rows, hq, d));
   return most;
 }
 
@@ -1165,7 +1166,7 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
     if ((int64_t)host_packed_len[b] + host_ctx_len[b] + host_n_rows[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
   const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
   if ((at(q) | at(pk) | at(pv) | at(k) | at(v) | at(o)) % 16) return CURE_ERR_INVALID_ARG;
-  const Plan p = plan_of(dtype, batch, rows, hq, hkv, d, host_n_rows, host_packed_len, host_ctx_len, kv_split);
+  const Plan p = plan_of(dtype, batch, rows, n_max, hq, hkv, d, host_n_rows, host_packed_len, host_ctx_len, kv_split);
   const size_t need = space_of(p, rows, hq, d);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CURE_ERR_WORKSPACE;
   if (need > 0 && at(workspace) % 16) return CURE_ERR_INVALID_ARG;

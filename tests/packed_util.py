@@ -86,8 +86,8 @@ class Case:
                     j = self.parents[b][j]
         return s
 
-    def check(self, got, every=1):
-        """o, lse, status of a call: every `every`-th row of each sequence within the bounds."""
+    def check(self, got, every=1, heads=None):
+        """o, lse, status of a call: every `every`-th row of each sequence, of some heads, within the bounds."""
         o, lse, status = got
         assert status.tolist() == [0] * len(self.rows)
         half = HALF[o.dtype]
@@ -102,7 +102,7 @@ class Case:
             keys, values = self.keys(b)
             seen = self.seen(b)
             at = np.unique(np.concatenate((np.arange(0, n, every), [n - 1])))
-            for h in range(self.hq):
+            for h in heads or range(self.hq):
                 kh, vh = keys[:, h // group], values[:, h // group]
                 x = q[self.first[b] + at, h]
                 e = (self.d + 6) * U * self.scale * np.max(np.where(seen[at], np.abs(x) @ np.abs(kh).T, 0.0), axis=1, keepdims=True)

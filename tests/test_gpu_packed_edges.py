@@ -8,10 +8,10 @@ import torch
 import paper_2608_00531_amd as pc
 from packed_util import Case
 from prompt_util import ints, random_parents
+from test_packed_plan import LENGTHS, MANY, shape
 
 pytestmark = pytest.mark.gpu
 
-LENGTHS = [0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 160, 193, 225]
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -112,3 +112,50 @@ def test_many_small_probabilities_beside_a_large_one(heads):
     want, want_lse = w * 100 * float(vs[0, 0]) / (1 + w), 25 * one + np.log1p(w)
     assert np.all(np.abs(o.double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -8) * want)
     assert np.all(np.abs(lse.double().cpu().numpy() - want_lse) <= ((d + 6) * 25 * one + n + 16) * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("planned", [1, 16, 40])
+@pytest.mark.parametrize("split", [0, 1, 3])
+def test_more_rows_than_planned(planned, split):
+    """Trees on the device with more nodes, up to n_max, than the host's sizes say."""
+    c = Case("bf16", [40, 33, 5], [640, 128, 64], [60, 0, 5], 8, 2, 128)
+    c.check(c.call(host_n_rows=[planned] * 3, kv_split=split), every=3)
+
+
+@pytest.mark.parametrize("rows,d,tree,waves", MANY)
+def test_lengths_of_many_rows(rows, d, tree, waves):
+    """The shapes at which the form of many rows is launched; every twelfth row of every eleventh head."""
+    at = shape(rows, d, tree)
+    parents = [random_parents(np.random.default_rng(rows), n) for n in at["rows"]] if tree else None
+    c = Case("bf16", at["rows"], at["packed"], at["ctx"], at["hq"], at["hkv"], d, form="tree" if tree else "padded", parents=parents, seed=d)
+    whole = c.call()
+    c.check(whole, every=12, heads=range(0, at["hq"], 11))
+    # Splits are a tile's own affair: the same rows in two parts are within the bounds too.
+    c.check(c.call(kv_split=2), every=12, heads=range(5, at["hq"], 23))
+
+
+def test_far_offsets_and_masks_of_many_rows():
+    """Blocks and rows more than 2^31 elements into their buffers, with infinities and NaN wherever nobody looks."""
+    hkv, d = 64, 128
+    at = shape(68, d, True)
+    parents = [random_parents(np.random.default_rng(3), n) for n in at["rows"]]
+    c = Case("bf16", at["rows"], at["packed"], at["ctx"], at["hq"], hkv, d, parents=parents)
+    c.vs[::2] *= 2.0 ** 20
+    c.vs[1::2] *= 2.0 ** -40
+    used = {c.blk_off[b] + i for b in range(len(c.rows)) for i in range((c.packed[b] + 63) // 64)}
+    rows = {c.kv_off[b] + i for b in range(len(c.rows)) for i in range(c.ctx[b] + c.rows[b])}
+    for i in set(range(c.blocks)) - used:
+        c.ks[i], c.vs[i] = float("nan"), float("inf")
+    for i in set(range(c.cache_rows)) - rows:
+        c.k[i], c.v[i] = float("nan"), float("inf")
+    blocks, far = (1 << 31) // (hkv * 64 * d) + c.blocks + 8, (1 << 31) // (hkv * d) + c.cache_rows + 8
+    pk, pv = (torch.zeros(blocks, hkv, 64 * d, dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros(blocks, hkv, device="cuda") for _ in range(2))
+    k, v = (torch.zeros(far, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    b0, r0 = blocks - c.blocks, far - c.cache_rows
+    for big, x in ((pk, c.pk), (pv, c.pv), (ks, c.ks), (vs, c.vs)):
+        big[b0:] = x.cuda()
+    for big, x in ((k, c.k), (v, c.v)):
+        big[r0:] = x.cuda()
+    c.check(c.call(pk=pk, pv=pv, k_scale=ks, v_scale=vs, k=k, v=v, blk_off=ints([b0 + x for x in c.blk_off], torch.int64),
+                   kv_off=ints([r0 + x for x in c.kv_off], torch.int64)), every=8, heads=range(0, at["hq"], 13))
