@@ -1024,7 +1024,7 @@ struct Form {
 constexpr double kJoin = 5;                          // of the launch that joins splits
 constexpr double kJoined = 1200000;                  // values of splits written and joined in a microsecond
 constexpr double kStream = 5900000;                  // bytes read in one
-constexpr int kFewest = 8;                           // steps of a split
+constexpr int kFewest = 4;                           // steps of a split
 
 // Parts of a call: rows * hq * slots of d + 1 floats.
 constexpr int64_t kMostBytes = int64_t(1) << 30;
@@ -1092,9 +1092,8 @@ Plan plan_of(int32_t dtype, int32_t batch, int64_t rows, int32_t n_max, int32_t 
       last = slots;
     }
   };
-  const double half = d == 128 ? 1 : 0.5;
   if (dtype == CURE_F32) {
-    consider_all(Form{0, kRows, kWaves, 2, 0.9 * half, 0.9 * half, 8});
+    consider_all(d == 128 ? Form{0, kRows, kWaves, 2, 1.2, 1.15, 12} : Form{0, kRows, kWaves, 2, 0.63, 0.55, 12});
     return best;
   }
   consider_all(d == 128 ? Form{0, kRows, kWaves, 2, 0.27, 0.21, 8} : Form{0, kRows, kWaves, 2, 0.2, 0.18, 8});
