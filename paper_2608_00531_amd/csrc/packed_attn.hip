@@ -726,8 +726,8 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
 // operand's 64 lanes of 16 bytes are 1 KB of LDS. Step i forms the probabilities and products of step
 // i, the scores of step i + 1 and the widened tile of step i + 2, while the bytes of the kRing steps behind
 // are on their way. Bound by issue: at
-// 128 rows on four times 32768 tokens, 8 kv-heads, the kernel takes 89 us of the call's 107 (0.65 PFLOP/s), of
-// which counters give the vector unit 46 % and the matrix unit 31 %, one seldom beside the other, and LDS 42 %. Tried
+// 128 rows on four times 32768 tokens, 8 kv-heads, the kernel takes 96 us of the call's 108 (0.64 PFLOP/s), of
+// which counters give the vector unit 44 % and the matrix unit 30 %, one seldom beside the other, and LDS 40 %. Tried
 // and no faster: 32 rows and half as many waves (113 us), bytes brought through registers (108), the scores'
 // products ahead of the softmax (108).
 template <int D>
