@@ -12,7 +12,8 @@
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
 // a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
 // to fp16 for its product, 2^-12 where bf16 would take 2^-9 and add half as much again to the error that the
-// output's own rounding makes; what lies 2^-21 below the largest P has fewer bits, down to 2^-32 of it. Open rows keep bf16's range: their products take P as two bf16 values.
+// output's own rounding makes; what lies 2^-21 below the largest P has fewer bits, down to 2^-32 of
+// it. Open rows keep bf16's range: their products take P as two bf16 values.
 // fp32: fp32 throughout.
 //
 // 32x32 matrix instructions (x16 for 16 bits, x2 eight times for fp32), 32 query rows per wave. Lane
@@ -89,8 +90,7 @@ struct Args {
   float* part_lse;                   // [row][hq][slots], of base 2
 };
 
-// A value at an address that the whole wave shares, through the scalar cache: a vector load would
-// have to wait for the DMA before it.
+// A value at an address that the whole wave shares, through the scalar cache.
 CURE_DEV float scalar_load(const float* p) {
   return *(const __attribute__((address_space(4))) float*)(uintptr_t)p;
 }

@@ -721,7 +721,8 @@ __global__ __launch_bounds__(kThreads32) void sample_f32(Args a) {
 // bf16: a bin is a value, of which [2^-30, 2^10) has 40 octaves of 128 to either sign, and zero. Weights
 // are formed once for each bin in use, so that an entry costs four packed integer instructions
 // and one LDS addition. Eight waves take a row and three rows share a CU, which hide each other's latency: 768
-// rows take 72 us, and 90 with 16 waves to a row and two to a CU; a single row 27 and 27. Rows with other magnitudes that count go the general way.
+// rows take 72 us, and 90 with 16 waves to a row and two to a CU; a single row 27 and 27. Rows with
+// other magnitudes that count go the general way.
 constexpr int kOctaves = 40 * 128;                 // bins of one sign
 constexpr int kSign = 8192;                        // a negative value's, whose byte offset has its sign bit
 constexpr int kPlaces = 2 * kOctaves;              // in a row's order
