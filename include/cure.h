@@ -569,6 +569,7 @@ cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* 
  *   block_stride  blocks between the layers of pk, pv, k_scale and v_scale (ignored when
  *              n_layers <= 1); each layer has `blocks`
  *   kv_off, blk_off  [batch] int64;  n_rows, packed_len, first  [batch] int32 (device)
+ *              (pointers of rows may be NULL where rows is 0, of blocks where blocks is 0)
  *   n_max      the most rows of a sequence: sizes the launch
  *   row_status [batch] int32 output: CURE_OK, or CURE_ERR_BAD_TREE when the sequence's
  *              sizes are negative, n_rows exceeds n_max, packed_len is no multiple of 64,
@@ -618,6 +619,7 @@ cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_sc
  *   parent     [batch][n_max] int32 as for cure_tree_attn, or NULL
  *   row_off, blk_off, kv_off  [batch] int64 (row_off may be NULL);
  *   n_rows, packed_len, ctx_len  [batch] int32 (device)
+ *              (pk, pv, k_scale and v_scale may be NULL where blocks is 0)
  *   host_*     host copies that the launch is planned from. The device's sizes may differ
  *              from them (n_rows up to n_max)
  *   row_status [batch] int32 output (may be NULL): CURE_OK, or CURE_ERR_BAD_TREE when the

@@ -312,7 +312,8 @@ cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int
   if (batch == 0) return CURE_OK;
   if (!a.kv_off || !a.n_rows || !a.blk_off || !a.from || !a.row_status) return CURE_ERR_INVALID_ARG;
   if (a.n_max > 0) {
-    if (!a.k || !a.v || !a.pk || !a.pv || !a.k_scale || !a.v_scale) return CURE_ERR_INVALID_ARG;
+    if (a.rows > 0 && (!a.k || !a.v)) return CURE_ERR_INVALID_ARG;
+    if (a.blocks > 0 && (!a.pk || !a.pv || !a.k_scale || !a.v_scale)) return CURE_ERR_INVALID_ARG;
     const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
     if ((at(a.k) | at(a.v) | at(a.pk) | at(a.pv)) % 16 || (at(a.k_scale) | at(a.v_scale)) % 4) return CURE_ERR_INVALID_ARG;
     if (n_layers > 1 && a.layer_stride % (dtype == CURE_BF16 ? 8 : 4)) return CURE_ERR_INVALID_ARG;

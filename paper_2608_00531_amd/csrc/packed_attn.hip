@@ -1158,7 +1158,8 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   if (batch == 0) return CURE_OK;
   if (!n_rows || !blk_off || !packed_len || !kv_off || !ctx_len || !host_n_rows || !host_packed_len || !host_ctx_len)
     return CURE_ERR_INVALID_ARG;
-  if (n_max > 0 && (!q || !pk || !pv || !k_scale || !v_scale || !k || !v || !o)) return CURE_ERR_INVALID_ARG;
+  if (n_max > 0 && (!q || !k || !v || !o)) return CURE_ERR_INVALID_ARG;
+  if (n_max > 0 && blocks > 0 && (!pk || !pv || !k_scale || !v_scale)) return CURE_ERR_INVALID_ARG;
   if (!row_off && n_max > 0 && rows / n_max < batch) return CURE_ERR_INVALID_ARG;      // padded rows
   if (!sizes_ok(batch, n_max, host_n_rows, host_packed_len, host_ctx_len)) return CURE_ERR_INVALID_ARG;
   for (int32_t b = 0; b < batch; ++b)

@@ -159,3 +159,19 @@ def test_far_offsets_and_masks_of_many_rows():
         big[r0:] = x.cuda()
     c.check(c.call(pk=pk, pv=pv, k_scale=ks, v_scale=vs, k=k, v=v, blk_off=ints([b0 + x for x in c.blk_off], torch.int64),
                    kv_off=ints([r0 + x for x in c.kv_off], torch.int64)), every=8, heads=range(0, at["hq"], 13))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nothing_packed_yet(dtype):
+    """A packed cache of no blocks: the first steps of a sequence. Calls that would need blocks say so."""
+    c = Case(dtype, [7, 3], [0, 0], [40, 0], 8, 2, 64)
+    none = dict(pk=c.pk[:0].cuda(), pv=c.pv[:0].cuda(), k_scale=c.ks[:0].cuda(), v_scale=c.vs[:0].cuda(), blk_off=ints([0, 0], torch.int64))
+    c.check(c.call(**none))
+    assert c.call(**{**none, "packed_len": ints([0, 1])})[2].tolist() == [0, pc.CURE_ERR_BAD_TREE]
+    a = c.args
+    st = pc.cure_kv_pack(a["k"], a["v"], ints([0, 0], torch.int64), ints([0, 5]), none["pk"], none["pv"], none["k_scale"], none["v_scale"],
+                         none["blk_off"], ints([0, 0]))
+    assert st.tolist() == [0, pc.CURE_ERR_BAD_TREE]
+    st = pc.cure_kv_unpack(none["pk"], none["pv"], none["k_scale"], none["v_scale"], none["blk_off"], ints([0, 0]), a["k"][:0], a["v"][:0],
+                           ints([0, 0], torch.int64), ints([0, 1]), n_max=4)
+    assert st.tolist() == [0, pc.CURE_ERR_BAD_TREE]
