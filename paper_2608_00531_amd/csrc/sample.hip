@@ -217,13 +217,14 @@ CURE_DEV int ties_to(double target, Amount before, Amount in, bool pass) {
 
 // ---------------------------------------------------------------------------
 // Any values, and fp32 in general: bins of width T / 32 below the maximum. Relative to its upper edge an entry of a
-// bin has a weight in (exp(-1/32), 1], and 2^44 times it, rounded, leaves room for 2^20 of them
-// in an integer. The bin of a place is gathered and put in order; where it holds too many entries
+// bin has a weight in (exp(-1/32), 1], and 2^43 times it, rounded, leaves room for 2^20 of them
+// in an integer of 64 bits. The bin of a place is gathered and put in order; where it holds too many entries
 // it is divided by their keys until it holds a single value.
 constexpr int kBins = 2048;
 constexpr double kPerT = 32.0;                     // bins of a width T
 constexpr int kGroups = kBins / kWave;
-constexpr double kUnit = 0x1p44;
+constexpr double kUnit = 0x1p43;
+static_assert(kUnit * kMaxVocab <= 0x1p63, "a bin may hold the whole row");
 
 // Order-preserving integer of a finite value; both zeros alike.
 CURE_DEV uint32_t key_of(float x) {
@@ -232,7 +233,7 @@ CURE_DEV uint32_t key_of(float x) {
 }
 CURE_DEV float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// 2^44 exp(-f / 32) for 0 <= f <= 1, rounded: the series' next term is below 2^-55, and 1.5 * 2^52 added leaves
+// 2^43 exp(-f / 32) for 0 <= f <= 1, rounded: the series' next term is below 2^-55, and 1.5 * 2^52 added leaves
 // the integer in the low bits.
 CURE_DEV unsigned long long units_of(double f) {
   constexpr double u = -1.0 / kPerT;
