@@ -562,7 +562,8 @@ cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* 
  * a multiple of 64. The rows are left as they are.
  * cure_kv_unpack is the way back: sequence b's tokens first[b] .. first[b] + n_rows[b] - 1,
  * from any token on, to rows kv_off[b] .. of k and v (one rounding to dtype) -- for a
- * sequence whose last block is filled further, or that is copied.
+ * sequence whose last block is filled further, or that is copied. Where 127 * scale passes
+ * float32's largest value, as it does for a block that holds it, the float below is the scale.
  *
  *   k, v       n_layers caches of token rows [hkv][d] dtype, layer l's from element
  *              l * layer_stride on (ignored when n_layers <= 1), `rows` rows each

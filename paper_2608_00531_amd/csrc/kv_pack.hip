@@ -248,6 +248,10 @@ __global__ __launch_bounds__(4 * kWave, sizeof(E) == 2 ? 7 : 5) void kv_pack(Arg
   for (int j = 0; j < L::kCols; ++j) reinterpret_cast<u32x4*>(dst)[j * kWave + lane] = turn[threadIdx.x / kWave][j * kWave + lane];
 }
 
+// The largest scale that 127 times is finite. The one above it, of a block that holds fp32's largest value, is
+// taken as this.
+constexpr float kMostScale = 0x1.020406p+121f;
+
 // The same pieces the other way.
 template <typename E, int D>
 __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
@@ -260,13 +264,10 @@ __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
   E* dst = static_cast<E*>(r.values ? a.v : a.k) + layer * a.layer_stride + (p.row - skip) * pitch + (int64_t)p.head * D;
   const int64_t block = (layer * a.block_stride + p.block) * a.hkv + p.head;
   const bool all = skip <= 0 && skip + p.n >= kBlockTokens / 2;
-  const float scale = (r.values ? a.v_scale : a.k_scale)[block];
+  float scale = (r.values ? a.v_scale : a.k_scale)[block];
+  scale = scale > kMostScale ? kMostScale : scale;
   const int8_t* src = (r.values ? a.pv : a.pk) + block * (kBlockTokens * D) + r.half * (kBlockTokens / 2 * D);
-  // scale * c as (c + 128) * scale - 128 * scale, rounded once.
-  const float less = -128.f * scale;
-  const auto value = [&](const u32x4& w, int i) {
-    return fmaf((float)(((w[i / 4] ^ 0x80808080u) >> (i % 4 * 8)) & 255u), scale, less);
-  };
+  const auto value = [&](const u32x4& w, int i) { return (float)(int8_t)(w[i / 4] >> (i % 4 * 8)) * scale; };
   const auto wanted = [&](int t) { return t >= skip && t < skip + p.n; };
   if (!r.values) {
     const int own = L::k_own(lane);
