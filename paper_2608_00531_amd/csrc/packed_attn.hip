@@ -7,7 +7,10 @@
 //   S = s_k (C_k Q^T),  P = s_v 2^(S - m),  l += P / s_v,  O^T += C_v^T P^T,  o = O / l
 // in one pass over the keys with the reference m, near a running maximum of S + log2 s_v, and l in fp32.
 // The value's scale is part of the exponent, so a block whose values are large and one
-// whose values are small both have P in the range of 16 bits where they count at all.
+// whose values are small both have P in the range of 16 bits where they count at all. A wave takes scales as
+// multiples of a power of two, by which it multiplies o at the end. Where one lies more than 2^32 from
+// that, P and P / s_v no longer both fit fp32: l has a reference of its own from there on, the scores' maximum, and
+// each score a second exponential.
 //
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
 // a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
@@ -94,6 +97,8 @@ struct Args {
 CURE_DEV float scalar_load(const float* p) {
   return *(const __attribute__((address_space(4))) float*)(uintptr_t)p;
 }
+
+CURE_DEV float first_lane(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 // A sequence's sizes as the device has them. ok: they can be.
 struct Seq {
@@ -237,7 +242,7 @@ CURE_DEV f32x16 zeros() {
 template <int kScores, int kLanes, int kBlocks, class Block>
 struct Sums {
   static constexpr int kEach = sizeof(Block) / sizeof(float);
-  float m = kNone, l = 0.f;
+  float m = kNone, l = 0.f;                        // m is a whole number
   Block o[kBlocks];
 
   CURE_DEV Sums() {
@@ -247,30 +252,42 @@ struct Sums {
       for (int r = 0; r < kEach; ++r) o[i][r] = 0.f;
   }
   // Scores x * factor of base 2 (-inf: not seen; factor > 0 there) of tokens whose values have scale 2^lv and
-  // its reciprocal rv: their P. The reference moves to where the largest P is 2^7, which leaves small ones of a
-  // million tokens precise in fp16, and does so where a lane's P sum up to more than 2^15, which fp16
-  // holds: at first, and seldom later. A maximum for each step would cost a tenth of it.
-  CURE_DEV void soften(const float (&x)[kScores], float factor, float lv, float rv, float (&p)[kScores]) {
-    float added = exps(x, factor, lv, p);
+  // its reciprocal rv, in the wave's unit: their P. The reference moves to where the largest P is 2^7 to 2^8, which
+  // leaves small ones of a million tokens precise in fp16, and does so where a lane's P sum up to more than 2^15, which
+  // fp16 holds: at first, and seldom later. A maximum for each step would cost a tenth of it. With lv infinite, which
+  // has every step come that way, rv is the scale's logarithm and l has a reference of its own, *own().
+  template <class Own>
+  CURE_DEV void soften(const float (&x)[kScores], float factor, float lv, float rv, const Own& own, float (&p)[kScores]) {
+    float added = exps(x, factor, lv - m, p);
     if (__builtin_expect(__any(!(added <= 0x1p15f)), 0)) {
+      const bool apart = lv == INFINITY;
+      if (apart) lv = rv;
       float high = x[0];
 #pragma unroll
       for (int r = 1; r < kScores; ++r) high = fmaxf(high, x[r]);
       if (kLanes == 4) high = fmaxf(high, __shfl_xor(high, 16));
-      high = fmaf(max_halves(high), factor, lv);
-      const float mn = fmaxf(m, high - 7.f), f = fast_exp2(m - mn);
+      high = max_halves(high) * factor;
+      const float mn = fmaxf(m, floorf(high + lv) - 7.f), f = fast_exp2(m - mn);
       m = mn;
-      l *= f;
 #pragma unroll
       for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
         for (int r = 0; r < kEach; ++r) o[i][r] *= f;
-      added = exps(x, factor, lv, p);
+      if (apart) {
+        rv = 0.f;
+        const float was = *own(), now = fmaxf(was, floorf(high));
+        *own() = now;
+        l *= fast_exp2(was - now);
+#pragma unroll
+        for (int r = 0; r < kScores; ++r) l += fast_exp2(fmaf(x[r], factor, -now));
+      } else {
+        l *= f;
+      }
+      added = exps(x, factor, lv - m, p);
     }
     l = fmaf(added, rv, l);
   }
-  CURE_DEV float exps(const float (&x)[kScores], float factor, float lv, float (&p)[kScores]) const {
-    const float c = lv - m;
+  CURE_DEV float exps(const float (&x)[kScores], float factor, float c, float (&p)[kScores]) const {
     float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < kScores; ++r) {
@@ -291,14 +308,42 @@ using FewSums = Sums<16, 2, D / 32, f32x16>;
 template <int D>
 using ManySums = Sums<8, 4, D / 16, f32x4>;
 
-// The scale of a block's values as soften takes it. Blocks of zeros have one that keeps their
-// probabilities in range; from 2^-116 on down the reciprocal would not.
+// The unit 2^z of a wave's value scales: 1, or near the first that lies more than 2^32 from that, where the wave
+// meets it first; and whether others lie too far from it (apart). Within 2^32 of it, P / s_v of 2^31 tokens is below
+// 2^100, and the P of a token whose score lies 24 below the largest above 2^-90. Open rows have scale 1.
+struct ScaleUnit {
+  uint32_t low = (127 - 32) << 23, span = (65 << 23) - 1;      // bits of the scales near enough: low .. low + span
+  float down = 1.f;                                // 2^-z
+  bool moved = false, apart = false;
+  CURE_DEV bool near(float s) const { return __float_as_uint(s) - low <= span; }
+  // One that is not near, the same for the whole wave. m: the row's reference, l's own from here on where apart.
+  template <class Own>
+  CURE_DEV void meet(float s, float m, const Own& own) {
+    const uint32_t bits = __float_as_uint(s), e = min(max(bits >> 23, 1u), 250u);
+    if (bits == 0 || apart) return;
+    if (moved || __any(m > kNone)) {
+      apart = true;
+      *own() = m;
+      return;
+    }
+    moved = true;
+    low = e > 32 ? (e - 32) << 23 : 1;
+    span = (min(e + 33, 255u) << 23) - 1 - low;
+    down = __uint_as_float((254 - e) << 23);
+  }
+  CURE_DEV float z() const { return (float)(127 - (int)(__float_as_uint(down) >> 23)); }
+};
+// A scale as soften takes it: in the unit, and its reciprocal. A block of zeros has any.
 struct ValueScale {
   float lv, rv;
-  CURE_DEV explicit ValueScale(float s) {
-    const float x = s > 0.f ? fmaxf(s, 0x1p-116f) : 0x1p-60f;
+  CURE_DEV ValueScale(float s, const ScaleUnit& u) {
+    const float x = s > 0.f ? s * u.down : 1.f;
     lv = __builtin_amdgcn_logf(x);
     rv = __builtin_amdgcn_rcpf(x);
+    if (__builtin_expect(u.apart, 0)) {
+      rv = s > 0.f ? __builtin_amdgcn_logf(s < 1.f ? s * 0x1p64f : s) - (s < 1.f ? 64.f : 0.f) - u.z() : 0.f;
+      lv = INFINITY;
+    }
   }
 };
 
@@ -500,36 +545,49 @@ CURE_DEV void write_lse(const Args& a, const Work& w, int64_t at, float m, float
   else if (a.lse) a.lse[at] = lse2 * kLn2;
 }
 
+// x 2^z for a whole number z.
+CURE_DEV f32x4 in_units(f32x4 x, float z) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = ldexpf(x[i], (int)z);
+  return x;
+}
+
 // Where a tile of few rows is joined: the same rows of each wave.
 template <int D>
 struct Out {
   float o[kWaves][kRows][D + 4];
-  float m[kWaves][kRows], l[kWaves][kRows];
+  float m[kWaves][kRows], l[kWaves][kRows];        // l's unit is 2^m
+  float unit[kWaves][kRows];                       // o's 2^unit; l's own references before
 };
 // Writes the tile's rows, the sums of what the waves have put into sh.
 template <int D>
 CURE_DEV void finish(const Args& a, const Work& w, const Out<D>& sh) {
-  constexpr int kChunks = D / 4;
+  constexpr int kLanes = 16;                       // of a row, four columns each
   __syncthreads();
-  for (int c = threadIdx.x; c < kRows * kChunks; c += kWaves * kWave) {
-    const int row = c / kChunks, j = c % kChunks * 4;
+  for (int row = threadIdx.x / kLanes; row < kRows; row += kWaves * kWave / kLanes) {
     if (w.r0 + row >= w.rows) break;
-    float m = kNone, l = 0.f, f[kWaves];
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, sh.m[k][row]);
+    float m = kNone, unit = kNone, l = 0.f, f[kWaves];
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
-      f[k] = fast_exp2(sh.m[k][row] - m);
-      l += f[k] * sh.l[k][row];
+      m = fmaxf(m, sh.m[k][row]);
+      unit = fmaxf(unit, sh.unit[k][row]);
     }
-    f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[k][row][j]);
-    x *= l > 0.f ? 1.f / l : 0.f;
+    for (int k = 0; k < kWaves; ++k) {
+      l += fast_exp2(sh.m[k][row] - m) * sh.l[k][row];
+      f[k] = fast_exp2(sh.unit[k][row] - unit);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
     const int R = w.r0 + row;
     const int64_t at = (w.s.row0 + R / a.group) * a.hq + w.hk * a.group + R % a.group;
-    if (j == 0) write_lse(a, w, at, m, l);
-    write<D>(a, w, at, j, x);
+#pragma unroll
+    for (int j = threadIdx.x % kLanes * 4; j < D; j += kLanes * 4) {
+      f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) x += f[k] * *reinterpret_cast<const f32x4*>(&sh.o[k][row][j]);
+      if (j == 0) write_lse(a, w, at, m, l);
+      write<D>(a, w, at, j, in_units(x * inv, unit - m));
+    }
   }
 }
 
@@ -578,6 +636,17 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
   const int R = min(w.r0 + col, w.rows - 1), node = R / a.group;
   const E* qsrc = static_cast<const E*>(a.q) + ((w.s.row0 + node) * a.hq + w.hk * a.group + R % a.group) * D + 16 * half;
   FewSums<D> sum;
+  ScaleUnit scales;
+  // Seldom used: from the thread's index, for no register to hold it.
+  const auto own = [&] {
+    int t = tid;
+    asm("" : "+v"(t));
+    return &out.unit[wave][t % 32];
+  };
+  const auto scale_of = [&](float s) {
+    if (__builtin_expect(!scales.near(s), 0)) scales.meet(s, sum.m, own);
+    return ValueScale(s, scales);
+  };
   int step = w.begin + wave;
   const int packed_end = min(w.end, w.steps.packed);
   if (step < packed_end) {
@@ -612,12 +681,12 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
           f.bytes(raw.k[i][2 * u], raw.k[i][2 * u + 1]);
           y = mma(f, q[i][u], y);
         }
-      const ValueScale vs(raw.vs);
       float x[16], p[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = y[r];
       const float factor = mask_packed<8>(x, w.s.packed - st * kStep, raw.ks * qs, 4 * half);
-      sum.soften(x, factor, vs.lv, vs.rv, p);
+      const ValueScale v = scale_of(raw.vs);
+      sum.soften(x, factor, v.lv, v.rv, own, p);
       Byte pf[2];
       pf[0].floats(p);
       pf[1].floats(p + 8);
@@ -663,23 +732,33 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
     // The wave's own part of the LDS turns the values.
     static_assert(sizeof(ValueTile<E, D>) <= sizeof(out.o[0]), "");
     ValueTile<E, D>& tile = *reinterpret_cast<ValueTile<E, D>*>(out.o[wave]);
+    ValueScale one = scale_of(1.f);
+    one.lv = first_lane(one.lv);
+    one.rv = first_lane(one.rv);
     for (; step < w.end; step += kWaves) {
       const int t0 = (step - w.steps.packed) * kStep;
       RowVec<E, 16> kx[kK];
       load_rows<E, D>(kp + min(t0 + col, open - 1) * pitch + 16 * half, kx);
       constexpr int kUnits = D / kWave;            // of values, per lane
+      static_assert(kUnits <= 2, "");
       ValueUnit<E, D, false> unit[kUnits];
-#pragma unroll
-      for (int i = 0; i < kUnits; ++i) unit[i].load(vp, pitch, t0, open - 1, i * kWave + lane);
+      const auto load_values = [&](int i) { unit[i].load(vp, pitch, t0, open - 1, i * kWave + lane); };
+      load_values(0);
       f32x16 y = zeros();
 #pragma unroll
-      for (int i = 0; i < kK; ++i)
+      for (int i = 0; i < kK; ++i) {
+        // In fp32 the second half waits for registers of keys that are done.
+        if (kUnits > 1 && i == (sizeof(E) == 4 ? kK / 2 : 0)) {
+          if (sizeof(E) == 4) __builtin_amdgcn_sched_barrier(0);
+          load_values(kUnits - 1);
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           RowF f;
           f.row(kx[i], u);
           y = mma(f, q[i][u], y);
         }
+      }
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) unit[i].store(tile, i * kWave + lane);
       wave_sync();
@@ -687,7 +766,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = y[r];
       mask_open<8>(x, seen_of(a, w, trees, node, t0), a.scale_log2, 4 * half);
-      sum.soften(x, 1.f, 0.f, 1.f, p);
+      sum.soften(x, 1.f, one.lv, one.rv, own, p);
       RowF pf[2], rest[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -707,15 +786,21 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
     }
   }
   const float l = sum.all();
-  if (half == 0) {
-    out.m[wave][col] = sum.m;
-    out.l[wave][col] = l;
+  const float ref = scales.apart ? *own() : sum.m;
+  wave_sync();
+  int t = tid;                                     // as above
+  asm("" : "+v"(t));
+  const int c = t % 32, h = t % kWave / 32;
+  if (h == 0) {
+    out.m[wave][c] = ref;
+    out.l[wave][c] = l;
+    out.unit[wave][c] = sum.m + scales.z();
   }
 #pragma unroll
   for (int i = 0; i < kK; ++i)
 #pragma unroll
     for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<f32x4*>(&out.o[wave][col][32 * i + 8 * (r / 4) + 4 * half]) =
+      *reinterpret_cast<f32x4*>(&out.o[wave][c][32 * i + 8 * (r / 4) + 4 * h]) =
           f32x4{sum.o[i][r], sum.o[i][r + 1], sum.o[i][r + 2], sum.o[i][r + 3]};
   finish<D>(a, w, out);
 }
@@ -754,6 +839,7 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
   constexpr uint32_t kTileBytes = sizeof(Tile<D>), kRawBytes = 2 * kStep * D, kValues = sizeof(Tile<D>::k);
   __shared__ __attribute__((aligned(1024))) Stage<D> in;
   __shared__ Trees<kGroups * kManyRows> trees;
+  __shared__ float refs[kGroups * kManyRows];      // l's own
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 16, quad = lane / 16, group = wave;
   Work w;
@@ -764,6 +850,14 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
   const bool idle = R0 >= w.rows;                  // this wave's rows are not there
   const E* qsrc = static_cast<const E*>(a.q) + ((w.s.row0 + node) * a.hq + w.hk * a.group + R % a.group) * D + 8 * quad;
   ManySums<D> sum;
+  ScaleUnit scales;
+  const auto own = [&] { return &refs[group * kManyRows + col]; };
+  // Value scales, one to a lane.
+  const auto meet = [&](float s) __attribute__((always_inline)) {
+    unsigned long long far;
+    while (!scales.apart && (far = __ballot(s != 0.f && !scales.near(s))))
+      scales.meet(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), __ffsll(far) - 1)), sum.m, own);
+  };
 
   const int packed_end = min(w.end, w.steps.packed), rounds = packed_end - w.begin;
   if (rounds > 0) {
@@ -848,11 +942,13 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
     // Scales of 64 blocks, a lane each: the keys' as factors of the scores, the values' as soften takes them.
     float key_of_block = 0.f, lv_of_block = 0.f, rv_of_block = 0.f;
     int block_of_lane0 = 0;                        // from the sequence's first one on
-    const auto load_scales = [&](int step) {
+    const auto load_scales = [&](int step) __attribute__((always_inline)) {
       block_of_lane0 = step / 2;
       const int64_t at = (w.s.block0 + min(block_of_lane0 + lane, (packed_end - 1) / 2)) * a.hkv + w.hk;
       key_of_block = a.k_scale[at];
-      const ValueScale v(a.v_scale[at]);
+      const float s = a.v_scale[at];
+      meet(s);
+      const ValueScale v(s, scales);
       lv_of_block = v.lv;
       rv_of_block = v.rv;
       // Waited for here, and not at each step's use.
@@ -871,11 +967,11 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
       fetch(kAfter * kRawBytes);
       if (!idle) {
         const int st = w.begin + i;
-        if (st / 2 - block_of_lane0 == kWave) load_scales(st);
+        if (__builtin_expect(st / 2 - block_of_lane0 == kWave, 0)) load_scales(st);
         const int at = st / 2 - block_of_lane0;
         const float factor = mask_packed<16>(x, w.s.packed - st * kStep, of_block(key_of_block, at) * qs, 4 * quad);
         float p[8];
-        sum.soften(x, factor, of_block(lv_of_block, at), of_block(rv_of_block, at), p);
+        sum.soften(x, factor, of_block(lv_of_block, at), of_block(rv_of_block, at), own, p);
         Half8 pf;
         pf.floats(p);
         scores(kNext * kTileBytes);
@@ -927,6 +1023,8 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
         unit.store(t.v, tid);
       }
     };
+    meet(1.f);
+    const ValueScale one(1.f, scales);
     stage(0);
     __syncthreads();
     for (int i = 0; i < more; ++i) {
@@ -945,7 +1043,7 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
           for (int r = 0; r < 4; ++r) x[4 * b + r] = y[r];
         }
         mask_open<16>(x, seen_of(a, w, trees, node, t0), a.scale_log2, 4 * quad);
-        sum.soften(x, 1.f, 0.f, 1.f, p);
+        sum.soften(x, 1.f, one.lv, one.rv, own, p);
         Bf8 pf, rest;
         pf.floats(p);
         rest.rest(p, pf);
@@ -963,10 +1061,10 @@ __global__ __launch_bounds__(kGroups * kWave) __attribute__((amdgpu_waves_per_eu
   const float l = sum.all();
   if (R0 + col >= w.rows) return;
   const int64_t at = (w.s.row0 + node) * a.hq + w.hk * a.group + (R - node * a.group);
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (quad == 0) write_lse(a, w, at, sum.m, l);
+  const float inv = l > 0.f ? 1.f / l : 0.f, ref = scales.apart ? *own() : sum.m, z = sum.m - ref + scales.z();
+  if (quad == 0) write_lse(a, w, at, ref, l);
 #pragma unroll
-  for (int i = 0; i < kO; ++i) write<D>(a, w, at, 16 * i + 4 * quad, sum.o[i] * inv);
+  for (int i = 0; i < kO; ++i) write<D>(a, w, at, 16 * i + 4 * quad, in_units(sum.o[i] * inv, z));
 }
 
 // Joins the splits of a row by their log-sum-exps: D / 4 lanes per (row, head), in two round trips of loads and
