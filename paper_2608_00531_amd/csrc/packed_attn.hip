@@ -237,6 +237,9 @@ CURE_DEV f32x16 zeros() {
   return x;
 }
 
+// x in another register: what a seldom taken branch replaces then keeps its own, and the other way needs no move.
+CURE_DEV float moved(float x) { return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xe4, 0xf, 0xf, false)); }
+
 // A lane's query row and what it has summed: kScores scores of a step, of which kLanes lanes
 // share a row, and kBlocks blocks of output.
 template <int kScores, int kLanes, int kBlocks, class Block>
@@ -254,36 +257,40 @@ struct Sums {
   // Scores x * factor of base 2 (-inf: not seen; factor > 0 there) of tokens whose values have scale 2^lv and
   // its reciprocal rv, in the wave's unit: their P. The reference moves to where the largest P is 2^7 to 2^8, which
   // leaves small ones of a million tokens precise in fp16, and does so where a lane's P sum up to more than 2^15, which
-  // fp16 holds: at first, and seldom later. A maximum for each step would cost a tenth of it. With lv infinite, which
-  // has every step come that way, rv is the scale's logarithm and l has a reference of its own, *own().
+  // fp16 holds: at first, and seldom later. A maximum for each step would cost a tenth of it. A step
+  // always comes that way with lv infinite, where rv is the scale's logarithm and l has a reference of its own, *own(),
+  // and with lv NaN, where the scale is 0: the tokens count, their values do not.
   template <class Own>
   CURE_DEV void soften(const float (&x)[kScores], float factor, float lv, float rv, const Own& own, float (&p)[kScores]) {
     float added = exps(x, factor, lv - m, p);
     if (__builtin_expect(__any(!(added <= 0x1p15f)), 0)) {
-      const bool apart = lv == INFINITY;
-      if (apart) lv = rv;
+      const bool apart = lv == INFINITY, none = lv != lv;
+      lv = apart ? rv : lv;
       float high = x[0];
 #pragma unroll
       for (int r = 1; r < kScores; ++r) high = fmaxf(high, x[r]);
       if (kLanes == 4) high = fmaxf(high, __shfl_xor(high, 16));
       high = max_halves(high) * factor;
-      const float mn = fmaxf(m, floorf(high + lv) - 7.f), f = fast_exp2(m - mn);
-      m = mn;
+      const float was = m;
+      m = fmaxf(m, floorf(high + (none ? 0.f : lv)) - 7.f);
+      const float f = fast_exp2(was - m);
 #pragma unroll
       for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
         for (int r = 0; r < kEach; ++r) o[i][r] *= f;
-      if (apart) {
-        rv = 0.f;
-        const float was = *own(), now = fmaxf(was, floorf(high));
-        *own() = now;
-        l *= fast_exp2(was - now);
+      if (apart || none) {
+        const float from = apart ? *own() : was, to = apart ? fmaxf(from, floorf(high)) : m;
+        if (apart) *own() = to;
+        l *= fast_exp2(from - to);
 #pragma unroll
-        for (int r = 0; r < kScores; ++r) l += fast_exp2(fmaf(x[r], factor, -now));
+        for (int r = 0; r < kScores; ++r) l += fast_exp2(fmaf(x[r], factor, -to));
+        rv = 0.f;
       } else {
         l *= f;
       }
-      added = exps(x, factor, lv - m, p);
+      added = exps(x, factor, (none ? -INFINITY : lv) - m, p);
+      m = moved(m);
+      l = moved(l);
     }
     l = fmaf(added, rv, l);
   }
@@ -333,15 +340,15 @@ struct ScaleUnit {
   }
   CURE_DEV float z() const { return (float)(127 - (int)(__float_as_uint(down) >> 23)); }
 };
-// A scale as soften takes it: in the unit, and its reciprocal. A block of zeros has any.
+// A scale as soften takes it: in the unit, and its reciprocal.
 struct ValueScale {
   float lv, rv;
   CURE_DEV ValueScale(float s, const ScaleUnit& u) {
     const float x = s > 0.f ? s * u.down : 1.f;
-    lv = __builtin_amdgcn_logf(x);
+    lv = s > 0.f ? __builtin_amdgcn_logf(x) : NAN;
     rv = __builtin_amdgcn_rcpf(x);
     if (__builtin_expect(u.apart, 0)) {
-      rv = s > 0.f ? __builtin_amdgcn_logf(s < 1.f ? s * 0x1p64f : s) - (s < 1.f ? 64.f : 0.f) - u.z() : 0.f;
+      rv = s > 0.f ? __builtin_amdgcn_logf(s < 1.f ? s * 0x1p64f : s) - (s < 1.f ? 64.f : 0.f) - u.z() : -INFINITY;
       lv = INFINITY;
     }
   }

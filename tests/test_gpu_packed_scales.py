@@ -1,10 +1,14 @@
 """Attention over blocks whose value scales lie anywhere in float32, alone, beside each other and beside open
 rows, in every order: a block's tokens count in the softmax by their scores alone. Bounds of packed_bounds.py."""
 
+import math
+
 import pytest
 import torch
 
+import paper_2608_00531_amd as pc
 from packed_bounds import Bounded
+from prompt_util import ints
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +85,43 @@ def test_new_rows_of_large_values(form):
         c = case(form, powers, 21, 1)
         c.v = (c.v.float().clamp(-3.9, 3.9) * 2.0 ** 77).to(c.t)
         c.check(c.call(out_dtype=torch.float32), **many)
+
+
+@pytest.mark.parametrize("others", [0, 60, -60, -110])
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_of_zero_with_any_bytes(form, others):
+    """Where a largest value's 127th part is below float32's smallest number the scale is 0 and the bytes are not:
+    keys and values are zeros, and such tokens count."""
+    many = dict(every=13, heads=range(0, 256, 51)) if form.startswith("many") else {}
+    c = case(form, [others], 7, 1)
+    for b in range(len(c.rows)):
+        c.vs[c.blk_off[b]:c.blk_off[b] + 6:2] = 0.0
+        c.ks[c.blk_off[b]:c.blk_off[b] + 6:3] = 0.0
+    c.check(c.call(out_dtype=torch.float32), **many)
+    c.vs[:] = 0.0
+    c.v[:] = 0.0
+    o, lse, status = c.call(out=torch.full((*c.shape, c.hq, c.d), 3.0, dtype=c.t, device="cuda"))
+    c.check((o, lse, status), **many)
+    for b, n in enumerate(c.rows):
+        assert not bool(o[b, :n].any())
+
+
+def test_packed_values_below_a_scale():
+    """fp32 rows of values up to 2^-143 pack to such blocks; beside ordinary ones they are nothing."""
+    n, hkv, d = 128, 1, 64
+    zero = ints([0], torch.int64)
+    k, v = torch.zeros(n + 1, hkv, d, device="cuda"), torch.ones(n + 1, hkv, d, device="cuda")
+    v[:64], v[n] = 2.0 ** -145, 0.0
+    blocks = [torch.zeros(2, hkv, 64 * d, dtype=torch.int8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(2, hkv, device="cuda") for _ in range(2)]
+    pc.cure_kv_pack(k, v, zero, ints([n]), *blocks, *scales, zero, ints([0]))
+    assert scales[1][0, 0] == 0 and bool((blocks[1][0] == 127).all())
+    q = torch.ones(1, 1, 1, d, device="cuda")
+    one = ints([1])
+    o, lse, _ = pc.cure_packed_attn(q, *blocks, *scales, zero, ints([n]), k[n:], v[n:], zero, ints([0]), one, [n], [0], [1], 0.125)
+    # 64 of 129 equal weights on values of 127 (1 / 127): three roundings of 2^-24, and of sums.
+    assert bool(((o - 64 / 129).abs() <= (129 + 16) * 2.0 ** -24).all()) and abs(lse.item() - math.log(129)) <= (129 + 16) * 2.0 ** -24 * 5
+    v[64:] = 0.0
+    pc.cure_kv_pack(k, v, zero, ints([n]), *blocks, *scales, zero, ints([0]))
+    o, _, _ = pc.cure_packed_attn(q, *blocks, *scales, zero, ints([n]), k[n:], v[n:], zero, ints([0]), one, [n], [0], [1], 0.125)
+    assert not bool(o.any())
