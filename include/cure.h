@@ -577,8 +577,9 @@ cure_status cure_prefix_attn(const void* q, const void* k, const void* v, void* 
  *              or its rows or blocks reach past `rows` or `blocks`. Nothing of such a
  *              sequence is written.
  * Rows, or blocks, of different sequences that are written must not overlap.
- * Supports d in {64, 128}, batch <= 65535, n_layers <= 65535, hkv <= 2^20, n_max * hkv < 2^30. k, v and
- * layer_stride in bytes must be multiples of 16. No workspace.
+ * Supports d in {64, 128}, batch <= 65535, n_layers <= 65535, hkv <= 2^20, hkv * ceil(n_max / 64) < 2^24
+ * (unpacking: hkv * (ceil(n_max / 64) + 1)). k, v and layer_stride in bytes must be multiples of 16.
+ * No workspace.
  */
 #define CURE_PACK_TOKENS 64
 

@@ -299,16 +299,17 @@ __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
   }
 }
 
-// The checks that both calls make, and the launch. *nothing: there is nothing to do.
-cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int32_t batch, bool* nothing) {
+// The checks that both calls make, and the launch. touched: blocks of a sequence; *nothing: there is nothing to do.
+cure_status check(const Args& a, int64_t touched, int32_t dtype, int32_t n_layers, int32_t d, int32_t batch, bool* nothing) {
   *nothing = false;
   if (dtype != CURE_F32 && dtype != CURE_BF16) return CURE_ERR_INVALID_ARG;
   if (n_layers < 1 || a.rows < 0 || a.hkv <= 0 || d <= 0 || batch < 0 || a.n_max < 0 || a.blocks < 0)
     return CURE_ERR_INVALID_ARG;
   if (n_layers > 1 && (a.layer_stride < 0 || a.block_stride < 0)) return CURE_ERR_INVALID_ARG;
   if (d != 64 && d != 128) return CURE_ERR_UNSUPPORTED;
-  if (batch > 65535 || n_layers > 65535 || a.hkv > 1 << 20 || (int64_t)a.n_max * a.hkv >= (int64_t(1) << 30))
-    return CURE_ERR_UNSUPPORTED;                   // offsets within some rows are of 32 bits
+  // A launch counts threads in 32 bits, and offsets within some rows are of 32.
+  if (batch > 65535 || n_layers > 65535 || a.hkv > 1 << 20 || touched * a.hkv * (4 * kWave) >= (int64_t(1) << 32))
+    return CURE_ERR_UNSUPPORTED;
   *nothing = batch == 0;
   if (batch == 0) return CURE_OK;
   if (!a.kv_off || !a.n_rows || !a.blk_off || !a.from || !a.row_status) return CURE_ERR_INVALID_ARG;
@@ -327,10 +328,10 @@ cure_status check(const Args& a, int32_t dtype, int32_t n_layers, int32_t d, int
 template <bool kPack>
 cure_status launch(Args a, int32_t dtype, int32_t n_layers, int32_t d, int32_t batch, void* stream) {
   bool nothing;
-  const cure_status st = check(a, dtype, n_layers, d, batch, &nothing);
+  const int64_t touched = a.n_max == 0 ? 1 : blocks_of(a.n_max) + (kPack ? 0 : 1);
+  const cure_status st = check(a, touched, dtype, n_layers, d, batch, &nothing);
   if (st != CURE_OK || nothing) return st;
   if (n_layers <= 1) a.layer_stride = a.block_stride = 0;
-  const int64_t touched = a.n_max == 0 ? 1 : blocks_of(a.n_max) + (kPack ? 0 : 1);
   const dim3 grid((unsigned)(touched * a.hkv), (unsigned)batch, (unsigned)n_layers), block(4 * kWave);
   hipStream_t s = as_stream(stream);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
