@@ -1316,7 +1316,8 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   const cure_status launched = launch_status();
   if (launched != CURE_OK || p.slots == 1 || n_max == 0) return launched;
   const int per = 256 / (d / 4);
-  const dim3 mgrid((unsigned)(((int64_t)n_max * hq + per - 1) / per), (unsigned)batch);
+  // No sequence has more than `rows`, which parts of 1 GB bound to 2^21 rows and heads.
+  const dim3 mgrid((unsigned)((std::min<int64_t>(n_max, rows) * hq + per - 1) / per), (unsigned)batch);
   if (d == 128) hipLaunchKernelGGL((packed_merge<128>), mgrid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((packed_merge<64>), mgrid, dim3(256), 0, st, a);
   return launch_status();

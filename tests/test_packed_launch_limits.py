@@ -72,3 +72,16 @@ def test_packing(launches, hkv, pack, unpack):
 
 def test_no_rows_at_all(launches):
     assert [s for s, _ in launches(dict(name="pack", hkv=1 << 20), dict(name="unpack", hkv=1 << 20))] == [0, 0]
+
+
+@pytest.mark.parametrize("dtype,d", [(0, 64), (0, 128), (1, 64), (1, 128)])
+def test_joined_splits(launches, dtype, d):
+    """Splits are joined for the rows that there are, however many a sequence might have by n_max."""
+    for hq, rows in ((256, 1000), (1, 1), (32, 9000), (1 << 20, 1)):
+        n_max = (1 << 28) // hq
+        (status, grids), (_, alike) = launches(dict(name="attend", n_max=n_max, hq=hq, hkv=1, d=d, rows=rows, dtype=dtype, split=2),
+                                               dict(name="attend", n_max=rows, hq=hq, hkv=1, d=d, rows=rows, dtype=dtype, split=2))
+        assert status == 0 and len(grids) in (1, 2) and grids == alike, (hq, rows, grids, alike)
+        if len(grids) == 2:
+            assert grids[1][0] == -(-rows * hq // (1024 // d))
+    assert len(grids) == 1 or d == 64                       # 2^20 heads: no room for parts at d = 128
