@@ -626,12 +626,13 @@ cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_sc
  *              from them (n_rows up to n_max)
  *   row_status [batch] int32 output (may be NULL): CURE_OK, or CURE_ERR_BAD_TREE when the
  *              sequence's parent array is malformed (its o and lse are then
- *              unspecified), or when its sizes are negative, n_rows exceeds n_max, or its
- *              rows, blocks or cache rows reach past rows, blocks or cache_rows (nothing
- *              of it is written then).
+ *              unspecified), or when its sizes are negative, n_rows exceeds n_max, its
+ *              rows, blocks or cache rows reach past rows, blocks or cache_rows, or it has more
+ *              tokens than are supported (nothing of it is written then).
  * The values that a row sees must be finite; what it does not see may be anything.
  * Supports d in {64, 128}, hq % hkv == 0, scale > 0 with scale * log2(e) finite, n_max <= 256
- * with parent, batch <= 65535, n_max * hq up to 2^28. o may be q where their types are one.
+ * with parent, batch <= 65535, n_max * hq up to 2^28, packed_len + ctx_len + n_rows up to
+ * 2^31 - 4097. o may be q where their types are one.
  * kv_split: 0 = automatic, else the number of splits of the longest context.
  * workspace: cure_packed_attn_workspace_size(...) bytes for the same arguments, 16-byte
  * aligned, as q, k, v, pk, pv and o are.

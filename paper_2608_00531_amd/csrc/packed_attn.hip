@@ -61,6 +61,7 @@ constexpr int kRing = 3;             // steps whose bytes are on their way or wa
 constexpr int kMaxSlots = 64;        // splits of a row's keys at most
 constexpr float kNone = -3e38f;      // reference of a row that has seen nothing
 constexpr int kAncWords = CURE_MAX_TREE_NODES / 32;
+constexpr int64_t kMostTokens = INT32_MAX - 4096;    // of a sequence: steps' ends stay within 32 bits
 
 struct Args {
   const void* q;
@@ -116,7 +117,7 @@ CURE_DEV Seq seq_of(const Args& a, int b) {
   s.row0 = a.row_off ? a.row_off[b] : (int64_t)b * a.n_max;
   s.ok = s.n >= 0 && s.n <= a.n_max && s.packed >= 0 && s.ctx >= 0 && s.row0 >= 0 && s.row0 <= a.rows - s.n &&
          s.block0 >= 0 && s.block0 <= a.blocks - blocks_of(s.packed) && s.kv0 >= 0 &&
-         s.kv0 <= a.cache_rows - s.ctx - s.n;
+         s.kv0 <= a.cache_rows - s.ctx - s.n && (int64_t)s.packed + s.ctx + s.n <= kMostTokens;
   return s;
 }
 
@@ -1289,7 +1290,7 @@ extern "C" cure_status cure_packed_attn(const void* q, const int8_t* pk, const i
   if (!row_off && n_max > 0 && rows / n_max < batch) return CURE_ERR_INVALID_ARG;      // padded rows
   if (!sizes_ok(batch, n_max, host_n_rows, host_packed_len, host_ctx_len)) return CURE_ERR_INVALID_ARG;
   for (int32_t b = 0; b < batch; ++b)
-    if ((int64_t)host_packed_len[b] + host_ctx_len[b] + host_n_rows[b] > INT32_MAX - 4096) return CURE_ERR_UNSUPPORTED;
+    if ((int64_t)host_packed_len[b] + host_ctx_len[b] + host_n_rows[b] > kMostTokens) return CURE_ERR_UNSUPPORTED;
   const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
   if ((at(q) | at(pk) | at(pv) | at(k) | at(v) | at(o)) % 16) return CURE_ERR_INVALID_ARG;
   const Plan p = plan_of(dtype, batch, rows, n_max, hq, hkv, d, host_n_rows, host_packed_len, host_ctx_len, kv_split);
