@@ -638,7 +638,7 @@ cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_sc
  * aligned, as q, k, v, pk, pv and o are.
  * bf16: query rows meet the bytes as fp16 times a power of two for each row (off by at most 2^-39 of
  * the row's largest value), and probabilities times the value's scale are rounded to fp16 for their
- * product, 2^-12, but for the open rows, whose products take them to 2^-17; their sum and lse take
+ * product, 2^-11, but for the open rows, whose products take them to 2^-17; their sum and lse take
  * them before. float32: float32 throughout. Blocks' scales may be of any size beside each other; where
  * one is zero, so are the values. Values of open and new rows that a row sees must stay below 2^80, as the sums of
  * those of 2^31 tokens do not fit float32 else.

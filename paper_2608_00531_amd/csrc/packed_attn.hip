@@ -14,7 +14,7 @@
 //
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
 // a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
-// to fp16 for its product, 2^-12 where bf16 would take 2^-9 and add half as much again to the error that the
+// to fp16 for its product, 2^-11 where bf16 would take 2^-8 and add half as much again to the error that the
 // output's own rounding makes; what lies 2^-21 below the largest P has fewer bits, down to 2^-32 of
 // it. Open rows keep bf16's range: their products take P as two bf16 values.
 // fp32: fp32 throughout.

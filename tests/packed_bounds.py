@@ -1,11 +1,12 @@
 """Tighter bounds for the attention over a packed context than those of packed_util.py, with what the header
 says of its roundings.
 
-For bf16, P is rounded to fp16 for packed tokens, 2^-12 of it or half a step of fp16's subnormals, which is 2^-32 of the
-largest P times 2^8 / 2^7 or less (the reference leaves the largest at 2^7 or more, and waves and splits have references
-of their own, none above the row's); for open rows to 2^-17. Query values are fp16 times a power of two, off by 2^-39 of the row's
-largest. With mass = sum p |v| of the packed and the open part and peak the largest p s:
-    |err o| <= 2^-12 packed + 2^-17 open + 2^-32 127 count peak [bf16] + (2 e + (n + 16) u) (mass + |o|), that (1 + 2^-7), + h |o|
+For bf16, P of packed tokens is rounded to fp16, whose 11 bits leave half a step of 2^(e - 11) to a number of 2^e or
+more: 2^-11 of it, or half a step of the subnormals, 2^-25, which is 2^-32 of the row's largest P (a reference leaves the largest
+that it has met at 2^7 or more, and those of waves and splits are none above the row's). P of open rows is two bf16
+numbers: the first leaves at most 2^(e - 8), the second of that 2^(e - 9 - 8): 2^-17. Query values are fp16 times a power of two, off
+by 2^-39 of the row's largest. With mass = sum p |v| of the packed and the open part and peak the largest p s:
+    |err o| <= 2^-11 packed + 2^-17 open + 2^-32 127 count peak [bf16] + (2 e + (n + 16) u) (mass + |o|), that (1 + 2^-7), + h |o|
     e = (d + 6) u scale sum |q k| + 2^-39 [bf16] scale max |q| sum |k|
 and lse as there. Rows may be of any magnitude: a type's smallest step is added.
 """
@@ -52,7 +53,7 @@ class Bounded(Case):
                 tol = (2 * e + (count + 16) * U) * (packed + opened + np.abs(ref))
                 if bf16:
                     peak = np.max(np.concatenate((p[:, :old] * scales[:, h // group], p[:, old:]), axis=1), axis=1, keepdims=True)
-                    tol = tol + 2.0 ** -12 * packed + 2.0 ** -17 * opened + 2.0 ** -32 * 127 * old * peak
+                    tol = tol + 2.0 ** -11 * packed + 2.0 ** -17 * opened + 2.0 ** -32 * 127 * old * peak
                 tol = tol * (1 + 2.0 ** -7)
                 tol = tol + half * (np.abs(ref) + tol) + step
                 err = np.abs(o[self.first[b] + at, h] - ref)
