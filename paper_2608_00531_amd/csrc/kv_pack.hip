@@ -252,6 +252,14 @@ __global__ __launch_bounds__(4 * kWave, sizeof(E) == 2 ? 7 : 5) void kv_pack(Arg
 // taken as this.
 constexpr float kMostScale = 0x1.020406p+121f;
 
+// Waits for what is loaded once, and not at every store that takes some of it, which would wait for the stores
+// before too.
+template <int kVecs>
+CURE_DEV void arrived(u32x4 (&w)[kVecs]) {
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(w[i]));
+}
+
 // The same pieces the other way.
 template <typename E, int D>
 __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
@@ -276,6 +284,7 @@ __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i)
       w[i] = *reinterpret_cast<const u32x4*>(src + L::k_byte(L::k_token(i) + own, L::k_col(lane)));
+    arrived(w);
 #pragma unroll
     for (int i = 0; i < L::kUnits; ++i) {
       RowVec<E, 16> x;
@@ -290,6 +299,7 @@ __global__ __launch_bounds__(4 * kWave) void kv_unpack(Args a) {
   u32x4 w[L::kCols];
 #pragma unroll
   for (int j = 0; j < L::kCols; ++j) w[j] = *reinterpret_cast<const u32x4*>(src + L::v_byte(lane, L::v_col(lane) + j));
+  arrived(w);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     RowVec<E, L::kCols> x;
