@@ -15,7 +15,7 @@
 // in neighbouring lanes; the 16 tokens that a lane of V's layout holds are its own 16 loads, so that its
 // bytes come together without exchange, and LDS turns them for the stores to be whole lines. Eight prompts
 // of 501 to 4001 rows, 8 heads of 128: packed in 25 us and 4.4 TB/s (32 where the rows pass through the
-// caches in the ordinary way), unpacked in 20 us and 5.4 TB/s (where its ordinary stores do better: 25).
+// caches in the ordinary way), unpacked in 21 us and 5.1 TB/s (where its ordinary stores do better: 25).
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"

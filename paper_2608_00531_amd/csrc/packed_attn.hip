@@ -54,7 +54,7 @@ constexpr int kWaves = 4;            // waves per workgroup of a tile of few row
 constexpr int kRows = 32;            // query rows of such a wave, and of the tile
 constexpr int kManyRows = 16;        // query rows of a wave where there are many
 // Waves of such a tile on a SIMD. At d = 64 registers and LDS leave room for three workgroups (chunks of
-// 256 to 512 tokens: 243 us, 281 with two).
+// 256 to 512 tokens: 251 us, 271 with two).
 template <int D>
 constexpr int kPerSimd = D == 64 ? 6 : 4;
 constexpr int kRing = 3;             // steps whose bytes are on their way or wait, of a tile of many rows
@@ -626,8 +626,8 @@ CURE_DEV void mask_open(float (&x)[kScores], uint32_t seen, float factor, int ow
 // Up to 32 query rows to a tile: the waves take the steps in turn, each with all rows and sums of its
 // own, which are joined at the end. Packed bytes go from memory to registers and into the
 // matrix unit, a step ahead of their use; past the caches where one tile is all (kOnce), for nothing reads
-// them twice (eight single tokens over 4096 to 32768: 57 us and 5.5 TB/s, 64 us without; 16 trees of 20 to 48
-// nodes 63 us, 67 with). Memory bounds it for one tile, issue for several.
+// them twice (eight single tokens over 4096 to 32768: 57 us and 5.6 TB/s, 63 us without; 16 trees of 20 to 48
+// nodes 61 us, 64 with). Memory bounds it for one tile, issue for several.
 template <typename E, int D, bool kOnce>
 __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void packed_few(Args a) {
   constexpr int kK = D / 32;                       // pieces of 32 columns
@@ -819,8 +819,8 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
 // operand's 64 lanes of 16 bytes are 1 KB of LDS. Step i forms the probabilities and products of step
 // i, the scores of step i + 1 and the widened tile of step i + 2, while the bytes of the kRing steps behind
 // are on their way. Bound by issue: at
-// 128 rows on four times 32768 tokens, 8 kv-heads, the kernel takes 96 us of the call's 108 (0.64 PFLOP/s), of
-// which counters give the vector unit 44 % and the matrix unit 30 %, one seldom beside the other, and LDS 40 %. Tried
+// 128 rows on four times 32768 tokens, 8 kv-heads, the kernel takes 95 us of the call's 103 (0.67 PFLOP/s), of
+// which counters give the vector unit 46 % and the matrix unit 31 %, one seldom beside the other, and LDS 41 %. Tried
 // and no faster: 32 rows and half as many waves (113 us), bytes brought through registers (108), the scores'
 // products ahead of the softmax (108).
 template <int D>
@@ -1142,8 +1142,8 @@ struct Plan {
 // A form of tile, and what its workgroup takes in us: a step alone on a CU, and at least, as a share of
 // the CU; and besides its steps. Fitted to trees of 20 to 48 nodes (d = 128; few rows: 0.27 and 0.21 for
 // 32 rows, many: 0.77 and 0.7 for 128, 1.05 for 256). Few rows do better where a workgroup has few steps (16 trees
-// on 1024 to 4096 tokens 62 us, 81 with many), as more and smaller ones spread better, many rows where it has
-// many (four trees of 32 nodes on 32768 tokens 108 us, 118 with few; prompts of 2048 on 4000 290 and 365).
+// on 1024 to 4096 tokens 61 us, 90 with many), as more and smaller ones spread better, many rows where it has
+// many (four trees of 32 nodes on 32768 tokens 101 us, 112 with few; a prompt of 2048 on 4000 262 and 288).
 struct Form {
   int32_t groups, tile, quantum, per_cu;             // per_cu workgroups fit on a CU
   double alone, least, start;

@@ -14,9 +14,10 @@
 // are added in one order.
 //
 // One workgroup takes a row, so that every bin is in one LDS. A row is read twice, for its histogram and for the
-// drawn value's entries: 544 bf16 rows of 128256 take 59 us, of which the LDS additions (about 8
-// cycles for a wave's 64, by their conflicts) are a half and the reads another third; one row 25 us, fifteen
-// of them latency of the steps between.
+// drawn value's entries. 544 bf16 rows of 128256 take 60 us: the first reading and the bins' computation 30 (the LDS
+// additions hide behind them and cost one), the search 17, the second reading 16, less what overlaps. 32 CUs have
+// three of the rows and the others two: 512 rows take 52 us. One row takes 25, ten of them its first reading by one
+// CU and the rest latency of the steps behind it.
 #include <hip/hip_runtime.h>
 
 #include "common.hpp"
@@ -723,7 +724,8 @@ __global__ __launch_bounds__(kThreads32) void sample_f32(Args a) {
 // are formed once for each bin in use, so that an entry costs four packed integer instructions
 // and one LDS addition. Eight waves take a row and three rows share a CU, which hide each other's latency: 768
 // rows take 72 us, and 90 with 16 waves to a row and two to a CU; a single row 27 and 27. Rows with
-// other magnitudes that count go the general way.
+// other magnitudes that count go the general way, entry by entry: one row of 128256 with an entry of 1100
+// takes 166 us, 544 of them 411, and one of a single such value, whose additions all meet in one bin, 3.5 ms.
 constexpr int kOctaves = 40 * 128;                 // bins of one sign
 constexpr int kSign = 8192;                        // a negative value's, whose byte offset has its sign bit
 constexpr int kPlaces = 2 * kOctaves;              // in a row's order
