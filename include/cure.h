@@ -637,11 +637,11 @@ cure_status cure_kv_unpack(const int8_t* pk, const int8_t* pv, const float* k_sc
  * workspace: cure_packed_attn_workspace_size(...) bytes for the same arguments, 16-byte
  * aligned, as q, k, v, pk, pv and o are.
  * bf16: query rows meet the bytes as fp16 times a power of two for each row (off by at most 2^-39 of
- * the row's largest value), and probabilities times the value's scale are rounded to fp16 for their
- * product, 2^-11, but for the open rows, whose products take them to 2^-17; their sum and lse take
- * them before. float32: float32 throughout. Blocks' scales may be of any size beside each other; where
- * one is zero, so are the values. Values of open and new rows that a row sees must stay below 2^80, as the sums of
- * those of 2^31 tokens do not fit float32 else.
+ * the row's largest value, where that is 2^-106 or more), and probabilities times the value's scale are
+ * rounded to fp16 for their product, 2^-11, but for the open rows, whose products take them to 2^-17;
+ * their sum and lse take them before. float32: float32 throughout. Blocks' scales may be of any size
+ * beside each other; where one is zero, so are the values. Values of open and new rows that a row sees
+ * must stay below 2^80: float32 holds the sums of 2^31 such tokens.
  */
 size_t cure_packed_attn_workspace_size(int32_t batch, int64_t rows, int32_t n_max, int32_t hq,
                                        int32_t hkv, int32_t d, const int32_t* host_n_rows,

@@ -13,10 +13,11 @@
 // each score a second exponential.
 //
 // bf16: the bytes are widened to fp16, which holds them exactly, and the query rows are too, times
-// a power of two for each row: what that loses is at most 2^-39 of the row's largest. P is rounded
-// to fp16 for its product, 2^-11 where bf16 would take 2^-8 and add half as much again to the error that the
-// output's own rounding makes; what lies 2^-21 below the largest P has fewer bits, down to 2^-32 of
-// it. Open rows keep bf16's range: their products take P as two bf16 values.
+// a power of two for each row: what that loses is at most 2^-39 of the row's largest, where that is
+// 2^-106 or more. P is rounded to fp16 for its product, 2^-11 where bf16 would take 2^-8 and add half
+// as much again to the error that the output's own rounding makes; what lies 2^-21 below the largest P
+// has fewer bits, down to 2^-32 of it. Open rows keep bf16's range: their products take P as two bf16
+// values.
 // fp32: fp32 throughout.
 //
 // 32x32 matrix instructions (x16 for 16 bits, x2 eight times for fp32), 32 query rows per wave. Lane
@@ -322,19 +323,19 @@ using ManySums = Sums<8, 4, D / 16, f32x4>;
 struct ScaleUnit {
   uint32_t low = (127 - 32) << 23, span = (65 << 23) - 1;      // bits of the scales near enough: low .. low + span
   float down = 1.f;                                // 2^-z
-  bool moved = false, apart = false;
+  bool chosen = false, apart = false;
   CURE_DEV bool near(float s) const { return __float_as_uint(s) - low <= span; }
   // One that is not near, the same for the whole wave. m: the row's reference, l's own from here on where apart.
   template <class Own>
   CURE_DEV void meet(float s, float m, const Own& own) {
     const uint32_t bits = __float_as_uint(s), e = min(max(bits >> 23, 1u), 250u);
     if (bits == 0 || apart) return;
-    if (moved || __any(m > kNone)) {
+    if (chosen || __any(m > kNone)) {
       apart = true;
       *own() = m;
       return;
     }
-    moved = true;
+    chosen = true;
     low = e > 32 ? (e - 32) << 23 : 1;
     span = (min(e + 33, 255u) << 23) - 1 - low;
     down = __uint_as_float((254 - e) << 23);
